@@ -326,6 +326,146 @@ typedef struct {
 
 SP_API sp_status sp_gather(const sp_gather_args* args, void* hip_stream);
 
+/* ---------------------------------------------------------------------------
+ * The cache between the calls above and the two models: sp_cache_append fills it (the draft's, which sp_score reads,
+ * or the base model's, whose prefill takes the kept tokens at their ORIGINAL positions, Sec. 3.2.4), sp_attend
+ * attends over it.  Both work on one layer and take the cache as sp_score does:
+ *   paged       d_block_table int32 [B, blocks_per_seq]; token i of sequence b is row i % page_size of page
+ *               d_block_table[b*blocks_per_seq + i/page_size]: element offset page*cache_page_stride +
+ *               (i % page_size)*cache_token_stride + g*cache_head_stride + t for KV head g; page_size a power of two >= 8
+ *   contiguous  d_block_table NULL; token i of sequence b is row d_cu_cache[b] + i at row*cache_token_stride +
+ *               g*cache_head_stride + t; sequence b owns the rows up to d_cu_cache[b+1] (int32 [B+1], non-decreasing)
+ * Keys and values are two arrays of the same layout and type (sp_k_dtype); 8-bit elements stand for
+ * scale[g] * decode(byte), one fp32 scale per KV head (finite) for the keys and one for the values, NULL = all 1.
+ * n_rows is the number of token rows of the pool (pages * page_size) or of the contiguous cache.  Nothing outside it
+ * is read or written, whatever the tables hold: a page number outside the pool or a row outside the cache is answered as
+ * stated at each call.  New tokens of sequence b are rows [d_cu_new[b], d_cu_new[b+1]) of a flat axis with
+ * room for T_new tokens (d_cu_new[0] = 0, non-decreasing, d_cu_new[B] <= T_new; rows at and beyond d_cu_new[B] are
+ * neither read nor written).  Limits: d 64 or 128, H <= 1024, H % H_kv == 0,
+ * H / H_kv <= 16, T_new * H < 2^31.
+ * Pointers to bf16 or 8-bit data are 16-byte aligned; strides count elements and are multiples of 8
+ * (of an 8-bit cache: 16).
+ * --------------------------------------------------------------------------- */
+
+/* sp_cache_append: for new token j of sequence b (flat row t = cu_new[b] + j), at cache index i = cache_len[b] + j and
+ * position p = pos[t] (NULL: p = i):
+ *     q_out[t, h, :] = R_p(q[t, h, :]),   K[i, g, :] = R_p(k[t, g, :]),   V[i, g, :] = v[t, g, :]
+ * R_p turns the pair (m, m + d/2) by the angle p * f_m, f_m = inv_freq[m] or rope_theta^(-2m/d): the angle in fp64, its
+ * cosine and sine rounded to fp32, the products and their sum separate fp32 operations.  Results are rounded once: to
+ * bf16 (nearest even), or divided by the scale in fp32 and rounded to E4M3 (nearest even; beyond +-448 the largest finite
+ * value; NaN stays NaN; a scale of zero stores zeros).  A bf16 cache filled so holds bit for bit what
+ * sp_score with rope_theta > 0 makes of an unrotated one.
+ * A token whose cache index lies outside its sequence's room (blocks_per_seq * page_size tokens, or its rows of a
+ * contiguous cache) or whose page number lies outside the pool is not written to the cache; its row of q_out is.
+ * No two tokens of a call may have the same place in the cache. */
+typedef struct {
+  int32_t B;                 /* sequences, >= 1                                                       */
+  int32_t H;                 /* query heads (ignored if d_q is NULL)                                  */
+  int32_t H_kv;              /* key and value heads                                                   */
+  int32_t d;                 /* head dim: 64 or 128                                                   */
+  int64_t T_new;             /* rows of q, k, v and q_out                                             */
+  const void* d_q;           /* bf16 [T_new, H, d], any token and head strides, or NULL (keys and values only) */
+  int64_t q_token_stride;
+  int64_t q_head_stride;
+  const void* d_k;           /* bf16 [T_new, H_kv, d], any token and head strides                     */
+  int64_t k_token_stride;
+  int64_t k_head_stride;
+  const void* d_v;           /* bf16 [T_new, H_kv, d], any token and head strides                     */
+  int64_t v_token_stride;
+  int64_t v_head_stride;
+  const int32_t* d_cu_new;   /* int32 [B+1]                                                           */
+  const int32_t* d_cache_len;/* int32 [B]: tokens the cache holds before the call, or NULL (none)     */
+  const int32_t* d_pos;      /* int32 [T_new] positions, or NULL; NULL without rotation               */
+  float rope_theta;          /* > 0: frequencies theta^(-2m/d); 0: no rotation unless d_inv_freq      */
+  const double* d_inv_freq;  /* fp64 [d/2] frequencies (scaled rotary encodings), or NULL; not with rope_theta > 0 */
+  void* d_q_out;             /* out bf16 [T_new, H, d] contiguous, NULL iff d_q is; may be d_q itself if that is contiguous */
+  void* d_k_cache;           /* out                                                                   */
+  void* d_v_cache;           /* out                                                                   */
+  int64_t cache_token_stride;
+  int64_t cache_head_stride;
+  int64_t cache_page_stride; /* (ignored if not paged)                                                */
+  const int32_t* d_cu_cache; /* contiguous cache: int32 [B+1], else NULL                              */
+  const int32_t* d_block_table; /* paged cache: int32 [B, blocks_per_seq], else NULL                  */
+  int32_t page_size;         /* (ignored if not paged)                                                */
+  int32_t blocks_per_seq;    /* (ignored if not paged)                                                */
+  int64_t n_rows;            /* token rows of the cache, < 2^31                                       */
+  int32_t cache_dtype;       /* sp_k_dtype                                                            */
+  const float* d_k_scale;    /* fp32 [H_kv] of an 8-bit cache, or NULL (all 1)                        */
+  const float* d_v_scale;    /* fp32 [H_kv] of an 8-bit cache, or NULL (all 1)                        */
+} sp_cache_append_args;
+
+/* Enqueue the append on hip_stream.  Needs no workspace. */
+SP_API sp_status sp_cache_append(const sp_cache_append_args* args, void* hip_stream);
+
+/* sp_attend: attention of the new tokens over the cache, causal.  Sequence b has kv_len[b] tokens in the cache, its
+ * n_b new ones (appended before the call) the last of them, so new token j sees the first
+ * n_vis = clamp(kv_len[b] - n_b + j + 1, 0, kv_len[b]) tokens.  For query head h and KV head g = h / (H/H_kv), t = cu_new[b] + j:
+ *     s_i = scale * k_scale[g] * <q[t, h, :], K[i, g, :]>,  i < n_vis
+ *     out[t, h, :] = sum_i softmax(s)_i * v_scale[g] * V[i, g, :]   (rounded once to bf16),   lse[t, h] = log sum_i exp(s_i)
+ * A row that sees no token gets out = 0 and lse = -infinity.  Logits, maxima, sums and the accumulation of out are
+ * fp32; the weights exp(s_i - m) are rounded to bf16 for the product with the values, as the values are.
+ * NaN/Inf among the queries, or the keys and values of the first kv_len[b] tokens, are precondition violations
+ * (undefined values in rows of that sequence, or of its group); what lies behind them in the cache is never used.
+ *
+ * Shared prefixes: sequences d_cu_group[g] .. d_cu_group[g+1]-1 form a group whose members hold the same first
+ * d_prefix_len[g] tokens (the same pages, or copies).  Results are those of the definition; the keys and values of those
+ * tokens are read through the FIRST member's block table, once for all members, where that pays.  A
+ * prefix is cut to what every query of the group sees.  Paged caches only.
+ *
+ * Two calls: sp_attend_plan turns the lengths (which only the device knows) into the list of pieces of work, once per
+ * step; sp_attend runs it, once per layer.  Both take the same struct; sp_attend_plan reads the shape fields and d_cu_new,
+ * d_kv_len, d_cu_cache, d_cu_group, d_prefix_len and writes d_plan.  sp_attend may be given other queries, caches, scales,
+ * outputs, strides and another workspace, but the shape fields B, H, H_kv, d, T_new, n_groups, page_size, blocks_per_seq,
+ * n_rows, cache_dtype must be those of the plan, and whether it is paged: on a plan made for others, or on none,
+ * every row of out and lse becomes NaN.  Lengths are those at the time of the plan.  A plan may be used by several
+ * sp_attend calls at once if each has a workspace of its own.
+ * Answered with NaN in out and lse: sequences whose kv_len is negative or beyond their room (all rows), and rows whose
+ * part of the work met a page number outside the pool.
+ * Both calls may be captured into graphs: nothing depends on lengths on the host. */
+typedef struct {
+  int32_t B;                 /* sequences, >= 1                                                       */
+  int32_t H;                 /* query heads                                                           */
+  int32_t H_kv;              /* key and value heads                                                   */
+  int32_t d;                 /* head dim: 64 or 128                                                   */
+  int64_t T_new;             /* rows of q, out and lse                                                */
+  int32_t n_groups;          /* groups of sequences that share a prefix, 0: none                      */
+  const int32_t* d_cu_new;   /* int32 [B+1]                                                           */
+  const int32_t* d_kv_len;   /* int32 [B]: tokens in the cache, the new ones included                 */
+  const int32_t* d_cu_group; /* int32 [n_groups+1] first sequences of the groups, 0 .. B, non-decreasing; NULL iff n_groups is 0 */
+  const int32_t* d_prefix_len; /* int32 [n_groups] shared tokens, NULL iff n_groups is 0              */
+  const int32_t* d_cu_cache; /* contiguous cache: int32 [B+1], else NULL                              */
+  const int32_t* d_block_table; /* paged cache: int32 [B, blocks_per_seq], else NULL                  */
+  int32_t page_size;         /* (ignored if not paged)                                                */
+  int32_t blocks_per_seq;    /* (ignored if not paged)                                                */
+  int64_t n_rows;            /* token rows of the cache, < 2^31                                       */
+  int32_t cache_dtype;       /* sp_k_dtype                                                            */
+  const void* d_q;           /* bf16 [T_new, H, d] (rotated), any token and head strides              */
+  int64_t q_token_stride;
+  int64_t q_head_stride;
+  const void* d_k_cache;
+  const void* d_v_cache;
+  int64_t cache_token_stride;
+  int64_t cache_head_stride;
+  int64_t cache_page_stride; /* (ignored if not paged)                                                */
+  const float* d_k_scale;    /* fp32 [H_kv] of an 8-bit cache, or NULL (all 1)                        */
+  const float* d_v_scale;    /* fp32 [H_kv] of an 8-bit cache, or NULL (all 1)                        */
+  float scale;               /* logit scale, finite, > 0                                              */
+  void* d_out;               /* out bf16 [T_new, H, d], any token and head strides                    */
+  int64_t out_token_stride;
+  int64_t out_head_stride;
+  float* d_lse;              /* out fp32 [T_new, H], or NULL                                          */
+  void* d_plan;              /* 256-byte aligned                                                      */
+  size_t plan_bytes;
+  void* d_workspace;         /* 256-byte aligned; not read by sp_attend_plan                          */
+  size_t workspace_bytes;
+} sp_attend_args;
+
+/* Bytes of d_plan and of d_workspace for the shape fields (pointers are not read); 0 if these are invalid. */
+SP_API size_t sp_attend_plan_bytes(const sp_attend_args* args);
+SP_API size_t sp_attend_workspace_bytes(const sp_attend_args* args);
+SP_API sp_status sp_attend_plan(const sp_attend_args* args, void* hip_stream);
+SP_API sp_status sp_attend(const sp_attend_args* args, void* hip_stream);
+
 /* Static, never-NULL description of a status code. */
 SP_API const char* sp_strerror(sp_status status);
 

@@ -24,7 +24,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libspecpref
 EXPORTS = (
     "sp_score_workspace_bytes", "sp_score", "sp_score_general", "sp_score_check", "sp_set_wait_budget",
     "sp_keep_upper_bound", "sp_pool_select_workspace_bytes", "sp_pool_select", "sp_pool_select_static", "sp_score_pool_select",
-    "sp_gather", "sp_strerror", "sp_version",
+    "sp_gather", "sp_cache_append", "sp_attend_plan_bytes", "sp_attend_workspace_bytes", "sp_attend_plan", "sp_attend",
+    "sp_strerror", "sp_version",
 )
 
 
@@ -66,6 +67,36 @@ class GatherArgs(C.Structure):
     ]
 
 
+class CacheAppendArgs(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("H", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32), ("T_new", C.c_int64),
+        ("d_q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+        ("d_k", C.c_void_p), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64),
+        ("d_v", C.c_void_p), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64),
+        ("d_cu_new", C.c_void_p), ("d_cache_len", C.c_void_p), ("d_pos", C.c_void_p),
+        ("rope_theta", C.c_float), ("d_inv_freq", C.c_void_p), ("d_q_out", C.c_void_p),
+        ("d_k_cache", C.c_void_p), ("d_v_cache", C.c_void_p), ("cache_token_stride", C.c_int64),
+        ("cache_head_stride", C.c_int64), ("cache_page_stride", C.c_int64), ("d_cu_cache", C.c_void_p),
+        ("d_block_table", C.c_void_p), ("page_size", C.c_int32), ("blocks_per_seq", C.c_int32), ("n_rows", C.c_int64),
+        ("cache_dtype", C.c_int32), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p),
+    ]
+
+
+class AttendArgs(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("H", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32), ("T_new", C.c_int64),
+        ("n_groups", C.c_int32), ("d_cu_new", C.c_void_p), ("d_kv_len", C.c_void_p), ("d_cu_group", C.c_void_p),
+        ("d_prefix_len", C.c_void_p), ("d_cu_cache", C.c_void_p), ("d_block_table", C.c_void_p),
+        ("page_size", C.c_int32), ("blocks_per_seq", C.c_int32), ("n_rows", C.c_int64), ("cache_dtype", C.c_int32),
+        ("d_q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+        ("d_k_cache", C.c_void_p), ("d_v_cache", C.c_void_p), ("cache_token_stride", C.c_int64),
+        ("cache_head_stride", C.c_int64), ("cache_page_stride", C.c_int64), ("d_k_scale", C.c_void_p),
+        ("d_v_scale", C.c_void_p), ("scale", C.c_float), ("d_out", C.c_void_p), ("out_token_stride", C.c_int64),
+        ("out_head_stride", C.c_int64), ("d_lse", C.c_void_p), ("d_plan", C.c_void_p), ("plan_bytes", C.c_size_t),
+        ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -100,6 +131,14 @@ def load_library() -> C.CDLL:
     lib.sp_score_pool_select.argtypes = [C.POINTER(ScoreArgs), C.POINTER(PoolSelectArgs), C.c_void_p]
     lib.sp_gather.restype = C.c_int
     lib.sp_gather.argtypes = [C.POINTER(GatherArgs), C.c_void_p]
+    lib.sp_cache_append.restype = C.c_int
+    lib.sp_cache_append.argtypes = [C.POINTER(CacheAppendArgs), C.c_void_p]
+    for name in ("sp_attend_plan_bytes", "sp_attend_workspace_bytes"):
+        getattr(lib, name).restype = C.c_size_t
+        getattr(lib, name).argtypes = [C.POINTER(AttendArgs)]
+    for name in ("sp_attend_plan", "sp_attend"):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = [C.POINTER(AttendArgs), C.c_void_p]
     lib.sp_strerror.restype = C.c_char_p
     lib.sp_strerror.argtypes = [C.c_int]
     lib.sp_version.restype = C.c_int32
@@ -283,3 +322,93 @@ def make_gather_args(cu_seqlens, cu_keep, kept_idx, kept_pos, decode_pos, *, tok
 
 def sp_gather(args: GatherArgs, stream=None) -> None:
     _check("sp_gather", load_library().sp_gather(C.byref(args), _stream_handle(stream)))
+
+
+# ----------------------------------------------------------------------------
+# sp_cache_append, sp_attend
+# ----------------------------------------------------------------------------
+def _fill_cache_fields(a, k_cache, v_cache, block_table, cu_cache) -> None:
+    """The cache as sp_cache_append and sp_attend take it: [pages, page_size, H_kv, d] with a block table, or [rows, H_kv, d]."""
+    paged = block_table is not None
+    if k_cache.dim() != (4 if paged else 3):
+        raise ValueError("a paged cache is [pages, page_size, H_kv, d], a contiguous one [rows, H_kv, d]")
+    if v_cache is not None and (v_cache.shape != k_cache.shape or v_cache.stride() != k_cache.stride() or v_cache.dtype != k_cache.dtype):
+        raise ValueError("keys and values must be of one shape, layout and type")
+    if k_cache.stride(-1) != 1:
+        raise ValueError("the head dim of the cache must be contiguous")
+    a.H_kv, a.d = int(k_cache.shape[-2]), int(k_cache.shape[-1])
+    a.cache_token_stride, a.cache_head_stride = int(k_cache.stride(-3)), int(k_cache.stride(-2))
+    a.cache_page_stride = int(k_cache.stride(0)) if paged else 0
+    a.page_size = int(k_cache.shape[1]) if paged else 0
+    a.blocks_per_seq = int(block_table.shape[1]) if paged else 0
+    a.n_rows = int(k_cache.shape[0]) * (int(k_cache.shape[1]) if paged else 1)
+    a.cache_dtype = SP_K_FP8_E4M3 if k_cache.element_size() == 1 else SP_K_BF16
+    a.d_block_table, a.d_cu_cache = _ptr(block_table), _ptr(cu_cache)
+
+
+def make_cache_append_args(k, v, cu_new, k_cache, v_cache, *, q=None, q_out=None, cache_len=None, pos=None,
+                           rope_theta: float = 0.0, inv_freq=None, block_table=None, cu_cache=None, k_scale=None,
+                           v_scale=None) -> CacheAppendArgs:
+    """k, v: bf16 [T_new, H_kv, d], q: bf16 [T_new, H, d] (any token and head strides)."""
+    a = CacheAppendArgs()
+    _fill_cache_fields(a, k_cache, v_cache, block_table, cu_cache)
+    a.B, a.T_new = int(cu_new.numel()) - 1, int(k.shape[0])
+    a.H = 0 if q is None else int(q.shape[1])
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        setattr(a, "d_" + name, _ptr(t))
+        setattr(a, name + "_token_stride", 0 if t is None else int(t.stride(0)))
+        setattr(a, name + "_head_stride", 0 if t is None else int(t.stride(1)))
+    a.d_cu_new, a.d_cache_len, a.d_pos = _ptr(cu_new), _ptr(cache_len), _ptr(pos)
+    a.rope_theta, a.d_inv_freq = float(rope_theta), _ptr(inv_freq)
+    a.d_q_out, a.d_k_cache, a.d_v_cache = _ptr(q_out), _ptr(k_cache), _ptr(v_cache)
+    a.d_k_scale, a.d_v_scale = _ptr(k_scale), _ptr(v_scale)
+    return a
+
+
+def sp_cache_append(args: CacheAppendArgs, stream=None) -> None:
+    _check("sp_cache_append", load_library().sp_cache_append(C.byref(args), _stream_handle(stream)))
+
+
+def make_attend_plan_args(cu_new, kv_len, k_cache, *, H: int, total_new: int, block_table=None, cu_cache=None, cu_group=None,
+                          prefix_len=None, plan=None) -> AttendArgs:
+    """The fields that a plan follows from; add_attend_args() fills in the rest."""
+    a = AttendArgs()
+    _fill_cache_fields(a, k_cache, None, block_table, cu_cache)
+    a.B, a.H, a.T_new = int(cu_new.numel()) - 1, int(H), int(total_new)
+    a.n_groups = 0 if cu_group is None else int(cu_group.numel()) - 1
+    a.d_cu_new, a.d_kv_len, a.d_cu_group, a.d_prefix_len = _ptr(cu_new), _ptr(kv_len), _ptr(cu_group), _ptr(prefix_len)
+    a.d_plan = _ptr(plan)
+    a.plan_bytes = 0 if plan is None else plan.numel() * plan.element_size()
+    return a
+
+
+def add_attend_args(plan_args: AttendArgs, q, k_cache, v_cache, out, *, scale: float, block_table=None, cu_cache=None,
+                    k_scale=None, v_scale=None, lse=None, workspace=None) -> AttendArgs:
+    """A copy of plan_args with one layer's queries bf16 [T_new, H, d], cache and outputs."""
+    a = AttendArgs()
+    C.memmove(C.byref(a), C.byref(plan_args), C.sizeof(AttendArgs))
+    _fill_cache_fields(a, k_cache, v_cache, block_table, cu_cache)
+    a.d_q, a.q_token_stride, a.q_head_stride = _ptr(q), int(q.stride(0)), int(q.stride(1))
+    a.d_out, a.out_token_stride, a.out_head_stride = _ptr(out), int(out.stride(0)), int(out.stride(1))
+    a.d_k_cache, a.d_v_cache = _ptr(k_cache), _ptr(v_cache)
+    a.d_k_scale, a.d_v_scale = _ptr(k_scale), _ptr(v_scale)
+    a.scale, a.d_lse = float(scale), _ptr(lse)
+    a.d_workspace = _ptr(workspace)
+    a.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return a
+
+
+def sp_attend_plan_bytes(args: AttendArgs) -> int:
+    return int(load_library().sp_attend_plan_bytes(C.byref(args)))
+
+
+def sp_attend_workspace_bytes(args: AttendArgs) -> int:
+    return int(load_library().sp_attend_workspace_bytes(C.byref(args)))
+
+
+def sp_attend_plan(args: AttendArgs, stream=None) -> None:
+    _check("sp_attend_plan", load_library().sp_attend_plan(C.byref(args), _stream_handle(stream)))
+
+
+def sp_attend(args: AttendArgs, stream=None) -> None:
+    _check("sp_attend", load_library().sp_attend(C.byref(args), _stream_handle(stream)))

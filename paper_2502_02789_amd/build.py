@@ -28,14 +28,14 @@ COMMON_FLAGS = [
     "-mllvm", "-instcombine-max-copied-from-constant-users=1000000",
     "-Wall", "-Wno-unused-function",
 ]
-# no NaN canonicalisation around fmax in the DEVICE code of the scoring kernels only (NaN inputs
+# no NaN canonicalisation around fmax in the DEVICE code of the scoring and attention kernels only (NaN inputs
 # are a documented precondition violation there).  Host code must still see NaNs (argument
 # checks), and so must the selection kernels, which report NaN scores in band.
 SCORE_DEVICE_FLAGS = ["-Xarch_device", "-fno-honor-nans"]
 
 
 def _extra_flags(src):
-    return SCORE_DEVICE_FLAGS if os.path.basename(src).startswith("sp_score") else []
+    return SCORE_DEVICE_FLAGS if os.path.basename(src).startswith("sp_score") or os.path.basename(src) == "sp_attend.hip" else []
 
 
 def sources():

@@ -1,0 +1,638 @@
+// sp_attend: attention of new tokens over a (paged, bf16 or E4M3) cache, the keys of a shared prefix read once for a group.
+//
+// One launch takes every piece of the plan (sp_attend_plan.h), a workgroup of four waves a piece and KV head.  Two forms:
+//   few rows (<= 16: single tokens, their heads)   bound by reading keys and values.  Each wave walks over 32-key tiles of its own
+//     with a 16x16 tile of logits, keys straight from memory into matrix operands, values through LDS for the transpose; nothing
+//     is shared before the end, and every wave has the next tile in flight.
+//   many rows (<= 128: prompts, prefixes of groups)  bound by the matrix cores.  The four waves share 64-key tiles in LDS (two
+//     buffers, one barrier a tile), each has 32 rows.
+// Both compute S^T = K Q^T, so that a lane has the logits of one row, turn the weights exp2(s - m) into bf16 in place -- the order
+// of keys in a matrix product's sum is free, and is chosen so that a lane's logits are its own operand of O^T = V^T P^T -- and read
+// V^T out of row-major LDS tiles with the transposing LDS read.  The running maximum m follows the logits only
+// where one exceeds it by more than 8 (weights stay below 2^8, sums in fp32), so sums are rarely rescaled.
+// Compiled on the assumption that there are no NaNs; those that mark invalid rows are written as bit patterns.
+#include "sp_attend_internal.h"
+#include "sp_lds.h"
+
+namespace sp {
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+constexpr uint32_t kNanF32 = 0x7fc00000u;
+constexpr int kNanBf16 = 0x7fc0;
+constexpr float kSlack = 8.f;   // logits (log2) may exceed the running maximum by this much
+constexpr int kTileKeys = 64;   // many rows
+
+// Place of 16-byte chunk c of row r in a tile of rows of C chunks, permuted so that neither the operand reads (16 or 32 rows,
+// one or two chunks) nor the transposing reads (4 or 8 rows, 2 or 4 chunks) meet in a bank more often than they must.
+template <int C>
+__device__ __forceinline__ int swizzled(int r, int c) {
+  if constexpr (C == 16) return c ^ (((r & 3) << 2) | ((r >> 2) & 3));
+  else return c ^ ((((r >> 1) & 1) << 2) | ((r >> 2) & 3));
+}
+
+__device__ __forceinline__ s16x4 lds_read_tr(const char* at) {
+  typedef __attribute__((address_space(3))) s16x4 lds_t;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t*)at);
+}
+__device__ __forceinline__ bf16x8 join8(s16x4 a, s16x4 b) {
+  typedef __attribute__((ext_vector_type(8))) short s16x8;
+  const s16x8 v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// 16 E4M3 codes -> 16 bf16 values (exact)
+__device__ __forceinline__ void widen_e4m3(const u32x4 w, u32x4& lo, u32x4& hi) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    lo[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.0f, false));
+    lo[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], 1.0f, true));
+    hi[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 + i], 1.0f, false));
+    hi[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 + i], 1.0f, true));
+  }
+}
+
+template <bool PAGED>
+struct KeyRows {  // byte offsets of key rows
+  const int32_t* table;
+  int lg_page, first;
+  uint32_t last;
+  int64_t ts, ps;
+  __device__ __forceinline__ KeyRows(const AttendDev& p, const AttendUnit& u) {
+    ts = p.c_ts; ps = p.c_ps; lg_page = p.lg_page;
+    table = PAGED ? p.table + (int64_t)u.seq * p.blocks_per_seq : nullptr;
+    first = PAGED ? 0 : p.cu_cache[u.seq];
+    last = PAGED ? p.last_page : p.last_row;
+  }
+  __device__ __forceinline__ uint32_t look_up(int key) const { return PAGED ? (uint32_t)table[key >> lg_page] : 0; }
+  // entry: what look_up() gave for this key; nothing outside the pool is addressed, a bad entry is noted
+  __device__ __forceinline__ int64_t offset(int key, uint32_t entry, bool& bad) const {
+    if constexpr (PAGED) {
+      bad |= entry > last;
+      return (int64_t)min(entry, last) * ps + (int64_t)(key & ((1 << lg_page) - 1)) * ts;
+    } else {
+      return (int64_t)min((uint32_t)(first + key), last) * ts;
+    }
+  }
+};
+
+// The logits' factor: its magnitude; its sign, or a zero, goes into the queries, so that maxima in front of it stay right
+__device__ __forceinline__ float key_factor(const AttendDev& p, int g, uint32_t& flip, uint32_t& keep) {
+  float c = p.k_scale ? p.scale_log2 * p.k_scale[g] : p.scale_log2;
+  flip = c < 0.f ? 0x80008000u : 0u;
+  keep = c == 0.f ? 0u : 0xffffffffu;
+  return c == 0.f ? 1.f : fabsf(c);
+}
+
+struct RowPlace { int token, h; };
+__device__ __forceinline__ RowPlace row_place(const AttendDev& p, int flat, int g) {
+  RowPlace r;
+  r.token = flat / p.G;
+  r.h = g * p.G + flat - r.token * p.G;
+  return r;
+}
+
+// index of row r of a piece among all rows of the workspace
+__device__ __forceinline__ int64_t slot_row(const AttendDev& p, int slot, int r, int g) {
+  return ((int64_t)(slot + r / kSlotRows) * p.H_kv + g) * kSlotRows + r % kSlotRows;
+}
+
+// (the sum of an invalid row is a NaN, as a bit pattern: the compiler takes it that no float is one)
+__device__ __forceinline__ void store_stats(const AttendDev& p, int64_t place, float top, float sum, int bad) {
+  *reinterpret_cast<uint2*>(p.stats + place) = make_uint2(__float_as_uint(top), bad ? kNanF32 : __float_as_uint(sum));
+}
+
+// ---------------------------------------------------------------- few rows
+template <int D, bool FP8>
+struct FewTile {
+  static constexpr int N = FP8 ? D / 64 : D / 32;  // 16-byte loads of a lane per key
+  u32x4 a[N], b[N];                                // keys (l & 15) and 16 + (l & 15) of the tile
+  __device__ __forceinline__ void load(const char* base, int64_t oa, int64_t ob) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      a[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base + oa + 64 * i));
+      b[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base + ob + 64 * i));
+    }
+  }
+};
+
+template <int D, bool FP8, bool PAGED>
+__device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit& u, int g, char* lds) {
+  constexpr int KS = D / 32;          // steps of the product with the queries
+  constexpr int DB = D / 16;          // blocks of values
+  constexpr int C = D / 8;            // 16-byte chunks of a bf16 row
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, row = l & 15, quad = l >> 4;
+  const bool mine = row < u.nr;
+  const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
+  uint32_t flip, keep;
+  const float c = key_factor(p, g, flip, keep);
+
+  // the queries, in the order in which a key's chunks are loaded
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const int d0 = FP8 ? (quad + 4 * (s >> 1)) * 16 + (s & 1) * 8 : s * 32 + quad * 8;
+    u32x4 x = {0, 0, 0, 0};
+    if (mine) x = *reinterpret_cast<const u32x4*>(p.q + at.token * p.q_ts + at.h * p.q_hs + d0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (x[i] ^ flip) & keep;
+    qf[s] = __builtin_bit_cast(bf16x8, x);
+  }
+  int limit = u.k1, least = u.k1;
+  if (u.off != kNoLimit) {
+    if (mine) limit = min(u.k1, at.token + u.off);
+    least = limit;
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) least = min(least, __shfl_xor(least, off, kWave));
+    least = __builtin_amdgcn_readfirstlane(least);
+  }
+
+  const KeyRows<PAGED> rows(p, u);
+  const char* const kb = p.k + (int64_t)g * p.c_hs + quad * 16;
+  const char* const vb = p.v + (int64_t)g * p.c_hs + quad * 16;
+  char* const vt = lds + w * (32 * D * 2);
+  const int last_key = u.k1 - 1;
+  bool bad = false;
+  f32x4 o[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, sum = 0.f;
+
+  int tile = u.k0 + 32 * w;
+  if (tile < u.k1) {
+    FewTile<D, FP8> kt, vl;
+    int ka = min(tile + row, last_key), kc = min(tile + 16 + row, last_key);
+    {
+      const int64_t oa = rows.offset(ka, rows.look_up(ka), bad), ob = rows.offset(kc, rows.look_up(kc), bad);
+      kt.load(kb, oa, ob);
+      vl.load(vb, oa, ob);
+    }
+    int na = min(tile + 128 + row, last_key), nc = min(tile + 144 + row, last_key);
+    uint32_t ea = rows.look_up(na), ec = rows.look_up(nc);
+    for (; tile < u.k1; tile += 128) {
+      const bool more = tile + 128 < u.k1;
+      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (FP8) {
+#pragma unroll
+        for (int i = 0; i < KS / 2; ++i) {
+          u32x4 lo, hi;
+          widen_e4m3(kt.a[i], lo, hi);
+          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), qf[2 * i], s0, 0, 0, 0);
+          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), qf[2 * i + 1], s0, 0, 0, 0);
+          widen_e4m3(kt.b[i], lo, hi);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), qf[2 * i], s1, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), qf[2 * i + 1], s1, 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kt.a[s]), qf[s], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kt.b[s]), qf[s], s1, 0, 0, 0);
+        }
+      }
+      int64_t oa = 0, ob = 0;
+      if (more) {
+        oa = rows.offset(na, ea, bad);
+        ob = rows.offset(nc, ec, bad);
+        na = min(tile + 256 + row, last_key);
+        nc = min(tile + 272 + row, last_key);
+        ea = rows.look_up(na);
+        ec = rows.look_up(nc);
+        kt.load(kb, oa, ob);
+      }
+      // values to LDS, as bf16
+#pragma unroll
+      for (int i = 0; i < FewTile<D, FP8>::N; ++i) {
+        if constexpr (FP8) {
+          const int ch = 2 * (quad + 4 * i);
+          u32x4 lo, hi;
+          widen_e4m3(vl.a[i], lo, hi);
+          *reinterpret_cast<u32x4*>(vt + row * (D * 2) + swizzled<C>(row, ch) * 16) = lo;
+          *reinterpret_cast<u32x4*>(vt + row * (D * 2) + swizzled<C>(row, ch + 1) * 16) = hi;
+          widen_e4m3(vl.b[i], lo, hi);
+          *reinterpret_cast<u32x4*>(vt + (16 + row) * (D * 2) + swizzled<C>(row, ch) * 16) = lo;
+          *reinterpret_cast<u32x4*>(vt + (16 + row) * (D * 2) + swizzled<C>(row, ch + 1) * 16) = hi;
+        } else {
+          const int ch = quad + 4 * i;
+          *reinterpret_cast<u32x4*>(vt + row * (D * 2) + swizzled<C>(row, ch) * 16) = vl.a[i];
+          *reinterpret_cast<u32x4*>(vt + (16 + row) * (D * 2) + swizzled<C>(row, ch) * 16) = vl.b[i];
+        }
+      }
+      if (more) vl.load(vb, oa, ob);
+
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { x[i] = s0[i] * c; x[4 + i] = s1[i] * c; }
+      if (tile + 32 > least) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (tile + 4 * quad + i >= limit) x[i] = -INFINITY;
+          if (tile + 16 + 4 * quad + i >= limit) x[4 + i] = -INFINITY;
+        }
+      }
+      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float next = fmaxf(m, top);
+        const float f = next == -INFINITY ? 1.f : fast_exp2(m - next);
+        m = next;
+        sum *= f;
+#pragma unroll
+        for (int i = 0; i < DB; ++i) o[i] *= f;
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { x[i] = fast_exp2(x[i] - base); sum += x[i]; }
+      const u32x4 pw = {pack_bf16_pair(x[0], x[1]), pack_bf16_pair(x[2], x[3]), pack_bf16_pair(x[4], x[5]), pack_bf16_pair(x[6], x[7])};
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      const int vr = 4 * quad + ((l & 15) >> 2);  // row of the tile that this lane reads from (and 16 + that)
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        const int ch = 2 * i + ((l & 3) >> 1);
+        const char* at0 = vt + vr * (D * 2) + swizzled<C>(vr, ch) * 16 + (l & 1) * 8;
+        const bf16x8 vf = join8(lds_read_tr(at0), lds_read_tr(at0 + 16 * D * 2));
+        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[i], 0, 0, 0);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+  }
+
+  // the four waves' sums joined, in the waves' order
+  sum += __shfl_xor(sum, 16, kWave);
+  sum += __shfl_xor(sum, 32, kWave);
+  float* const stat = reinterpret_cast<float*>(lds + 4 * 16 * (D + 4) * 4);  // [2][4][16]
+  const int any_bad = __syncthreads_or(bad);  // (also: every wave is done with its tile in LDS)
+  if (quad == 0) {
+    stat[w * 16 + row] = m;
+    stat[64 + w * 16 + row] = sum;
+  }
+  __syncthreads();
+  {
+    float top = fmaxf(fmaxf(stat[row], stat[16 + row]), fmaxf(stat[32 + row], stat[48 + row]));
+    const float f = fast_exp2(m - (top == -INFINITY ? 0.f : top));
+    float* const part = reinterpret_cast<float*>(lds) + (w * 16 + row) * (D + 4);
+#pragma unroll
+    for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(part + 16 * i + 4 * quad) = o[i] * f;
+  }
+  __syncthreads();
+  const int r = threadIdx.x >> 4, lane = threadIdx.x & 15;
+  if (r >= u.nr) return;
+  constexpr int V = D / 16;
+  float acc[V], l_all = 0.f;
+  const float top = fmaxf(fmaxf(stat[r], stat[16 + r]), fmaxf(stat[32 + r], stat[48 + r]));
+  const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = 0.f;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    l_all += stat[64 + x * 16 + r] * fast_exp2(stat[x * 16 + r] - base);
+    const float* part = reinterpret_cast<const float*>(lds) + (x * 16 + r) * (D + 4) + lane * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] += part[i];
+  }
+  if (u.slot >= 0) {
+    const int64_t place = slot_row(p, u.slot, r, g);
+    float* dst = p.sums + place * D + lane * V;
+#pragma unroll
+    for (int i = 0; i < V; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+    if (lane == 0) store_stats(p, place, top, l_all, any_bad);
+    return;
+  }
+  const RowPlace to = row_place(p, u.r0 + r, g);
+  const float mul = (l_all == 0.f ? 0.f : 1.f / l_all) * (p.v_scale ? p.v_scale[g] : 1.f);
+  const uint32_t nan2 = kNanBf16 * 0x10001u;
+  uint32_t out[V / 2];
+#pragma unroll
+  for (int i = 0; i < V; i += 2) out[i / 2] = any_bad ? nan2 : pack_bf16_pair(acc[i] * mul, acc[i + 1] * mul);
+  uint16_t* dst = p.out + to.token * p.o_ts + to.h * p.o_hs + lane * V;
+  if constexpr (V == 8) *reinterpret_cast<u32x4*>(dst) = u32x4{out[0], out[1], out[2], out[3]};
+  else *reinterpret_cast<uint2*>(dst) = make_uint2(out[0], out[1]);
+  if (lane == 0 && p.lse) {
+    const float lse = l_all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(l_all)) * 0.69314718055994531f;
+    reinterpret_cast<uint32_t*>(p.lse)[(int64_t)to.token * p.H + to.h] = any_bad ? kNanF32 : __float_as_uint(lse);
+  }
+}
+
+// ---------------------------------------------------------------- many rows
+// one lane's share of a 64-key tile of keys or values: chunks tid + 256 i of the tile's 16-byte chunks
+template <int D, bool FP8>
+struct ManyTile {
+  static constexpr int C = FP8 ? D / 16 : D / 8;           // 16-byte chunks of a stored row
+  static constexpr int N = kTileKeys * C / 256;
+  static constexpr int STEP = 256 / C;                     // rows between a lane's chunks
+  u32x4 x[N];
+  __device__ __forceinline__ void load(const char* base, const int64_t (&off)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const u32x4*>(base + off[i]);
+  }
+  __device__ __forceinline__ void store(char* tile, int tid) const {
+    const int ch = tid % C;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = tid / C + STEP * i;
+      char* row = tile + r * (D * 2);
+      if constexpr (FP8) {
+        u32x4 lo, hi;
+        widen_e4m3(x[i], lo, hi);
+        *reinterpret_cast<u32x4*>(row + swizzled<D / 8>(r, 2 * ch) * 16) = lo;
+        *reinterpret_cast<u32x4*>(row + swizzled<D / 8>(r, 2 * ch + 1) * 16) = hi;
+      } else {
+        *reinterpret_cast<u32x4*>(row + swizzled<D / 8>(r, ch) * 16) = x[i];
+      }
+    }
+  }
+};
+
+template <int D, bool FP8, bool PAGED>
+__device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit& u, int g, char* lds) {
+  constexpr int KS = D / 16;   // steps of the product with the queries
+  constexpr int DB = D / 32;   // blocks of values
+  constexpr int C = D / 8;
+  constexpr int TILE = kTileKeys * D * 2;  // bytes of a tile of keys or of values
+  using Tile = ManyTile<D, FP8>;
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, half = l >> 5;
+  const int row = w * 32 + (l & 31);
+  const bool mine = row < u.nr;
+  const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
+  uint32_t flip, keep;
+  const float c = key_factor(p, g, flip, keep);
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    u32x4 x = {0, 0, 0, 0};
+    if (mine) x = *reinterpret_cast<const u32x4*>(p.q + at.token * p.q_ts + at.h * p.q_hs + s * 16 + half * 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (x[i] ^ flip) & keep;
+    qf[s] = __builtin_bit_cast(bf16x8, x);
+  }
+  // the keys that the wave's rows see: all see those below `least`, none those from `most` on
+  int limit = mine ? u.k1 : u.k0;
+  if (mine && u.off != kNoLimit) limit = min(u.k1, at.token + u.off);
+  int least = mine ? limit : u.k1, most = limit;
+#pragma unroll
+  for (int off = 16; off >= 1; off >>= 1) {
+    least = min(least, __shfl_xor(least, off, kWave));
+    most = max(most, __shfl_xor(most, off, kWave));
+  }
+  least = __builtin_amdgcn_readfirstlane(least);
+  most = __builtin_amdgcn_readfirstlane(most);
+
+  const KeyRows<PAGED> rows(p, u);
+  const int ch = tid % Tile::C, kr = tid / Tile::C;
+  const char* const kb = p.k + (int64_t)g * p.c_hs + ch * 16;
+  const char* const vb = p.v + (int64_t)g * p.c_hs + ch * 16;
+  const int last_key = u.k1 - 1;
+  bool bad = false;
+
+  f32x16 o[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+  float m = -INFINITY, sum = 0.f;
+
+  // addresses of the operands in a tile
+  int k_at[KS], v_at[DB][2];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) k_at[s] = (l & 31) * (D * 2) + swizzled<C>(l & 31, 2 * s + half) * 16;
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int vr = 8 * x + 4 * half + ((l & 15) >> 2);
+      v_at[i][x] = vr * (D * 2) + swizzled<C>(vr, 4 * i + 2 * ((l >> 4) & 1) + ((l & 3) >> 1)) * 16 + (l & 1) * 8;
+    }
+
+  Tile kt, vl;
+  uint32_t entry[Tile::N];
+  int64_t off[Tile::N];
+  auto look_up = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < Tile::N; ++i) entry[i] = rows.look_up(min(tile + kr + Tile::STEP * i, last_key));
+  };
+  auto load = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < Tile::N; ++i) off[i] = rows.offset(min(tile + kr + Tile::STEP * i, last_key), entry[i], bad);
+    kt.load(kb, off);
+    vl.load(vb, off);
+  };
+  if (u.k0 < u.k1) {
+    look_up(u.k0);
+    load(u.k0);
+    look_up(min(u.k0 + kTileKeys, last_key));
+  }
+  int buffer = 0;
+  for (int tile = u.k0; tile < u.k1; tile += kTileKeys, buffer ^= 2 * TILE) {
+    char* const kd = lds + buffer;
+    char* const vd = kd + TILE;
+    kt.store(kd, tid);
+    vl.store(vd, tid);
+    __syncthreads();
+    if (tile + kTileKeys < u.k1) {
+      load(tile + kTileKeys);
+      look_up(min(tile + 2 * kTileKeys, last_key));
+    }
+    if (tile >= most) continue;  // (the wave's rows see none of these keys)
+    f32x16 s[2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[x][j] = 0.f;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kd + k_at[i] + x * 32 * (D * 2));
+        s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[x], 0, 0, 0);
+      }
+    }
+    if (tile + kTileKeys > least) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (tile + 32 * x + 8 * (j >> 2) + 4 * half + (j & 3) >= limit) s[x][j] = -INFINITY;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) top = fmaxf(top, s[x][j]);
+    top *= c;
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      const float next = fmaxf(m, top);
+      const float f = next == -INFINITY ? 1.f : fast_exp2(m - next);
+      m = next;
+      sum *= f;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i] *= f;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    bf16x8 pf[4];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        s[x][j] = fast_exp2(__builtin_fmaf(s[x][j], c, -base));
+        sum += s[x][j];
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const u32x4 pw = {pack_bf16_pair(s[x][8 * e], s[x][8 * e + 1]), pack_bf16_pair(s[x][8 * e + 2], s[x][8 * e + 3]),
+                          pack_bf16_pair(s[x][8 * e + 4], s[x][8 * e + 5]), pack_bf16_pair(s[x][8 * e + 6], s[x][8 * e + 7])};
+        pf[2 * x + e] = __builtin_bit_cast(bf16x8, pw);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        const bf16x8 vf = join8(lds_read_tr(vd + v_at[i][0] + e * 16 * (D * 2)), lds_read_tr(vd + v_at[i][1] + e * 16 * (D * 2)));
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[e], o[i], 0, 0, 0);
+      }
+  }
+
+  const int any_bad = __syncthreads_or(bad);
+  sum += __shfl_xor(sum, 32, kWave);
+  if (!mine) return;
+  if (u.slot >= 0) {
+    const int64_t place = slot_row(p, u.slot, row, g);
+    float* dst = p.sums + place * D + 4 * half;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<f32x4*>(dst + 32 * i + 8 * j) = f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
+    if (half == 0) store_stats(p, place, m, sum, any_bad);
+    return;
+  }
+  const float mul = (sum == 0.f ? 0.f : 1.f / sum) * (p.v_scale ? p.v_scale[g] : 1.f);
+  const uint32_t nan2 = kNanBf16 * 0x10001u;
+  uint16_t* dst = p.out + at.token * p.o_ts + at.h * p.o_hs + 4 * half;
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint2 x = make_uint2(pack_bf16_pair(o[i][4 * j] * mul, o[i][4 * j + 1] * mul), pack_bf16_pair(o[i][4 * j + 2] * mul, o[i][4 * j + 3] * mul));
+      *reinterpret_cast<uint2*>(dst + 32 * i + 8 * j) = any_bad ? make_uint2(nan2, nan2) : x;
+    }
+  if (half == 0 && p.lse) {
+    const float lse = sum == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+    reinterpret_cast<uint32_t*>(p.lse)[(int64_t)at.token * p.H + at.h] = any_bad ? kNanF32 : __float_as_uint(lse);
+  }
+}
+
+// every row of the call, or of one piece and KV head, becomes NaN
+__device__ __forceinline__ void nan_rows(const AttendDev& p, int d, int64_t r0, int64_t nr, int heads, int h0, int64_t first, int64_t stride) {
+  const int vec = d / 8;
+  const uint32_t nan2 = kNanBf16 * 0x10001u;
+  for (int64_t x = first; x < nr * vec; x += stride) {
+    const int64_t flat = r0 + x / vec, token = flat / heads;
+    const int h = h0 + (int)(flat % heads);
+    *reinterpret_cast<u32x4*>(p.out + token * p.o_ts + h * p.o_hs + x % vec * 8) = u32x4{nan2, nan2, nan2, nan2};
+    if (x % vec == 0 && p.lse) reinterpret_cast<uint32_t*>(p.lse)[token * p.H + h] = kNanF32;
+  }
+}
+
+}  // namespace
+
+template <int D, bool FP8, bool PAGED>
+__global__ __launch_bounds__(256, 2) void attend_kernel(const AttendDev p) {
+  __shared__ __align__(16) char lds[2 * 2 * kTileKeys * D * 2];  // (few rows need 34 KB of the 64, or 17.5 of the 32)
+  if (p.header->print != p.print) {
+    nan_rows(p, D, 0, (int64_t)p.T_new * p.H, p.H, 0, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+    return;
+  }
+  // The KV heads of a piece are neighbours: with eight of them, each has the L2 of one XCD, which the rows of a
+  // block share, as workgroups go to the XCDs in turn.
+  const int n = (int)(blockIdx.x / (uint32_t)p.H_kv), g = (int)(blockIdx.x % (uint32_t)p.H_kv);
+  if (n >= p.header->n_units) return;
+  const AttendUnit u = p.units[n];
+  if (u.bad) {
+    nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, 256);
+    return;
+  }
+  if (u.nr <= kFewRows) attend_few<D, FP8, PAGED>(p, u, g, lds);
+  else attend_many<D, FP8, PAGED>(p, u, g, lds);
+}
+
+namespace {
+
+sp_status check_attend(const sp_attend_args* a) {
+  const sp_status st = check_attend_plan_args(a);
+  if (st != SP_OK) return st;
+  if (!finite_f32(a->scale) || a->scale <= 0.f) return SP_EINVAL;
+  const bool fp8 = a->cache_dtype == SP_K_FP8_E4M3;
+  if (!fp8 && (a->d_k_scale || a->d_v_scale)) return SP_EINVAL;
+  if (!a->d_q || !a->d_k_cache || !a->d_v_cache || !a->d_out) return SP_ENULL;
+  const int64_t row[] = {a->q_token_stride, a->q_head_stride, a->out_token_stride, a->out_head_stride};
+  const int64_t cache[] = {a->cache_token_stride, a->cache_head_stride, a->d_block_table ? a->cache_page_stride : 0};
+  for (int64_t s : row) if (s < 0) return SP_EINVAL;
+  for (int64_t s : cache) if (s < 0) return SP_EINVAL;
+  for (int64_t s : row) if (s & 7) return SP_EALIGN;
+  for (int64_t s : cache) if (s & (fp8 ? 15 : 7)) return SP_EALIGN;
+  if (!aligned16(a->d_q) || !aligned16(a->d_k_cache) || !aligned16(a->d_v_cache) || !aligned16(a->d_out)) return SP_EALIGN;
+  if (!a->d_workspace || a->workspace_bytes < sp_attend_workspace_bytes(a)) return SP_EWORKSPACE;
+  if (reinterpret_cast<uintptr_t>(a->d_workspace) & 255u) return SP_EALIGN;
+  return SP_OK;
+}
+
+template <int D, bool FP8>
+void launch_attend(const AttendDev& p, bool paged, uint32_t grid, hipStream_t stream) {
+  if (paged) hipLaunchKernelGGL((attend_kernel<D, FP8, true>), dim3(grid), dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((attend_kernel<D, FP8, false>), dim3(grid), dim3(256), 0, stream, p);
+}
+
+}  // namespace
+
+}  // namespace sp
+
+extern "C" size_t sp_attend_workspace_bytes(const sp_attend_args* a) {
+  return sp::check_attend_shape(a) == SP_OK ? sp::attend_workspace(a) : 0;
+}
+
+extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
+  using namespace sp;
+  const sp_status st = check_attend(a);
+  if (st != SP_OK) return st;
+  if (a->T_new == 0) return SP_OK;
+  const AttendCaps caps = attend_caps(a);
+  const AttendPlanLayout l = attend_plan_layout(a);
+  const char* base = static_cast<const char*>(a->d_plan);
+  const bool fp8 = a->cache_dtype == SP_K_FP8_E4M3, paged = a->d_block_table != nullptr;
+  const int E = fp8 ? 1 : 2;
+  AttendDev p;
+  p.B = a->B; p.H = a->H; p.H_kv = a->H_kv; p.G = a->H / a->H_kv; p.T_new = (int)a->T_new;
+  p.lg_page = 0;
+  while (paged && (1 << p.lg_page) < a->page_size) ++p.lg_page;
+  p.blocks_per_seq = a->blocks_per_seq;
+  p.last_page = paged ? (uint32_t)(a->n_rows / a->page_size - 1) : 0;
+  p.last_row = (uint32_t)(a->n_rows - 1);
+  p.join_slices = (int64_t)a->T_new * p.G > kFewRows ? kManyRows / kSlotRows : 1;
+  p.scale_log2 = a->scale * 1.44269504088896340736f;
+  p.q_ts = a->q_token_stride; p.q_hs = a->q_head_stride;
+  p.o_ts = a->out_token_stride; p.o_hs = a->out_head_stride;
+  p.c_ts = a->cache_token_stride * E; p.c_hs = a->cache_head_stride * E; p.c_ps = a->cache_page_stride * E;
+  p.print = attend_print(a);
+  p.header = reinterpret_cast<const AttendHeader*>(base);
+  p.units = reinterpret_cast<const AttendUnit*>(base + l.units);
+  p.joins = reinterpret_cast<const AttendJoin*>(base + l.joins);
+  p.table = a->d_block_table; p.cu_cache = a->d_cu_cache;
+  p.q = static_cast<const uint16_t*>(a->d_q);
+  p.k = static_cast<const char*>(a->d_k_cache); p.v = static_cast<const char*>(a->d_v_cache);
+  p.k_scale = a->d_k_scale; p.v_scale = a->d_v_scale;
+  p.out = static_cast<uint16_t*>(a->d_out); p.lse = a->d_lse;
+  p.sums = static_cast<float*>(a->d_workspace);
+  p.stats = reinterpret_cast<float2*>(static_cast<char*>(a->d_workspace) + attend_sums_bytes(a));
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const uint32_t grid = (uint32_t)(caps.units * a->H_kv);
+  if (a->d == 128) fp8 ? launch_attend<128, true>(p, paged, grid, stream) : launch_attend<128, false>(p, paged, grid, stream);
+  else fp8 ? launch_attend<64, true>(p, paged, grid, stream) : launch_attend<64, false>(p, paged, grid, stream);
+  launch_attend_join(p, a->d, caps.joins * p.join_slices * a->H_kv, stream);
+  return launch_status();
+}

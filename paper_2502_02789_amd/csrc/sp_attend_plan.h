@@ -1,0 +1,157 @@
+// How sp_attend cuts a call into pieces of work.  Plain C++: the kernel that makes the plan and a test without a GPU go
+// through the same functions.
+//
+// The rows of a call are (token, head of a KV head's group) pairs, row = token * G + head, flat over all tokens: the rows of a
+// sequence, and of a group of sequences, lie side by side.  A segment is a set of rows that attend to the same keys: the shared
+// prefix of a group (all rows of its members), or what a sequence has for itself.  A segment is cut into blocks of 16 rows
+// (if it has no more: one small matrix tile, bound by reading the keys) or of 128 (bound by the matrix cores), and a block's
+// keys into pieces.  A piece times a KV head is what one workgroup does.
+//
+// A block of one piece whose rows have no shared prefix is finished by its workgroup; the pieces of all others leave their
+// sums in slots of the workspace, which a second kernel joins.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "specprefill.h"
+
+#ifdef __HIPCC__
+#define SP_ATTEND_FN __host__ __device__ __forceinline__
+#else
+#define SP_ATTEND_FN inline
+#endif
+
+namespace sp {
+
+constexpr int kFewRows = 16;      // rows of a block of a small segment
+constexpr int kManyRows = 128;    // ... and of any other
+constexpr int kSlotRows = 16;     // rows of a workspace slot
+constexpr int kPieceStep = 64;    // pieces are cut at multiples of so many keys
+constexpr int kMinPiece = 128;    // no piece is made shorter than this
+constexpr int kAttendItems = 1024;  // workgroups that a call's keys are cut for: four for each of 256 compute units
+
+struct AttendUnit {   // one piece of one block
+  int32_t r0, nr;     // first row, rows (nr <= 16: the kernel part for few rows)
+  int32_t seq;        // whose block table is read
+  int32_t k0, k1;     // keys [k0, k1)
+  int32_t off;        // token t sees keys below t + off (kNoLimit: all of the piece)
+  int32_t slot;       // where the sums go, or -1: the block is finished here
+  int32_t bad;        // 1: the sequence's length is invalid, its rows become NaN
+};
+struct AttendJoin {   // one block of a sequence's own rows that slots are joined for
+  int32_t r0, nr;
+  int32_t own_slot, own_pieces, own_step;           // slot of the first piece, pieces, slots of a piece
+  int32_t pre_slot, pre_pieces, pre_r0, pre_rows;   // the group's prefix: slot of its first block, pieces of a block (0: none), its first row, rows of a block
+  int32_t pad[3];
+};
+struct AttendHeader {
+  uint64_t print;     // of the shape fields the plan was made for
+  int32_t n_units, n_joins, n_slots, pad;
+};
+
+constexpr int kNoLimit = 0x7fffffff;
+
+struct AttendCaps {
+  int64_t blocks, units, joins, slots;
+};
+
+// Upper bounds for any lengths that the shape fields allow.  Blocks: a segment of R rows has at most R / 128 + 1; own segments
+// with a block: at most B and at most one per row; prefix segments: n_groups.  Pieces: make_cut() adds at most kAttendItems / H_kv to one per block.
+// Slots: prefix blocks, blocks of sequences with a prefix, and blocks of several pieces, of which there are at most as many as pieces added; a
+// prefix is only shared where a group has fewer than 128 rows per member on average (shares()), so rows in such groups are fewer than 128 B.
+inline AttendCaps attend_caps(const sp_attend_args* a) {
+  const int64_t rows = a->T_new * (a->H / a->H_kv), added = kAttendItems / a->H_kv + 1;
+  const int64_t own_segments = rows < a->B ? rows : a->B, own = rows / kManyRows + own_segments;
+  const int64_t shared_rows = rows < (int64_t)kManyRows * a->B ? rows : (int64_t)kManyRows * a->B;
+  const int64_t groups = a->n_groups < own_segments ? a->n_groups : own_segments;  // those with a row
+  const int64_t prefix = a->n_groups ? shared_rows / kManyRows + groups : 0;
+  AttendCaps c;
+  c.blocks = own + prefix;
+  c.units = c.blocks + added;
+  c.joins = own;
+  // blocks that may leave sums, in blocks of 128 rows and in all; own segments of over 16 rows: at most one per 17
+  const int64_t big_segments = own_segments < rows / (kFewRows + 1) ? own_segments : rows / (kFewRows + 1);
+  const int64_t shared_big = a->n_groups ? 2 * (shared_rows / kManyRows) + big_segments + (groups < rows / (kFewRows + 1) ? groups : rows / (kFewRows + 1)) : 0;
+  const int64_t shared_few = a->n_groups ? own_segments + groups : 0;
+  const bool any_big = rows > kFewRows;
+  // pieces of blocks that are cut: at most two for each piece added
+  c.slots = (any_big ? (kManyRows / kSlotRows) : 1) * (2 * added) + (kManyRows / kSlotRows) * shared_big + shared_few;
+  return c;
+}
+
+// What a member's shared prefix saves: a block's rows are filled up by several members, and its keys read once for them all.  With 128 rows of its own
+// for each member there is nothing to gain.
+SP_ATTEND_FN bool shares(int64_t group_rows, int members) { return members >= 2 && group_rows < (int64_t)kManyRows * members; }
+
+SP_ATTEND_FN int block_rows(int64_t rows) { return rows <= kFewRows ? kFewRows : kManyRows; }
+SP_ATTEND_FN int segment_blocks(int64_t rows) { return (int)((rows + block_rows(rows) - 1) / block_rows(rows)); }
+
+// One past the last key that row `row` of a sequence sees (its rows counted from 0, G to a token), n new tokens, len keys.
+SP_ATTEND_FN int row_limit(int64_t row, int G, int n, int len) {
+  const int64_t v = (int64_t)len - n + row / G + 1;
+  return v < 0 ? 0 : v > len ? len : (int)v;
+}
+
+// The keys of block i of a sequence's own segment: [shared, the limit of its last row)
+SP_ATTEND_FN int own_block_keys(int64_t rows, int i, int G, int n, int len, int shared) {
+  const int m = block_rows(rows);
+  const int64_t last = (int64_t)(i + 1) * m < rows ? (int64_t)(i + 1) * m - 1 : rows - 1;
+  const int v = row_limit(last, G, n, len) - shared;
+  return v < 0 ? 0 : v;
+}
+
+// Most keys of a piece, for `total` keys summed over all blocks: 1024 workgroups have equal shares, where that
+// leaves them 128 keys.
+SP_ATTEND_FN int make_cut(int64_t total, int H_kv) {
+  const int items = kAttendItems / H_kv > 0 ? kAttendItems / H_kv : 1;
+  const int64_t share = (total + items - 1) / items;
+  const int64_t cut = (share + kPieceStep - 1) / kPieceStep * kPieceStep;
+  return cut < kMinPiece ? kMinPiece : cut > 0x40000000 ? 0x40000000 : (int)cut;
+}
+SP_ATTEND_FN int pieces_of(int keys, int cut) { return keys <= cut ? 1 : (int)(((int64_t)keys + cut - 1) / cut); }
+// first key (counted from the block's first) of piece p
+SP_ATTEND_FN int piece_start(int keys, int pieces, int p) {
+  const int steps = (keys + kPieceStep - 1) / kPieceStep;
+  const int64_t s = (int64_t)steps * p / pieces * kPieceStep;
+  return s < keys ? (int)s : keys;
+}
+
+SP_ATTEND_FN uint64_t attend_print(const sp_attend_args* a) {
+  const uint64_t v[] = {0x61747465ull, (uint64_t)(uint32_t)a->B, (uint64_t)(uint32_t)a->H, (uint64_t)(uint32_t)a->H_kv, (uint64_t)(uint32_t)a->d,
+                        (uint64_t)a->T_new, (uint64_t)(uint32_t)a->n_groups, a->d_block_table ? (uint64_t)(uint32_t)a->page_size : 0,
+                        a->d_block_table ? (uint64_t)(uint32_t)a->blocks_per_seq : 0, (uint64_t)a->n_rows, (uint64_t)(uint32_t)a->cache_dtype};
+  uint64_t h = 1469598103934665603ull;  // each field mixed in by a product and a shift
+  for (uint64_t x : v) {
+    h = (h ^ x) * 0x9E3779B97F4A7C15ull;
+    h ^= h >> 29;
+  }
+  return h | 1;  // never zero: cleared memory is no plan
+}
+
+// Offsets of the parts of d_plan
+struct AttendPlanLayout {
+  size_t units, joins, seg_start, seqs, groups, bytes;
+};
+inline size_t attend_round(size_t x) { return (x + 255) / 256 * 256; }
+inline AttendPlanLayout attend_plan_layout(const sp_attend_args* a) {
+  const AttendCaps c = attend_caps(a);
+  AttendPlanLayout l;
+  size_t at = 256;
+  l.units = at; at += attend_round(sizeof(AttendUnit) * (size_t)c.units);
+  l.joins = at; at += attend_round(sizeof(AttendJoin) * (size_t)c.joins);
+  l.seg_start = at; at += attend_round(4 * ((size_t)a->B + (size_t)a->n_groups + 1));
+  l.seqs = at; at += attend_round(16 * (size_t)a->B);
+  l.groups = at; at += attend_round(32 * (size_t)a->n_groups);
+  l.bytes = at;
+  return l;
+}
+// Workspace: sums fp32 [slot][KV head][16 rows][d], then (maximum, sum of weights) [slot][KV head][16 rows]
+inline size_t attend_sums_bytes(const sp_attend_args* a) {
+  return attend_round((size_t)attend_caps(a).slots * (size_t)a->H_kv * kSlotRows * (size_t)a->d * 4);
+}
+inline size_t attend_workspace(const sp_attend_args* a) {
+  return attend_sums_bytes(a) + attend_round((size_t)attend_caps(a).slots * (size_t)a->H_kv * kSlotRows * 8);
+}
+
+}  // namespace sp

@@ -36,12 +36,17 @@ void fill_score_dev(const sp_score_args* a, ScoreDev* p);
 // at position pos turns by pos * theta^(-2t/d).  The angle is formed in fp64, its cosine and sine
 // are rounded to fp32, the two products and their sum or difference are separate fp32
 // operations, and the result is rounded to bf16 (nearest even) as a cache would hold it -- every
-// kernel that rotates goes through these two functions, so all of them produce the same bits.
-__device__ __forceinline__ float2 rope_cos_sin(double pos, int t, int half, double log2_theta) {
-  const double inv_freq = exp2(-((double)t / (double)half) * log2_theta);
+// kernel that rotates goes through these functions, so all of them produce the same bits.
+__device__ __forceinline__ double rope_inv_freq(int t, int half, double log2_theta) {
+  return exp2(-((double)t / (double)half) * log2_theta);
+}
+__device__ __forceinline__ float2 rope_cos_sin_of(double angle) {
   double sn, cs;
-  sincos(pos * inv_freq, &sn, &cs);
+  sincos(angle, &sn, &cs);
   return make_float2((float)cs, (float)sn);
+}
+__device__ __forceinline__ float2 rope_cos_sin(double pos, int t, int half, double log2_theta) {
+  return rope_cos_sin_of(pos * rope_inv_freq(t, half, log2_theta));
 }
 // lo, hi: the pair's values (exact bf16 values held as fp32); returns the rotated pair before rounding
 __device__ __forceinline__ float2 rope_turn_exact(float lo, float hi, float2 cs) {

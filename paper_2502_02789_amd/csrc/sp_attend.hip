@@ -56,27 +56,37 @@ __device__ __forceinline__ void widen_e4m3(const u32x4 w, u32x4& lo, u32x4& hi) 
   }
 }
 
+// Where the rows of a piece's keys lie.  Tiles start at multiples of 8 keys and pages hold multiples of 8, so the 8 keys of an
+// octet lie at one stride from one base, which is looked up and formed in scalar registers, once for all lanes of a wave.
 template <bool PAGED>
-struct KeyRows {  // byte offsets of key rows
-  const int32_t* table;
-  int lg_page, first;
+struct KeyRows {
+  ScalarTable table;
+  int lg_page, first, last_key;
   uint32_t last;
-  int64_t ts, ps;
+  int32_t ts;
+  int64_t ps;
   __device__ __forceinline__ KeyRows(const AttendDev& p, const AttendUnit& u) {
-    ts = p.c_ts; ps = p.c_ps; lg_page = p.lg_page;
-    table = PAGED ? p.table + (int64_t)u.seq * p.blocks_per_seq : nullptr;
-    first = PAGED ? 0 : p.cu_cache[u.seq];
+    ts = p.c_ts; ps = p.c_ps; lg_page = p.lg_page; last_key = u.k1 - 1;
+    table = scalar_table(PAGED ? p.table + (int64_t)u.seq * p.blocks_per_seq : nullptr);
+    first = PAGED ? 0 : scalar_table(p.cu_cache)[u.seq];
     last = PAGED ? p.last_page : p.last_row;
   }
-  __device__ __forceinline__ uint32_t look_up(int key) const { return PAGED ? (uint32_t)table[key >> lg_page] : 0; }
-  // entry: what look_up() gave for this key; nothing outside the pool is addressed, a bad entry is noted
-  __device__ __forceinline__ int64_t offset(int key, uint32_t entry, bool& bad) const {
+  // first key of the octet that `key` (wave-uniform) lies in, no further than the last key's
+  __device__ __forceinline__ int octet(int key) const { return min(key, last_key) & ~7; }
+  __device__ __forceinline__ uint32_t look_up(int octet) const { return PAGED ? (uint32_t)table[octet >> lg_page] : 0; }
+  // byte offset of the octet's first key; entry: what look_up() gave.  Nothing outside the pool is addressed, a bad entry is noted.
+  __device__ __forceinline__ int64_t base(int octet, uint32_t entry, uint32_t& bad) const {
     if constexpr (PAGED) {
       bad |= entry > last;
-      return (int64_t)min(entry, last) * ps + (int64_t)(key & ((1 << lg_page) - 1)) * ts;
+      return (int64_t)min(entry, last) * ps + (int64_t)(octet & ((1 << lg_page) - 1)) * ts;
     } else {
-      return (int64_t)min((uint32_t)(first + key), last) * ts;
+      return (int64_t)min((uint32_t)(first + octet), last) * ts;
     }
+  }
+  // ... of `key` behind the octet's first: of the last key, where it lies beyond that (its weight is zero there, and it is finite)
+  __device__ __forceinline__ uint32_t within(int octet, int key) const {
+    if constexpr (PAGED) return (uint32_t)(min(key, last_key) - octet) * (uint32_t)ts;
+    else return (min((uint32_t)(first + min(key, last_key)), last) - min((uint32_t)(first + octet), last)) * (uint32_t)ts;
   }
 };
 
@@ -107,15 +117,32 @@ __device__ __forceinline__ void store_stats(const AttendDev& p, int64_t place, f
 }
 
 // ---------------------------------------------------------------- few rows
+// One wave's 32-key tile of keys or values on its way from memory to LDS.  A load instruction covers whole rows (256 bytes of
+// each of 4 keys, bf16 and d = 128), so that every request is for a whole line.
 template <int D, bool FP8>
 struct FewTile {
-  static constexpr int N = FP8 ? D / 64 : D / 32;  // 16-byte loads of a lane per key
-  u32x4 a[N], b[N];                                // keys (l & 15) and 16 + (l & 15) of the tile
-  __device__ __forceinline__ void load(const char* base, int64_t oa, int64_t ob) {
+  static constexpr int C = FP8 ? D / 16 : D / 8;  // 16-byte chunks of a stored row
+  static constexpr int R = 64 / C;                // rows of a load
+  static constexpr int N = 32 / R;                // loads of a tile
+  u32x4 x[N];
+  __device__ __forceinline__ void load(const char* base, const int64_t (&at)[N], const uint32_t (&in)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base + at[i] + in[i]));
+  }
+  __device__ __forceinline__ void store(char* tile, int l) const {  // as bf16
+    const int ch = l % C;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      a[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base + oa + 64 * i));
-      b[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base + ob + 64 * i));
+      const int r = l / C + R * i;
+      char* row = tile + r * (D * 2);
+      if constexpr (FP8) {
+        u32x4 lo, hi;
+        widen_e4m3(x[i], lo, hi);
+        *reinterpret_cast<u32x4*>(row + swizzled<D / 8>(r, 2 * ch) * 16) = lo;
+        *reinterpret_cast<u32x4*>(row + swizzled<D / 8>(r, 2 * ch + 1) * 16) = hi;
+      } else {
+        *reinterpret_cast<u32x4*>(row + swizzled<D / 8>(r, ch) * 16) = x[i];
+      }
     }
   }
 };
@@ -125,19 +152,59 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   constexpr int KS = D / 32;          // steps of the product with the queries
   constexpr int DB = D / 16;          // blocks of values
   constexpr int C = D / 8;            // 16-byte chunks of a bf16 row
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, row = l & 15, quad = l >> 4;
+  using Tile = FewTile<D, FP8>;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, row = l & 15, quad = l >> 4;
   const bool mine = row < u.nr;
   const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
+
+  const KeyRows<PAGED> rows(p, u);
+  const char* const kb = p.k + (int64_t)g * p.c_hs;
+  const char* const vb = p.v + (int64_t)g * p.c_hs;
+  char* const kd = lds + w * (2 * 32 * D * 2);
+  char* const vd = kd + 32 * D * 2;
+  const int lane_row = l / Tile::C, lane_chunk = (l % Tile::C) * 16;
+  uint32_t bad = 0;
+  Tile kt, vl;
+  int64_t oct_at[Tile::N];
+  uint32_t in[Tile::N], entry[4];
+  auto look_up = [&](int tile) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) entry[j] = rows.look_up(rows.octet(tile + 8 * j));
+  };
+  auto place = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < Tile::N; ++i) {
+      constexpr int R = Tile::R;
+      const int j = R * i / 8, oct = rows.octet(tile + 8 * j);
+      if constexpr (R <= 8) {
+        oct_at[i] = rows.base(oct, entry[j], bad);
+        in[i] = rows.within(oct, tile + R * i + lane_row) + lane_chunk;
+      } else {                        // a load covers two octets
+        const int oct1 = rows.octet(tile + 8 * j + 8);
+        const int64_t b0 = rows.base(oct, entry[j], bad), b1 = rows.base(oct1, entry[j + 1], bad);
+        const bool second = lane_row >= 8;
+        oct_at[i] = second ? b1 : b0;
+        in[i] = rows.within(second ? oct1 : oct, tile + R * i + lane_row) + lane_chunk;
+      }
+    }
+  };
+  int tile = u.k0 < u.k1 ? (u.k0 & ~31) + 32 * w : u.k1;
+  if (tile < u.k1) {
+    look_up(tile);
+    place(tile);
+    kt.load(kb, oct_at, in);
+    vl.load(vb, oct_at, in);
+    look_up(tile + 128);
+  }
+
+  // the queries
   uint32_t flip, keep;
   const float c = key_factor(p, g, flip, keep);
-
-  // the queries, in the order in which a key's chunks are loaded
   bf16x8 qf[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
-    const int d0 = FP8 ? (quad + 4 * (s >> 1)) * 16 + (s & 1) * 8 : s * 32 + quad * 8;
     u32x4 x = {0, 0, 0, 0};
-    if (mine) x = *reinterpret_cast<const u32x4*>(p.q + at.token * p.q_ts + at.h * p.q_hs + d0);
+    if (mine) x = *reinterpret_cast<const u32x4*>(p.q + at.token * p.q_ts + at.h * p.q_hs + s * 32 + quad * 8);
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = (x[i] ^ flip) & keep;
     qf[s] = __builtin_bit_cast(bf16x8, x);
@@ -150,124 +217,75 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
     for (int off = 8; off >= 1; off >>= 1) least = min(least, __shfl_xor(least, off, kWave));
     least = __builtin_amdgcn_readfirstlane(least);
   }
-
-  const KeyRows<PAGED> rows(p, u);
-  const char* const kb = p.k + (int64_t)g * p.c_hs + quad * 16;
-  const char* const vb = p.v + (int64_t)g * p.c_hs + quad * 16;
-  char* const vt = lds + w * (32 * D * 2);
-  const int last_key = u.k1 - 1;
-  bool bad = false;
   f32x4 o[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, sum = 0.f;
 
-  int tile = u.k0 + 32 * w;
-  if (tile < u.k1) {
-    FewTile<D, FP8> kt, vl;
-    int ka = min(tile + row, last_key), kc = min(tile + 16 + row, last_key);
-    {
-      const int64_t oa = rows.offset(ka, rows.look_up(ka), bad), ob = rows.offset(kc, rows.look_up(kc), bad);
-      kt.load(kb, oa, ob);
-      vl.load(vb, oa, ob);
+  for (; tile < u.k1; tile += 128) {
+    const bool more = tile + 128 < u.k1;
+    kt.store(kd, l);
+    if (more) {
+      place(tile + 128);
+      kt.load(kb, oct_at, in);
     }
-    int na = min(tile + 128 + row, last_key), nc = min(tile + 144 + row, last_key);
-    uint32_t ea = rows.look_up(na), ec = rows.look_up(nc);
-    for (; tile < u.k1; tile += 128) {
-      const bool more = tile + 128 < u.k1;
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-      if constexpr (FP8) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < KS / 2; ++i) {
-          u32x4 lo, hi;
-          widen_e4m3(kt.a[i], lo, hi);
-          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), qf[2 * i], s0, 0, 0, 0);
-          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), qf[2 * i + 1], s0, 0, 0, 0);
-          widen_e4m3(kt.b[i], lo, hi);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), qf[2 * i], s1, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), qf[2 * i + 1], s1, 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kt.a[s]), qf[s], s0, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kt.b[s]), qf[s], s1, 0, 0, 0);
-        }
-      }
-      int64_t oa = 0, ob = 0;
-      if (more) {
-        oa = rows.offset(na, ea, bad);
-        ob = rows.offset(nc, ec, bad);
-        na = min(tile + 256 + row, last_key);
-        nc = min(tile + 272 + row, last_key);
-        ea = rows.look_up(na);
-        ec = rows.look_up(nc);
-        kt.load(kb, oa, ob);
-      }
-      // values to LDS, as bf16
-#pragma unroll
-      for (int i = 0; i < FewTile<D, FP8>::N; ++i) {
-        if constexpr (FP8) {
-          const int ch = 2 * (quad + 4 * i);
-          u32x4 lo, hi;
-          widen_e4m3(vl.a[i], lo, hi);
-          *reinterpret_cast<u32x4*>(vt + row * (D * 2) + swizzled<C>(row, ch) * 16) = lo;
-          *reinterpret_cast<u32x4*>(vt + row * (D * 2) + swizzled<C>(row, ch + 1) * 16) = hi;
-          widen_e4m3(vl.b[i], lo, hi);
-          *reinterpret_cast<u32x4*>(vt + (16 + row) * (D * 2) + swizzled<C>(row, ch) * 16) = lo;
-          *reinterpret_cast<u32x4*>(vt + (16 + row) * (D * 2) + swizzled<C>(row, ch + 1) * 16) = hi;
-        } else {
-          const int ch = quad + 4 * i;
-          *reinterpret_cast<u32x4*>(vt + row * (D * 2) + swizzled<C>(row, ch) * 16) = vl.a[i];
-          *reinterpret_cast<u32x4*>(vt + (16 + row) * (D * 2) + swizzled<C>(row, ch) * 16) = vl.b[i];
-        }
-      }
-      if (more) vl.load(vb, oa, ob);
+    for (int s = 0; s < KS; ++s) {
+      const char* at0 = kd + row * (D * 2) + swizzled<C>(row, 4 * s + quad) * 16;  // (rows 16 apart are permuted alike)
+      s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(at0), qf[s], s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(at0 + 16 * D * 2), qf[s], s1, 0, 0, 0);
+    }
+    vl.store(vd, l);
+    if (more) {
+      vl.load(vb, oct_at, in);
+      look_up(tile + 256);
+    }
 
-      float x[8];
+    float x[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { x[i] = s0[i] * c; x[4 + i] = s1[i] * c; }
-      if (tile + 32 > least) {
+    for (int i = 0; i < 4; ++i) { x[i] = s0[i] * c; x[4 + i] = s1[i] * c; }
+    if (tile + 32 > least || tile < u.k0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (tile + 4 * quad + i >= limit) x[i] = -INFINITY;
-          if (tile + 16 + 4 * quad + i >= limit) x[4 + i] = -INFINITY;
-        }
+      for (int i = 0; i < 8; ++i) {
+        const int key = tile + 16 * (i >> 2) + 4 * quad + (i & 3);
+        if (key >= limit || key < u.k0) x[i] = -INFINITY;
       }
-      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
-        top = fmaxf(top, __shfl_xor(top, 16, kWave));
-        top = fmaxf(top, __shfl_xor(top, 32, kWave));
-        const float next = fmaxf(m, top);
-        const float f = next == -INFINITY ? 1.f : fast_exp2(m - next);
-        m = next;
-        sum *= f;
-#pragma unroll
-        for (int i = 0; i < DB; ++i) o[i] *= f;
-      }
-      const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) { x[i] = fast_exp2(x[i] - base); sum += x[i]; }
-      const u32x4 pw = {pack_bf16_pair(x[0], x[1]), pack_bf16_pair(x[2], x[3]), pack_bf16_pair(x[4], x[5]), pack_bf16_pair(x[6], x[7])};
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      const int vr = 4 * quad + ((l & 15) >> 2);  // row of the tile that this lane reads from (and 16 + that)
-#pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        const int ch = 2 * i + ((l & 3) >> 1);
-        const char* at0 = vt + vr * (D * 2) + swizzled<C>(vr, ch) * 16 + (l & 1) * 8;
-        const bf16x8 vf = join8(lds_read_tr(at0), lds_read_tr(at0 + 16 * D * 2));
-        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[i], 0, 0, 0);
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 16, kWave));
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      const float next = fmaxf(m, top);
+      const float f = next == -INFINITY ? 1.f : fast_exp2(m - next);
+      m = next;
+      sum *= f;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) o[i] *= f;
+    }
+    const float base_m = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { x[i] = fast_exp2(x[i] - base_m); sum += x[i]; }
+    const u32x4 pw = {pack_bf16_pair(x[0], x[1]), pack_bf16_pair(x[2], x[3]), pack_bf16_pair(x[4], x[5]), pack_bf16_pair(x[6], x[7])};
+    const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int vr = 4 * quad + ((l & 15) >> 2);  // row of the tile that this lane reads from (and 16 + that)
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+      const int ch = 2 * i + ((l & 3) >> 1);
+      const char* at0 = vd + vr * (D * 2) + swizzled<C>(vr, ch) * 16 + (l & 1) * 8;
+      const bf16x8 vf = join8(lds_read_tr(at0), lds_read_tr(at0 + 16 * D * 2));
+      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[i], 0, 0, 0);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
   // the four waves' sums joined, in the waves' order
   sum += __shfl_xor(sum, 16, kWave);
   sum += __shfl_xor(sum, 32, kWave);
   float* const stat = reinterpret_cast<float*>(lds + 4 * 16 * (D + 4) * 4);  // [2][4][16]
-  const int any_bad = __syncthreads_or(bad);  // (also: every wave is done with its tile in LDS)
+  const int any_bad = __syncthreads_or(bad != 0);  // (also: every wave is done with its tile in LDS)
   if (quad == 0) {
     stat[w * 16 + row] = m;
     stat[64 + w * 16 + row] = sum;
@@ -327,9 +345,9 @@ struct ManyTile {
   static constexpr int N = kTileKeys * C / 256;
   static constexpr int STEP = 256 / C;                     // rows between a lane's chunks
   u32x4 x[N];
-  __device__ __forceinline__ void load(const char* base, const int64_t (&off)[N]) {
+  __device__ __forceinline__ void load(const char* base, const int64_t (&at)[N], const uint32_t (&in)[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const u32x4*>(base + off[i]);
+    for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const u32x4*>(base + at[i] + in[i]);
   }
   __device__ __forceinline__ void store(char* tile, int tid) const {
     const int ch = tid % C;
@@ -356,7 +374,7 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
   constexpr int C = D / 8;
   constexpr int TILE = kTileKeys * D * 2;  // bytes of a tile of keys or of values
   using Tile = ManyTile<D, FP8>;
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, half = l >> 5;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, half = l >> 5;
   const int row = w * 32 + (l & 31);
   const bool mine = row < u.nr;
   const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
@@ -384,11 +402,10 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
   most = __builtin_amdgcn_readfirstlane(most);
 
   const KeyRows<PAGED> rows(p, u);
-  const int ch = tid % Tile::C, kr = tid / Tile::C;
-  const char* const kb = p.k + (int64_t)g * p.c_hs + ch * 16;
-  const char* const vb = p.v + (int64_t)g * p.c_hs + ch * 16;
-  const int last_key = u.k1 - 1;
-  bool bad = false;
+  const char* const kb = p.k + (int64_t)g * p.c_hs;
+  const char* const vb = p.v + (int64_t)g * p.c_hs;
+  const int lane_row = l / Tile::C, lane_chunk = (l % Tile::C) * 16;
+  uint32_t bad = 0;
 
   f32x16 o[DB];
 #pragma unroll
@@ -409,26 +426,42 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       v_at[i][x] = vr * (D * 2) + swizzled<C>(vr, 4 * i + 2 * ((l >> 4) & 1) + ((l & 3) >> 1)) * 16 + (l & 1) * 8;
     }
 
+  // the wave's loads cover rows w R + STEP i of a tile, R <= 8 of one octet or R = 16 of two
+  constexpr int R = 64 / Tile::C, O = R > 8 ? 2 : 1;
   Tile kt, vl;
-  uint32_t entry[Tile::N];
-  int64_t off[Tile::N];
+  uint32_t entry[Tile::N][O];
   auto look_up = [&](int tile) {
 #pragma unroll
-    for (int i = 0; i < Tile::N; ++i) entry[i] = rows.look_up(min(tile + kr + Tile::STEP * i, last_key));
+    for (int i = 0; i < Tile::N; ++i)
+#pragma unroll
+      for (int j = 0; j < O; ++j) entry[i][j] = rows.look_up(rows.octet(tile + R * w + Tile::STEP * i + 8 * j));
   };
   auto load = [&](int tile) {
+    int64_t at[Tile::N];
+    uint32_t in[Tile::N];
 #pragma unroll
-    for (int i = 0; i < Tile::N; ++i) off[i] = rows.offset(min(tile + kr + Tile::STEP * i, last_key), entry[i], bad);
-    kt.load(kb, off);
-    vl.load(vb, off);
+    for (int i = 0; i < Tile::N; ++i) {
+      const int first = tile + R * w + Tile::STEP * i;
+      int oct = rows.octet(first);
+      at[i] = rows.base(oct, entry[i][0], bad);
+      if constexpr (O == 2) {
+        const int oct1 = rows.octet(first + 8);
+        const int64_t at1 = rows.base(oct1, entry[i][1], bad);
+        if (lane_row >= 8) { at[i] = at1; oct = oct1; }
+      }
+      in[i] = rows.within(oct, first + lane_row) + lane_chunk;
+    }
+    kt.load(kb, at, in);
+    vl.load(vb, at, in);
   };
-  if (u.k0 < u.k1) {
-    look_up(u.k0);
-    load(u.k0);
-    look_up(min(u.k0 + kTileKeys, last_key));
+  const int first_tile = u.k0 < u.k1 ? u.k0 & ~(kTileKeys - 1) : u.k1;
+  if (first_tile < u.k1) {
+    look_up(first_tile);
+    load(first_tile);
+    look_up(first_tile + kTileKeys);
   }
   int buffer = 0;
-  for (int tile = u.k0; tile < u.k1; tile += kTileKeys, buffer ^= 2 * TILE) {
+  for (int tile = first_tile; tile < u.k1; tile += kTileKeys, buffer ^= 2 * TILE) {
     char* const kd = lds + buffer;
     char* const vd = kd + TILE;
     kt.store(kd, tid);
@@ -436,7 +469,7 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
     __syncthreads();
     if (tile + kTileKeys < u.k1) {
       load(tile + kTileKeys);
-      look_up(min(tile + 2 * kTileKeys, last_key));
+      look_up(tile + 2 * kTileKeys);
     }
     if (tile >= most) continue;  // (the wave's rows see none of these keys)
     f32x16 s[2];
@@ -450,12 +483,14 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
         s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[x], 0, 0, 0);
       }
     }
-    if (tile + kTileKeys > least) {
+    if (tile + kTileKeys > least || tile < u.k0) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (tile + 32 * x + 8 * (j >> 2) + 4 * half + (j & 3) >= limit) s[x][j] = -INFINITY;
+        for (int j = 0; j < 16; ++j) {
+          const int key = tile + 32 * x + 8 * (j >> 2) + 4 * half + (j & 3);
+          if (key >= limit || key < u.k0) s[x][j] = -INFINITY;
+        }
     }
     float top = s[0][0];
 #pragma unroll
@@ -497,7 +532,7 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       }
   }
 
-  const int any_bad = __syncthreads_or(bad);
+  const int any_bad = __syncthreads_or(bad != 0);
   sum += __shfl_xor(sum, 32, kWave);
   if (!mine) return;
   if (u.slot >= 0) {
@@ -544,15 +579,22 @@ __device__ __forceinline__ void nan_rows(const AttendDev& p, int d, int64_t r0, 
 template <int D, bool FP8, bool PAGED>
 __global__ __launch_bounds__(256, 2) void attend_kernel(const AttendDev p) {
   __shared__ __align__(16) char lds[2 * 2 * kTileKeys * D * 2];  // (few rows need 34 KB of the 64, or 17.5 of the 32)
-  if (p.header->print != p.print) {
-    nan_rows(p, D, 0, (int64_t)p.T_new * p.H, p.H, 0, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
-    return;
-  }
   // The KV heads of a piece are neighbours: with eight of them, each has the L2 of one XCD, which the rows of a
   // block share, as workgroups go to the XCDs in turn.
   const int n = (int)(blockIdx.x / (uint32_t)p.H_kv), g = (int)(blockIdx.x % (uint32_t)p.H_kv);
-  if (n >= p.header->n_units) return;
-  const AttendUnit u = p.units[n];
+  // header and piece through the scalar cache, together (the list has room for every workgroup's index)
+  const auto header = reinterpret_cast<const __attribute__((address_space(4))) AttendHeader*>(reinterpret_cast<uintptr_t>(p.header));
+  const auto units = reinterpret_cast<const __attribute__((address_space(4))) AttendUnit*>(reinterpret_cast<uintptr_t>(p.units));
+  const uint64_t print = header->print;
+  const int n_units = header->n_units;
+  AttendUnit u;
+  u.r0 = units[n].r0; u.nr = units[n].nr; u.seq = units[n].seq; u.k0 = units[n].k0;
+  u.k1 = units[n].k1; u.off = units[n].off; u.slot = units[n].slot; u.bad = units[n].bad;
+  if (print != p.print) {
+    nan_rows(p, D, 0, (int64_t)p.T_new * p.H, p.H, 0, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+    return;
+  }
+  if (n >= n_units) return;
   if (u.bad) {
     nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, 256);
     return;
@@ -569,6 +611,7 @@ sp_status check_attend(const sp_attend_args* a) {
   if (!finite_f32(a->scale) || a->scale <= 0.f) return SP_EINVAL;
   const bool fp8 = a->cache_dtype == SP_K_FP8_E4M3;
   if (!fp8 && (a->d_k_scale || a->d_v_scale)) return SP_EINVAL;
+  if (a->cache_token_stride >= INT64_C(1) << 26) return SP_EINVAL;
   if (!a->d_q || !a->d_k_cache || !a->d_v_cache || !a->d_out) return SP_ENULL;
   const int64_t row[] = {a->q_token_stride, a->q_head_stride, a->out_token_stride, a->out_head_stride};
   const int64_t cache[] = {a->cache_token_stride, a->cache_head_stride, a->d_block_table ? a->cache_page_stride : 0};
@@ -613,15 +656,14 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.blocks_per_seq = a->blocks_per_seq;
   p.last_page = paged ? (uint32_t)(a->n_rows / a->page_size - 1) : 0;
   p.last_row = (uint32_t)(a->n_rows - 1);
-  p.join_slices = (int64_t)a->T_new * p.G > kFewRows ? kManyRows / kSlotRows : 1;
   p.scale_log2 = a->scale * 1.44269504088896340736f;
   p.q_ts = a->q_token_stride; p.q_hs = a->q_head_stride;
   p.o_ts = a->out_token_stride; p.o_hs = a->out_head_stride;
-  p.c_ts = a->cache_token_stride * E; p.c_hs = a->cache_head_stride * E; p.c_ps = a->cache_page_stride * E;
+  p.c_ts = (int32_t)(a->cache_token_stride * E); p.c_hs = a->cache_head_stride * E; p.c_ps = a->cache_page_stride * E;
   p.print = attend_print(a);
   p.header = reinterpret_cast<const AttendHeader*>(base);
   p.units = reinterpret_cast<const AttendUnit*>(base + l.units);
-  p.joins = reinterpret_cast<const AttendJoin*>(base + l.joins);
+  p.rows = reinterpret_cast<const AttendRow*>(base + l.rows);
   p.table = a->d_block_table; p.cu_cache = a->d_cu_cache;
   p.q = static_cast<const uint16_t*>(a->d_q);
   p.k = static_cast<const char*>(a->d_k_cache); p.v = static_cast<const char*>(a->d_v_cache);
@@ -633,6 +675,6 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   const uint32_t grid = (uint32_t)(caps.units * a->H_kv);
   if (a->d == 128) fp8 ? launch_attend<128, true>(p, paged, grid, stream) : launch_attend<128, false>(p, paged, grid, stream);
   else fp8 ? launch_attend<64, true>(p, paged, grid, stream) : launch_attend<64, false>(p, paged, grid, stream);
-  launch_attend_join(p, a->d, caps.joins * p.join_slices * a->H_kv, stream);
+  launch_attend_join(p, a->d, caps.rows * a->H_kv, stream);
   return launch_status();
 }

@@ -12,14 +12,14 @@ struct AttendDev {
   int B, H, H_kv, G, T_new;
   int lg_page, blocks_per_seq;
   uint32_t last_page, last_row;  // of the pool, of a contiguous cache
-  int join_slices;               // 16-row slices that a join entry may have
   float scale_log2;              // logit scale times log2(e)
   int64_t q_ts, q_hs, o_ts, o_hs;
-  int64_t c_ts, c_hs, c_ps;      // of the cache, in bytes
+  int32_t c_ts;                  // of the cache, in bytes
+  int64_t c_hs, c_ps;
   uint64_t print;
   const AttendHeader* header;
   const AttendUnit* units;
-  const AttendJoin* joins;
+  const AttendRow* rows;
   const int32_t* table;
   const int32_t* cu_cache;
   const uint16_t* q;
@@ -35,6 +35,6 @@ struct AttendDev {
 
 sp_status check_attend_shape(const sp_attend_args* a);
 sp_status check_attend_plan_args(const sp_attend_args* a);
-void launch_attend_join(const AttendDev& p, int d, int64_t items, hipStream_t stream);
+void launch_attend_join(const AttendDev& p, int d, int64_t rows, hipStream_t stream);
 
 }  // namespace sp

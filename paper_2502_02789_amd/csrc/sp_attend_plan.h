@@ -43,17 +43,26 @@ struct AttendJoin {   // one block of a sequence's own rows that slots are joine
   int32_t r0, nr;
   int32_t own_slot, own_pieces, own_step;           // slot of the first piece, pieces, slots of a piece
   int32_t pre_slot, pre_pieces, pre_r0, pre_rows;   // the group's prefix: slot of its first block, pieces of a block (0: none), its first row, rows of a block
-  int32_t pad[3];
+  int32_t first;                                    // its first row among all that are joined
+  int32_t pad[2];
+};
+struct AttendRow {    // one of these rows: where its sums are, slot * 16 + row of the slot (KV heads aside), and how far apart
+  int32_t row;
+  int32_t own_at, own_pieces, own_step;
+  int32_t pre_at, pre_pieces, pre_step;
+  int32_t pad;
 };
 struct AttendHeader {
   uint64_t print;     // of the shape fields the plan was made for
-  int32_t n_units, n_joins, n_slots, pad;
+  int32_t n_units, n_rows;  // pieces, rows to join
+  int32_t most_pieces;      // of a row to join
+  int32_t n_slots;
 };
 
 constexpr int kNoLimit = 0x7fffffff;
 
 struct AttendCaps {
-  int64_t blocks, units, joins, slots;
+  int64_t blocks, units, joins, rows, slots;
 };
 
 // Upper bounds for any lengths that the shape fields allow.  Blocks: a segment of R rows has at most R / 128 + 1; own segments
@@ -70,6 +79,9 @@ inline AttendCaps attend_caps(const sp_attend_args* a) {
   c.blocks = own + prefix;
   c.units = c.blocks + added;
   c.joins = own;
+  // rows to join: of blocks that are cut (of which there are at most as many as pieces added) and of sequences that share
+  const int64_t cut_rows = kManyRows * added + (a->n_groups ? shared_rows : 0);
+  c.rows = rows < cut_rows ? rows : cut_rows;
   // blocks that may leave sums, in blocks of 128 rows and in all; own segments of over 16 rows: at most one per 17
   const int64_t big_segments = own_segments < rows / (kFewRows + 1) ? own_segments : rows / (kFewRows + 1);
   const int64_t shared_big = a->n_groups ? 2 * (shared_rows / kManyRows) + big_segments + (groups < rows / (kFewRows + 1) ? groups : rows / (kFewRows + 1)) : 0;
@@ -110,11 +122,12 @@ SP_ATTEND_FN int make_cut(int64_t total, int H_kv) {
   return cut < kMinPiece ? kMinPiece : cut > 0x40000000 ? 0x40000000 : (int)cut;
 }
 SP_ATTEND_FN int pieces_of(int keys, int cut) { return keys <= cut ? 1 : (int)(((int64_t)keys + cut - 1) / cut); }
-// first key (counted from the block's first) of piece p
-SP_ATTEND_FN int piece_start(int keys, int pieces, int p) {
-  const int steps = (keys + kPieceStep - 1) / kPieceStep;
-  const int64_t s = (int64_t)steps * p / pieces * kPieceStep;
-  return s < keys ? (int)s : keys;
+// First key of piece p of a block with keys [first, first + keys); pieces are cut at multiples of 64 keys of the sequence, so
+// that only a block's first and last tile are not whole
+SP_ATTEND_FN int piece_start(int first, int keys, int pieces, int p) {
+  if (p == 0 || p == pieces) return p == 0 ? first : first + keys;
+  const int base = first & ~(kPieceStep - 1), steps = (int)(((int64_t)first - base + keys + kPieceStep - 1) / kPieceStep);
+  return base + (int)((int64_t)steps * p / pieces) * kPieceStep;
 }
 
 SP_ATTEND_FN uint64_t attend_print(const sp_attend_args* a) {
@@ -131,7 +144,7 @@ SP_ATTEND_FN uint64_t attend_print(const sp_attend_args* a) {
 
 // Offsets of the parts of d_plan
 struct AttendPlanLayout {
-  size_t units, joins, seg_start, seqs, groups, bytes;
+  size_t units, joins, rows, seg_start, seqs, groups, bytes;
 };
 inline size_t attend_round(size_t x) { return (x + 255) / 256 * 256; }
 inline AttendPlanLayout attend_plan_layout(const sp_attend_args* a) {
@@ -140,6 +153,7 @@ inline AttendPlanLayout attend_plan_layout(const sp_attend_args* a) {
   size_t at = 256;
   l.units = at; at += attend_round(sizeof(AttendUnit) * (size_t)c.units);
   l.joins = at; at += attend_round(sizeof(AttendJoin) * (size_t)c.joins);
+  l.rows = at; at += attend_round(sizeof(AttendRow) * (size_t)c.rows);
   l.seg_start = at; at += attend_round(4 * ((size_t)a->B + (size_t)a->n_groups + 1));
   l.seqs = at; at += attend_round(16 * (size_t)a->B);
   l.groups = at; at += attend_round(32 * (size_t)a->n_groups);

@@ -13,11 +13,12 @@ struct PlanGroup { int32_t shared, active, t0, tokens, slot, pieces, pad[2]; };
 struct PlanDev {
   sp_attend_args a;   // (host pointers in it are not used)
   int G;
-  int64_t cap_units, cap_joins, cap_slots;
+  int64_t cap_units, cap_joins, cap_rows, cap_slots;
   uint64_t print;
   AttendHeader* header;
   AttendUnit* units;
   AttendJoin* joins;
+  AttendRow* rows;
   int32_t* seg_start;
   PlanSeq* seqs;
   PlanGroup* groups;
@@ -31,21 +32,32 @@ __device__ __forceinline__ int group_of(const PlanDev& p, int b) {
   return upper_segment(p.a.d_cu_group, n, b);
 }
 
-// exclusive prefix of v over the workgroup's 1024 threads, and the sum over all of them
-__device__ __forceinline__ int64_t block_exclusive(int64_t v, int64_t* lds, int64_t* total) {
-  const int t = threadIdx.x;
-  lds[t] = v;
-  __syncthreads();
-  for (int off = 1; off < 1024; off <<= 1) {
-    const int64_t x = t >= off ? lds[t - off] : 0;
-    __syncthreads();
-    lds[t] += x;
-    __syncthreads();
+// exclusive prefixes of N numbers over the workgroup's 1024 threads, and their sums over all of them
+template <int N>
+__device__ __forceinline__ void block_exclusive(int64_t (&v)[N], int64_t (&total)[N]) {
+  __shared__ int64_t waves[16][N];
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    int64_t x = v[i];
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int64_t y = __shfl_up(x, off, kWave);
+      if (l >= off) x += y;
+    }
+    if (l == 63) waves[w][i] = x;
+    v[i] = x - v[i];
   }
-  const int64_t incl = lds[t];
-  *total = lds[1023];
   __syncthreads();
-  return incl - v;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    total[i] = 0;
+    for (int x = 0; x < 16; ++x) {
+      if (x == w) v[i] += total[i];
+      total[i] += waves[x][i];
+    }
+  }
+  __syncthreads();
 }
 
 struct Block {       // a block of rows, as the walk over all blocks meets it
@@ -57,9 +69,12 @@ struct Block {       // a block of rows, as the walk over all blocks meets it
 }  // namespace
 
 __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
-  __shared__ int64_t scan[1024];
+  __shared__ int most_pieces;
   const int tid = threadIdx.x, B = p.a.B, n_groups = p.a.n_groups, G = p.G, T = (int)p.a.T_new;
-  if (tid == 0) p.header->print = 0;
+  if (tid == 0) {
+    p.header->print = 0;
+    most_pieces = 0;
+  }
 
   // the sequences' new tokens and lengths, as far as they are valid
   for (int b = tid; b < B; b += 1024) {
@@ -142,28 +157,30 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       visit(k);
     }
   };
-  int64_t keys = 0, total_keys;
-  walk([&](const Block& k) { keys += k.keys; });
-  block_exclusive(keys, scan, &total_keys);
-  const int cut = make_cut(total_keys, p.a.H_kv);
+  int64_t keys[1] = {0}, total_keys[1];
+  walk([&](const Block& k) { keys[0] += k.keys; });
+  block_exclusive(keys, total_keys);
+  const int cut = make_cut(total_keys[0], p.a.H_kv);
   auto joined = [&](const Block& k) { return k.seg >= n_groups && p.seqs[k.seg - n_groups].shared > 0; };
   auto leaves_sums = [&](const Block& k, int pieces) { return pieces > 1 || k.seg < n_groups || joined(k); };
 
-  int64_t units = 0, slots = 0, joins = 0, n_units, n_slots, n_joins;
+  enum { kUnits, kSlots, kJoins, kRows };
+  int64_t at[4] = {0, 0, 0, 0}, n[4];
+  auto rows_of = [&](const Block& k) { return (int)min((int64_t)block_rows(k.rows), k.rows - (int64_t)k.i * block_rows(k.rows)); };
   walk([&](const Block& k) {
     const int pieces = pieces_of(k.keys, cut);
-    units += pieces;
+    at[kUnits] += pieces;
     if (leaves_sums(k, pieces)) {
-      slots += (int64_t)pieces * (block_rows(k.rows) / kSlotRows);
-      joins += k.seg >= n_groups;
+      at[kSlots] += (int64_t)pieces * (block_rows(k.rows) / kSlotRows);
+      at[kJoins] += k.seg >= n_groups;
+      at[kRows] += k.seg >= n_groups ? rows_of(k) : 0;
     }
   });
-  units = block_exclusive(units, scan, &n_units);
-  slots = block_exclusive(slots, scan, &n_slots);
-  joins = block_exclusive(joins, scan, &n_joins);
-  if (n_units > p.cap_units || n_slots > p.cap_slots || n_joins > p.cap_joins) return;  // offsets that do not ascend: no plan
+  block_exclusive(at, n);
+  // (offsets that do not ascend may ask for more than there is room for: no plan then)
+  if (n[kUnits] > p.cap_units || n[kSlots] > p.cap_slots || n[kJoins] > p.cap_joins || n[kRows] > p.cap_rows) return;
 
-  int64_t u = units, slot = slots;
+  int64_t u = at[kUnits], slot = at[kSlots];
   walk([&](const Block& k) {
     const int pieces = pieces_of(k.keys, cut), m = block_rows(k.rows), step = m / kSlotRows;
     const bool sums = leaves_sums(k, pieces);
@@ -187,10 +204,10 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       unit.bad = s.len < 0;
     }
     unit.r0 = t0 * G + k.i * m;
-    unit.nr = (int)min((int64_t)m, k.rows - (int64_t)k.i * m);
+    unit.nr = rows_of(k);
     for (int q = 0; q < pieces; ++q) {
-      unit.k0 = first + piece_start(k.keys, pieces, q);
-      unit.k1 = first + piece_start(k.keys, pieces, q + 1);
+      unit.k0 = piece_start(first, k.keys, pieces, q);
+      unit.k1 = piece_start(first, k.keys, pieces, q + 1);
       unit.slot = sums ? (int)(slot + (int64_t)q * step) : -1;
       p.units[u + q] = unit;
     }
@@ -198,8 +215,8 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     if (sums) slot += (int64_t)pieces * step;
   });
   __syncthreads();
-  slot = slots;
-  int64_t j = joins;
+  slot = at[kSlots];
+  int64_t j = at[kJoins], row = at[kRows];
   walk([&](const Block& k) {
     const int pieces = pieces_of(k.keys, cut), m = block_rows(k.rows), step = m / kSlotRows;
     if (!leaves_sums(k, pieces)) return;
@@ -207,7 +224,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       const int b = k.seg - n_groups;
       AttendJoin e = {};
       e.r0 = p.seqs[b].t0 * G + k.i * m;
-      e.nr = (int)min((int64_t)m, k.rows - (int64_t)k.i * m);
+      e.nr = rows_of(k);
       e.own_slot = (int)slot;
       e.own_pieces = pieces;
       e.own_step = step;
@@ -218,85 +235,130 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
         e.pre_r0 = g.t0 * G;
         e.pre_rows = block_rows((int64_t)g.tokens * G);
       }
+      e.first = (int)row;
+      row += e.nr;
+      atomicMax(&most_pieces, e.own_pieces + e.pre_pieces);
       p.joins[j++] = e;
     }
     slot += (int64_t)pieces * step;
   });
   __syncthreads();
+  // a wave for each block that is joined, a lane for each row
+  for (int64_t x = tid >> 6; x < n[kJoins]; x += 16) {
+    const AttendJoin e = p.joins[x];
+    for (int r = tid & 63; r < e.nr; r += 64) {
+      AttendRow o = {};
+      o.row = e.r0 + r;
+      o.own_at = e.own_slot * kSlotRows + r;
+      o.own_pieces = e.own_pieces;
+      o.own_step = e.own_step * kSlotRows;
+      if (e.pre_pieces > 0) {
+        const int in = o.row - e.pre_r0, block = in / e.pre_rows;
+        o.pre_at = (e.pre_slot + block * e.pre_pieces * (e.pre_rows / kSlotRows)) * kSlotRows + in % e.pre_rows;
+        o.pre_pieces = e.pre_pieces;
+        o.pre_step = e.pre_rows;
+      }
+      p.rows[e.first + r] = o;
+    }
+  }
   if (tid == 0) {
-    p.header->n_units = (int)n_units;
-    p.header->n_joins = (int)n_joins;
-    p.header->n_slots = (int)n_slots;
+    p.header->n_units = (int)n[kUnits];
+    p.header->n_rows = (int)n[kRows];
+    p.header->n_slots = (int)n[kSlots];
+    p.header->most_pieces = most_pieces;
     p.header->print = p.print;
   }
 }
 
-// Rows of several pieces: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^(m_p - max m), in the pieces' order, so that results
-// do not depend on when the pieces were done.  A workgroup takes 16 rows of one KV head, 16 lanes a row, 8 (or 4) values a lane.
-// (compiled with NaNs honoured: pieces mark invalid rows by a NaN in l)
+// Rows of several pieces: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^(m_p - max m), added in an order that the plan alone
+// fixes.  Bound by its dependent reads (record, maxima, sums) where rows are few and by reading the sums where they are many: d / 4 lanes
+// take a row's pieces one after the other, 16 bytes a lane; with more than 16 pieces to a row all of the workgroup's
+// lanes take one row, every eighth (sixteenth, d = 64) piece each group of lanes.  (Compiled with NaNs honoured: invalid rows
+// have a NaN for l.)
 template <int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(const AttendDev p) {
-  constexpr int V = D / 16;
+  constexpr int L = D / 4, GROUPS = 256 / L;
+  __shared__ float4 part[GROUPS][L];
+  __shared__ float2 stat[GROUPS];
   if (p.header->print != p.print) return;  // (the pieces' kernel has filled the outputs)
-  const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
-  const int64_t n_items = (int64_t)p.header->n_joins * p.join_slices * p.H_kv;
-  for (int64_t item = blockIdx.x; item < n_items; item += gridDim.x) {
+  const int n_rows = p.header->n_rows;
+  const bool together = p.header->most_pieces > 16;
+  const int group = threadIdx.x / L, c = threadIdx.x % L, step = together ? GROUPS : 1, first = together ? group : 0;
+  const int64_t n_items = (int64_t)n_rows * p.H_kv, stride = (int64_t)gridDim.x * (together ? 1 : GROUPS);
+  for (int64_t item0 = (int64_t)blockIdx.x * (together ? 1 : GROUPS); item0 < n_items; item0 += stride) {
+    const int64_t item = together ? item0 : item0 + group;
+    const bool active = item < n_items;
     const int g = (int)(item % p.H_kv);
-    const int64_t e_i = item / p.H_kv;
-    const AttendJoin e = p.joins[e_i / p.join_slices];
-    const int slice = (int)(e_i % p.join_slices), r = slice * kSlotRows + row;
-    if (r >= e.nr) continue;
-    const int64_t flat = (int64_t)e.r0 + r;
-    const int own = e.own_slot + slice;
-    int pre = 0, pre_row = 0, pre_step = 0;
-    if (e.pre_pieces > 0) {
-      const int64_t at = flat - e.pre_r0;
-      const int block = (int)(at / e.pre_rows), in = (int)(at % e.pre_rows);
-      pre_step = e.pre_rows / kSlotRows;
-      pre = e.pre_slot + block * e.pre_pieces * pre_step + in / kSlotRows;
-      pre_row = in % kSlotRows;
-    }
-    const int n = e.own_pieces + e.pre_pieces;
+    AttendRow r = {};
+    if (active) r = p.rows[item / p.H_kv];
+    const int n = r.own_pieces + r.pre_pieces, mine = n > first ? (n - first + step - 1) / step : 0;
     // index of piece q's row among all rows of the workspace
     auto place = [&](int q) -> int64_t {
-      const bool mine = q < e.own_pieces;
-      const int64_t slot = mine ? own + (int64_t)q * e.own_step : pre + (int64_t)(q - e.own_pieces) * pre_step;
-      return (slot * p.H_kv + g) * kSlotRows + (mine ? row : pre_row);
+      const int at = q < r.own_pieces ? r.own_at + q * r.own_step : r.pre_at + (q - r.own_pieces) * r.pre_step;
+      return ((int64_t)(at / kSlotRows) * p.H_kv + g) * kSlotRows + at % kSlotRows;
     };
-    float top = -INFINITY;
-    for (int q = c; q < n; q += 16) top = fmaxf(top, p.stats[place(q)].x);
+    float top = -INFINITY, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int q0 = 0; q0 < mine; q0 += L) {  // a lane holds the factor of one piece
+      float2 s = make_float2(-INFINITY, 0.f);
+      if (q0 + c < mine) s = p.stats[place(first + (q0 + c) * step)];
+      float next = s.x;
 #pragma unroll
-    for (int off = 8; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 16));
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, acc[V] = {};
-#pragma unroll 4
-    for (int q = 0; q < n; ++q) {
-      const int64_t at = place(q);
-      const float2 s = p.stats[at];
-      const float f = exp2f(s.x - base);
-      sum += f * s.y;
-      const float* o = p.sums + at * D + c * V;
+      for (int off = L / 2; off >= 1; off >>= 1) next = fmaxf(next, __shfl_xor(next, off, L));
+      next = fmaxf(next, top);
+      const float base = next == -INFINITY ? 0.f : next, old = exp2f(top - base), f = exp2f(s.x - base);
+      float add = f * s.y;
 #pragma unroll
-      for (int i = 0; i < V; i += 4) {
-        const float4 x = *reinterpret_cast<const float4*>(o + i);
-        acc[i] += f * x.x; acc[i + 1] += f * x.y; acc[i + 2] += f * x.z; acc[i + 3] += f * x.w;
+      for (int off = L / 2; off >= 1; off >>= 1) add += __shfl_xor(add, off, L);
+      top = next;
+      sum = sum * old + add;
+      acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
+      const int count = min(L, mine - q0);
+      for (int q = 0; q < count; q += 8) {  // (beyond the last: its values again, with a factor of zero)
+        float4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          x[i] = *reinterpret_cast<const float4*>(p.sums + place(first + (q0 + min(q + i, count - 1)) * step) * D + c * 4);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float w = __shfl(f, q + i, L);
+          acc.x += w * x[i].x; acc.y += w * x[i].y; acc.z += w * x[i].z; acc.w += w * x[i].w;
+        }
       }
     }
-    const int64_t token = flat / p.G;
-    const int h = g * p.G + (int)(flat % p.G);
-    const float mul = (sum == 0.f ? 0.f : 1.f / sum) * (p.v_scale ? p.v_scale[g] : 1.f);
-    uint32_t w[V / 2];
+    if (together) {  // the groups' sums, in their order
+      part[group][c] = acc;
+      if (c == 0) stat[group] = make_float2(top, sum);
+      __syncthreads();
+      if (group == 0) {
+        top = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < V; i += 2) w[i / 2] = pack_bf16_pair(acc[i] * mul, acc[i + 1] * mul);
-    uint16_t* dst = p.out + token * p.o_ts + h * p.o_hs + c * V;
-    if constexpr (V == 8) *reinterpret_cast<u32x4*>(dst) = u32x4{w[0], w[1], w[2], w[3]};
-    else *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-    if (c == 0 && p.lse) p.lse[token * p.H + h] = sum == 0.f ? -INFINITY : (base + log2f(sum)) * 0.69314718055994531f;
+        for (int x = 0; x < GROUPS; ++x) top = fmaxf(top, stat[x].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        sum = 0.f;
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int x = 0; x < GROUPS; ++x) {
+          const float f = exp2f(stat[x].x - base);
+          sum += f * stat[x].y;
+          const float4 o = part[x][c];
+          acc.x += f * o.x; acc.y += f * o.y; acc.z += f * o.z; acc.w += f * o.w;
+        }
+      }
+      __syncthreads();
+      if (group != 0) continue;
+    }
+    if (!active) continue;
+    const int token = r.row / p.G, h = g * p.G + r.row % p.G;
+    const float mul = (sum == 0.f ? 0.f : 1.f / sum) * (p.v_scale ? p.v_scale[g] : 1.f);
+    uint16_t* dst = p.out + token * p.o_ts + h * p.o_hs + c * 4;
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16_pair(acc.x * mul, acc.y * mul), pack_bf16_pair(acc.z * mul, acc.w * mul));
+    if (c == 0 && p.lse) p.lse[(int64_t)token * p.H + h] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.69314718055994531f;
   }
 }
 
-void launch_attend_join(const AttendDev& p, int d, int64_t items, hipStream_t stream) {
-  const int grid = (int)(items < 2048 ? items : 2048);
+void launch_attend_join(const AttendDev& p, int d, int64_t rows, hipStream_t stream) {
+  const int grid = (int)(rows < 2048 ? rows : 2048);
   if (grid < 1) return;
   if (d == 128) hipLaunchKernelGGL(attend_join_kernel<128>, dim3(grid), dim3(256), 0, stream, p);
   else hipLaunchKernelGGL(attend_join_kernel<64>, dim3(grid), dim3(256), 0, stream, p);
@@ -327,7 +389,7 @@ sp_status check_attend_plan_args(const sp_attend_args* a) {
   if (a->n_groups == 0 && (a->d_cu_group || a->d_prefix_len)) return SP_EINVAL;
   if (a->n_groups > 0 && !a->d_block_table) return SP_EUNSUPPORTED;
   const AttendCaps c = attend_caps(a);
-  if (c.slots >= INT64_C(0x7fffffff) || c.units * a->H_kv >= INT64_C(0x7fffffff)) return SP_EINVAL;
+  if (c.slots * kSlotRows >= INT64_C(0x7fffffff) || c.rows >= INT64_C(0x7fffffff) || c.units * a->H_kv >= INT64_C(0x7fffffff)) return SP_EINVAL;
   if (!a->d_plan) return SP_ENULL;
   if (reinterpret_cast<uintptr_t>(a->d_plan) & 255u) return SP_EALIGN;
   if (a->plan_bytes < attend_plan_layout(a).bytes) return SP_EWORKSPACE;
@@ -350,11 +412,12 @@ extern "C" sp_status sp_attend_plan(const sp_attend_args* a, void* hip_stream) {
   PlanDev p;
   p.a = *a;
   p.G = a->H / a->H_kv;
-  p.cap_units = c.units; p.cap_joins = c.joins; p.cap_slots = c.slots;
+  p.cap_units = c.units; p.cap_joins = c.joins; p.cap_rows = c.rows; p.cap_slots = c.slots;
   p.print = attend_print(a);
   p.header = reinterpret_cast<AttendHeader*>(base);
   p.units = reinterpret_cast<AttendUnit*>(base + l.units);
   p.joins = reinterpret_cast<AttendJoin*>(base + l.joins);
+  p.rows = reinterpret_cast<AttendRow*>(base + l.rows);
   p.seg_start = reinterpret_cast<int32_t*>(base + l.seg_start);
   p.seqs = reinterpret_cast<PlanSeq*>(base + l.seqs);
   p.groups = reinterpret_cast<PlanGroup*>(base + l.groups);

@@ -23,7 +23,7 @@ extern "C" void caps(const sp_attend_args* a, int64_t* out) {
   const AttendPlanLayout l = attend_plan_layout(a);
   out[0] = c.blocks; out[1] = c.units; out[2] = c.joins; out[3] = c.slots; out[4] = (int64_t)l.bytes; out[5] = (int64_t)l.units;
   out[6] = (int64_t)l.joins; out[7] = (int64_t)l.seg_start; out[8] = (int64_t)l.seqs; out[9] = (int64_t)l.groups;
-  out[10] = sizeof(AttendUnit); out[11] = sizeof(AttendJoin); out[12] = (int64_t)attend_workspace(a); out[13] = (int64_t)attend_sums_bytes(a);
+  out[10] = sizeof(AttendUnit); out[11] = sizeof(AttendJoin); out[12] = (int64_t)attend_workspace(a); out[13] = (int64_t)attend_sums_bytes(a); out[14] = c.rows; out[15] = sizeof(AttendRow); out[16] = (int64_t)l.rows;
 }
 extern "C" uint64_t print_of(const sp_attend_args* a) { return attend_print(a); }
 extern "C" int share(int64_t rows, int members) { return shares(rows, members); }
@@ -43,7 +43,7 @@ extern "C" int cut_up(int n_seg, const int64_t* rows, const int* n, const int* l
         b[0] = s; b[1] = i; b[2] = keys; b[3] = p; b[4] = block_rows(rows[s]);
         for (int q = 0; q < p; ++q, ++*n_pieces) {
           int* x = pieces + 3 * *n_pieces;
-          x[0] = nb; x[1] = piece_start(keys, p, q); x[2] = piece_start(keys, p, q + 1);
+          x[0] = nb; x[1] = piece_start(shared[s] * (n[s] != 0), keys, p, q); x[2] = piece_start(shared[s] * (n[s] != 0), keys, p, q + 1);
         }
       }
   }
@@ -73,9 +73,9 @@ def _args(**kw):
 
 
 def _caps(shim, a):
-    out = (C.c_int64 * 14)()
+    out = (C.c_int64 * 17)()
     shim.caps(C.byref(a), out)
-    return dict(zip("blocks units joins slots bytes at_units at_joins at_seg at_seqs at_groups unit join workspace sums".split(), out))
+    return dict(zip("blocks units joins slots bytes at_units at_joins at_seg at_seqs at_groups unit join workspace sums rows row at_rows".split(), out))
 
 
 def _batches():
@@ -126,7 +126,8 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads):
         # the keys of a block, in order and without gaps; whole steps of 64 apart from the end
         for i, (s, k, keys, p, m) in enumerate(blocks):
             mine = pieces[pieces[:, 0] == i]
-            assert len(mine) == p and mine[0, 1] == 0 and mine[-1, 2] == keys
+            first_key = sh[s] if n[s] else 0
+            assert len(mine) == p and mine[0, 1] == first_key and mine[-1, 2] == first_key + keys
             assert (mine[1:, 1] == mine[:-1, 2]).all() and (mine[1:, 1] % 64 == 0).all()
             assert p == 1 or (mine[:, 2] > mine[:, 1]).all()
             if n[s]:   # no row of the block sees a key beyond the last row's
@@ -142,7 +143,9 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads):
         slots = sum(int(b[3]) * int(b[4]) // 16 for x, b in zip(leaves, blocks) if x)
         assert slots <= caps["slots"], (new, length, groups)
         assert caps["at_units"] + caps["units"] * caps["unit"] <= caps["at_joins"]
-        assert caps["at_joins"] + caps["joins"] * caps["join"] <= caps["at_seg"]
+        assert caps["at_joins"] + caps["joins"] * caps["join"] <= caps["at_rows"]
+        assert sum(min(int(b[4]), int(rows[b[0]] - b[1] * b[4])) for x, b in zip(leaves, blocks) if x and b[0] >= n_prefix) <= caps["rows"]
+        assert caps["at_rows"] + caps["rows"] * caps["row"] <= caps["at_seg"]
         assert caps["at_seg"] + 4 * (B + len(groups) + 1) <= caps["at_seqs"] and caps["at_seqs"] + 16 * B <= caps["at_groups"]
         assert caps["at_groups"] + 32 * len(groups) <= caps["bytes"]
         assert caps["sums"] >= caps["slots"] * H_kv * 16 * 128 * 4 and caps["workspace"] >= caps["sums"] + caps["slots"] * H_kv * 16 * 8

@@ -1,6 +1,6 @@
 // sp_attend: attention of new tokens over a (paged, bf16 or E4M3) cache, the keys of a shared prefix read once for a group.
 //
-// One launch takes every piece of the plan (sp_attend_plan.h), a workgroup of four waves a piece and KV head.  Two forms:
+// One launch takes every piece of the plan (sp_attend_plan.h), a workgroup of four waves a stretch of pieces for one KV head.  Two forms:
 //   few rows (<= 16: single tokens, their heads)   bound by reading keys and values.  Each wave walks over 32-key tiles of its own
 //     with a 16x16 tile of logits, keys straight from memory into matrix operands, values through LDS for the transpose; nothing
 //     is shared before the end, and every wave has the next tile in flight.
@@ -14,6 +14,8 @@
 #include "sp_attend_internal.h"
 #include "sp_lds.h"
 
+#include <type_traits>
+
 namespace sp {
 
 namespace {
@@ -26,6 +28,10 @@ constexpr uint32_t kNanF32 = 0x7fc00000u;
 constexpr int kNanBf16 = 0x7fc0;
 constexpr float kSlack = 8.f;   // logits (log2) may exceed the running maximum by this much
 constexpr int kTileKeys = 64;   // many rows
+constexpr int kAhead = 6;       // operands that are read before the first product that takes one
+
+// kinds of instructions, for __builtin_amdgcn_sched_group_barrier
+constexpr int kSchedValu = 0x2, kSchedMfma = 0x8, kSchedLdsRead = 0x100;
 
 // Place of 16-byte chunk c of row r in a tile of rows of C chunks, permuted so that neither the operand reads (16 or 32 rows,
 // one or two chunks) nor the transposing reads (4 or 8 rows, 2 or 4 chunks) meet in a bank more often than they must.
@@ -98,6 +104,13 @@ __device__ __forceinline__ float key_factor(const AttendDev& p, int g, uint32_t&
   return c == 0.f ? 1.f : fabsf(c);
 }
 
+// threadIdx.x, as a value of its own for every piece: what is computed from it is not kept in registers across the loop over pieces
+__device__ __forceinline__ int thread_of_piece() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
 struct RowPlace { int token, h; };
 __device__ __forceinline__ RowPlace row_place(const AttendDev& p, int flat, int g) {
   RowPlace r;
@@ -153,7 +166,7 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   constexpr int DB = D / 16;          // blocks of values
   constexpr int C = D / 8;            // 16-byte chunks of a bf16 row
   using Tile = FewTile<D, FP8>;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, row = l & 15, quad = l >> 4;
+  const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, row = l & 15, quad = l >> 4;
   const bool mine = row < u.nr;
   const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
 
@@ -299,7 +312,7 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
     for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(part + 16 * i + 4 * quad) = o[i] * f;
   }
   __syncthreads();
-  const int r = threadIdx.x >> 4, lane = threadIdx.x & 15;
+  const int r = tid >> 4, lane = tid & 15;
   if (r >= u.nr) return;
   constexpr int V = D / 16;
   float acc[V], l_all = 0.f;
@@ -374,7 +387,7 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
   constexpr int C = D / 8;
   constexpr int TILE = kTileKeys * D * 2;  // bytes of a tile of keys or of values
   using Tile = ManyTile<D, FP8>;
-  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, half = l >> 5;
+  const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, half = l >> 5;
   const int row = w * 32 + (l & 31);
   const bool mine = row < u.nr;
   const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
@@ -460,9 +473,11 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
     load(first_tile);
     look_up(first_tile + kTileKeys);
   }
-  int buffer = 0;
-  for (int tile = first_tile; tile < u.k1; tile += kTileKeys, buffer ^= 2 * TILE) {
-    char* const kd = lds + buffer;
+  // One tile out of buffer BUF (a constant, so that the operands' addresses are too).  The compiler is told how to mix reads, products and
+  // the rest: operands are read several products ahead, and the weights of the next 16 keys are formed while the
+  // matrix cores work on these.
+  auto step = [&](auto buf, int tile) {
+    char* const kd = lds + decltype(buf)::value * 2 * TILE;
     char* const vd = kd + TILE;
     kt.store(kd, tid);
     vl.store(vd, tid);
@@ -471,18 +486,26 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       load(tile + kTileKeys);
       look_up(tile + 2 * kTileKeys);
     }
-    if (tile >= most) continue;  // (the wave's rows see none of these keys)
+    if (tile >= most) return;  // (the wave's rows see none of these keys)
     f32x16 s[2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int j = 0; j < 16; ++j) s[x][j] = 0.f;
 #pragma unroll
-      for (int i = 0; i < KS; ++i) {
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
         const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kd + k_at[i] + x * 32 * (D * 2));
         s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[x], 0, 0, 0);
       }
+    __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, kAhead, 0);
+#pragma unroll
+    for (int i = 0; i < 2 * KS - kAhead; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 1, 0);
     }
+    __builtin_amdgcn_sched_group_barrier(kSchedMfma, kAhead, 0);
     if (tile + kTileKeys > least || tile < u.k0) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -508,28 +531,39 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       for (int i = 0; i < DB; ++i) o[i] *= f;
     }
     const float base = m == -INFINITY ? 0.f : m;
-    bf16x8 pf[4];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
+    for (int e = 0; e < 4; ++e) {
+      float x[8], part = 0.f;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        s[x][j] = fast_exp2(__builtin_fmaf(s[x][j], c, -base));
-        sum += s[x][j];
+      for (int j = 0; j < 8; ++j) {
+        x[j] = fast_exp2(__builtin_fmaf(s[e >> 1][8 * (e & 1) + j], c, -base));
+        part += x[j];
       }
+      sum += part;
+      const u32x4 pw = {pack_bf16_pair(x[0], x[1]), pack_bf16_pair(x[2], x[3]), pack_bf16_pair(x[4], x[5]), pack_bf16_pair(x[6], x[7])};
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const u32x4 pw = {pack_bf16_pair(s[x][8 * e], s[x][8 * e + 1]), pack_bf16_pair(s[x][8 * e + 2], s[x][8 * e + 3]),
-                          pack_bf16_pair(s[x][8 * e + 4], s[x][8 * e + 5]), pack_bf16_pair(s[x][8 * e + 6], s[x][8 * e + 7])};
-        pf[2 * x + e] = __builtin_bit_cast(bf16x8, pw);
+      for (int i = 0; i < DB; ++i) {
+        const bf16x8 vf = join8(lds_read_tr(vd + v_at[i][0] + e * 16 * (D * 2)), lds_read_tr(vd + v_at[i][1] + e * 16 * (D * 2)));
+        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[i], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 2 * DB, 0);
+    __builtin_amdgcn_sched_group_barrier(kSchedValu, 28, 0);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
       for (int i = 0; i < DB; ++i) {
-        const bf16x8 vf = join8(lds_read_tr(vd + v_at[i][0] + e * 16 * (D * 2)), lds_read_tr(vd + v_at[i][1] + e * 16 * (D * 2)));
-        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[e], o[i], 0, 0, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+        if (e < 3) {
+          __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 2, 0);
+          __builtin_amdgcn_sched_group_barrier(kSchedValu, 28 / DB, 0);
+        }
       }
+  };
+  for (int tile = first_tile; tile < u.k1; tile += 2 * kTileKeys) {
+    step(std::integral_constant<int, 0>(), tile);
+    if (tile + kTileKeys < u.k1) step(std::integral_constant<int, 1>(), tile + kTileKeys);
   }
 
   const int any_bad = __syncthreads_or(bad != 0);
@@ -577,30 +611,33 @@ __device__ __forceinline__ void nan_rows(const AttendDev& p, int d, int64_t r0, 
 }  // namespace
 
 template <int D, bool FP8, bool PAGED>
-__global__ __launch_bounds__(256, 2) void attend_kernel(const AttendDev p) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_kernel(const AttendDev p) {
   __shared__ __align__(16) char lds[2 * 2 * kTileKeys * D * 2];  // (few rows need 34 KB of the 64, or 17.5 of the 32)
   // The KV heads of a piece are neighbours: with eight of them, each has the L2 of one XCD, which the rows of a
   // block share, as workgroups go to the XCDs in turn.
   const int n = (int)(blockIdx.x / (uint32_t)p.H_kv), g = (int)(blockIdx.x % (uint32_t)p.H_kv);
-  // header and piece through the scalar cache, together (the list has room for every workgroup's index)
+  // the plan through the scalar cache; header and stretch together (the list has room for every workgroup's index)
   const auto header = reinterpret_cast<const __attribute__((address_space(4))) AttendHeader*>(reinterpret_cast<uintptr_t>(p.header));
-  const auto units = reinterpret_cast<const __attribute__((address_space(4))) AttendUnit*>(reinterpret_cast<uintptr_t>(p.units));
+  const ScalarTable stretch = scalar_table(p.stretches);
   const uint64_t print = header->print;
-  const int n_units = header->n_units;
-  AttendUnit u;
-  u.r0 = units[n].r0; u.nr = units[n].nr; u.seq = units[n].seq; u.k0 = units[n].k0;
-  u.k1 = units[n].k1; u.off = units[n].off; u.slot = units[n].slot; u.bad = units[n].bad;
+  const int n_stretches = header->n_stretches;
+  int x = stretch[n];
+  const int end = stretch[n + 1];
   if (print != p.print) {
     nan_rows(p, D, 0, (int64_t)p.T_new * p.H, p.H, 0, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
     return;
   }
-  if (n >= n_units) return;
-  if (u.bad) {
-    nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, 256);
-    return;
+  if (n >= n_stretches) return;
+  for (; x < end; ++x) {
+    const auto unit = reinterpret_cast<const __attribute__((address_space(4))) AttendUnit*>(reinterpret_cast<uintptr_t>(p.units + x));
+    AttendUnit u;
+    u.r0 = unit->r0; u.nr = unit->nr; u.seq = unit->seq; u.k0 = unit->k0;
+    u.k1 = unit->k1; u.off = unit->off; u.slot = unit->slot; u.bad = unit->bad;
+    if (u.bad) nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, 256);
+    else if (u.nr <= kFewRows) attend_few<D, FP8, PAGED>(p, u, g, lds);
+    else attend_many<D, FP8, PAGED>(p, u, g, lds);
+    __syncthreads();  // (the next piece uses the same LDS)
   }
-  if (u.nr <= kFewRows) attend_few<D, FP8, PAGED>(p, u, g, lds);
-  else attend_many<D, FP8, PAGED>(p, u, g, lds);
 }
 
 namespace {
@@ -663,6 +700,7 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.print = attend_print(a);
   p.header = reinterpret_cast<const AttendHeader*>(base);
   p.units = reinterpret_cast<const AttendUnit*>(base + l.units);
+  p.stretches = reinterpret_cast<const int32_t*>(base + l.stretches);
   p.rows = reinterpret_cast<const AttendRow*>(base + l.rows);
   p.table = a->d_block_table; p.cu_cache = a->d_cu_cache;
   p.q = static_cast<const uint16_t*>(a->d_q);

@@ -4,8 +4,13 @@
 // The rows of a call are (token, head of a KV head's group) pairs, row = token * G + head, flat over all tokens: the rows of a
 // sequence, and of a group of sequences, lie side by side.  A segment is a set of rows that attend to the same keys: the shared
 // prefix of a group (all rows of its members), or what a sequence has for itself.  A segment is cut into blocks of 16 rows
-// (if it has no more: one small matrix tile, bound by reading the keys) or of 128 (bound by the matrix cores), and a block's
-// keys into pieces.  A piece times a KV head is what one workgroup does.
+// (if it has no more: one small matrix tile, bound by reading the keys) or of 128 (bound by the matrix cores).
+//
+// The device has room for attend_items() workgroups at once.  Fewer than three times as many (block, KV head) pairs are laid end to end,
+// each at its cost, and cut into as many stretches of equal cost as there is room for: every workgroup has one, and all end together.
+// (One block to a workgroup instead, in whole rounds, pieces cut to 1/1024 of the keys -> stretches: MEASURED_STRETCHES.)
+// With more blocks than that a workgroup takes one block, and takes the next as it gets done, longest first; only a block longer than a
+// workgroup's equal share is cut.
 //
 // A block of one piece whose rows have no shared prefix is finished by its workgroup; the pieces of all others leave their
 // sums in slots of the workspace, which a second kernel joins.
@@ -28,8 +33,11 @@ constexpr int kFewRows = 16;      // rows of a block of a small segment
 constexpr int kManyRows = 128;    // ... and of any other
 constexpr int kSlotRows = 16;     // rows of a workspace slot
 constexpr int kPieceStep = 64;    // pieces are cut at multiples of so many keys
-constexpr int kMinPiece = 128;    // no piece is made shorter than this
-constexpr int kAttendItems = 1024;  // workgroups that a call's keys are cut for: four for each of 256 compute units
+constexpr int kMinSteps = 2;      // no piece is made shorter than so many steps
+constexpr int kMostStretchBlocks = 3 * 768;  // blocks that stretches are made for, at most
+
+// Workgroups that the device has room for: 256 compute units with two each (three where d = 64 takes half the LDS)
+SP_ATTEND_FN int attend_items(int d) { return d == 64 ? 768 : 512; }
 
 struct AttendUnit {   // one piece of one block
   int32_t r0, nr;     // first row, rows (nr <= 16: the kernel part for few rows)
@@ -42,9 +50,9 @@ struct AttendUnit {   // one piece of one block
 struct AttendJoin {   // one block of a sequence's own rows that slots are joined for
   int32_t r0, nr;
   int32_t own_slot, own_pieces, own_step;           // slot of the first piece, pieces, slots of a piece
-  int32_t pre_slot, pre_pieces, pre_r0, pre_rows;   // the group's prefix: slot of its first block, pieces of a block (0: none), its first row, rows of a block
   int32_t first;                                    // its first row among all that are joined
-  int32_t pad[2];
+  int32_t group;                                    // whose prefix the rows have as well, or -1
+  int32_t pad;
 };
 struct AttendRow {    // one of these rows: where its sums are, slot * 16 + row of the slot (KV heads aside), and how far apart
   int32_t row;
@@ -54,7 +62,7 @@ struct AttendRow {    // one of these rows: where its sums are, slot * 16 + row 
 };
 struct AttendHeader {
   uint64_t print;     // of the shape fields the plan was made for
-  int32_t n_units, n_rows;  // pieces, rows to join
+  int32_t n_stretches, n_rows;  // workgroups for each KV head, rows to join
   int32_t most_pieces;      // of a row to join
   int32_t n_slots;
 };
@@ -66,11 +74,11 @@ struct AttendCaps {
 };
 
 // Upper bounds for any lengths that the shape fields allow.  Blocks: a segment of R rows has at most R / 128 + 1; own segments
-// with a block: at most B and at most one per row; prefix segments: n_groups.  Pieces: make_cut() adds at most kAttendItems / H_kv to one per block.
+// with a block: at most B and at most one per row; prefix segments: n_groups.  Pieces: cuts add at most attend_items() / H_kv to one per block.
 // Slots: prefix blocks, blocks of sequences with a prefix, and blocks of several pieces, of which there are at most as many as pieces added; a
 // prefix is only shared where a group has fewer than 128 rows per member on average (shares()), so rows in such groups are fewer than 128 B.
 inline AttendCaps attend_caps(const sp_attend_args* a) {
-  const int64_t rows = a->T_new * (a->H / a->H_kv), added = kAttendItems / a->H_kv + 1;
+  const int64_t rows = a->T_new * (a->H / a->H_kv), added = attend_items(a->d) / a->H_kv + 1;
   const int64_t own_segments = rows < a->B ? rows : a->B, own = rows / kManyRows + own_segments;
   const int64_t shared_rows = rows < (int64_t)kManyRows * a->B ? rows : (int64_t)kManyRows * a->B;
   const int64_t groups = a->n_groups < own_segments ? a->n_groups : own_segments;  // those with a row
@@ -113,21 +121,45 @@ SP_ATTEND_FN int own_block_keys(int64_t rows, int i, int G, int n, int len, int 
   return v < 0 ? 0 : v;
 }
 
-// Most keys of a piece, for `total` keys summed over all blocks: 1024 workgroups have equal shares, where that
-// leaves them 128 keys.
-SP_ATTEND_FN int make_cut(int64_t total, int H_kv) {
-  const int items = kAttendItems / H_kv > 0 ? kAttendItems / H_kv : 1;
-  const int64_t share = (total + items - 1) / items;
+// Steps of 64 keys of a block's keys [first, first + keys), cut at multiples of 64 keys of the sequence
+SP_ATTEND_FN int block_steps(int first, int keys) { return (int)(((int64_t)(first & (kPieceStep - 1)) + keys + kPieceStep - 1) / kPieceStep); }
+
+// What a step costs a workgroup, in units of 0.55 us on a full device: 128 rows are bound by the matrix cores, 16 by reading 64 keys and values
+// (COSTS_MEASURED); and what a piece costs besides.
+SP_ATTEND_FN int step_cost(bool few, int d, bool fp8) { return !few ? 4 : d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5); }
+constexpr int kBlockCost = 4;
+constexpr int kMinStretch = 10;   // no stretch costs less: two steps of the dearest kind, and more than one of any
+
+SP_ATTEND_FN bool by_stretches(int64_t blocks, int d, int H_kv) { return blocks * H_kv < 3 * (int64_t)attend_items(d) && blocks <= kMostStretchBlocks; }
+// Stretches for each KV head, blocks of `cost` in all: what the device has room for, as long as that leaves each enough to do
+SP_ATTEND_FN int stretch_count(int64_t cost, int d, int H_kv) {
+  const int64_t room = attend_items(d) / H_kv > 0 ? attend_items(d) / H_kv : 1, most = cost / kMinStretch;
+  return (int)(most < 1 ? 1 : most < room ? most : room);
+}
+// Where stretch s of n begins, blocks laid end to end
+SP_ATTEND_FN int64_t stretch_start(int64_t cost, int n, int s) { return cost * s / n; }
+// ... as a step of the block whose share begins at `start` (what the block costs besides spread over its steps): `steps` (the next
+// block's first) or 0 where a piece would get too short
+SP_ATTEND_FN int step_at(int64_t x, int64_t start, int steps, int per_step) {
+  const int64_t cost = (int64_t)steps * per_step + kBlockCost, j = (2 * (x - start) * steps + cost) / (2 * cost);
+  return j < kMinSteps ? 0 : steps - j < kMinSteps ? steps : (int)j;
+}
+SP_ATTEND_FN int step_key(int first, int keys, int steps, int j) {
+  return j <= 0 ? first : j >= steps ? first + keys : (first & ~(kPieceStep - 1)) + j * kPieceStep;
+}
+
+// Otherwise: most keys of a piece, for `total` keys summed over all blocks
+SP_ATTEND_FN int make_cut(int64_t total, int d, int H_kv) {
+  const int items = attend_items(d) / H_kv > 0 ? attend_items(d) / H_kv : 1;
+  const int64_t share = (total + items - 1) / items, least = kMinSteps * kPieceStep;
   const int64_t cut = (share + kPieceStep - 1) / kPieceStep * kPieceStep;
-  return cut < kMinPiece ? kMinPiece : cut > 0x40000000 ? 0x40000000 : (int)cut;
+  return cut < least ? (int)least : cut > 0x40000000 ? 0x40000000 : (int)cut;
 }
 SP_ATTEND_FN int pieces_of(int keys, int cut) { return keys <= cut ? 1 : (int)(((int64_t)keys + cut - 1) / cut); }
-// First key of piece p of a block with keys [first, first + keys); pieces are cut at multiples of 64 keys of the sequence, so
-// that only a block's first and last tile are not whole
+// first key of piece p
 SP_ATTEND_FN int piece_start(int first, int keys, int pieces, int p) {
-  if (p == 0 || p == pieces) return p == 0 ? first : first + keys;
-  const int base = first & ~(kPieceStep - 1), steps = (int)(((int64_t)first - base + keys + kPieceStep - 1) / kPieceStep);
-  return base + (int)((int64_t)steps * p / pieces) * kPieceStep;
+  const int steps = block_steps(first, keys);
+  return step_key(first, keys, steps, p == pieces ? steps : (int)((int64_t)steps * p / pieces));
 }
 
 SP_ATTEND_FN uint64_t attend_print(const sp_attend_args* a) {
@@ -144,7 +176,7 @@ SP_ATTEND_FN uint64_t attend_print(const sp_attend_args* a) {
 
 // Offsets of the parts of d_plan
 struct AttendPlanLayout {
-  size_t units, joins, rows, seg_start, seqs, groups, bytes;
+  size_t units, stretches, joins, rows, seg_start, seqs, groups, bytes;
 };
 inline size_t attend_round(size_t x) { return (x + 255) / 256 * 256; }
 inline AttendPlanLayout attend_plan_layout(const sp_attend_args* a) {
@@ -152,6 +184,7 @@ inline AttendPlanLayout attend_plan_layout(const sp_attend_args* a) {
   AttendPlanLayout l;
   size_t at = 256;
   l.units = at; at += attend_round(sizeof(AttendUnit) * (size_t)c.units);
+  l.stretches = at; at += attend_round(4 * ((size_t)c.units + 1));
   l.joins = at; at += attend_round(sizeof(AttendJoin) * (size_t)c.joins);
   l.rows = at; at += attend_round(sizeof(AttendRow) * (size_t)c.rows);
   l.seg_start = at; at += attend_round(4 * ((size_t)a->B + (size_t)a->n_groups + 1));

@@ -13,10 +13,11 @@ struct PlanGroup { int32_t shared, active, t0, tokens, slot, pieces, pad[2]; };
 struct PlanDev {
   sp_attend_args a;   // (host pointers in it are not used)
   int G;
-  int64_t cap_units, cap_joins, cap_rows, cap_slots;
+  int64_t cap_blocks, cap_units, cap_joins, cap_rows, cap_slots;
   uint64_t print;
   AttendHeader* header;
   AttendUnit* units;
+  int32_t* stretches;
   AttendJoin* joins;
   AttendRow* rows;
   int32_t* seg_start;
@@ -60,16 +61,40 @@ __device__ __forceinline__ void block_exclusive(int64_t (&v)[N], int64_t (&total
   __syncthreads();
 }
 
-struct Block {       // a block of rows, as the walk over all blocks meets it
+struct Block {       // a block of rows
   int seg, i;        // segment (prefixes first, then sequences), block of it
   int64_t rows;      // of the segment
-  int keys;          // of the block
+  int m, nr;         // rows of a whole block, of this one
+  int first, keys;   // its keys are [first, first + keys)
+  int steps, cost;   // ... and a step's cost
 };
+
+// largest i in [0, n) with table[i] <= x (table[0] <= x)
+template <typename T>
+__device__ __forceinline__ int last_at_most(const T* table, int n, T x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (table[mid] <= x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+constexpr int kLdsSeqs = 512;        // sequences and segments that are kept in LDS
+constexpr int kMostStretches = 768;  // (attend_items())
 
 }  // namespace
 
 __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   __shared__ int most_pieces;
+  __shared__ PlanSeq lds_seqs[kLdsSeqs];
+  __shared__ int32_t lds_seg[2 * kLdsSeqs + 1];
+  __shared__ int64_t start[kMostStretchBlocks + 1];   // by stretches: the blocks laid end to end
+  __shared__ int64_t cuts[kMostStretches + 1];        // (block, step) that each stretch begins at
+  __shared__ int32_t first_unit[kMostStretches + 1];
+  __shared__ int32_t slot_of[kMostStretchBlocks];
+  PlanSeq* const seqs = p.a.B <= kLdsSeqs ? lds_seqs : p.seqs;
+  int32_t* const seg_start = p.a.B <= kLdsSeqs ? lds_seg : p.seg_start;  // (no more groups than sequences)
   const int tid = threadIdx.x, B = p.a.B, n_groups = p.a.n_groups, G = p.G, T = (int)p.a.T_new;
   if (tid == 0) {
     p.header->print = 0;
@@ -91,7 +116,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       room = first < 0 ? -1 : end - first;
     }
     if (s.len < 0 || s.len > room) s.len = -1;
-    p.seqs[b] = s;
+    seqs[b] = s;
   }
   for (int g = tid; g < n_groups; g += 1024) {
     PlanGroup x = {};
@@ -107,7 +132,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     for (int b = tid; b < B; b += 1024) {
       const int g = group_of(p, b);
       if (g < 0) continue;
-      const PlanSeq s = p.seqs[b];
+      const PlanSeq s = seqs[b];
       if (b == p.a.d_cu_group[g]) atomicMin(&p.groups[g].shared, max(s.len, 0));
       if (s.n > 0) {
         atomicMin(&p.groups[g].shared, s.len < 0 ? 0 : max(s.len - s.n, 0));
@@ -123,121 +148,189 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     __syncthreads();
     for (int b = tid; b < B; b += 1024) {
       const int g = group_of(p, b);
-      if (g >= 0) p.seqs[b].shared = p.groups[g].shared;
+      if (g >= 0) seqs[b].shared = p.groups[g].shared;
     }
     __syncthreads();
   }
   block_prefix_table(n_groups + B, [&](int s) -> int32_t {
     if (s < n_groups) return p.groups[s].shared > 0 ? segment_blocks((int64_t)p.groups[s].tokens * G) : 0;
-    const int n = p.seqs[s - n_groups].n;
+    const int n = seqs[s - n_groups].n;
     return n > 0 ? segment_blocks((int64_t)n * G) : 0;
-  }, p.seg_start);
-  const int n_blocks = p.seg_start[n_groups + B], n_prefix = p.seg_start[n_groups];
+  }, seg_start);
+  const int n_blocks = seg_start[n_groups + B], n_prefix = seg_start[n_groups];
+  if (n_blocks > p.cap_blocks) return;  // (offsets that do not ascend may ask for more than there is room for: no plan then)
 
-  // Every thread walks over a run of blocks, several times.  Prefixes first, then the sequences' blocks from the last to the
-  // first: of a causal segment's blocks the last have the most keys.
-  const int per = (n_blocks + 1023) / 1024;
-  const int x0 = min(n_blocks, tid * per), x1 = min(n_blocks, x0 + per);
+  // Blocks in the order that they are laid out in: prefixes first, then the sequences' blocks from the last to the first (of
+  // a causal segment's blocks the last have the most keys).
+  const bool fp8 = p.a.cache_dtype == SP_K_FP8_E4M3;
+  auto block_at = [&](int x, int hint) {
+    const int flat = x < n_prefix ? x : n_blocks - 1 - (x - n_prefix);
+    Block k;
+    k.seg = hint >= 0 && flat >= seg_start[hint] && flat < seg_start[hint + 1] ? hint : upper_segment(seg_start, n_groups + B, flat);
+    k.i = flat - seg_start[k.seg];
+    if (k.seg < n_groups) {
+      k.rows = (int64_t)p.groups[k.seg].tokens * G;
+      k.first = 0;
+      k.keys = p.groups[k.seg].shared;
+    } else {
+      const PlanSeq s = seqs[k.seg - n_groups];
+      k.rows = (int64_t)s.n * G;
+      k.first = s.shared;
+      k.keys = s.len < 0 ? 0 : own_block_keys(k.rows, k.i, G, s.n, s.len, s.shared);
+    }
+    k.m = block_rows(k.rows);
+    k.nr = (int)min((int64_t)k.m, k.rows - (int64_t)k.i * k.m);
+    k.steps = block_steps(k.first, k.keys);
+    k.cost = step_cost(k.m == kFewRows, p.a.d, fp8);
+    return k;
+  };
+  // every thread walks over a run of blocks, several times
+  const int per = (n_blocks + 1023) / 1024, x0 = min(n_blocks, tid * per), x1 = min(n_blocks, x0 + per);
   auto walk = [&](auto&& visit) {
     int seg = -1;
     for (int x = x0; x < x1; ++x) {
-      const int flat = x < n_prefix ? x : n_blocks - 1 - (x - n_prefix);
-      if (seg < 0 || flat < p.seg_start[seg] || flat >= p.seg_start[seg + 1]) seg = upper_segment(p.seg_start, n_groups + B, flat);
-      Block k;
-      k.seg = seg;
-      k.i = flat - p.seg_start[seg];
-      if (seg < n_groups) {
-        k.rows = (int64_t)p.groups[seg].tokens * G;
-        k.keys = p.groups[seg].shared;
-      } else {
-        const PlanSeq s = p.seqs[seg - n_groups];
-        k.rows = (int64_t)s.n * G;
-        k.keys = s.len < 0 ? 0 : own_block_keys(k.rows, k.i, G, s.n, s.len, s.shared);
-      }
-      visit(k);
+      const Block k = block_at(x, seg);
+      seg = k.seg;
+      visit(x, k);
     }
   };
-  int64_t keys[1] = {0}, total_keys[1];
-  walk([&](const Block& k) { keys[0] += k.keys; });
-  block_exclusive(keys, total_keys);
-  const int cut = make_cut(total_keys[0], p.a.H_kv);
-  auto joined = [&](const Block& k) { return k.seg >= n_groups && p.seqs[k.seg - n_groups].shared > 0; };
+
+  // where the blocks are cut
+  const bool stretched = by_stretches(n_blocks, p.a.d, p.a.H_kv);
+  int64_t sum[2] = {0, 0}, total[2];  // cost, keys
+  walk([&](int, const Block& k) {
+    sum[0] += (int64_t)k.steps * k.cost + kBlockCost;
+    sum[1] += k.keys;
+  });
+  block_exclusive(sum, total);
+  const int cut = make_cut(total[1], p.a.d, p.a.H_kv);
+  const int n_cuts = stretched ? stretch_count(total[0], p.a.d, p.a.H_kv) : 0;
+  if (stretched) {
+    int64_t at = sum[0];
+    walk([&](int x, const Block& k) {
+      start[x] = at;
+      at += (int64_t)k.steps * k.cost + kBlockCost;
+    });
+    __syncthreads();
+    for (int s = tid; s <= n_cuts; s += 1024) {
+      int b = s < n_cuts && n_blocks > 0 ? 0 : n_blocks, j = 0;
+      if (s > 0 && s < n_cuts) {
+        const int64_t x = stretch_start(total[0], n_cuts, s);
+        b = last_at_most(start, n_blocks, x);
+        const Block k = block_at(b, -1);
+        j = step_at(x, start[b], k.steps, k.cost);
+        if (j >= k.steps && j > 0) { ++b; j = 0; }
+      }
+      cuts[s] = ((int64_t)b << 32) | j;
+    }
+    __syncthreads();
+  }
+  // cuts inside block x: those with (x, 0) < cut < (x + 1, 0) are `first_cut` and those behind it
+  auto first_cut = [&](int x) { return last_at_most(cuts, n_cuts + 1, (int64_t)x << 32) + 1; };
+  auto pieces_at = [&](int x, const Block& k) {
+    return stretched ? 1 + last_at_most(cuts, n_cuts + 1, ((int64_t)(x + 1) << 32) - 1) - (first_cut(x) - 1) : pieces_of(k.keys, cut);
+  };
+  auto joined = [&](const Block& k) { return k.seg >= n_groups && seqs[k.seg - n_groups].shared > 0; };
   auto leaves_sums = [&](const Block& k, int pieces) { return pieces > 1 || k.seg < n_groups || joined(k); };
 
   enum { kUnits, kSlots, kJoins, kRows };
   int64_t at[4] = {0, 0, 0, 0}, n[4];
-  auto rows_of = [&](const Block& k) { return (int)min((int64_t)block_rows(k.rows), k.rows - (int64_t)k.i * block_rows(k.rows)); };
-  walk([&](const Block& k) {
-    const int pieces = pieces_of(k.keys, cut);
+  walk([&](int x, const Block& k) {
+    const int pieces = pieces_at(x, k);
     at[kUnits] += pieces;
     if (leaves_sums(k, pieces)) {
-      at[kSlots] += (int64_t)pieces * (block_rows(k.rows) / kSlotRows);
+      at[kSlots] += (int64_t)pieces * (k.m / kSlotRows);
       at[kJoins] += k.seg >= n_groups;
-      at[kRows] += k.seg >= n_groups ? rows_of(k) : 0;
+      at[kRows] += k.seg >= n_groups ? k.nr : 0;
     }
   });
   block_exclusive(at, n);
-  // (offsets that do not ascend may ask for more than there is room for: no plan then)
   if (n[kUnits] > p.cap_units || n[kSlots] > p.cap_slots || n[kJoins] > p.cap_joins || n[kRows] > p.cap_rows) return;
+  if (stretched) {
+    int64_t count[1] = {0}, units[1];
+    if (tid < n_cuts) {
+      const int64_t a = cuts[tid], b = cuts[tid + 1];
+      count[0] = (b >> 32) + ((b & 0xffffffff) != 0) - (a >> 32);
+    }
+    block_exclusive(count, units);
+    if (tid < n_cuts) p.stretches[tid] = first_unit[tid] = (int)count[0];
+    if (tid == 0) p.stretches[n_cuts] = first_unit[n_cuts] = (int)units[0];
+  }
 
-  int64_t u = at[kUnits], slot = at[kSlots];
-  walk([&](const Block& k) {
-    const int pieces = pieces_of(k.keys, cut), m = block_rows(k.rows), step = m / kSlotRows;
-    const bool sums = leaves_sums(k, pieces);
+  auto unit_of = [&](const Block& k, int j0, int j1, int64_t slot) {
     AttendUnit unit;
-    int t0, first = 0;
+    int t0;
     if (k.seg < n_groups) {
       t0 = p.groups[k.seg].t0;
       unit.seq = clamp_int(p.a.d_cu_group[k.seg], 0, B - 1);
       unit.off = kNoLimit;
       unit.bad = 0;
-      if (k.i == 0) {
-        p.groups[k.seg].slot = (int)slot;
-        p.groups[k.seg].pieces = pieces;
-      }
     } else {
-      const PlanSeq s = p.seqs[k.seg - n_groups];
+      const PlanSeq s = seqs[k.seg - n_groups];
       t0 = s.t0;
-      first = s.shared;
       unit.seq = k.seg - n_groups;
       unit.off = s.len - s.n + 1 - s.t0;
       unit.bad = s.len < 0;
     }
-    unit.r0 = t0 * G + k.i * m;
-    unit.nr = rows_of(k);
-    for (int q = 0; q < pieces; ++q) {
-      unit.k0 = piece_start(first, k.keys, pieces, q);
-      unit.k1 = piece_start(first, k.keys, pieces, q + 1);
-      unit.slot = sums ? (int)(slot + (int64_t)q * step) : -1;
-      p.units[u + q] = unit;
-    }
-    u += pieces;
-    if (sums) slot += (int64_t)pieces * step;
-  });
+    unit.r0 = t0 * G + k.i * k.m;
+    unit.nr = k.nr;
+    unit.k0 = step_key(k.first, k.keys, k.steps, j0);
+    unit.k1 = step_key(k.first, k.keys, k.steps, j1);
+    unit.slot = (int)slot;
+    return unit;
+  };
+  {
+    int64_t u = at[kUnits], slot = at[kSlots];
+    walk([&](int x, const Block& k) {
+      const int pieces = pieces_at(x, k), step = k.m / kSlotRows;
+      const bool sums = leaves_sums(k, pieces);
+      if (k.seg < n_groups && k.i == 0) {
+        p.groups[k.seg].slot = (int)slot;
+        p.groups[k.seg].pieces = pieces;
+      }
+      if (stretched) {
+        slot_of[x] = sums ? (int)slot : -1;
+      } else {
+        for (int q = 0; q < pieces; ++q) {
+          p.units[u + q] = unit_of(k, (int)((int64_t)k.steps * q / pieces), q + 1 == pieces ? k.steps : (int)((int64_t)k.steps * (q + 1) / pieces),
+                                   sums ? slot + (int64_t)q * step : -1);
+          p.stretches[u + q] = (int)(u + q);
+        }
+        u += pieces;
+      }
+      if (sums) slot += (int64_t)pieces * step;
+    });
+  }
   __syncthreads();
-  slot = at[kSlots];
-  int64_t j = at[kJoins], row = at[kRows];
-  walk([&](const Block& k) {
-    const int pieces = pieces_of(k.keys, cut), m = block_rows(k.rows), step = m / kSlotRows;
+  if (stretched) {
+    for (int u = tid; u < (int)n[kUnits]; u += 1024) {
+      const int s = last_at_most(first_unit, n_cuts, u);
+      const int64_t a = cuts[s], b = cuts[s + 1];
+      const int x = (int)(a >> 32) + u - first_unit[s];
+      const Block k = block_at(x, -1);
+      const int j0 = x == (int)(a >> 32) ? (int)a : 0, j1 = x == (int)(b >> 32) ? (int)b : k.steps;
+      const int q = j0 > 0 ? s - first_cut(x) + 1 : 0;
+      p.units[u] = unit_of(k, j0, j1, slot_of[x] < 0 ? -1 : slot_of[x] + (int64_t)q * (k.m / kSlotRows));
+    }
+  } else if (tid == 0) {
+    p.stretches[n[kUnits]] = (int)n[kUnits];
+  }
+  int64_t slot = at[kSlots], j = at[kJoins], row = at[kRows];
+  walk([&](int x, const Block& k) {
+    const int pieces = pieces_at(x, k), step = k.m / kSlotRows;
     if (!leaves_sums(k, pieces)) return;
     if (k.seg >= n_groups) {
       const int b = k.seg - n_groups;
       AttendJoin e = {};
-      e.r0 = p.seqs[b].t0 * G + k.i * m;
-      e.nr = rows_of(k);
+      e.r0 = seqs[b].t0 * G + k.i * k.m;
+      e.nr = k.nr;
       e.own_slot = (int)slot;
       e.own_pieces = pieces;
       e.own_step = step;
-      if (p.seqs[b].shared > 0) {
-        const PlanGroup g = p.groups[group_of(p, b)];
-        e.pre_slot = g.slot;
-        e.pre_pieces = g.pieces;
-        e.pre_r0 = g.t0 * G;
-        e.pre_rows = block_rows((int64_t)g.tokens * G);
-      }
       e.first = (int)row;
       row += e.nr;
-      atomicMax(&most_pieces, e.own_pieces + e.pre_pieces);
+      e.group = seqs[b].shared > 0 ? group_of(p, b) : -1;
+      if (e.group < 0) atomicMax(&most_pieces, pieces);
       p.joins[j++] = e;
     }
     slot += (int64_t)pieces * step;
@@ -252,17 +345,22 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       o.own_at = e.own_slot * kSlotRows + r;
       o.own_pieces = e.own_pieces;
       o.own_step = e.own_step * kSlotRows;
-      if (e.pre_pieces > 0) {
-        const int in = o.row - e.pre_r0, block = in / e.pre_rows;
-        o.pre_at = (e.pre_slot + block * e.pre_pieces * (e.pre_rows / kSlotRows)) * kSlotRows + in % e.pre_rows;
-        o.pre_pieces = e.pre_pieces;
-        o.pre_step = e.pre_rows;
+      if (e.group >= 0) {  // (the blocks of a prefix may be cut differently)
+        const PlanGroup g = p.groups[e.group];
+        const int m = block_rows((int64_t)g.tokens * G), in = o.row - g.t0 * G, x = seg_start[e.group] + in / m;
+        if (in >= 0 && in < g.tokens * G) {
+          o.pre_pieces = stretched ? pieces_at(x, Block()) : g.pieces;
+          o.pre_at = (stretched ? slot_of[x] : g.slot + in / m * g.pieces * (m / kSlotRows)) * kSlotRows + in % m;
+          o.pre_step = m;
+        }
+        atomicMax(&most_pieces, o.own_pieces + o.pre_pieces);
       }
       p.rows[e.first + r] = o;
     }
   }
+  __syncthreads();
   if (tid == 0) {
-    p.header->n_units = (int)n[kUnits];
+    p.header->n_stretches = stretched ? n_cuts : (int)n[kUnits];
     p.header->n_rows = (int)n[kRows];
     p.header->n_slots = (int)n[kSlots];
     p.header->most_pieces = most_pieces;
@@ -412,10 +510,11 @@ extern "C" sp_status sp_attend_plan(const sp_attend_args* a, void* hip_stream) {
   PlanDev p;
   p.a = *a;
   p.G = a->H / a->H_kv;
-  p.cap_units = c.units; p.cap_joins = c.joins; p.cap_rows = c.rows; p.cap_slots = c.slots;
+  p.cap_blocks = c.blocks; p.cap_units = c.units; p.cap_joins = c.joins; p.cap_rows = c.rows; p.cap_slots = c.slots;
   p.print = attend_print(a);
   p.header = reinterpret_cast<AttendHeader*>(base);
   p.units = reinterpret_cast<AttendUnit*>(base + l.units);
+  p.stretches = reinterpret_cast<int32_t*>(base + l.stretches);
   p.joins = reinterpret_cast<AttendJoin*>(base + l.joins);
   p.rows = reinterpret_cast<AttendRow*>(base + l.rows);
   p.seg_start = reinterpret_cast<int32_t*>(base + l.seg_start);

@@ -16,6 +16,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SHIM = r"""
 #include "sp_attend_plan.h"
 #include <algorithm>
+#include <utility>
 #include <vector>
 using namespace sp;
 extern "C" void caps(const sp_attend_args* a, int64_t* out) {
@@ -23,30 +24,57 @@ extern "C" void caps(const sp_attend_args* a, int64_t* out) {
   const AttendPlanLayout l = attend_plan_layout(a);
   out[0] = c.blocks; out[1] = c.units; out[2] = c.joins; out[3] = c.slots; out[4] = (int64_t)l.bytes; out[5] = (int64_t)l.units;
   out[6] = (int64_t)l.joins; out[7] = (int64_t)l.seg_start; out[8] = (int64_t)l.seqs; out[9] = (int64_t)l.groups;
-  out[10] = sizeof(AttendUnit); out[11] = sizeof(AttendJoin); out[12] = (int64_t)attend_workspace(a); out[13] = (int64_t)attend_sums_bytes(a); out[14] = c.rows; out[15] = sizeof(AttendRow); out[16] = (int64_t)l.rows;
+  out[10] = sizeof(AttendUnit); out[11] = sizeof(AttendJoin); out[12] = (int64_t)attend_workspace(a); out[13] = (int64_t)attend_sums_bytes(a); out[14] = c.rows; out[15] = sizeof(AttendRow); out[16] = (int64_t)l.rows; out[17] = (int64_t)l.stretches;
 }
 extern "C" uint64_t print_of(const sp_attend_args* a) { return attend_print(a); }
+extern "C" int by_stretches_of(int64_t blocks, int d, int H_kv) { return by_stretches(blocks, d, H_kv); }
 extern "C" int share(int64_t rows, int members) { return shares(rows, members); }
-// segments: rows, n (0: a prefix), len, shared; blocks out: segment, i, keys, pieces, rows of a block; pieces out: block, first key, end
-extern "C" int cut_up(int n_seg, const int64_t* rows, const int* n, const int* len, const int* shared, int G, int H_kv, int* blocks, int* pieces, int* n_pieces) {
-  int64_t total = 0;
+// segments (prefixes first): rows, n (0: a prefix), len, shared.  blocks out, in the order that they are laid out in: segment, i,
+// first key, keys, pieces, rows of a block, cost of a step, steps; pieces out: block, first key, end, stretch.  Returns the number of blocks.
+extern "C" int cut_up(int n_seg, const int64_t* rows, const int* n, const int* len, const int* shared, int G, int H_kv, int d, int fp8, int* blocks,
+                      int* pieces, int* n_pieces, int* n_stretches) {
   int nb = 0;
-  for (int pass = 0; pass < 2; ++pass) {
-    const int cut = make_cut(total, H_kv);
-    nb = 0; *n_pieces = 0;
-    for (int s = 0; s < n_seg; ++s)
-      for (int i = 0; rows[s] > 0 && i < segment_blocks(rows[s]); ++i, ++nb) {
-        const int keys = n[s] ? own_block_keys(rows[s], i, G, n[s], len[s], shared[s]) : shared[s];
-        if (pass == 0) { total += keys; continue; }
-        const int p = pieces_of(keys, cut);
-        int* b = blocks + 5 * nb;
-        b[0] = s; b[1] = i; b[2] = keys; b[3] = p; b[4] = block_rows(rows[s]);
-        for (int q = 0; q < p; ++q, ++*n_pieces) {
-          int* x = pieces + 3 * *n_pieces;
-          x[0] = nb; x[1] = piece_start(shared[s] * (n[s] != 0), keys, p, q); x[2] = piece_start(shared[s] * (n[s] != 0), keys, p, q + 1);
-        }
-      }
+  int64_t keys_all = 0, cost_all = 0;
+  std::vector<int64_t> start;
+  auto add = [&](int s, int i) {
+    int* b = blocks + 8 * nb++;
+    b[0] = s; b[1] = i; b[2] = n[s] ? shared[s] : 0;
+    b[3] = n[s] ? own_block_keys(rows[s], i, G, n[s], len[s], shared[s]) : shared[s];
+    b[4] = 0; b[5] = block_rows(rows[s]); b[6] = step_cost(b[5] == kFewRows, d, fp8); b[7] = block_steps(b[2], b[3]);
+    start.push_back(cost_all);
+    keys_all += b[3]; cost_all += (int64_t)b[7] * b[6] + kBlockCost;
+  };
+  for (int s = 0; s < n_seg; ++s) if (!n[s]) for (int i = 0; rows[s] > 0 && i < segment_blocks(rows[s]); ++i) add(s, i);
+  for (int s = n_seg - 1; s >= 0; --s) if (n[s]) for (int i = segment_blocks(rows[s]) - 1; i >= 0; --i) add(s, i);
+  *n_pieces = 0;
+  auto piece = [&](int b, int k0, int k1, int s) { int* x = pieces + 4 * (*n_pieces)++; x[0] = b; x[1] = k0; x[2] = k1; x[3] = s; ++blocks[8 * b + 4]; };
+  if (!by_stretches(nb, d, H_kv)) {
+    const int cut = make_cut(keys_all, d, H_kv);
+    for (int b = 0; b < nb; ++b) {
+      const int* k = blocks + 8 * b;
+      const int p = pieces_of(k[3], cut);
+      for (int q = 0; q < p; ++q) piece(b, piece_start(k[2], k[3], p, q), piece_start(k[2], k[3], p, q + 1), *n_pieces);
+    }
+    *n_stretches = *n_pieces;
+    return nb;
   }
+  const int ns = stretch_count(cost_all, d, H_kv);
+  *n_stretches = ns;
+  std::vector<std::pair<int, int>> cuts;
+  for (int s = 0; s <= ns; ++s) {
+    if (s == 0 || s == ns) { cuts.push_back({s == 0 ? 0 : nb, 0}); continue; }
+    const int64_t x = stretch_start(cost_all, ns, s);
+    int b = (int)(std::upper_bound(start.begin(), start.end(), x) - start.begin()) - 1;
+    int j = step_at(x, start[b], blocks[8 * b + 7], blocks[8 * b + 6]);
+    if (j > 0 && j >= blocks[8 * b + 7]) { ++b; j = 0; }
+    cuts.push_back({b, j});
+  }
+  for (int s = 0; s < ns; ++s)
+    for (int b = cuts[s].first; b < cuts[s + 1].first + (cuts[s + 1].second > 0); ++b) {
+      const int* k = blocks + 8 * b;
+      const int j0 = b == cuts[s].first ? cuts[s].second : 0, j1 = b == cuts[s + 1].first ? cuts[s + 1].second : k[7];
+      piece(b, step_key(k[2], k[3], k[7], j0), step_key(k[2], k[3], k[7], j1), s);
+    }
   return nb;
 }
 """
@@ -62,6 +90,7 @@ def shim(tmp_path_factory):
     lib = C.CDLL(str(where / "shim.so"))
     lib.print_of.restype = C.c_uint64
     lib.share.argtypes = [C.c_int64, C.c_int]
+    lib.by_stretches_of.argtypes = [C.c_int64, C.c_int, C.c_int]
     return lib
 
 
@@ -73,9 +102,9 @@ def _args(**kw):
 
 
 def _caps(shim, a):
-    out = (C.c_int64 * 17)()
+    out = (C.c_int64 * 18)()
     shim.caps(C.byref(a), out)
-    return dict(zip("blocks units joins slots bytes at_units at_joins at_seg at_seqs at_groups unit join workspace sums rows row at_rows".split(), out))
+    return dict(zip("blocks units joins slots bytes at_units at_joins at_seg at_seqs at_groups unit join workspace sums rows row at_rows at_stretches".split(), out))
 
 
 def _batches():
@@ -96,10 +125,21 @@ def _batches():
     return fixed
 
 
-@pytest.mark.parametrize("heads", [(32, 8), (8, 8), (128, 8), (24, 8), (7, 1), (1024, 1024)])
-def test_pieces_cover_every_block_within_the_reserved_room(shim, heads):
+def _cut(shim, segs, G, H_kv, d=128, fp8=0):
+    arr = lambda i, t: np.array([s[i] for s in segs], dtype=t)  # noqa: E731
+    arrays = [arr(0, np.int64), arr(1, np.int32), arr(2, np.int32), arr(3, np.int32)]
+    blocks, pieces = np.zeros(8 * 80000, np.int32), np.zeros(4 * 80000, np.int32)
+    n_pieces, n_stretches = C.c_int(), C.c_int()
+    ptr = lambda x: x.ctypes.data_as(C.c_void_p)  # noqa: E731
+    nb = shim.cut_up(len(segs), *[ptr(x) for x in arrays], G, H_kv, d, fp8, ptr(blocks), ptr(pieces), C.byref(n_pieces), C.byref(n_stretches))
+    return blocks[:8 * nb].reshape(-1, 8), pieces[:4 * n_pieces.value].reshape(-1, 4), n_stretches.value
+
+
+@pytest.mark.parametrize("heads", [(32, 8), (8, 8), (128, 8), (24, 8), (7, 1), (1024, 1024), (64, 2)])
+@pytest.mark.parametrize("kind", [(128, 0), (128, 1), (64, 0)])
+def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
     H, H_kv = heads
-    G = H // H_kv
+    G, (d, fp8) = H // H_kv, kind
     for new, length, groups in _batches():
         B = len(new)
         shared = [0] * B
@@ -115,18 +155,12 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads):
                 segs.append((rows, 0, 0, p))
         n_prefix = len(segs)
         segs += [(n * G, n, m, s) for n, m, s in zip(new, length, shared)]
-        arr = lambda i, t: np.array([s[i] for s in segs], dtype=t)  # noqa: E731
-        rows, n, ln, sh = arr(0, np.int64), arr(1, np.int32), arr(2, np.int32), arr(3, np.int32)
-        blocks, pieces = np.zeros(5 * 40000, np.int32), np.zeros(3 * 40000, np.int32)
-        n_pieces = C.c_int()
-        ptr = lambda x: x.ctypes.data_as(C.c_void_p)  # noqa: E731
-        nb = shim.cut_up(len(segs), ptr(rows), ptr(n), ptr(ln), ptr(sh), G, H_kv, ptr(blocks), ptr(pieces), C.byref(n_pieces))
-        blocks, pieces = blocks[:5 * nb].reshape(-1, 5), pieces[:3 * n_pieces.value].reshape(-1, 3)
-        caps = _caps(shim, _args(B=B, H=H, H_kv=H_kv, T_new=sum(new), n_groups=len(groups)))
-        # the keys of a block, in order and without gaps; whole steps of 64 apart from the end
-        for i, (s, k, keys, p, m) in enumerate(blocks):
+        rows, n, ln, sh = ([s[i] for s in segs] for i in range(4))
+        blocks, pieces, n_stretches = _cut(shim, segs, G, H_kv, d, fp8)
+        caps = _caps(shim, _args(B=B, H=H, H_kv=H_kv, d=d, T_new=sum(new), n_groups=len(groups), cache_dtype=fp8))
+        # the keys of a block, in order and without gaps; whole steps of 64 of the sequence apart from the ends
+        for i, (s, k, first_key, keys, p, m, cost, steps) in enumerate(blocks):
             mine = pieces[pieces[:, 0] == i]
-            first_key = sh[s] if n[s] else 0
             assert len(mine) == p and mine[0, 1] == first_key and mine[-1, 2] == first_key + keys
             assert (mine[1:, 1] == mine[:-1, 2]).all() and (mine[1:, 1] % 64 == 0).all()
             assert p == 1 or (mine[:, 2] > mine[:, 1]).all()
@@ -136,33 +170,41 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads):
                 assert keys == max(0, want)
                 first = ln[s] - n[s] + (k * m) // G + 1
                 assert sh[s] == 0 or first > sh[s]    # every row sees the whole prefix and a key behind it
+        assert sorted(set(zip(blocks[:, 0], blocks[:, 1]))) == sorted((s, i) for s in range(len(segs)) for i in range(-(-rows[s] // (16 if rows[s] <= 16 else 128))))
+        # every stretch is a run of pieces; none has much more than its share
+        assert (np.diff(pieces[:, 3]) >= 0).all() and (len(pieces) == 0 or pieces[-1, 3] < n_stretches)
+        if shim.by_stretches_of(len(blocks), d, H_kv) and len(pieces):
+            cost = [4 + -(-(int(x[2]) - (int(x[1]) & ~63)) // 64) * int(blocks[x[0], 6]) for x in pieces]
+            per = np.bincount(pieces[:, 3], weights=cost, minlength=n_stretches)
+            share = (blocks[:, 7] * blocks[:, 6] + 4).sum() / n_stretches
+            assert per.max() <= share + 4 + 4 * 5 + 4 + 1     # a snapped end on either side, a cut block's cost again
         # room
-        leaves = [bool(p > 1 or s < n_prefix or sh[s] > 0) for s, _, _, p, _ in blocks]
-        assert nb <= caps["blocks"] and len(pieces) <= caps["units"]
+        leaves = [bool(b[4] > 1 or b[0] < n_prefix or sh[b[0]] > 0) for b in blocks]
+        assert len(blocks) <= caps["blocks"] and len(pieces) <= caps["units"] and n_stretches <= max(caps["units"], 1)
         assert sum(1 for x, b in zip(leaves, blocks) if x and b[0] >= n_prefix) <= caps["joins"]
-        slots = sum(int(b[3]) * int(b[4]) // 16 for x, b in zip(leaves, blocks) if x)
+        slots = sum(int(b[4]) * int(b[5]) // 16 for x, b in zip(leaves, blocks) if x)
         assert slots <= caps["slots"], (new, length, groups)
-        assert caps["at_units"] + caps["units"] * caps["unit"] <= caps["at_joins"]
+        assert caps["at_units"] + caps["units"] * caps["unit"] <= caps["at_stretches"]
+        assert caps["at_stretches"] + 4 * (caps["units"] + 1) <= caps["at_joins"]
         assert caps["at_joins"] + caps["joins"] * caps["join"] <= caps["at_rows"]
-        assert sum(min(int(b[4]), int(rows[b[0]] - b[1] * b[4])) for x, b in zip(leaves, blocks) if x and b[0] >= n_prefix) <= caps["rows"]
+        assert sum(min(int(b[5]), int(rows[b[0]] - b[1] * b[5])) for x, b in zip(leaves, blocks) if x and b[0] >= n_prefix) <= caps["rows"]
         assert caps["at_rows"] + caps["rows"] * caps["row"] <= caps["at_seg"]
         assert caps["at_seg"] + 4 * (B + len(groups) + 1) <= caps["at_seqs"] and caps["at_seqs"] + 16 * B <= caps["at_groups"]
         assert caps["at_groups"] + 32 * len(groups) <= caps["bytes"]
-        assert caps["sums"] >= caps["slots"] * H_kv * 16 * 128 * 4 and caps["workspace"] >= caps["sums"] + caps["slots"] * H_kv * 16 * 8
+        assert caps["sums"] >= caps["slots"] * H_kv * 16 * d * 4 and caps["workspace"] >= caps["sums"] + caps["slots"] * H_kv * 16 * 8
 
 
 def test_equal_work_is_spread_over_the_device(shim):
-    """One long sequence: about a thousand workgroups of equal pieces; short ones: pieces of 128 keys; many blocks: no cuts."""
-    def pieces_of(rows, n, ln):
-        arrays = [np.array([rows], np.int64), np.array([n], np.int32), np.array([ln], np.int32), np.zeros(1, np.int32)]
-        blocks, pieces, count = np.zeros(5 * 4000, np.int32), np.zeros(3 * 8000, np.int32), C.c_int()
-        shim.cut_up(1, *[x.ctypes.data_as(C.c_void_p) for x in arrays], 4, 8, blocks.ctypes.data_as(C.c_void_p), pieces.ctypes.data_as(C.c_void_p), C.byref(count))
-        p = pieces[:3 * count.value].reshape(-1, 3)
-        return p[:, 2] - p[:, 1]
-    long = pieces_of(4, 1, 131072)
-    assert 100 <= len(long) <= 128 and long.max() <= 1.1 * long.mean() + 64
-    assert pieces_of(4, 1, 1000).max() <= 128
-    assert len(pieces_of(4 * 20000, 20000, 20000)) == 4 * 20000 // 128
+    """One long sequence: 64 stretches for each of 8 KV heads; a short one: pieces of 128 keys; many blocks: no cuts."""
+    blocks, pieces, n = _cut(shim, [(4, 1, 131072, 0)], 4, 8)
+    size = pieces[:, 2] - pieces[:, 1]
+    assert n == len(pieces) == 64 and size.max() <= 1.1 * size.mean() + 64
+    assert (lambda p: (p[:, 2] - p[:, 1]).max())(_cut(shim, [(4, 1, 1000, 0)], 4, 8)[1]) == 128
+    blocks, pieces, n = _cut(shim, [(4 * 20000, 20000, 20000, 0)], 4, 8)
+    assert n == len(pieces) == len(blocks) == 4 * 20000 // 128
+    assert (np.diff(pieces[:, 2]) <= 0).all()          # the longest first
+    blocks, pieces, n = _cut(shim, [(4, 1, 1000 + 37 * i, 0) for i in range(64)], 4, 8)
+    assert n == 64 and len(pieces) <= 64 + 63
 
 
 def test_a_plan_knows_the_shape_it_was_made_for(shim):

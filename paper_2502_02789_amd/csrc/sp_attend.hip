@@ -63,26 +63,46 @@ __device__ __forceinline__ void widen_e4m3(const u32x4 w, u32x4& lo, u32x4& hi) 
 }
 
 // Where the rows of a piece's keys lie.  Tiles start at multiples of 8 keys and pages hold multiples of 8, so the 8 keys of an
-// octet lie at one stride from one base, which is looked up and formed in scalar registers, once for all lanes of a wave.
+// octet lie at one stride from one base, formed in scalar registers, once for all lanes of a wave.  The page numbers come in
+// vector registers, 64 at a time and 64 ahead, a lane each (scalar loads would share a counter with the LDS reads, each of
+// whose waits would then wait for them too: 202 -> 196 us for 64 new tokens behind 128K keys of 32 over 8 heads).
 template <bool PAGED>
 struct KeyRows {
-  ScalarTable table;
-  int lg_page, first, last_key;
-  uint32_t last;
+  const int32_t* table;
+  int lg_page, first, last_key, lane, chunk;
+  uint32_t last, pages, next;
   int32_t ts;
   int64_t ps;
-  __device__ __forceinline__ KeyRows(const AttendDev& p, const AttendUnit& u) {
-    ts = p.c_ts; ps = p.c_ps; lg_page = p.lg_page; last_key = u.k1 - 1;
-    table = scalar_table(PAGED ? p.table + (int64_t)u.seq * p.blocks_per_seq : nullptr);
+  // key: the first that will be asked for
+  __device__ __forceinline__ KeyRows(const AttendDev& p, const AttendUnit& u, int l, int key) {
+    ts = p.c_ts; ps = p.c_ps; lg_page = p.lg_page; last_key = u.k1 - 1; lane = l;
     first = PAGED ? 0 : scalar_table(p.cu_cache)[u.seq];
     last = PAGED ? p.last_page : p.last_row;
+    table = p.table + (int64_t)u.seq * p.blocks_per_seq;
+    if (PAGED && u.k0 < u.k1) {
+      chunk = min(key, last_key) >> lg_page >> 6;
+      pages = load(chunk);
+      next = load(chunk + 1);
+    }
+  }
+  __device__ __forceinline__ uint32_t load(int c) const { return (uint32_t)table[min(c * 64 + lane, last_key >> lg_page)]; }
+  // before the octets of a tile (its keys' pages lie in one run of 64) that begins at `key`, fewer than 64 pages on from the one before
+  __device__ __forceinline__ void advance(int key) {
+    if constexpr (PAGED) {
+      const int c = min(key, last_key) >> lg_page >> 6;
+      if (c != chunk) {
+        chunk = c;
+        pages = next;
+        next = load(c + 1);
+      }
+    }
   }
   // first key of the octet that `key` (wave-uniform) lies in, no further than the last key's
   __device__ __forceinline__ int octet(int key) const { return min(key, last_key) & ~7; }
-  __device__ __forceinline__ uint32_t look_up(int octet) const { return PAGED ? (uint32_t)table[octet >> lg_page] : 0; }
-  // byte offset of the octet's first key; entry: what look_up() gave.  Nothing outside the pool is addressed, a bad entry is noted.
-  __device__ __forceinline__ int64_t base(int octet, uint32_t entry, uint32_t& bad) const {
+  // byte offset of the octet's first key.  Nothing outside the pool is addressed, a bad page is noted.
+  __device__ __forceinline__ int64_t base(int octet, uint32_t& bad) const {
     if constexpr (PAGED) {
+      const uint32_t entry = (uint32_t)__builtin_amdgcn_readlane((int)pages, (octet >> lg_page) & 63);
       bad |= entry > last;
       return (int64_t)min(entry, last) * ps + (int64_t)(octet & ((1 << lg_page) - 1)) * ts;
     } else {
@@ -170,7 +190,8 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   const bool mine = row < u.nr;
   const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
 
-  const KeyRows<PAGED> rows(p, u);
+  int tile = u.k0 < u.k1 ? (u.k0 & ~31) + 32 * w : u.k1;
+  KeyRows<PAGED> rows(p, u, l, tile);
   const char* const kb = p.k + (int64_t)g * p.c_hs;
   const char* const vb = p.v + (int64_t)g * p.c_hs;
   char* const kd = lds + w * (2 * 32 * D * 2);
@@ -179,35 +200,29 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   uint32_t bad = 0;
   Tile kt, vl;
   int64_t oct_at[Tile::N];
-  uint32_t in[Tile::N], entry[4];
-  auto look_up = [&](int tile) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) entry[j] = rows.look_up(rows.octet(tile + 8 * j));
-  };
+  uint32_t in[Tile::N];
   auto place = [&](int tile) {
+    rows.advance(tile);
 #pragma unroll
     for (int i = 0; i < Tile::N; ++i) {
       constexpr int R = Tile::R;
-      const int j = R * i / 8, oct = rows.octet(tile + 8 * j);
+      const int oct = rows.octet(tile + R * i);
       if constexpr (R <= 8) {
-        oct_at[i] = rows.base(oct, entry[j], bad);
+        oct_at[i] = rows.base(oct, bad);
         in[i] = rows.within(oct, tile + R * i + lane_row) + lane_chunk;
       } else {                        // a load covers two octets
-        const int oct1 = rows.octet(tile + 8 * j + 8);
-        const int64_t b0 = rows.base(oct, entry[j], bad), b1 = rows.base(oct1, entry[j + 1], bad);
+        const int oct1 = rows.octet(tile + R * i + 8);
+        const int64_t b0 = rows.base(oct, bad), b1 = rows.base(oct1, bad);
         const bool second = lane_row >= 8;
         oct_at[i] = second ? b1 : b0;
         in[i] = rows.within(second ? oct1 : oct, tile + R * i + lane_row) + lane_chunk;
       }
     }
   };
-  int tile = u.k0 < u.k1 ? (u.k0 & ~31) + 32 * w : u.k1;
   if (tile < u.k1) {
-    look_up(tile);
     place(tile);
     kt.load(kb, oct_at, in);
     vl.load(vb, oct_at, in);
-    look_up(tile + 128);
   }
 
   // the queries
@@ -251,10 +266,7 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
       s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(at0 + 16 * D * 2), qf[s], s1, 0, 0, 0);
     }
     vl.store(vd, l);
-    if (more) {
-      vl.load(vb, oct_at, in);
-      look_up(tile + 256);
-    }
+    if (more) vl.load(vb, oct_at, in);
 
     float x[8];
 #pragma unroll
@@ -414,7 +426,8 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
   least = __builtin_amdgcn_readfirstlane(least);
   most = __builtin_amdgcn_readfirstlane(most);
 
-  const KeyRows<PAGED> rows(p, u);
+  const int first_tile = u.k0 < u.k1 ? u.k0 & ~(kTileKeys - 1) : u.k1;
+  KeyRows<PAGED> rows(p, u, l, first_tile);
   const char* const kb = p.k + (int64_t)g * p.c_hs;
   const char* const vb = p.v + (int64_t)g * p.c_hs;
   const int lane_row = l / Tile::C, lane_chunk = (l % Tile::C) * 16;
@@ -440,26 +453,20 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
     }
 
   // the wave's loads cover rows w R + STEP i of a tile, R <= 8 of one octet or R = 16 of two
-  constexpr int R = 64 / Tile::C, O = R > 8 ? 2 : 1;
+  constexpr int R = 64 / Tile::C;
   Tile kt, vl;
-  uint32_t entry[Tile::N][O];
-  auto look_up = [&](int tile) {
-#pragma unroll
-    for (int i = 0; i < Tile::N; ++i)
-#pragma unroll
-      for (int j = 0; j < O; ++j) entry[i][j] = rows.look_up(rows.octet(tile + R * w + Tile::STEP * i + 8 * j));
-  };
   auto load = [&](int tile) {
     int64_t at[Tile::N];
     uint32_t in[Tile::N];
+    rows.advance(tile);
 #pragma unroll
     for (int i = 0; i < Tile::N; ++i) {
       const int first = tile + R * w + Tile::STEP * i;
       int oct = rows.octet(first);
-      at[i] = rows.base(oct, entry[i][0], bad);
-      if constexpr (O == 2) {
+      at[i] = rows.base(oct, bad);
+      if constexpr (R > 8) {
         const int oct1 = rows.octet(first + 8);
-        const int64_t at1 = rows.base(oct1, entry[i][1], bad);
+        const int64_t at1 = rows.base(oct1, bad);
         if (lane_row >= 8) { at[i] = at1; oct = oct1; }
       }
       in[i] = rows.within(oct, first + lane_row) + lane_chunk;
@@ -467,12 +474,7 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
     kt.load(kb, at, in);
     vl.load(vb, at, in);
   };
-  const int first_tile = u.k0 < u.k1 ? u.k0 & ~(kTileKeys - 1) : u.k1;
-  if (first_tile < u.k1) {
-    look_up(first_tile);
-    load(first_tile);
-    look_up(first_tile + kTileKeys);
-  }
+  if (first_tile < u.k1) load(first_tile);
   // One tile out of buffer BUF (a constant, so that the operands' addresses are too).  The compiler is told how to mix reads, products and
   // the rest: operands are read several products ahead, and the weights of the next 16 keys are formed while the
   // matrix cores work on these.
@@ -482,11 +484,9 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
     kt.store(kd, tid);
     vl.store(vd, tid);
     __syncthreads();
-    if (tile + kTileKeys < u.k1) {
-      load(tile + kTileKeys);
-      look_up(tile + 2 * kTileKeys);
-    }
+    if (tile + kTileKeys < u.k1) load(tile + kTileKeys);
     if (tile >= most) return;  // (the wave's rows see none of these keys)
+    __builtin_amdgcn_s_setprio(1);  // products first: the other wave's other instructions fill the gaps
     f32x16 s[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -506,6 +506,7 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       __builtin_amdgcn_sched_group_barrier(kSchedLdsRead, 1, 0);
     }
     __builtin_amdgcn_sched_group_barrier(kSchedMfma, kAhead, 0);
+    __builtin_amdgcn_s_setprio(0);
     if (tile + kTileKeys > least || tile < u.k0) {
 #pragma unroll
       for (int x = 0; x < 2; ++x)
@@ -531,6 +532,7 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       for (int i = 0; i < DB; ++i) o[i] *= f;
     }
     const float base = m == -INFINITY ? 0.f : m;
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float x[8], part = 0.f;
@@ -560,6 +562,7 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
           __builtin_amdgcn_sched_group_barrier(kSchedValu, 28 / DB, 0);
         }
       }
+    __builtin_amdgcn_s_setprio(0);
   };
   for (int tile = first_tile; tile < u.k1; tile += 2 * kTileKeys) {
     step(std::integral_constant<int, 0>(), tile);

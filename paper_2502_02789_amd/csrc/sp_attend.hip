@@ -182,6 +182,7 @@ struct FewTile {
 
 template <int D, bool FP8, bool PAGED>
 __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit& u, int g, char* lds) {
+  constexpr int NW = attend_waves(D);
   constexpr int KS = D / 32;          // steps of the product with the queries
   constexpr int DB = D / 16;          // blocks of values
   constexpr int C = D / 8;            // 16-byte chunks of a bf16 row
@@ -250,11 +251,11 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   for (int i = 0; i < DB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, sum = 0.f;
 
-  for (; tile < u.k1; tile += 128) {
-    const bool more = tile + 128 < u.k1;
+  for (; tile < u.k1; tile += 32 * NW) {
+    const bool more = tile + 32 * NW < u.k1;
     kt.store(kd, l);
     if (more) {
-      place(tile + 128);
+      place(tile + 32 * NW);
       kt.load(kb, oct_at, in);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -306,19 +307,25 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
-  // the four waves' sums joined, in the waves' order
+  // the waves' sums joined, in the waves' order
   sum += __shfl_xor(sum, 16, kWave);
   sum += __shfl_xor(sum, 32, kWave);
-  float* const stat = reinterpret_cast<float*>(lds + 4 * 16 * (D + 4) * 4);  // [2][4][16]
+  float* const tops = reinterpret_cast<float*>(lds + NW * 16 * (D + 4) * 4);  // [NW][16], twice
+  float* const sums = tops + NW * 16;
   const int any_bad = __syncthreads_or(bad != 0);  // (also: every wave is done with its tile in LDS)
   if (quad == 0) {
-    stat[w * 16 + row] = m;
-    stat[64 + w * 16 + row] = sum;
+    tops[w * 16 + row] = m;
+    sums[w * 16 + row] = sum;
   }
   __syncthreads();
+  auto top_of = [&](int r) {
+    float top = tops[r];
+#pragma unroll
+    for (int x = 1; x < NW; ++x) top = fmaxf(top, tops[x * 16 + r]);
+    return top;
+  };
   {
-    float top = fmaxf(fmaxf(stat[row], stat[16 + row]), fmaxf(stat[32 + row], stat[48 + row]));
-    const float f = fast_exp2(m - (top == -INFINITY ? 0.f : top));
+    const float top = top_of(row), f = fast_exp2(m - (top == -INFINITY ? 0.f : top));
     float* const part = reinterpret_cast<float*>(lds) + (w * 16 + row) * (D + 4);
 #pragma unroll
     for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(part + 16 * i + 4 * quad) = o[i] * f;
@@ -328,13 +335,13 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   if (r >= u.nr) return;
   constexpr int V = D / 16;
   float acc[V], l_all = 0.f;
-  const float top = fmaxf(fmaxf(stat[r], stat[16 + r]), fmaxf(stat[32 + r], stat[48 + r]));
+  const float top = top_of(r);
   const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.f;
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    l_all += stat[64 + x * 16 + r] * fast_exp2(stat[x * 16 + r] - base);
+  for (int x = 0; x < NW; ++x) {
+    l_all += sums[x * 16 + r] * fast_exp2(tops[x * 16 + r] - base);
     const float* part = reinterpret_cast<const float*>(lds) + (x * 16 + r) * (D + 4) + lane * V;
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] += part[i];
@@ -363,12 +370,12 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
 }
 
 // ---------------------------------------------------------------- many rows
-// one lane's share of a 64-key tile of keys or values: chunks tid + 256 i of the tile's 16-byte chunks
-template <int D, bool FP8>
+// one lane's share of a 64-key tile of keys or values that T threads load: chunks tid + T i of the tile's 16-byte chunks
+template <int D, bool FP8, int T>
 struct ManyTile {
   static constexpr int C = FP8 ? D / 16 : D / 8;           // 16-byte chunks of a stored row
-  static constexpr int N = kTileKeys * C / 256;
-  static constexpr int STEP = 256 / C;                     // rows between a lane's chunks
+  static constexpr int N = kTileKeys * C / T;
+  static constexpr int STEP = T / C;                       // rows between a lane's chunks
   u32x4 x[N];
   __device__ __forceinline__ void load(const char* base, const int64_t (&at)[N], const uint32_t (&in)[N]) {
 #pragma unroll
@@ -392,15 +399,22 @@ struct ManyTile {
   }
 };
 
-template <int D, bool FP8, bool PAGED>
+// SPLIT: the block has no more rows than half of the waves take: the two halves of the workgroup have the same rows and take tiles in turn, each
+// with two buffers of its own, and add their sums up at the end.
+template <int D, bool FP8, bool PAGED, bool SPLIT>
 __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit& u, int g, char* lds) {
+  constexpr int NW = attend_waves(D), TW = SPLIT ? NW / 2 : NW;  // waves, waves that share a tile
+  constexpr int SETS = NW == 8 && !SPLIT ? 2 : 1;                // tiles on their way from memory
+  constexpr int STRIDE = SPLIT ? 2 * kTileKeys : kTileKeys;      // keys from one tile of a wave to the next
   constexpr int KS = D / 16;   // steps of the product with the queries
   constexpr int DB = D / 32;   // blocks of values
   constexpr int C = D / 8;
   constexpr int TILE = kTileKeys * D * 2;  // bytes of a tile of keys or of values
-  using Tile = ManyTile<D, FP8>;
-  const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, half = l >> 5;
+  using Tile = ManyTile<D, FP8, 64 * TW>;
+  const int all_tid = thread_of_piece(), share = SPLIT ? __builtin_amdgcn_readfirstlane(all_tid / (64 * TW)) : 0, tid = all_tid - share * 64 * TW;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, half = l >> 5;
   const int row = w * 32 + (l & 31);
+  char* const tiles = lds + share * 4 * TILE;
   const bool mine = row < u.nr;
   const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
   uint32_t flip, keep;
@@ -426,8 +440,8 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
   least = __builtin_amdgcn_readfirstlane(least);
   most = __builtin_amdgcn_readfirstlane(most);
 
-  const int first_tile = u.k0 < u.k1 ? u.k0 & ~(kTileKeys - 1) : u.k1;
-  KeyRows<PAGED> rows(p, u, l, first_tile);
+  const int first_tile = u.k0 < u.k1 ? u.k0 & ~(kTileKeys - 1) : u.k1, my_first = first_tile + share * kTileKeys;
+  KeyRows<PAGED> rows(p, u, l, my_first);
   const char* const kb = p.k + (int64_t)g * p.c_hs;
   const char* const vb = p.v + (int64_t)g * p.c_hs;
   const int lane_row = l / Tile::C, lane_chunk = (l % Tile::C) * 16;
@@ -454,8 +468,8 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
 
   // the wave's loads cover rows w R + STEP i of a tile, R <= 8 of one octet or R = 16 of two
   constexpr int R = 64 / Tile::C;
-  Tile kt, vl;
-  auto load = [&](int tile) {
+  Tile kt[SETS], vl[SETS];
+  auto load = [&](int tile, Tile& kt, Tile& vl) {
     int64_t at[Tile::N];
     uint32_t in[Tile::N];
     rows.advance(tile);
@@ -474,17 +488,21 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
     kt.load(kb, at, in);
     vl.load(vb, at, in);
   };
-  if (first_tile < u.k1) load(first_tile);
+  if (my_first < u.k1) load(my_first, kt[0], vl[0]);
+  if (SETS == 2 && my_first + STRIDE < u.k1) load(my_first + STRIDE, kt[SETS - 1], vl[SETS - 1]);
   // One tile out of buffer BUF (a constant, so that the operands' addresses are too).  The compiler is told how to mix reads, products and
   // the rest: operands are read several products ahead, and the weights of the next 16 keys are formed while the
   // matrix cores work on these.
   auto step = [&](auto buf, int tile) {
-    char* const kd = lds + decltype(buf)::value * 2 * TILE;
+    constexpr int SET = decltype(buf)::value % SETS;
+    char* const kd = tiles + decltype(buf)::value * 2 * TILE;
     char* const vd = kd + TILE;
-    kt.store(kd, tid);
-    vl.store(vd, tid);
+    if (!SPLIT || tile < u.k1) {
+      kt[SET].store(kd, tid);
+      vl[SET].store(vd, tid);
+    }
     __syncthreads();
-    if (tile + kTileKeys < u.k1) load(tile + kTileKeys);
+    if (tile + SETS * STRIDE < u.k1) load(tile + SETS * STRIDE, kt[SET], vl[SET]);
     if (tile >= most) return;  // (the wave's rows see none of these keys)
     __builtin_amdgcn_s_setprio(1);  // products first: the other wave's other instructions fill the gaps
     f32x16 s[2];
@@ -564,13 +582,43 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       }
     __builtin_amdgcn_s_setprio(0);
   };
-  for (int tile = first_tile; tile < u.k1; tile += 2 * kTileKeys) {
-    step(std::integral_constant<int, 0>(), tile);
-    if (tile + kTileKeys < u.k1) step(std::integral_constant<int, 1>(), tile + kTileKeys);
+  for (int tile = first_tile; tile < u.k1; tile += 2 * STRIDE) {  // (both halves go through as many barriers)
+    step(std::integral_constant<int, 0>(), tile + share * kTileKeys);
+    if (tile + STRIDE < u.k1) step(std::integral_constant<int, 1>(), tile + STRIDE + share * kTileKeys);
   }
 
   const int any_bad = __syncthreads_or(bad != 0);
   sum += __shfl_xor(sum, 32, kWave);
+  if constexpr (SPLIT) {
+    // the second half's sums through LDS: blocks of 4 values of a row side by side for 32 rows, so that a wave writes and reads whole runs
+    float* const part = reinterpret_cast<float*>(lds) + w * (32 * D);
+    float* const stat = reinterpret_cast<float*>(lds + TW * 32 * D * 4) + w * 64;
+    if (share == 1) {
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *reinterpret_cast<f32x4*>(part + ((i * 4 + j) * 64 + l) * 4) = f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
+      if (half == 0) {
+        stat[l] = m;
+        stat[32 + l] = sum;
+      }
+    }
+    __syncthreads();
+    if (share == 1) return;
+    const float other = stat[l & 31], top = fmaxf(m, other), base = top == -INFINITY ? 0.f : top;
+    const float f = fast_exp2(m - base), h = fast_exp2(other - base);
+    sum = sum * f + stat[32 + (l & 31)] * h;
+    m = top;
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(part + ((i * 4 + j) * 64 + l) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][4 * j + e] = o[i][4 * j + e] * f + x[e] * h;
+      }
+  }
   if (!mine) return;
   if (u.slot >= 0) {
     const int64_t place = slot_row(p, u.slot, row, g);
@@ -614,8 +662,9 @@ __device__ __forceinline__ void nan_rows(const AttendDev& p, int d, int64_t r0, 
 }  // namespace
 
 template <int D, bool FP8, bool PAGED>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_kernel(const AttendDev p) {
-  __shared__ __align__(16) char lds[2 * 2 * kTileKeys * D * 2];  // (few rows need 34 KB of the 64, or 17.5 of the 32)
+__global__ __launch_bounds__(64 * attend_waves(D), D == 64 ? 3 : 2) void attend_kernel(const AttendDev p) {
+  constexpr int T = 64 * attend_waves(D);
+  __shared__ __align__(16) char lds[attend_waves(D) * 64 * D * 2];  // tiles: 16 KB a wave (8, d = 64); the sums of waves need less
   // The KV heads of a piece are neighbours: with eight of them, each has the L2 of one XCD, which the rows of a
   // block share, as workgroups go to the XCDs in turn.
   const int n = (int)(blockIdx.x / (uint32_t)p.H_kv), g = (int)(blockIdx.x % (uint32_t)p.H_kv);
@@ -627,7 +676,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_kernel(const Atte
   int x = stretch[n];
   const int end = stretch[n + 1];
   if (print != p.print) {
-    nan_rows(p, D, 0, (int64_t)p.T_new * p.H, p.H, 0, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256);
+    nan_rows(p, D, 0, (int64_t)p.T_new * p.H, p.H, 0, (int64_t)blockIdx.x * T + threadIdx.x, (int64_t)gridDim.x * T);
     return;
   }
   if (n >= n_stretches) return;
@@ -636,9 +685,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attend_kernel(const Atte
     AttendUnit u;
     u.r0 = unit->r0; u.nr = unit->nr; u.seq = unit->seq; u.k0 = unit->k0;
     u.k1 = unit->k1; u.off = unit->off; u.slot = unit->slot; u.bad = unit->bad;
-    if (u.bad) nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, 256);
+    if (u.bad) nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, T);
     else if (u.nr <= kFewRows) attend_few<D, FP8, PAGED>(p, u, g, lds);
-    else attend_many<D, FP8, PAGED>(p, u, g, lds);
+    else if (attend_waves(D) == 8 && u.nr <= many_rows(D) / 2) attend_many<D, FP8, PAGED, attend_waves(D) == 8>(p, u, g, lds);
+    else attend_many<D, FP8, PAGED, false>(p, u, g, lds);
     __syncthreads();  // (the next piece uses the same LDS)
   }
 }
@@ -667,8 +717,8 @@ sp_status check_attend(const sp_attend_args* a) {
 
 template <int D, bool FP8>
 void launch_attend(const AttendDev& p, bool paged, uint32_t grid, hipStream_t stream) {
-  if (paged) hipLaunchKernelGGL((attend_kernel<D, FP8, true>), dim3(grid), dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((attend_kernel<D, FP8, false>), dim3(grid), dim3(256), 0, stream, p);
+  if (paged) hipLaunchKernelGGL((attend_kernel<D, FP8, true>), dim3(grid), dim3(64 * attend_waves(D)), 0, stream, p);
+  else hipLaunchKernelGGL((attend_kernel<D, FP8, false>), dim3(grid), dim3(64 * attend_waves(D)), 0, stream, p);
 }
 
 }  // namespace

@@ -4,7 +4,7 @@
 // The rows of a call are (token, head of a KV head's group) pairs, row = token * G + head, flat over all tokens: the rows of a
 // sequence, and of a group of sequences, lie side by side.  A segment is a set of rows that attend to the same keys: the shared
 // prefix of a group (all rows of its members), or what a sequence has for itself.  A segment is cut into blocks of 16 rows
-// (if it has no more: one small matrix tile, bound by reading the keys) or of 128 (bound by the matrix cores).
+// (if it has no more: one small matrix tile, bound by reading the keys) or of many_rows() (bound by the matrix cores).
 //
 // The device has room for attend_items() workgroups at once.  Fewer than three times as many (block, KV head) pairs are laid end to end,
 // each at its cost, and cut into as many stretches of equal cost as there is room for: every workgroup has one, and all end together.
@@ -30,14 +30,18 @@
 namespace sp {
 
 constexpr int kFewRows = 16;      // rows of a block of a small segment
-constexpr int kManyRows = 128;    // ... and of any other
 constexpr int kSlotRows = 16;     // rows of a workspace slot
+constexpr int kShareRows = 128;   // see shares()
 constexpr int kPieceStep = 64;    // pieces are cut at multiples of so many keys
 constexpr int kMinSteps = 2;      // no piece is made shorter than so many steps
 constexpr int kMostStretchBlocks = 3 * 768;  // blocks that stretches are made for, at most
 
-// Workgroups that the device has room for: 256 compute units with two each (three where d = 64 takes half the LDS)
-SP_ATTEND_FN int attend_items(int d) { return d == 64 ? 768 : 512; }
+// Waves of a workgroup, and the workgroups that the device has room for: one of eight waves on each of 256 compute units, or, as
+// d = 64 takes a quarter of the LDS and fewer registers, three of four
+SP_ATTEND_FN constexpr int attend_waves(int d) { return d == 64 ? 4 : 8; }
+SP_ATTEND_FN constexpr int attend_items(int d) { return d == 64 ? 768 : 256; }
+// Rows of a block that has more than 16: 32 for each wave
+SP_ATTEND_FN constexpr int many_rows(int d) { return 32 * attend_waves(d); }
 
 struct AttendUnit {   // one piece of one block
   int32_t r0, nr;     // first row, rows (nr <= 16: the kernel part for few rows)
@@ -73,39 +77,39 @@ struct AttendCaps {
   int64_t blocks, units, joins, rows, slots;
 };
 
-// Upper bounds for any lengths that the shape fields allow.  Blocks: a segment of R rows has at most R / 128 + 1; own segments
+// Upper bounds for any lengths that the shape fields allow.  Blocks: a segment of R rows has at most R / many_rows() + 1; own segments
 // with a block: at most B and at most one per row; prefix segments: n_groups.  Pieces: cuts add at most attend_items() / H_kv to one per block.
 // Slots: prefix blocks, blocks of sequences with a prefix, and blocks of several pieces, of which there are at most as many as pieces added; a
 // prefix is only shared where a group has fewer than 128 rows per member on average (shares()), so rows in such groups are fewer than 128 B.
 inline AttendCaps attend_caps(const sp_attend_args* a) {
-  const int64_t rows = a->T_new * (a->H / a->H_kv), added = attend_items(a->d) / a->H_kv + 1;
-  const int64_t own_segments = rows < a->B ? rows : a->B, own = rows / kManyRows + own_segments;
-  const int64_t shared_rows = rows < (int64_t)kManyRows * a->B ? rows : (int64_t)kManyRows * a->B;
+  const int64_t many = many_rows(a->d), rows = a->T_new * (a->H / a->H_kv), added = attend_items(a->d) / a->H_kv + 1;
+  const int64_t own_segments = rows < a->B ? rows : a->B, own = rows / many + own_segments;
+  const int64_t shared_rows = rows < (int64_t)kShareRows * a->B ? rows : (int64_t)kShareRows * a->B;
   const int64_t groups = a->n_groups < own_segments ? a->n_groups : own_segments;  // those with a row
-  const int64_t prefix = a->n_groups ? shared_rows / kManyRows + groups : 0;
+  const int64_t prefix = a->n_groups ? shared_rows / many + groups : 0;
   AttendCaps c;
   c.blocks = own + prefix;
   c.units = c.blocks + added;
   c.joins = own;
   // rows to join: of blocks that are cut (of which there are at most as many as pieces added) and of sequences that share
-  const int64_t cut_rows = kManyRows * added + (a->n_groups ? shared_rows : 0);
+  const int64_t cut_rows = many * added + (a->n_groups ? shared_rows : 0);
   c.rows = rows < cut_rows ? rows : cut_rows;
-  // blocks that may leave sums, in blocks of 128 rows and in all; own segments of over 16 rows: at most one per 17
+  // blocks that may leave sums, in large blocks and in all; own segments of over 16 rows: at most one per 17
   const int64_t big_segments = own_segments < rows / (kFewRows + 1) ? own_segments : rows / (kFewRows + 1);
-  const int64_t shared_big = a->n_groups ? 2 * (shared_rows / kManyRows) + big_segments + (groups < rows / (kFewRows + 1) ? groups : rows / (kFewRows + 1)) : 0;
+  const int64_t shared_big = a->n_groups ? 2 * (shared_rows / many) + big_segments + (groups < rows / (kFewRows + 1) ? groups : rows / (kFewRows + 1)) : 0;
   const int64_t shared_few = a->n_groups ? own_segments + groups : 0;
   const bool any_big = rows > kFewRows;
   // pieces of blocks that are cut: at most two for each piece added
-  c.slots = (any_big ? (kManyRows / kSlotRows) : 1) * (2 * added) + (kManyRows / kSlotRows) * shared_big + shared_few;
+  c.slots = (any_big ? (many / kSlotRows) : 1) * (2 * added) + (many / kSlotRows) * shared_big + shared_few;
   return c;
 }
 
 // What a member's shared prefix saves: a block's rows are filled up by several members, and its keys read once for them all.  With 128 rows of its own
-// for each member there is nothing to gain.
-SP_ATTEND_FN bool shares(int64_t group_rows, int members) { return members >= 2 && group_rows < (int64_t)kManyRows * members; }
+// for each member there is little to gain.
+SP_ATTEND_FN bool shares(int64_t group_rows, int members) { return members >= 2 && group_rows < (int64_t)kShareRows * members; }
 
-SP_ATTEND_FN int block_rows(int64_t rows) { return rows <= kFewRows ? kFewRows : kManyRows; }
-SP_ATTEND_FN int segment_blocks(int64_t rows) { return (int)((rows + block_rows(rows) - 1) / block_rows(rows)); }
+SP_ATTEND_FN int block_rows(int64_t rows, int d) { return rows <= kFewRows ? kFewRows : many_rows(d); }
+SP_ATTEND_FN int segment_blocks(int64_t rows, int d) { return (int)((rows + block_rows(rows, d) - 1) / block_rows(rows, d)); }
 
 // One past the last key that row `row` of a sequence sees (its rows counted from 0, G to a token), n new tokens, len keys.
 SP_ATTEND_FN int row_limit(int64_t row, int G, int n, int len) {
@@ -113,9 +117,8 @@ SP_ATTEND_FN int row_limit(int64_t row, int G, int n, int len) {
   return v < 0 ? 0 : v > len ? len : (int)v;
 }
 
-// The keys of block i of a sequence's own segment: [shared, the limit of its last row)
-SP_ATTEND_FN int own_block_keys(int64_t rows, int i, int G, int n, int len, int shared) {
-  const int m = block_rows(rows);
+// The keys of block i (of m rows) of a sequence's own segment: [shared, the limit of its last row)
+SP_ATTEND_FN int own_block_keys(int64_t rows, int i, int m, int G, int n, int len, int shared) {
   const int64_t last = (int64_t)(i + 1) * m < rows ? (int64_t)(i + 1) * m - 1 : rows - 1;
   const int v = row_limit(last, G, n, len) - shared;
   return v < 0 ? 0 : v;
@@ -124,24 +127,28 @@ SP_ATTEND_FN int own_block_keys(int64_t rows, int i, int G, int n, int len, int 
 // Steps of 64 keys of a block's keys [first, first + keys), cut at multiples of 64 keys of the sequence
 SP_ATTEND_FN int block_steps(int first, int keys) { return (int)(((int64_t)(first & (kPieceStep - 1)) + keys + kPieceStep - 1) / kPieceStep); }
 
-// What a step costs a workgroup, in units of 0.55 us on a full device: 128 rows are bound by the matrix cores, 16 by reading 64 keys and values
-// (COSTS_MEASURED); and what a piece costs besides.
-SP_ATTEND_FN int step_cost(bool few, int d, bool fp8) { return !few ? 4 : d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5); }
-constexpr int kBlockCost = 4;
-constexpr int kMinStretch = 10;   // no stretch costs less: two steps of the dearest kind, and more than one of any
+// What a step costs a workgroup, in units of 0.27 us (d = 128) and 0.67 us on a full device: 16 rows are bound by reading 64 keys and
+// values, more by the matrix cores (eight waves with up to 128 rows work on two steps at a time); and what a piece costs besides.
+SP_ATTEND_FN int step_cost(int rows, int d, bool fp8) {
+  if (rows <= kFewRows) return d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5);
+  return d == 64 ? 4 : rows <= many_rows(d) / 2 ? 6 : 8;
+}
+SP_ATTEND_FN int piece_cost(int d) { return d == 64 ? 4 : 8; }
+// No stretch costs less: more than one step and a half of any kind
+SP_ATTEND_FN int least_stretch(int d) { return d == 64 ? 10 : 20; }
 
 SP_ATTEND_FN bool by_stretches(int64_t blocks, int d, int H_kv) { return blocks * H_kv < 3 * (int64_t)attend_items(d) && blocks <= kMostStretchBlocks; }
 // Stretches for each KV head, blocks of `cost` in all: what the device has room for, as long as that leaves each enough to do
 SP_ATTEND_FN int stretch_count(int64_t cost, int d, int H_kv) {
-  const int64_t room = attend_items(d) / H_kv > 0 ? attend_items(d) / H_kv : 1, most = cost / kMinStretch;
+  const int64_t room = attend_items(d) / H_kv > 0 ? attend_items(d) / H_kv : 1, most = cost / least_stretch(d);
   return (int)(most < 1 ? 1 : most < room ? most : room);
 }
 // Where stretch s of n begins, blocks laid end to end
 SP_ATTEND_FN int64_t stretch_start(int64_t cost, int n, int s) { return cost * s / n; }
 // ... as a step of the block whose share begins at `start` (what the block costs besides spread over its steps): `steps` (the next
 // block's first) or 0 where a piece would get too short
-SP_ATTEND_FN int step_at(int64_t x, int64_t start, int steps, int per_step) {
-  const int64_t cost = (int64_t)steps * per_step + kBlockCost, j = (2 * (x - start) * steps + cost) / (2 * cost);
+SP_ATTEND_FN int step_at(int64_t x, int64_t start, int steps, int per_step, int d) {
+  const int64_t cost = (int64_t)steps * per_step + piece_cost(d), j = (2 * (x - start) * steps + cost) / (2 * cost);
   return j < kMinSteps ? 0 : steps - j < kMinSteps ? steps : (int)j;
 }
 SP_ATTEND_FN int step_key(int first, int keys, int steps, int j) {

@@ -153,9 +153,9 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     __syncthreads();
   }
   block_prefix_table(n_groups + B, [&](int s) -> int32_t {
-    if (s < n_groups) return p.groups[s].shared > 0 ? segment_blocks((int64_t)p.groups[s].tokens * G) : 0;
+    if (s < n_groups) return p.groups[s].shared > 0 ? segment_blocks((int64_t)p.groups[s].tokens * G, p.a.d) : 0;
     const int n = seqs[s - n_groups].n;
-    return n > 0 ? segment_blocks((int64_t)n * G) : 0;
+    return n > 0 ? segment_blocks((int64_t)n * G, p.a.d) : 0;
   }, seg_start);
   const int n_blocks = seg_start[n_groups + B], n_prefix = seg_start[n_groups];
   if (n_blocks > p.cap_blocks) return;  // (offsets that do not ascend may ask for more than there is room for: no plan then)
@@ -168,20 +168,19 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     Block k;
     k.seg = hint >= 0 && flat >= seg_start[hint] && flat < seg_start[hint + 1] ? hint : upper_segment(seg_start, n_groups + B, flat);
     k.i = flat - seg_start[k.seg];
+    k.rows = (int64_t)(k.seg < n_groups ? p.groups[k.seg].tokens : seqs[k.seg - n_groups].n) * G;
+    k.m = block_rows(k.rows, p.a.d);
     if (k.seg < n_groups) {
-      k.rows = (int64_t)p.groups[k.seg].tokens * G;
       k.first = 0;
       k.keys = p.groups[k.seg].shared;
     } else {
       const PlanSeq s = seqs[k.seg - n_groups];
-      k.rows = (int64_t)s.n * G;
       k.first = s.shared;
-      k.keys = s.len < 0 ? 0 : own_block_keys(k.rows, k.i, G, s.n, s.len, s.shared);
+      k.keys = s.len < 0 ? 0 : own_block_keys(k.rows, k.i, k.m, G, s.n, s.len, s.shared);
     }
-    k.m = block_rows(k.rows);
     k.nr = (int)min((int64_t)k.m, k.rows - (int64_t)k.i * k.m);
     k.steps = block_steps(k.first, k.keys);
-    k.cost = step_cost(k.m == kFewRows, p.a.d, fp8);
+    k.cost = step_cost(k.nr, p.a.d, fp8);
     return k;
   };
   // every thread walks over a run of blocks, several times
@@ -199,7 +198,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   const bool stretched = by_stretches(n_blocks, p.a.d, p.a.H_kv);
   int64_t sum[2] = {0, 0}, total[2];  // cost, keys
   walk([&](int, const Block& k) {
-    sum[0] += (int64_t)k.steps * k.cost + kBlockCost;
+    sum[0] += (int64_t)k.steps * k.cost + piece_cost(p.a.d);
     sum[1] += k.keys;
   });
   block_exclusive(sum, total);
@@ -209,7 +208,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     int64_t at = sum[0];
     walk([&](int x, const Block& k) {
       start[x] = at;
-      at += (int64_t)k.steps * k.cost + kBlockCost;
+      at += (int64_t)k.steps * k.cost + piece_cost(p.a.d);
     });
     __syncthreads();
     for (int s = tid; s <= n_cuts; s += 1024) {
@@ -218,7 +217,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
         const int64_t x = stretch_start(total[0], n_cuts, s);
         b = last_at_most(start, n_blocks, x);
         const Block k = block_at(b, -1);
-        j = step_at(x, start[b], k.steps, k.cost);
+        j = step_at(x, start[b], k.steps, k.cost, p.a.d);
         if (j >= k.steps && j > 0) { ++b; j = 0; }
       }
       cuts[s] = ((int64_t)b << 32) | j;
@@ -347,7 +346,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       o.own_step = e.own_step * kSlotRows;
       if (e.group >= 0) {  // (the blocks of a prefix may be cut differently)
         const PlanGroup g = p.groups[e.group];
-        const int m = block_rows((int64_t)g.tokens * G), in = o.row - g.t0 * G, x = seg_start[e.group] + in / m;
+        const int m = block_rows((int64_t)g.tokens * G, p.a.d), in = o.row - g.t0 * G, x = seg_start[e.group] + in / m;
         if (in >= 0 && in < g.tokens * G) {
           o.pre_pieces = stretched ? pieces_at(x, Block()) : g.pieces;
           o.pre_at = (stretched ? slot_of[x] : g.slot + in / m * g.pieces * (m / kSlotRows)) * kSlotRows + in % m;

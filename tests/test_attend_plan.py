@@ -39,13 +39,13 @@ extern "C" int cut_up(int n_seg, const int64_t* rows, const int* n, const int* l
   auto add = [&](int s, int i) {
     int* b = blocks + 8 * nb++;
     b[0] = s; b[1] = i; b[2] = n[s] ? shared[s] : 0;
-    b[3] = n[s] ? own_block_keys(rows[s], i, G, n[s], len[s], shared[s]) : shared[s];
-    b[4] = 0; b[5] = block_rows(rows[s]); b[6] = step_cost(b[5] == kFewRows, d, fp8); b[7] = block_steps(b[2], b[3]);
+    b[3] = n[s] ? own_block_keys(rows[s], i, block_rows(rows[s], d), G, n[s], len[s], shared[s]) : shared[s];
+    b[4] = 0; b[5] = block_rows(rows[s], d); b[6] = step_cost((int)std::min<int64_t>(b[5], rows[s] - (int64_t)i * b[5]), d, fp8); b[7] = block_steps(b[2], b[3]);
     start.push_back(cost_all);
-    keys_all += b[3]; cost_all += (int64_t)b[7] * b[6] + kBlockCost;
+    keys_all += b[3]; cost_all += (int64_t)b[7] * b[6] + piece_cost(d);
   };
-  for (int s = 0; s < n_seg; ++s) if (!n[s]) for (int i = 0; rows[s] > 0 && i < segment_blocks(rows[s]); ++i) add(s, i);
-  for (int s = n_seg - 1; s >= 0; --s) if (n[s]) for (int i = segment_blocks(rows[s]) - 1; i >= 0; --i) add(s, i);
+  for (int s = 0; s < n_seg; ++s) if (!n[s]) for (int i = 0; rows[s] > 0 && i < segment_blocks(rows[s], d); ++i) add(s, i);
+  for (int s = n_seg - 1; s >= 0; --s) if (n[s]) for (int i = segment_blocks(rows[s], d) - 1; i >= 0; --i) add(s, i);
   *n_pieces = 0;
   auto piece = [&](int b, int k0, int k1, int s) { int* x = pieces + 4 * (*n_pieces)++; x[0] = b; x[1] = k0; x[2] = k1; x[3] = s; ++blocks[8 * b + 4]; };
   if (!by_stretches(nb, d, H_kv)) {
@@ -65,7 +65,7 @@ extern "C" int cut_up(int n_seg, const int64_t* rows, const int* n, const int* l
     if (s == 0 || s == ns) { cuts.push_back({s == 0 ? 0 : nb, 0}); continue; }
     const int64_t x = stretch_start(cost_all, ns, s);
     int b = (int)(std::upper_bound(start.begin(), start.end(), x) - start.begin()) - 1;
-    int j = step_at(x, start[b], blocks[8 * b + 7], blocks[8 * b + 6]);
+    int j = step_at(x, start[b], blocks[8 * b + 7], blocks[8 * b + 6], d);
     if (j > 0 && j >= blocks[8 * b + 7]) { ++b; j = 0; }
     cuts.push_back({b, j});
   }
@@ -140,6 +140,7 @@ def _cut(shim, segs, G, H_kv, d=128, fp8=0):
 def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
     H, H_kv = heads
     G, (d, fp8) = H // H_kv, kind
+    many, extra = (128, 4) if d == 64 else (256, 8)
     for new, length, groups in _batches():
         B = len(new)
         shared = [0] * B
@@ -170,14 +171,14 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
                 assert keys == max(0, want)
                 first = ln[s] - n[s] + (k * m) // G + 1
                 assert sh[s] == 0 or first > sh[s]    # every row sees the whole prefix and a key behind it
-        assert sorted(set(zip(blocks[:, 0], blocks[:, 1]))) == sorted((s, i) for s in range(len(segs)) for i in range(-(-rows[s] // (16 if rows[s] <= 16 else 128))))
+        assert sorted(set(zip(blocks[:, 0], blocks[:, 1]))) == sorted((s, i) for s in range(len(segs)) for i in range(-(-rows[s] // (16 if rows[s] <= 16 else many))))
         # every stretch is a run of pieces; none has much more than its share
         assert (np.diff(pieces[:, 3]) >= 0).all() and (len(pieces) == 0 or pieces[-1, 3] < n_stretches)
         if shim.by_stretches_of(len(blocks), d, H_kv) and len(pieces):
-            cost = [4 + -(-(int(x[2]) - (int(x[1]) & ~63)) // 64) * int(blocks[x[0], 6]) for x in pieces]
+            cost = [extra + -(-(int(x[2]) - (int(x[1]) & ~63)) // 64) * int(blocks[x[0], 6]) for x in pieces]
             per = np.bincount(pieces[:, 3], weights=cost, minlength=n_stretches)
-            share = (blocks[:, 7] * blocks[:, 6] + 4).sum() / n_stretches
-            assert per.max() <= share + 4 + 4 * 5 + 4 + 1     # a snapped end on either side, a cut block's cost again
+            share = (blocks[:, 7] * blocks[:, 6] + extra).sum() / n_stretches
+            assert per.max() <= share + 2 * extra + 4 * 8 + 1     # a snapped end on either side, a cut block's cost again
         # room
         leaves = [bool(b[4] > 1 or b[0] < n_prefix or sh[b[0]] > 0) for b in blocks]
         assert len(blocks) <= caps["blocks"] and len(pieces) <= caps["units"] and n_stretches <= max(caps["units"], 1)
@@ -195,16 +196,16 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
 
 
 def test_equal_work_is_spread_over_the_device(shim):
-    """One long sequence: 64 stretches for each of 8 KV heads; a short one: pieces of 128 keys; many blocks: no cuts."""
+    """One long sequence: 32 stretches for each of 8 KV heads; a short one: pieces of 256 keys; many blocks: no cuts."""
     blocks, pieces, n = _cut(shim, [(4, 1, 131072, 0)], 4, 8)
     size = pieces[:, 2] - pieces[:, 1]
-    assert n == len(pieces) == 64 and size.max() <= 1.1 * size.mean() + 64
-    assert (lambda p: (p[:, 2] - p[:, 1]).max())(_cut(shim, [(4, 1, 1000, 0)], 4, 8)[1]) == 128
+    assert n == len(pieces) == 32 and size.max() <= 1.1 * size.mean() + 64
+    assert (lambda p: (p[:, 2] - p[:, 1]).max())(_cut(shim, [(4, 1, 1000, 0)], 4, 8)[1]) == 256
     blocks, pieces, n = _cut(shim, [(4 * 20000, 20000, 20000, 0)], 4, 8)
-    assert n == len(pieces) == len(blocks) == 4 * 20000 // 128
+    assert n == len(pieces) == len(blocks) == -(-4 * 20000 // 256)
     assert (np.diff(pieces[:, 2]) <= 0).all()          # the longest first
     blocks, pieces, n = _cut(shim, [(4, 1, 1000 + 37 * i, 0) for i in range(64)], 4, 8)
-    assert n == 64 and len(pieces) <= 64 + 63
+    assert n == 32 and len(pieces) <= 64 + 31
 
 
 def test_a_plan_knows_the_shape_it_was_made_for(shim):

@@ -149,6 +149,16 @@ __device__ __forceinline__ void store_stats(const AttendDev& p, int64_t place, f
   *reinterpret_cast<uint2*>(p.stats + place) = make_uint2(__float_as_uint(top), bad ? kNanF32 : __float_as_uint(sum));
 }
 
+__device__ __forceinline__ void store_values(uint16_t* dst, f32x4 x, bool bad) {  // four of a row
+  const uint32_t nan2 = kNanBf16 * 0x10001u;
+  const uint2 v = make_uint2(pack_bf16_pair(x[0], x[1]), pack_bf16_pair(x[2], x[3]));
+  *reinterpret_cast<uint2*>(dst) = bad ? make_uint2(nan2, nan2) : v;
+}
+__device__ __forceinline__ void store_lse(const AttendDev& p, int token, int h, float top, float sum, bool bad) {
+  const float lse = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
+  reinterpret_cast<uint32_t*>(p.lse)[(int64_t)token * p.H + h] = bad ? kNanF32 : __float_as_uint(lse);
+}
+
 // ---------------------------------------------------------------- few rows
 // One wave's 32-key tile of keys or values on its way from memory to LDS.  A load instruction covers whole rows (256 bytes of
 // each of 4 keys, bf16 and d = 128), so that every request is for a whole line.
@@ -180,9 +190,9 @@ struct FewTile {
   }
 };
 
-template <int D, bool FP8, bool PAGED>
+// W waves take the piece: all of the workgroup's, or one (every wave with a piece of its own; nothing is shared, no barrier)
+template <int D, bool FP8, bool PAGED, int W>
 __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit& u, int g, char* lds) {
-  constexpr int NW = attend_waves(D);
   constexpr int KS = D / 32;          // steps of the product with the queries
   constexpr int DB = D / 16;          // blocks of values
   constexpr int C = D / 8;            // 16-byte chunks of a bf16 row
@@ -191,7 +201,7 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   const bool mine = row < u.nr;
   const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
 
-  int tile = u.k0 < u.k1 ? (u.k0 & ~31) + 32 * w : u.k1;
+  int tile = u.k0 < u.k1 ? (u.k0 & ~31) + (W > 1 ? 32 * w : 0) : u.k1;
   KeyRows<PAGED> rows(p, u, l, tile);
   const char* const kb = p.k + (int64_t)g * p.c_hs;
   const char* const vb = p.v + (int64_t)g * p.c_hs;
@@ -251,11 +261,11 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   for (int i = 0; i < DB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, sum = 0.f;
 
-  for (; tile < u.k1; tile += 32 * NW) {
-    const bool more = tile + 32 * NW < u.k1;
+  for (; tile < u.k1; tile += 32 * W) {
+    const bool more = tile + 32 * W < u.k1;
     kt.store(kd, l);
     if (more) {
-      place(tile + 32 * NW);
+      place(tile + 32 * W);
       kt.load(kb, oct_at, in);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -310,8 +320,26 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   // the waves' sums joined, in the waves' order
   sum += __shfl_xor(sum, 16, kWave);
   sum += __shfl_xor(sum, 32, kWave);
-  float* const tops = reinterpret_cast<float*>(lds + NW * 16 * (D + 4) * 4);  // [NW][16], twice
-  float* const sums = tops + NW * 16;
+  if constexpr (W == 1) {
+    const bool any_bad = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
+    if (!mine) return;
+    if (u.slot >= 0) {
+      const int64_t place = slot_row(p, u.slot, row, g);
+      float* dst = p.sums + place * D + 4 * quad;
+#pragma unroll
+      for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(dst + 16 * i) = o[i];
+      if (quad == 0) store_stats(p, place, m, sum, any_bad);
+      return;
+    }
+    const float mul = (sum == 0.f ? 0.f : 1.f / sum) * (p.v_scale ? p.v_scale[g] : 1.f);
+    uint16_t* dst = p.out + at.token * p.o_ts + at.h * p.o_hs + 4 * quad;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) store_values(dst + 16 * i, o[i] * mul, any_bad);
+    if (quad == 0 && p.lse) store_lse(p, at.token, at.h, m, sum, any_bad);
+    return;
+  } else {
+  float* const tops = reinterpret_cast<float*>(lds + W * 16 * (D + 4) * 4);  // [W][16], twice
+  float* const sums = tops + W * 16;
   const int any_bad = __syncthreads_or(bad != 0);  // (also: every wave is done with its tile in LDS)
   if (quad == 0) {
     tops[w * 16 + row] = m;
@@ -321,7 +349,7 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   auto top_of = [&](int r) {
     float top = tops[r];
 #pragma unroll
-    for (int x = 1; x < NW; ++x) top = fmaxf(top, tops[x * 16 + r]);
+    for (int x = 1; x < W; ++x) top = fmaxf(top, tops[x * 16 + r]);
     return top;
   };
   {
@@ -340,7 +368,7 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.f;
 #pragma unroll
-  for (int x = 0; x < NW; ++x) {
+  for (int x = 0; x < W; ++x) {
     l_all += sums[x * 16 + r] * fast_exp2(tops[x * 16 + r] - base);
     const float* part = reinterpret_cast<const float*>(lds) + (x * 16 + r) * (D + 4) + lane * V;
 #pragma unroll
@@ -363,9 +391,7 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   uint16_t* dst = p.out + to.token * p.o_ts + to.h * p.o_hs + lane * V;
   if constexpr (V == 8) *reinterpret_cast<u32x4*>(dst) = u32x4{out[0], out[1], out[2], out[3]};
   else *reinterpret_cast<uint2*>(dst) = make_uint2(out[0], out[1]);
-  if (lane == 0 && p.lse) {
-    const float lse = l_all == 0.f ? -INFINITY : (base + __builtin_amdgcn_logf(l_all)) * 0.69314718055994531f;
-    reinterpret_cast<uint32_t*>(p.lse)[(int64_t)to.token * p.H + to.h] = any_bad ? kNanF32 : __float_as_uint(lse);
+  if (lane == 0 && p.lse) store_lse(p, to.token, to.h, top, l_all, any_bad);
   }
 }
 
@@ -632,19 +658,14 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
     return;
   }
   const float mul = (sum == 0.f ? 0.f : 1.f / sum) * (p.v_scale ? p.v_scale[g] : 1.f);
-  const uint32_t nan2 = kNanBf16 * 0x10001u;
   uint16_t* dst = p.out + at.token * p.o_ts + at.h * p.o_hs + 4 * half;
 #pragma unroll
   for (int i = 0; i < DB; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint2 x = make_uint2(pack_bf16_pair(o[i][4 * j] * mul, o[i][4 * j + 1] * mul), pack_bf16_pair(o[i][4 * j + 2] * mul, o[i][4 * j + 3] * mul));
-      *reinterpret_cast<uint2*>(dst + 32 * i + 8 * j) = any_bad ? make_uint2(nan2, nan2) : x;
+      store_values(dst + 32 * i + 8 * j, f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]} * mul, any_bad);
     }
-  if (half == 0 && p.lse) {
-    const float lse = sum == 0.f ? -INFINITY : ((m == -INFINITY ? 0.f : m) + __builtin_amdgcn_logf(sum)) * 0.69314718055994531f;
-    reinterpret_cast<uint32_t*>(p.lse)[(int64_t)at.token * p.H + at.h] = any_bad ? kNanF32 : __float_as_uint(lse);
-  }
+  if (half == 0 && p.lse) store_lse(p, at.token, at.h, m, sum, any_bad);
 }
 
 // every row of the call, or of one piece and KV head, becomes NaN
@@ -668,27 +689,42 @@ __global__ __launch_bounds__(64 * attend_waves(D), D == 64 ? 3 : 2) void attend_
   // The KV heads of a piece are neighbours: with eight of them, each has the L2 of one XCD, which the rows of a
   // block share, as workgroups go to the XCDs in turn.
   const int n = (int)(blockIdx.x / (uint32_t)p.H_kv), g = (int)(blockIdx.x % (uint32_t)p.H_kv);
-  // the plan through the scalar cache; header and stretch together (the list has room for every workgroup's index)
+  // the plan through the scalar cache; header, stretch and its first piece together (the list has room for every workgroup's index)
   const auto header = reinterpret_cast<const __attribute__((address_space(4))) AttendHeader*>(reinterpret_cast<uintptr_t>(p.header));
-  const ScalarTable stretch = scalar_table(p.stretches);
+  typedef const __attribute__((address_space(4))) AttendStretch* StretchPtr;
+  typedef const __attribute__((address_space(4))) AttendUnit* UnitPtr;
+  const auto stretch = reinterpret_cast<StretchPtr>(reinterpret_cast<uintptr_t>(p.stretches + n));
+  auto read = [&](UnitPtr x) {
+    AttendUnit u;
+    u.r0 = x->r0; u.nr = x->nr; u.seq = x->seq; u.k0 = x->k0;
+    u.k1 = x->k1; u.off = x->off; u.slot = x->slot; u.run = x->run;
+    return u;
+  };
   const uint64_t print = header->print;
   const int n_stretches = header->n_stretches;
-  int x = stretch[n];
-  const int end = stretch[n + 1];
+  int x = stretch->first;
+  const int end = stretch->end;
+  AttendUnit u = read(&stretch->unit);
   if (print != p.print) {
     nan_rows(p, D, 0, (int64_t)p.T_new * p.H, p.H, 0, (int64_t)blockIdx.x * T + threadIdx.x, (int64_t)gridDim.x * T);
     return;
   }
-  if (n >= n_stretches) return;
-  for (; x < end; ++x) {
-    const auto unit = reinterpret_cast<const __attribute__((address_space(4))) AttendUnit*>(reinterpret_cast<uintptr_t>(p.units + x));
-    AttendUnit u;
-    u.r0 = unit->r0; u.nr = unit->nr; u.seq = unit->seq; u.k0 = unit->k0;
-    u.k1 = unit->k1; u.off = unit->off; u.slot = unit->slot; u.bad = unit->bad;
-    if (u.bad) nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, T);
-    else if (u.nr <= kFewRows) attend_few<D, FP8, PAGED>(p, u, g, lds);
-    else if (attend_waves(D) == 8 && u.nr <= many_rows(D) / 2) attend_many<D, FP8, PAGED, attend_waves(D) == 8>(p, u, g, lds);
-    else attend_many<D, FP8, PAGED, false>(p, u, g, lds);
+  if (n >= n_stretches || x >= end) return;
+  const auto unit_at = [&](int i) { return reinterpret_cast<UnitPtr>(reinterpret_cast<uintptr_t>(p.units + i)); };
+  for (;;) {
+    if (u.run > 0) {
+      const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      if (w < u.run) attend_few<D, FP8, PAGED, 1>(p, w == 0 ? u : read(unit_at(x + w)), g, lds);
+      x += u.run;
+    } else {
+      if (u.run == kBadUnit) nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, T);
+      else if (u.nr <= kFewRows) attend_few<D, FP8, PAGED, attend_waves(D)>(p, u, g, lds);
+      else if (attend_waves(D) == 8 && u.nr <= many_rows(D) / 2) attend_many<D, FP8, PAGED, attend_waves(D) == 8>(p, u, g, lds);
+      else attend_many<D, FP8, PAGED, false>(p, u, g, lds);
+      ++x;
+    }
+    if (x >= end) return;
+    u = read(unit_at(x));
     __syncthreads();  // (the next piece uses the same LDS)
   }
 }
@@ -753,7 +789,7 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.print = attend_print(a);
   p.header = reinterpret_cast<const AttendHeader*>(base);
   p.units = reinterpret_cast<const AttendUnit*>(base + l.units);
-  p.stretches = reinterpret_cast<const int32_t*>(base + l.stretches);
+  p.stretches = reinterpret_cast<const AttendStretch*>(base + l.stretches);
   p.rows = reinterpret_cast<const AttendRow*>(base + l.rows);
   p.table = a->d_block_table; p.cu_cache = a->d_cu_cache;
   p.q = static_cast<const uint16_t*>(a->d_q);

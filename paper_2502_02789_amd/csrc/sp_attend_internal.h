@@ -19,7 +19,7 @@ struct AttendDev {
   uint64_t print;
   const AttendHeader* header;
   const AttendUnit* units;
-  const int32_t* stretches;      // first piece of every workgroup's
+  const AttendStretch* stretches;
   const AttendRow* rows;
   const int32_t* table;
   const int32_t* cu_cache;

@@ -6,7 +6,7 @@
 // prefix of a group (all rows of its members), or what a sequence has for itself.  A segment is cut into blocks of 16 rows
 // (if it has no more: one small matrix tile, bound by reading the keys) or of many_rows() (bound by the matrix cores).
 //
-// The device has room for attend_items() workgroups at once.  Fewer than three times as many (block, KV head) pairs are laid end to end,
+// The device has room for attend_items() workgroups at once.  With fewer than three times as many (large block, KV head) pairs, blocks are laid end to end,
 // each at its cost, and cut into as many stretches of equal cost as there is room for: every workgroup has one, and all end together.
 // (One block to a workgroup instead, in whole rounds, pieces cut to 1/1024 of the keys -> stretches: MEASURED_STRETCHES.)
 // With more blocks than that a workgroup takes one block, and takes the next as it gets done, longest first; only a block longer than a
@@ -49,7 +49,12 @@ struct AttendUnit {   // one piece of one block
   int32_t k0, k1;     // keys [k0, k1)
   int32_t off;        // token t sees keys below t + off (kNoLimit: all of the piece)
   int32_t slot;       // where the sums go, or -1: the block is finished here
-  int32_t bad;        // 1: the sequence's length is invalid, its rows become NaN
+  int32_t run;        // kBadUnit: the sequence's length is invalid, its rows become NaN; else how many units from this one on a wave each takes (0: all waves take this one)
+};
+struct AttendStretch {  // what one workgroup does, for each KV head: units [first, end), the first of them a copy
+  int32_t first, end;
+  int32_t pad[2];
+  AttendUnit unit;
 };
 struct AttendJoin {   // one block of a sequence's own rows that slots are joined for
   int32_t r0, nr;
@@ -72,6 +77,7 @@ struct AttendHeader {
 };
 
 constexpr int kNoLimit = 0x7fffffff;
+constexpr int kBadUnit = -1;
 
 struct AttendCaps {
   int64_t blocks, units, joins, rows, slots;
@@ -127,17 +133,23 @@ SP_ATTEND_FN int own_block_keys(int64_t rows, int i, int m, int G, int n, int le
 // Steps of 64 keys of a block's keys [first, first + keys), cut at multiples of 64 keys of the sequence
 SP_ATTEND_FN int block_steps(int first, int keys) { return (int)(((int64_t)(first & (kPieceStep - 1)) + keys + kPieceStep - 1) / kPieceStep); }
 
+// A piece of few rows and few keys is not worth all waves: where several follow one another, each is a wave's
+SP_ATTEND_FN bool wave_sized(int rows, int keys) { return rows <= kFewRows && keys <= 512; }
+
 // What a step costs a workgroup, in units of 0.27 us (d = 128) and 0.67 us on a full device: 16 rows are bound by reading 64 keys and
 // values, more by the matrix cores (eight waves with up to 128 rows work on two steps at a time); and what a piece costs besides.
 SP_ATTEND_FN int step_cost(int rows, int d, bool fp8) {
   if (rows <= kFewRows) return d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5);
   return d == 64 ? 4 : rows <= many_rows(d) / 2 ? 6 : 8;
 }
-SP_ATTEND_FN int piece_cost(int d) { return d == 64 ? 4 : 8; }
+SP_ATTEND_FN int piece_cost(int rows, int keys, int d) { return d == 64 ? (wave_sized(rows, keys) ? 2 : 4) : wave_sized(rows, keys) ? 3 : 12; }
 // No stretch costs less: more than one step and a half of any kind
 SP_ATTEND_FN int least_stretch(int d) { return d == 64 ? 10 : 20; }
 
-SP_ATTEND_FN bool by_stretches(int64_t blocks, int d, int H_kv) { return blocks * H_kv < 3 * (int64_t)attend_items(d) && blocks <= kMostStretchBlocks; }
+// many: blocks of more than 16 rows (the others are cheap to cut)
+SP_ATTEND_FN bool by_stretches(int64_t blocks, int64_t many, int d, int H_kv) {
+  return many * H_kv < 3 * (int64_t)attend_items(d) && blocks <= kMostStretchBlocks;
+}
 // Stretches for each KV head, blocks of `cost` in all: what the device has room for, as long as that leaves each enough to do
 SP_ATTEND_FN int stretch_count(int64_t cost, int d, int H_kv) {
   const int64_t room = attend_items(d) / H_kv > 0 ? attend_items(d) / H_kv : 1, most = cost / least_stretch(d);
@@ -147,8 +159,8 @@ SP_ATTEND_FN int stretch_count(int64_t cost, int d, int H_kv) {
 SP_ATTEND_FN int64_t stretch_start(int64_t cost, int n, int s) { return cost * s / n; }
 // ... as a step of the block whose share begins at `start` (what the block costs besides spread over its steps): `steps` (the next
 // block's first) or 0 where a piece would get too short
-SP_ATTEND_FN int step_at(int64_t x, int64_t start, int steps, int per_step, int d) {
-  const int64_t cost = (int64_t)steps * per_step + piece_cost(d), j = (2 * (x - start) * steps + cost) / (2 * cost);
+SP_ATTEND_FN int step_at(int64_t x, int64_t start, int steps, int per_step, int extra) {
+  const int64_t cost = (int64_t)steps * per_step + extra, j = (2 * (x - start) * steps + cost) / (2 * cost);
   return j < kMinSteps ? 0 : steps - j < kMinSteps ? steps : (int)j;
 }
 SP_ATTEND_FN int step_key(int first, int keys, int steps, int j) {
@@ -191,7 +203,7 @@ inline AttendPlanLayout attend_plan_layout(const sp_attend_args* a) {
   AttendPlanLayout l;
   size_t at = 256;
   l.units = at; at += attend_round(sizeof(AttendUnit) * (size_t)c.units);
-  l.stretches = at; at += attend_round(4 * ((size_t)c.units + 1));
+  l.stretches = at; at += attend_round(sizeof(AttendStretch) * (size_t)c.units);
   l.joins = at; at += attend_round(sizeof(AttendJoin) * (size_t)c.joins);
   l.rows = at; at += attend_round(sizeof(AttendRow) * (size_t)c.rows);
   l.seg_start = at; at += attend_round(4 * ((size_t)a->B + (size_t)a->n_groups + 1));

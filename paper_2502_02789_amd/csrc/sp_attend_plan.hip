@@ -17,7 +17,7 @@ struct PlanDev {
   uint64_t print;
   AttendHeader* header;
   AttendUnit* units;
-  int32_t* stretches;
+  AttendStretch* stretches;
   AttendJoin* joins;
   AttendRow* rows;
   int32_t* seg_start;
@@ -67,6 +67,7 @@ struct Block {       // a block of rows
   int m, nr;         // rows of a whole block, of this one
   int first, keys;   // its keys are [first, first + keys)
   int steps, cost;   // ... and a step's cost
+  int extra;         // what the block costs besides
 };
 
 // largest i in [0, n) with table[i] <= x (table[0] <= x)
@@ -93,6 +94,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   __shared__ int64_t cuts[kMostStretches + 1];        // (block, step) that each stretch begins at
   __shared__ int32_t first_unit[kMostStretches + 1];
   __shared__ int32_t slot_of[kMostStretchBlocks];
+  __shared__ uint8_t runs[kMostStretchBlocks + kMostStretches];
   PlanSeq* const seqs = p.a.B <= kLdsSeqs ? lds_seqs : p.seqs;
   int32_t* const seg_start = p.a.B <= kLdsSeqs ? lds_seg : p.seg_start;  // (no more groups than sequences)
   const int tid = threadIdx.x, B = p.a.B, n_groups = p.a.n_groups, G = p.G, T = (int)p.a.T_new;
@@ -181,6 +183,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     k.nr = (int)min((int64_t)k.m, k.rows - (int64_t)k.i * k.m);
     k.steps = block_steps(k.first, k.keys);
     k.cost = step_cost(k.nr, p.a.d, fp8);
+    k.extra = piece_cost(k.nr, k.keys, p.a.d);
     return k;
   };
   // every thread walks over a run of blocks, several times
@@ -195,20 +198,21 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   };
 
   // where the blocks are cut
-  const bool stretched = by_stretches(n_blocks, p.a.d, p.a.H_kv);
-  int64_t sum[2] = {0, 0}, total[2];  // cost, keys
+  int64_t sum[3] = {0, 0, 0}, total[3];  // cost, keys, large blocks
   walk([&](int, const Block& k) {
-    sum[0] += (int64_t)k.steps * k.cost + piece_cost(p.a.d);
+    sum[0] += (int64_t)k.steps * k.cost + k.extra;
     sum[1] += k.keys;
+    sum[2] += k.nr > kFewRows;
   });
   block_exclusive(sum, total);
+  const bool stretched = by_stretches(n_blocks, total[2], p.a.d, p.a.H_kv);
   const int cut = make_cut(total[1], p.a.d, p.a.H_kv);
   const int n_cuts = stretched ? stretch_count(total[0], p.a.d, p.a.H_kv) : 0;
   if (stretched) {
     int64_t at = sum[0];
     walk([&](int x, const Block& k) {
       start[x] = at;
-      at += (int64_t)k.steps * k.cost + piece_cost(p.a.d);
+      at += (int64_t)k.steps * k.cost + k.extra;
     });
     __syncthreads();
     for (int s = tid; s <= n_cuts; s += 1024) {
@@ -217,7 +221,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
         const int64_t x = stretch_start(total[0], n_cuts, s);
         b = last_at_most(start, n_blocks, x);
         const Block k = block_at(b, -1);
-        j = step_at(x, start[b], k.steps, k.cost, p.a.d);
+        j = step_at(x, start[b], k.steps, k.cost, k.extra);
         if (j >= k.steps && j > 0) { ++b; j = 0; }
       }
       cuts[s] = ((int64_t)b << 32) | j;
@@ -252,8 +256,8 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       count[0] = (b >> 32) + ((b & 0xffffffff) != 0) - (a >> 32);
     }
     block_exclusive(count, units);
-    if (tid < n_cuts) p.stretches[tid] = first_unit[tid] = (int)count[0];
-    if (tid == 0) p.stretches[n_cuts] = first_unit[n_cuts] = (int)units[0];
+    if (tid < n_cuts) first_unit[tid] = (int)count[0];
+    if (tid == 0) first_unit[n_cuts] = (int)units[0];
   }
 
   auto unit_of = [&](const Block& k, int j0, int j1, int64_t slot) {
@@ -263,13 +267,13 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       t0 = p.groups[k.seg].t0;
       unit.seq = clamp_int(p.a.d_cu_group[k.seg], 0, B - 1);
       unit.off = kNoLimit;
-      unit.bad = 0;
+      unit.run = 0;
     } else {
       const PlanSeq s = seqs[k.seg - n_groups];
       t0 = s.t0;
       unit.seq = k.seg - n_groups;
       unit.off = s.len - s.n + 1 - s.t0;
-      unit.bad = s.len < 0;
+      unit.run = s.len < 0 ? kBadUnit : 0;
     }
     unit.r0 = t0 * G + k.i * k.m;
     unit.nr = k.nr;
@@ -291,9 +295,12 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
         slot_of[x] = sums ? (int)slot : -1;
       } else {
         for (int q = 0; q < pieces; ++q) {
-          p.units[u + q] = unit_of(k, (int)((int64_t)k.steps * q / pieces), q + 1 == pieces ? k.steps : (int)((int64_t)k.steps * (q + 1) / pieces),
-                                   sums ? slot + (int64_t)q * step : -1);
-          p.stretches[u + q] = (int)(u + q);
+          AttendStretch s;
+          s.unit = p.units[u + q] = unit_of(k, (int)((int64_t)k.steps * q / pieces), q + 1 == pieces ? k.steps : (int)((int64_t)k.steps * (q + 1) / pieces),
+                                            sums ? slot + (int64_t)q * step : -1);
+          s.first = (int)(u + q);
+          s.end = s.first + 1;
+          p.stretches[u + q] = s;
         }
         u += pieces;
       }
@@ -311,8 +318,31 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       const int q = j0 > 0 ? s - first_cut(x) + 1 : 0;
       p.units[u] = unit_of(k, j0, j1, slot_of[x] < 0 ? -1 : slot_of[x] + (int64_t)q * (k.m / kSlotRows));
     }
-  } else if (tid == 0) {
-    p.stretches[n[kUnits]] = (int)n[kUnits];
+    __syncthreads();
+    // pieces that a wave each takes: as many as follow one another in a stretch, up to the waves of a workgroup
+    const int waves = attend_waves(p.a.d);
+    auto alone = [&](int u) {
+      const AttendUnit x = p.units[u];
+      return x.run != kBadUnit && wave_sized(x.nr, x.k1 - x.k0);
+    };
+    for (int u = tid; u < (int)n[kUnits]; u += 1024) {
+      const int end = first_unit[last_at_most(first_unit, n_cuts, u) + 1];
+      int run = 0;
+      while (run < waves && u + run < end && alone(u + run)) ++run;
+      if (run > 1) runs[u] = run;   // (the units themselves are still being read)
+      else runs[u] = 0;
+    }
+    __syncthreads();
+    for (int u = tid; u < (int)n[kUnits]; u += 1024)
+      if (runs[u] > 0) p.units[u].run = runs[u];
+    __syncthreads();
+    for (int s = tid; s < n_cuts; s += 1024) {
+      AttendStretch x = {};
+      x.first = first_unit[s];
+      x.end = first_unit[s + 1];
+      if (x.first < x.end) x.unit = p.units[x.first];
+      p.stretches[s] = x;
+    }
   }
   int64_t slot = at[kSlots], j = at[kJoins], row = at[kRows];
   walk([&](int x, const Block& k) {
@@ -377,11 +407,12 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendDev p) {
   constexpr int L = D / 4, GROUPS = 256 / L;
   __shared__ float4 part[GROUPS][L];
   __shared__ float2 stat[GROUPS];
-  if (p.header->print != p.print) return;  // (the pieces' kernel has filled the outputs)
+  const uint64_t print = p.header->print;
   const int n_rows = p.header->n_rows;
   const bool together = p.header->most_pieces > 16;
   const int group = threadIdx.x / L, c = threadIdx.x % L, step = together ? GROUPS : 1, first = together ? group : 0;
-  const int64_t n_items = (int64_t)n_rows * p.H_kv, stride = (int64_t)gridDim.x * (together ? 1 : GROUPS);
+  // (without a plan the pieces' kernel has filled the outputs)
+  const int64_t n_items = print == p.print ? (int64_t)n_rows * p.H_kv : 0, stride = (int64_t)gridDim.x * (together ? 1 : GROUPS);
   for (int64_t item0 = (int64_t)blockIdx.x * (together ? 1 : GROUPS); item0 < n_items; item0 += stride) {
     const int64_t item = together ? item0 : item0 + group;
     const bool active = item < n_items;
@@ -397,8 +428,16 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendDev p) {
     float top = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int q0 = 0; q0 < mine; q0 += L) {  // a lane holds the factor of one piece
+      const int count = min(L, mine - q0);
+      float4 x[8];
+      auto read = [&](int q) {  // (beyond the last: its values again, with a factor of zero)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          x[i] = *reinterpret_cast<const float4*>(p.sums + place(first + (q0 + min(q + i, count - 1)) * step) * D + c * 4);
+      };
       float2 s = make_float2(-INFINITY, 0.f);
       if (q0 + c < mine) s = p.stats[place(first + (q0 + c) * step)];
+      read(0);
       float next = s.x;
 #pragma unroll
       for (int off = L / 2; off >= 1; off >>= 1) next = fmaxf(next, __shfl_xor(next, off, L));
@@ -410,17 +449,15 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendDev p) {
       top = next;
       sum = sum * old + add;
       acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
-      const int count = min(L, mine - q0);
-      for (int q = 0; q < count; q += 8) {  // (beyond the last: its values again, with a factor of zero)
-        float4 x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          x[i] = *reinterpret_cast<const float4*>(p.sums + place(first + (q0 + min(q + i, count - 1)) * step) * D + c * 4);
+      for (int q = 0;;) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float w = __shfl(f, q + i, L);
           acc.x += w * x[i].x; acc.y += w * x[i].y; acc.z += w * x[i].z; acc.w += w * x[i].w;
         }
+        q += 8;
+        if (q >= count) break;
+        read(q);
       }
     }
     if (together) {  // the groups' sums, in their order
@@ -513,7 +550,7 @@ extern "C" sp_status sp_attend_plan(const sp_attend_args* a, void* hip_stream) {
   p.print = attend_print(a);
   p.header = reinterpret_cast<AttendHeader*>(base);
   p.units = reinterpret_cast<AttendUnit*>(base + l.units);
-  p.stretches = reinterpret_cast<int32_t*>(base + l.stretches);
+  p.stretches = reinterpret_cast<AttendStretch*>(base + l.stretches);
   p.joins = reinterpret_cast<AttendJoin*>(base + l.joins);
   p.rows = reinterpret_cast<AttendRow*>(base + l.rows);
   p.seg_start = reinterpret_cast<int32_t*>(base + l.seg_start);

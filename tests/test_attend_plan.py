@@ -24,34 +24,37 @@ extern "C" void caps(const sp_attend_args* a, int64_t* out) {
   const AttendPlanLayout l = attend_plan_layout(a);
   out[0] = c.blocks; out[1] = c.units; out[2] = c.joins; out[3] = c.slots; out[4] = (int64_t)l.bytes; out[5] = (int64_t)l.units;
   out[6] = (int64_t)l.joins; out[7] = (int64_t)l.seg_start; out[8] = (int64_t)l.seqs; out[9] = (int64_t)l.groups;
-  out[10] = sizeof(AttendUnit); out[11] = sizeof(AttendJoin); out[12] = (int64_t)attend_workspace(a); out[13] = (int64_t)attend_sums_bytes(a); out[14] = c.rows; out[15] = sizeof(AttendRow); out[16] = (int64_t)l.rows; out[17] = (int64_t)l.stretches;
+  out[10] = sizeof(AttendUnit); out[11] = sizeof(AttendJoin); out[12] = (int64_t)attend_workspace(a); out[13] = (int64_t)attend_sums_bytes(a); out[14] = c.rows; out[15] = sizeof(AttendRow); out[16] = (int64_t)l.rows; out[17] = (int64_t)l.stretches; out[18] = sizeof(AttendStretch);
 }
 extern "C" uint64_t print_of(const sp_attend_args* a) { return attend_print(a); }
-extern "C" int by_stretches_of(int64_t blocks, int d, int H_kv) { return by_stretches(blocks, d, H_kv); }
+extern "C" int by_stretches_of(int64_t blocks, int64_t many, int d, int H_kv) { return by_stretches(blocks, many, d, H_kv); }
 extern "C" int share(int64_t rows, int members) { return shares(rows, members); }
 // segments (prefixes first): rows, n (0: a prefix), len, shared.  blocks out, in the order that they are laid out in: segment, i,
 // first key, keys, pieces, rows of a block, cost of a step, steps; pieces out: block, first key, end, stretch.  Returns the number of blocks.
 extern "C" int cut_up(int n_seg, const int64_t* rows, const int* n, const int* len, const int* shared, int G, int H_kv, int d, int fp8, int* blocks,
                       int* pieces, int* n_pieces, int* n_stretches) {
   int nb = 0;
-  int64_t keys_all = 0, cost_all = 0;
+  int64_t keys_all = 0, cost_all = 0, many = 0;
   std::vector<int64_t> start;
   auto add = [&](int s, int i) {
-    int* b = blocks + 8 * nb++;
+    int* b = blocks + 9 * nb++;
     b[0] = s; b[1] = i; b[2] = n[s] ? shared[s] : 0;
     b[3] = n[s] ? own_block_keys(rows[s], i, block_rows(rows[s], d), G, n[s], len[s], shared[s]) : shared[s];
     b[4] = 0; b[5] = block_rows(rows[s], d); b[6] = step_cost((int)std::min<int64_t>(b[5], rows[s] - (int64_t)i * b[5]), d, fp8); b[7] = block_steps(b[2], b[3]);
+    const int nr = (int)std::min<int64_t>(b[5], rows[s] - (int64_t)i * b[5]);
+    b[8] = piece_cost(nr, b[3], d);
+    many += nr > kFewRows;
     start.push_back(cost_all);
-    keys_all += b[3]; cost_all += (int64_t)b[7] * b[6] + piece_cost(d);
+    keys_all += b[3]; cost_all += (int64_t)b[7] * b[6] + b[8];
   };
   for (int s = 0; s < n_seg; ++s) if (!n[s]) for (int i = 0; rows[s] > 0 && i < segment_blocks(rows[s], d); ++i) add(s, i);
   for (int s = n_seg - 1; s >= 0; --s) if (n[s]) for (int i = segment_blocks(rows[s], d) - 1; i >= 0; --i) add(s, i);
   *n_pieces = 0;
-  auto piece = [&](int b, int k0, int k1, int s) { int* x = pieces + 4 * (*n_pieces)++; x[0] = b; x[1] = k0; x[2] = k1; x[3] = s; ++blocks[8 * b + 4]; };
-  if (!by_stretches(nb, d, H_kv)) {
+  auto piece = [&](int b, int k0, int k1, int s) { int* x = pieces + 4 * (*n_pieces)++; x[0] = b; x[1] = k0; x[2] = k1; x[3] = s; ++blocks[9 * b + 4]; };
+  if (!by_stretches(nb, many, d, H_kv)) {
     const int cut = make_cut(keys_all, d, H_kv);
     for (int b = 0; b < nb; ++b) {
-      const int* k = blocks + 8 * b;
+      const int* k = blocks + 9 * b;
       const int p = pieces_of(k[3], cut);
       for (int q = 0; q < p; ++q) piece(b, piece_start(k[2], k[3], p, q), piece_start(k[2], k[3], p, q + 1), *n_pieces);
     }
@@ -65,13 +68,13 @@ extern "C" int cut_up(int n_seg, const int64_t* rows, const int* n, const int* l
     if (s == 0 || s == ns) { cuts.push_back({s == 0 ? 0 : nb, 0}); continue; }
     const int64_t x = stretch_start(cost_all, ns, s);
     int b = (int)(std::upper_bound(start.begin(), start.end(), x) - start.begin()) - 1;
-    int j = step_at(x, start[b], blocks[8 * b + 7], blocks[8 * b + 6], d);
-    if (j > 0 && j >= blocks[8 * b + 7]) { ++b; j = 0; }
+    int j = step_at(x, start[b], blocks[9 * b + 7], blocks[9 * b + 6], blocks[9 * b + 8]);
+    if (j > 0 && j >= blocks[9 * b + 7]) { ++b; j = 0; }
     cuts.push_back({b, j});
   }
   for (int s = 0; s < ns; ++s)
     for (int b = cuts[s].first; b < cuts[s + 1].first + (cuts[s + 1].second > 0); ++b) {
-      const int* k = blocks + 8 * b;
+      const int* k = blocks + 9 * b;
       const int j0 = b == cuts[s].first ? cuts[s].second : 0, j1 = b == cuts[s + 1].first ? cuts[s + 1].second : k[7];
       piece(b, step_key(k[2], k[3], k[7], j0), step_key(k[2], k[3], k[7], j1), s);
     }
@@ -90,7 +93,7 @@ def shim(tmp_path_factory):
     lib = C.CDLL(str(where / "shim.so"))
     lib.print_of.restype = C.c_uint64
     lib.share.argtypes = [C.c_int64, C.c_int]
-    lib.by_stretches_of.argtypes = [C.c_int64, C.c_int, C.c_int]
+    lib.by_stretches_of.argtypes = [C.c_int64, C.c_int64, C.c_int, C.c_int]
     return lib
 
 
@@ -102,9 +105,9 @@ def _args(**kw):
 
 
 def _caps(shim, a):
-    out = (C.c_int64 * 18)()
+    out = (C.c_int64 * 19)()
     shim.caps(C.byref(a), out)
-    return dict(zip("blocks units joins slots bytes at_units at_joins at_seg at_seqs at_groups unit join workspace sums rows row at_rows at_stretches".split(), out))
+    return dict(zip("blocks units joins slots bytes at_units at_joins at_seg at_seqs at_groups unit join workspace sums rows row at_rows at_stretches stretch".split(), out))
 
 
 def _batches():
@@ -128,11 +131,11 @@ def _batches():
 def _cut(shim, segs, G, H_kv, d=128, fp8=0):
     arr = lambda i, t: np.array([s[i] for s in segs], dtype=t)  # noqa: E731
     arrays = [arr(0, np.int64), arr(1, np.int32), arr(2, np.int32), arr(3, np.int32)]
-    blocks, pieces = np.zeros(8 * 80000, np.int32), np.zeros(4 * 80000, np.int32)
+    blocks, pieces = np.zeros(9 * 80000, np.int32), np.zeros(4 * 80000, np.int32)
     n_pieces, n_stretches = C.c_int(), C.c_int()
     ptr = lambda x: x.ctypes.data_as(C.c_void_p)  # noqa: E731
     nb = shim.cut_up(len(segs), *[ptr(x) for x in arrays], G, H_kv, d, fp8, ptr(blocks), ptr(pieces), C.byref(n_pieces), C.byref(n_stretches))
-    return blocks[:8 * nb].reshape(-1, 8), pieces[:4 * n_pieces.value].reshape(-1, 4), n_stretches.value
+    return blocks[:9 * nb].reshape(-1, 9), pieces[:4 * n_pieces.value].reshape(-1, 4), n_stretches.value
 
 
 @pytest.mark.parametrize("heads", [(32, 8), (8, 8), (128, 8), (24, 8), (7, 1), (1024, 1024), (64, 2)])
@@ -140,7 +143,7 @@ def _cut(shim, segs, G, H_kv, d=128, fp8=0):
 def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
     H, H_kv = heads
     G, (d, fp8) = H // H_kv, kind
-    many, extra = (128, 4) if d == 64 else (256, 8)
+    many = 128 if d == 64 else 256
     for new, length, groups in _batches():
         B = len(new)
         shared = [0] * B
@@ -160,7 +163,7 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
         blocks, pieces, n_stretches = _cut(shim, segs, G, H_kv, d, fp8)
         caps = _caps(shim, _args(B=B, H=H, H_kv=H_kv, d=d, T_new=sum(new), n_groups=len(groups), cache_dtype=fp8))
         # the keys of a block, in order and without gaps; whole steps of 64 of the sequence apart from the ends
-        for i, (s, k, first_key, keys, p, m, cost, steps) in enumerate(blocks):
+        for i, (s, k, first_key, keys, p, m, cost, steps, extra) in enumerate(blocks):
             mine = pieces[pieces[:, 0] == i]
             assert len(mine) == p and mine[0, 1] == first_key and mine[-1, 2] == first_key + keys
             assert (mine[1:, 1] == mine[:-1, 2]).all() and (mine[1:, 1] % 64 == 0).all()
@@ -174,11 +177,12 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
         assert sorted(set(zip(blocks[:, 0], blocks[:, 1]))) == sorted((s, i) for s in range(len(segs)) for i in range(-(-rows[s] // (16 if rows[s] <= 16 else many))))
         # every stretch is a run of pieces; none has much more than its share
         assert (np.diff(pieces[:, 3]) >= 0).all() and (len(pieces) == 0 or pieces[-1, 3] < n_stretches)
-        if shim.by_stretches_of(len(blocks), d, H_kv) and len(pieces):
-            cost = [extra + -(-(int(x[2]) - (int(x[1]) & ~63)) // 64) * int(blocks[x[0], 6]) for x in pieces]
+        large = sum(min(int(b[5]), int(rows[b[0]] - b[1] * b[5])) > 16 for b in blocks)
+        if shim.by_stretches_of(len(blocks), large, d, H_kv) and len(pieces):
+            cost = [int(blocks[x[0], 8]) + -(-(int(x[2]) - (int(x[1]) & ~63)) // 64) * int(blocks[x[0], 6]) for x in pieces]
             per = np.bincount(pieces[:, 3], weights=cost, minlength=n_stretches)
-            share = (blocks[:, 7] * blocks[:, 6] + extra).sum() / n_stretches
-            assert per.max() <= share + 2 * extra + 4 * 8 + 1     # a snapped end on either side, a cut block's cost again
+            share = (blocks[:, 7] * blocks[:, 6] + blocks[:, 8]).sum() / n_stretches
+            assert per.max() <= share + 2 * 12 + 4 * 8 + 1     # a snapped end on either side, a cut block's cost again
         # room
         leaves = [bool(b[4] > 1 or b[0] < n_prefix or sh[b[0]] > 0) for b in blocks]
         assert len(blocks) <= caps["blocks"] and len(pieces) <= caps["units"] and n_stretches <= max(caps["units"], 1)
@@ -186,7 +190,7 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
         slots = sum(int(b[4]) * int(b[5]) // 16 for x, b in zip(leaves, blocks) if x)
         assert slots <= caps["slots"], (new, length, groups)
         assert caps["at_units"] + caps["units"] * caps["unit"] <= caps["at_stretches"]
-        assert caps["at_stretches"] + 4 * (caps["units"] + 1) <= caps["at_joins"]
+        assert caps["at_stretches"] + caps["stretch"] * caps["units"] <= caps["at_joins"]
         assert caps["at_joins"] + caps["joins"] * caps["join"] <= caps["at_rows"]
         assert sum(min(int(b[5]), int(rows[b[0]] - b[1] * b[5])) for x, b in zip(leaves, blocks) if x and b[0] >= n_prefix) <= caps["rows"]
         assert caps["at_rows"] + caps["rows"] * caps["row"] <= caps["at_seg"]

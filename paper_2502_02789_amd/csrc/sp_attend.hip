@@ -76,9 +76,9 @@ struct KeyRows {
   // key: the first that will be asked for
   __device__ __forceinline__ KeyRows(const AttendDev& p, const AttendUnit& u, int l, int key) {
     ts = p.c_ts; ps = p.c_ps; lg_page = p.lg_page; last_key = u.k1 - 1; lane = l;
-    first = PAGED ? 0 : scalar_table(p.cu_cache)[u.seq];
+    first = PAGED ? 0 : u.seq;
     last = PAGED ? p.last_page : p.last_row;
-    table = p.table + (int64_t)u.seq * p.blocks_per_seq;
+    table = PAGED ? p.table + (int64_t)u.seq * p.blocks_per_seq : nullptr;
     if (PAGED && u.k0 < u.k1) {
       chunk = min(key, last_key) >> lg_page >> 6;
       pages = load(chunk);
@@ -338,41 +338,40 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
     if (quad == 0 && p.lse) store_lse(p, at.token, at.h, m, sum, any_bad);
     return;
   } else {
-  float* const tops = reinterpret_cast<float*>(lds + W * 16 * (D + 4) * 4);  // [W][16], twice
+  // every wave's sums in what was its own tile, then one barrier
+  float* const tops = reinterpret_cast<float*>(lds + W * (2 * 32 * D * 2));  // [W][16], sums of weights, bad pages
   float* const sums = tops + W * 16;
-  const int any_bad = __syncthreads_or(bad != 0);  // (also: every wave is done with its tile in LDS)
+  uint32_t* const bads = reinterpret_cast<uint32_t*>(sums + W * 16);
+  constexpr int ROW = D + 4;  // floats from one row to the next: rows begin in different banks
+  float* const parts = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(parts + w * (32 * D) + row * ROW + 16 * i + 4 * quad) = o[i];
   if (quad == 0) {
     tops[w * 16 + row] = m;
     sums[w * 16 + row] = sum;
   }
-  __syncthreads();
-  auto top_of = [&](int r) {
-    float top = tops[r];
-#pragma unroll
-    for (int x = 1; x < W; ++x) top = fmaxf(top, tops[x * 16 + r]);
-    return top;
-  };
-  {
-    const float top = top_of(row), f = fast_exp2(m - (top == -INFINITY ? 0.f : top));
-    float* const part = reinterpret_cast<float*>(lds) + (w * 16 + row) * (D + 4);
-#pragma unroll
-    for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(part + 16 * i + 4 * quad) = o[i] * f;
-  }
+  if (l == 0) bads[w] = bad;
   __syncthreads();
   const int r = tid >> 4, lane = tid & 15;
   if (r >= u.nr) return;
   constexpr int V = D / 16;
-  float acc[V], l_all = 0.f;
-  const float top = top_of(r);
+  float acc[V], l_all = 0.f, top = tops[r];
+  uint32_t any_bad = bads[0];
+#pragma unroll
+  for (int x = 1; x < W; ++x) {
+    top = fmaxf(top, tops[x * 16 + r]);
+    any_bad |= bads[x];
+  }
   const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.f;
 #pragma unroll
   for (int x = 0; x < W; ++x) {
-    l_all += sums[x * 16 + r] * fast_exp2(tops[x * 16 + r] - base);
-    const float* part = reinterpret_cast<const float*>(lds) + (x * 16 + r) * (D + 4) + lane * V;
+    const float f = fast_exp2(tops[x * 16 + r] - base);
+    l_all += sums[x * 16 + r] * f;
+    const float* part = parts + x * (32 * D) + r * ROW + lane * V;
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] += part[i];
+    for (int i = 0; i < V; ++i) acc[i] += part[i] * f;
   }
   if (u.slot >= 0) {
     const int64_t place = slot_row(p, u.slot, r, g);
@@ -685,7 +684,7 @@ __device__ __forceinline__ void nan_rows(const AttendDev& p, int d, int64_t r0, 
 template <int D, bool FP8, bool PAGED>
 __global__ __launch_bounds__(64 * attend_waves(D), D == 64 ? 3 : 2) void attend_kernel(const AttendDev p) {
   constexpr int T = 64 * attend_waves(D);
-  __shared__ __align__(16) char lds[attend_waves(D) * 64 * D * 2];  // tiles: 16 KB a wave (8, d = 64); the sums of waves need less
+  __shared__ __align__(16) char lds[attend_waves(D) * (64 * D * 2 + 2 * 16 * 4 + 4)];  // tiles: 16 KB a wave (8, d = 64), and few rows' statistics
   // The KV heads of a piece are neighbours: with eight of them, each has the L2 of one XCD, which the rows of a
   // block share, as workgroups go to the XCDs in turn.
   const int n = (int)(blockIdx.x / (uint32_t)p.H_kv), g = (int)(blockIdx.x % (uint32_t)p.H_kv);
@@ -782,6 +781,7 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.blocks_per_seq = a->blocks_per_seq;
   p.last_page = paged ? (uint32_t)(a->n_rows / a->page_size - 1) : 0;
   p.last_row = (uint32_t)(a->n_rows - 1);
+  p.most_items = (uint32_t)(caps.rows * a->H_kv);  // (no more than T_new * H)
   p.scale_log2 = a->scale * 1.44269504088896340736f;
   p.q_ts = a->q_token_stride; p.q_hs = a->q_head_stride;
   p.o_ts = a->out_token_stride; p.o_hs = a->out_head_stride;
@@ -791,7 +791,7 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.units = reinterpret_cast<const AttendUnit*>(base + l.units);
   p.stretches = reinterpret_cast<const AttendStretch*>(base + l.stretches);
   p.rows = reinterpret_cast<const AttendRow*>(base + l.rows);
-  p.table = a->d_block_table; p.cu_cache = a->d_cu_cache;
+  p.table = a->d_block_table;
   p.q = static_cast<const uint16_t*>(a->d_q);
   p.k = static_cast<const char*>(a->d_k_cache); p.v = static_cast<const char*>(a->d_v_cache);
   p.k_scale = a->d_k_scale; p.v_scale = a->d_v_scale;
@@ -799,9 +799,9 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.sums = static_cast<float*>(a->d_workspace);
   p.stats = reinterpret_cast<float2*>(static_cast<char*>(a->d_workspace) + attend_sums_bytes(a));
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const uint32_t grid = (uint32_t)(caps.units * a->H_kv);
+  const uint32_t grid = (uint32_t)(most_stretches(a) * a->H_kv);
   if (a->d == 128) fp8 ? launch_attend<128, true>(p, paged, grid, stream) : launch_attend<128, false>(p, paged, grid, stream);
   else fp8 ? launch_attend<64, true>(p, paged, grid, stream) : launch_attend<64, false>(p, paged, grid, stream);
-  launch_attend_join(p, a->d, caps.rows * a->H_kv, stream);
+  launch_attend_join(p, a->d, stream);
   return launch_status();
 }

@@ -12,6 +12,7 @@ struct AttendDev {
   int B, H, H_kv, G, T_new;
   int lg_page, blocks_per_seq;
   uint32_t last_page, last_row;  // of the pool, of a contiguous cache
+  uint32_t most_items;           // (row, KV head) pairs to join that the list has room for
   float scale_log2;              // logit scale times log2(e)
   int64_t q_ts, q_hs, o_ts, o_hs;
   int32_t c_ts;                  // of the cache, in bytes
@@ -22,7 +23,6 @@ struct AttendDev {
   const AttendStretch* stretches;
   const AttendRow* rows;
   const int32_t* table;
-  const int32_t* cu_cache;
   const uint16_t* q;
   const char* k;
   const char* v;
@@ -36,6 +36,6 @@ struct AttendDev {
 
 sp_status check_attend_shape(const sp_attend_args* a);
 sp_status check_attend_plan_args(const sp_attend_args* a);
-void launch_attend_join(const AttendDev& p, int d, int64_t rows, hipStream_t stream);
+void launch_attend_join(const AttendDev& p, int d, hipStream_t stream);
 
 }  // namespace sp

@@ -45,7 +45,7 @@ SP_ATTEND_FN constexpr int many_rows(int d) { return 32 * attend_waves(d); }
 
 struct AttendUnit {   // one piece of one block
   int32_t r0, nr;     // first row, rows (nr <= 16: the kernel part for few rows)
-  int32_t seq;        // whose block table is read
+  int32_t seq;        // whose block table is read; of a contiguous cache: the row of its first token
   int32_t k0, k1;     // keys [k0, k1)
   int32_t off;        // token t sees keys below t + off (kNoLimit: all of the piece)
   int32_t slot;       // where the sums go, or -1: the block is finished here
@@ -154,6 +154,17 @@ SP_ATTEND_FN bool by_stretches(int64_t blocks, int64_t many, int d, int H_kv) {
 SP_ATTEND_FN int stretch_count(int64_t cost, int d, int H_kv) {
   const int64_t room = attend_items(d) / H_kv > 0 ? attend_items(d) / H_kv : 1, most = cost / least_stretch(d);
   return (int)(most < 1 ? 1 : most < room ? most : room);
+}
+// Most workgroups for each KV head that any lengths can give: of stretches where there cannot be too many blocks for them, and
+// no more than the longest sequences that the cache has room for ask for
+inline int64_t most_stretches(const sp_attend_args* a) {
+  const AttendCaps c = attend_caps(a);
+  const int64_t rows = a->T_new * (a->H / a->H_kv);
+  const int64_t large = rows > kFewRows ? c.blocks : 0;
+  if (!by_stretches(c.blocks, large, a->d, a->H_kv)) return c.units;
+  const int64_t room = a->d_block_table ? (int64_t)a->blocks_per_seq * a->page_size : a->n_rows;
+  const int64_t steps = room / kPieceStep + 2, step = a->d == 64 ? 4 : large ? 8 : 5, extra = 12;
+  return stretch_count(c.blocks * (steps * step + extra), a->d, a->H_kv);
 }
 // Where stretch s of n begins, blocks laid end to end
 SP_ATTEND_FN int64_t stretch_start(int64_t cost, int n, int s) { return cost * s / n; }

@@ -271,7 +271,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     } else {
       const PlanSeq s = seqs[k.seg - n_groups];
       t0 = s.t0;
-      unit.seq = k.seg - n_groups;
+      unit.seq = p.a.d_block_table ? k.seg - n_groups : p.a.d_cu_cache[k.seg - n_groups];
       unit.off = s.len - s.n + 1 - s.t0;
       unit.run = s.len < 0 ? kBadUnit : 0;
     }
@@ -408,17 +408,17 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendDev p) {
   __shared__ float4 part[GROUPS][L];
   __shared__ float2 stat[GROUPS];
   const uint64_t print = p.header->print;
-  const int n_rows = p.header->n_rows;
+  const uint32_t n_rows = (uint32_t)p.header->n_rows, H_kv = (uint32_t)p.H_kv;
   const bool together = p.header->most_pieces > 16;
   const int group = threadIdx.x / L, c = threadIdx.x % L, step = together ? GROUPS : 1, first = together ? group : 0;
   // (without a plan the pieces' kernel has filled the outputs)
-  const int64_t n_items = print == p.print ? (int64_t)n_rows * p.H_kv : 0, stride = (int64_t)gridDim.x * (together ? 1 : GROUPS);
-  for (int64_t item0 = (int64_t)blockIdx.x * (together ? 1 : GROUPS); item0 < n_items; item0 += stride) {
-    const int64_t item = together ? item0 : item0 + group;
+  const uint32_t n_items = print == p.print ? n_rows * H_kv : 0, stride = gridDim.x * (together ? 1 : GROUPS);
+  for (uint32_t item0 = blockIdx.x * (together ? 1 : GROUPS); item0 < n_items; item0 += stride) {
+    const uint32_t item = together ? item0 : item0 + group;
     const bool active = item < n_items;
-    const int g = (int)(item % p.H_kv);
+    const int g = (int)(item % H_kv);
     AttendRow r = {};
-    if (active) r = p.rows[item / p.H_kv];
+    if (active) r = p.rows[item / H_kv];
     const int n = r.own_pieces + r.pre_pieces, mine = n > first ? (n - first + step - 1) / step : 0;
     // index of piece q's row among all rows of the workspace
     auto place = [&](int q) -> int64_t {
@@ -491,8 +491,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendDev p) {
   }
 }
 
-void launch_attend_join(const AttendDev& p, int d, int64_t rows, hipStream_t stream) {
-  const int grid = (int)(rows < 2048 ? rows : 2048);
+void launch_attend_join(const AttendDev& p, int d, hipStream_t stream) {
+  const int grid = (int)(p.most_items < 2048 ? p.most_items : 2048);
   if (grid < 1) return;
   if (d == 128) hipLaunchKernelGGL(attend_join_kernel<128>, dim3(grid), dim3(256), 0, stream, p);
   else hipLaunchKernelGGL(attend_join_kernel<64>, dim3(grid), dim3(256), 0, stream, p);

@@ -24,7 +24,7 @@ extern "C" void caps(const sp_attend_args* a, int64_t* out) {
   const AttendPlanLayout l = attend_plan_layout(a);
   out[0] = c.blocks; out[1] = c.units; out[2] = c.joins; out[3] = c.slots; out[4] = (int64_t)l.bytes; out[5] = (int64_t)l.units;
   out[6] = (int64_t)l.joins; out[7] = (int64_t)l.seg_start; out[8] = (int64_t)l.seqs; out[9] = (int64_t)l.groups;
-  out[10] = sizeof(AttendUnit); out[11] = sizeof(AttendJoin); out[12] = (int64_t)attend_workspace(a); out[13] = (int64_t)attend_sums_bytes(a); out[14] = c.rows; out[15] = sizeof(AttendRow); out[16] = (int64_t)l.rows; out[17] = (int64_t)l.stretches; out[18] = sizeof(AttendStretch);
+  out[10] = sizeof(AttendUnit); out[11] = sizeof(AttendJoin); out[12] = (int64_t)attend_workspace(a); out[13] = (int64_t)attend_sums_bytes(a); out[14] = c.rows; out[15] = sizeof(AttendRow); out[16] = (int64_t)l.rows; out[17] = (int64_t)l.stretches; out[18] = sizeof(AttendStretch); out[19] = most_stretches(a);
 }
 extern "C" uint64_t print_of(const sp_attend_args* a) { return attend_print(a); }
 extern "C" int by_stretches_of(int64_t blocks, int64_t many, int d, int H_kv) { return by_stretches(blocks, many, d, H_kv); }
@@ -105,9 +105,9 @@ def _args(**kw):
 
 
 def _caps(shim, a):
-    out = (C.c_int64 * 19)()
+    out = (C.c_int64 * 20)()
     shim.caps(C.byref(a), out)
-    return dict(zip("blocks units joins slots bytes at_units at_joins at_seg at_seqs at_groups unit join workspace sums rows row at_rows at_stretches stretch".split(), out))
+    return dict(zip("blocks units joins slots bytes at_units at_joins at_seg at_seqs at_groups unit join workspace sums rows row at_rows at_stretches stretch most_stretches".split(), out))
 
 
 def _batches():
@@ -161,7 +161,7 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
         segs += [(n * G, n, m, s) for n, m, s in zip(new, length, shared)]
         rows, n, ln, sh = ([s[i] for s in segs] for i in range(4))
         blocks, pieces, n_stretches = _cut(shim, segs, G, H_kv, d, fp8)
-        caps = _caps(shim, _args(B=B, H=H, H_kv=H_kv, d=d, T_new=sum(new), n_groups=len(groups), cache_dtype=fp8))
+        caps = _caps(shim, _args(B=B, H=H, H_kv=H_kv, d=d, T_new=sum(new), n_groups=len(groups), cache_dtype=fp8, page_size=8, blocks_per_seq=-(-max(length) // 8)))
         # the keys of a block, in order and without gaps; whole steps of 64 of the sequence apart from the ends
         for i, (s, k, first_key, keys, p, m, cost, steps, extra) in enumerate(blocks):
             mine = pieces[pieces[:, 0] == i]
@@ -186,6 +186,7 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
         # room
         leaves = [bool(b[4] > 1 or b[0] < n_prefix or sh[b[0]] > 0) for b in blocks]
         assert len(blocks) <= caps["blocks"] and len(pieces) <= caps["units"] and n_stretches <= max(caps["units"], 1)
+        assert n_stretches <= max(caps["most_stretches"], 1) and caps["most_stretches"] <= max(caps["units"], 1)
         assert sum(1 for x, b in zip(leaves, blocks) if x and b[0] >= n_prefix) <= caps["joins"]
         slots = sum(int(b[4]) * int(b[5]) // 16 for x, b in zip(leaves, blocks) if x)
         assert slots <= caps["slots"], (new, length, groups)

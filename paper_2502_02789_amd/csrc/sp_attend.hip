@@ -190,18 +190,20 @@ struct FewTile {
   }
 };
 
-// W waves take the piece: all of the workgroup's, or one (every wave with a piece of its own; nothing is shared, no barrier)
-template <int D, bool FP8, bool PAGED, int W>
-__device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit& u, int g, char* lds) {
+// W waves (a power of two of those of the workgroup, side by side) take the piece; the others take others at the same time, and
+// all meet at one barrier.
+template <int D, bool FP8, bool PAGED>
+__device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit& u, int g, int W, char* lds) {
   constexpr int KS = D / 32;          // steps of the product with the queries
   constexpr int DB = D / 16;          // blocks of values
   constexpr int C = D / 8;            // 16-byte chunks of a bf16 row
   using Tile = FewTile<D, FP8>;
-  const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, row = l & 15, quad = l >> 4;
+  constexpr int NW = attend_waves(D);
+  const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), turn = w & (W - 1), l = tid & 63, row = l & 15, quad = l >> 4;
   const bool mine = row < u.nr;
   const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
 
-  int tile = u.k0 < u.k1 ? (u.k0 & ~31) + (W > 1 ? 32 * w : 0) : u.k1;
+  int tile = u.k0 < u.k1 ? (u.k0 & ~31) + 32 * turn : u.k1;
   KeyRows<PAGED> rows(p, u, l, tile);
   const char* const kb = p.k + (int64_t)g * p.c_hs;
   const char* const vb = p.v + (int64_t)g * p.c_hs;
@@ -320,28 +322,10 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   // the waves' sums joined, in the waves' order
   sum += __shfl_xor(sum, 16, kWave);
   sum += __shfl_xor(sum, 32, kWave);
-  if constexpr (W == 1) {
-    const bool any_bad = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
-    if (!mine) return;
-    if (u.slot >= 0) {
-      const int64_t place = slot_row(p, u.slot, row, g);
-      float* dst = p.sums + place * D + 4 * quad;
-#pragma unroll
-      for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(dst + 16 * i) = o[i];
-      if (quad == 0) store_stats(p, place, m, sum, any_bad);
-      return;
-    }
-    const float mul = (sum == 0.f ? 0.f : 1.f / sum) * (p.v_scale ? p.v_scale[g] : 1.f);
-    uint16_t* dst = p.out + at.token * p.o_ts + at.h * p.o_hs + 4 * quad;
-#pragma unroll
-    for (int i = 0; i < DB; ++i) store_values(dst + 16 * i, o[i] * mul, any_bad);
-    if (quad == 0 && p.lse) store_lse(p, at.token, at.h, m, sum, any_bad);
-    return;
-  } else {
   // every wave's sums in what was its own tile, then one barrier
-  float* const tops = reinterpret_cast<float*>(lds + W * (2 * 32 * D * 2));  // [W][16], sums of weights, bad pages
-  float* const sums = tops + W * 16;
-  uint32_t* const bads = reinterpret_cast<uint32_t*>(sums + W * 16);
+  float* const tops = reinterpret_cast<float*>(lds + NW * (2 * 32 * D * 2));  // [wave][16], sums of weights, bad pages
+  float* const sums = tops + NW * 16;
+  uint32_t* const bads = reinterpret_cast<uint32_t*>(sums + NW * 16);
   constexpr int ROW = D + 4;  // floats from one row to the next: rows begin in different banks
   float* const parts = reinterpret_cast<float*>(lds);
 #pragma unroll
@@ -352,45 +336,41 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   }
   if (l == 0) bads[w] = bad;
   __syncthreads();
-  const int r = tid >> 4, lane = tid & 15;
-  if (r >= u.nr) return;
+  // the piece's waves join them, in their order, 16 lanes to a row
   constexpr int V = D / 16;
-  float acc[V], l_all = 0.f, top = tops[r];
-  uint32_t any_bad = bads[0];
+  const int w0 = w - turn, lane = tid & 15;
+  for (int r = (turn * 64 + l) >> 4; r < u.nr; r += 4 * W) {
+    float acc[V], l_all = 0.f, top = tops[w0 * 16 + r];
+    uint32_t any_bad = bads[w0];
+    for (int x = w0 + 1; x < w0 + W; ++x) {
+      top = fmaxf(top, tops[x * 16 + r]);
+      any_bad |= bads[x];
+    }
+    const float base = top == -INFINITY ? 0.f : top;
 #pragma unroll
-  for (int x = 1; x < W; ++x) {
-    top = fmaxf(top, tops[x * 16 + r]);
-    any_bad |= bads[x];
-  }
-  const float base = top == -INFINITY ? 0.f : top;
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
+#pragma unroll 2
+    for (int x = w0; x < w0 + W; ++x) {
+      const float f = fast_exp2(tops[x * 16 + r] - base);
+      l_all += sums[x * 16 + r] * f;
+      const float* part = parts + x * (32 * D) + r * ROW + lane * V;
 #pragma unroll
-  for (int i = 0; i < V; ++i) acc[i] = 0.f;
+      for (int i = 0; i < V; ++i) acc[i] += part[i] * f;
+    }
+    if (u.slot >= 0) {
+      const int64_t place = slot_row(p, u.slot, r, g);
+      float* dst = p.sums + place * D + lane * V;
 #pragma unroll
-  for (int x = 0; x < W; ++x) {
-    const float f = fast_exp2(tops[x * 16 + r] - base);
-    l_all += sums[x * 16 + r] * f;
-    const float* part = parts + x * (32 * D) + r * ROW + lane * V;
+      for (int i = 0; i < V; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+      if (lane == 0) store_stats(p, place, top, l_all, any_bad);
+      continue;
+    }
+    const RowPlace to = row_place(p, u.r0 + r, g);
+    const float mul = (l_all == 0.f ? 0.f : 1.f / l_all) * (p.v_scale ? p.v_scale[g] : 1.f);
+    uint16_t* dst = p.out + to.token * p.o_ts + to.h * p.o_hs + lane * V;
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] += part[i] * f;
-  }
-  if (u.slot >= 0) {
-    const int64_t place = slot_row(p, u.slot, r, g);
-    float* dst = p.sums + place * D + lane * V;
-#pragma unroll
-    for (int i = 0; i < V; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
-    if (lane == 0) store_stats(p, place, top, l_all, any_bad);
-    return;
-  }
-  const RowPlace to = row_place(p, u.r0 + r, g);
-  const float mul = (l_all == 0.f ? 0.f : 1.f / l_all) * (p.v_scale ? p.v_scale[g] : 1.f);
-  const uint32_t nan2 = kNanBf16 * 0x10001u;
-  uint32_t out[V / 2];
-#pragma unroll
-  for (int i = 0; i < V; i += 2) out[i / 2] = any_bad ? nan2 : pack_bf16_pair(acc[i] * mul, acc[i + 1] * mul);
-  uint16_t* dst = p.out + to.token * p.o_ts + to.h * p.o_hs + lane * V;
-  if constexpr (V == 8) *reinterpret_cast<u32x4*>(dst) = u32x4{out[0], out[1], out[2], out[3]};
-  else *reinterpret_cast<uint2*>(dst) = make_uint2(out[0], out[1]);
-  if (lane == 0 && p.lse) store_lse(p, to.token, to.h, top, l_all, any_bad);
+    for (int i = 0; i < V; i += 4) store_values(dst + i, f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]} * mul, any_bad);
+    if (lane == 0 && p.lse) store_lse(p, to.token, to.h, top, l_all, any_bad);
   }
 }
 
@@ -711,13 +691,19 @@ __global__ __launch_bounds__(64 * attend_waves(D), D == 64 ? 3 : 2) void attend_
   if (n >= n_stretches || x >= end) return;
   const auto unit_at = [&](int i) { return reinterpret_cast<UnitPtr>(reinterpret_cast<uintptr_t>(p.units + i)); };
   for (;;) {
-    if (u.run > 0) {
-      const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-      if (w < u.run) attend_few<D, FP8, PAGED, 1>(p, w == 0 ? u : read(unit_at(x + w)), g, lds);
-      x += u.run;
+    if (u.run != kBadUnit && u.nr <= kFewRows) {
+      // one piece, or several short ones side by side
+      const int run = u.run > 1 ? u.run : 1;
+      int W = attend_waves(D);
+      while (W > 1 && run * W > attend_waves(D)) W >>= 1;
+      const int mine = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / W;
+      AttendUnit v = u;
+      if (mine > 0 && mine < run) v = read(unit_at(x + mine));
+      if (mine >= run) v.nr = v.k0 = v.k1 = 0;
+      attend_few<D, FP8, PAGED>(p, v, g, W, lds);
+      x += run;
     } else {
       if (u.run == kBadUnit) nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, T);
-      else if (u.nr <= kFewRows) attend_few<D, FP8, PAGED, attend_waves(D)>(p, u, g, lds);
       else if (attend_waves(D) == 8 && u.nr <= many_rows(D) / 2) attend_many<D, FP8, PAGED, attend_waves(D) == 8>(p, u, g, lds);
       else attend_many<D, FP8, PAGED, false>(p, u, g, lds);
       ++x;

@@ -49,7 +49,7 @@ struct AttendUnit {   // one piece of one block
   int32_t k0, k1;     // keys [k0, k1)
   int32_t off;        // token t sees keys below t + off (kNoLimit: all of the piece)
   int32_t slot;       // where the sums go, or -1: the block is finished here
-  int32_t run;        // kBadUnit: the sequence's length is invalid, its rows become NaN; else how many units from this one on a wave each takes (0: all waves take this one)
+  int32_t run;        // kBadUnit: the sequence's length is invalid, its rows become NaN; else how many units from this one on are taken side by side (0: this one alone)
 };
 struct AttendStretch {  // what one workgroup does, for each KV head: units [first, end), the first of them a copy
   int32_t first, end;
@@ -133,8 +133,8 @@ SP_ATTEND_FN int own_block_keys(int64_t rows, int i, int m, int G, int n, int le
 // Steps of 64 keys of a block's keys [first, first + keys), cut at multiples of 64 keys of the sequence
 SP_ATTEND_FN int block_steps(int first, int keys) { return (int)(((int64_t)(first & (kPieceStep - 1)) + keys + kPieceStep - 1) / kPieceStep); }
 
-// A piece of few rows and few keys is not worth all waves: where several follow one another, each is a wave's
-SP_ATTEND_FN bool wave_sized(int rows, int keys) { return rows <= kFewRows && keys <= 512; }
+// A piece of few rows and few keys is not worth all waves: where several follow one another, they share the waves
+SP_ATTEND_FN bool is_short(int rows, int keys) { return rows <= kFewRows && keys <= 1024; }
 
 // What a step costs a workgroup, in units of 0.27 us (d = 128) and 0.67 us on a full device: 16 rows are bound by reading 64 keys and
 // values, more by the matrix cores (eight waves with up to 128 rows work on two steps at a time); and what a piece costs besides.
@@ -142,9 +142,9 @@ SP_ATTEND_FN int step_cost(int rows, int d, bool fp8) {
   if (rows <= kFewRows) return d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5);
   return d == 64 ? 4 : rows <= many_rows(d) / 2 ? 6 : 8;
 }
-SP_ATTEND_FN int piece_cost(int rows, int keys, int d) { return d == 64 ? (wave_sized(rows, keys) ? 2 : 4) : wave_sized(rows, keys) ? 3 : 12; }
-// No stretch costs less: more than one step and a half of any kind
-SP_ATTEND_FN int least_stretch(int d) { return d == 64 ? 10 : 20; }
+SP_ATTEND_FN int piece_cost(int rows, int keys, int d) { return d == 64 ? (is_short(rows, keys) ? 2 : 4) : is_short(rows, keys) ? 3 : 12; }
+// No stretch costs less: more than a step of any kind
+SP_ATTEND_FN int least_stretch(int d) { return d == 64 ? 10 : 11; }
 
 // many: blocks of more than 16 rows (the others are cheap to cut)
 SP_ATTEND_FN bool by_stretches(int64_t blocks, int64_t many, int d, int H_kv) {

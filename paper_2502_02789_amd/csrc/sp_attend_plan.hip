@@ -319,11 +319,11 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       p.units[u] = unit_of(k, j0, j1, slot_of[x] < 0 ? -1 : slot_of[x] + (int64_t)q * (k.m / kSlotRows));
     }
     __syncthreads();
-    // pieces that a wave each takes: as many as follow one another in a stretch, up to the waves of a workgroup
+    // short pieces that are taken side by side: as many as follow one another in a stretch, up to the waves of a workgroup
     const int waves = attend_waves(p.a.d);
     auto alone = [&](int u) {
       const AttendUnit x = p.units[u];
-      return x.run != kBadUnit && wave_sized(x.nr, x.k1 - x.k0);
+      return x.run != kBadUnit && is_short(x.nr, x.k1 - x.k0);
     };
     for (int u = tid; u < (int)n[kUnits]; u += 1024) {
       const int end = first_unit[last_at_most(first_unit, n_cuts, u) + 1];
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
 // lanes take one row, every eighth (sixteenth, d = 64) piece each group of lanes.  (Compiled with NaNs honoured: invalid rows
 // have a NaN for l.)
 template <int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(const AttendDev p) {
+__global__ __launch_bounds__(256, 4) void attend_join_kernel(const AttendDev p) {
   constexpr int L = D / 4, GROUPS = 256 / L;
   __shared__ float4 part[GROUPS][L];
   __shared__ float2 stat[GROUPS];
@@ -429,10 +429,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendDev p) {
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int q0 = 0; q0 < mine; q0 += L) {  // a lane holds the factor of one piece
       const int count = min(L, mine - q0);
-      float4 x[8];
+      float4 x[4];
       auto read = [&](int q) {  // (beyond the last: its values again, with a factor of zero)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 4; ++i)
           x[i] = *reinterpret_cast<const float4*>(p.sums + place(first + (q0 + min(q + i, count - 1)) * step) * D + c * 4);
       };
       float2 s = make_float2(-INFINITY, 0.f);
@@ -451,11 +451,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const AttendDev p) {
       acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
       for (int q = 0;;) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 4; ++i) {
           const float w = __shfl(f, q + i, L);
           acc.x += w * x[i].x; acc.y += w * x[i].y; acc.z += w * x[i].z; acc.w += w * x[i].w;
         }
-        q += 8;
+        q += 4;
         if (q >= count) break;
         read(q);
       }

@@ -201,11 +201,11 @@ def test_pieces_cover_every_block_within_the_reserved_room(shim, heads, kind):
 
 
 def test_equal_work_is_spread_over_the_device(shim):
-    """One long sequence: 32 stretches for each of 8 KV heads; a short one: pieces of 256 keys; many blocks: no cuts."""
+    """One long sequence: 32 stretches for each of 8 KV heads; a short one: pieces of two or three steps; many blocks: no cuts."""
     blocks, pieces, n = _cut(shim, [(4, 1, 131072, 0)], 4, 8)
     size = pieces[:, 2] - pieces[:, 1]
     assert n == len(pieces) == 32 and size.max() <= 1.1 * size.mean() + 64
-    assert (lambda p: (p[:, 2] - p[:, 1]).max())(_cut(shim, [(4, 1, 1000, 0)], 4, 8)[1]) == 256
+    assert (lambda p: (p[:, 2] - p[:, 1]).max())(_cut(shim, [(4, 1, 1000, 0)], 4, 8)[1]) <= 192
     blocks, pieces, n = _cut(shim, [(4 * 20000, 20000, 20000, 0)], 4, 8)
     assert n == len(pieces) == len(blocks) == -(-4 * 20000 // 256)
     assert (np.diff(pieces[:, 2]) <= 0).all()          # the longest first

@@ -112,26 +112,32 @@ inline AttendCaps attend_caps(const sp_attend_args* a) {
 
 // What a member's shared prefix saves: a block's rows are filled up by several members, and its keys read once for them all.  With 128 rows of its own
 // for each member there is little to gain.
-SP_ATTEND_FN bool shares(int64_t group_rows, int members) { return members >= 2 && group_rows < (int64_t)kShareRows * members; }
+SP_ATTEND_FN bool shares(int rows, int members) { return members >= 2 && rows / kShareRows < members; }
 
-SP_ATTEND_FN int block_rows(int64_t rows, int d) { return rows <= kFewRows ? kFewRows : many_rows(d); }
-SP_ATTEND_FN int segment_blocks(int64_t rows, int d) { return (int)((rows + block_rows(rows, d) - 1) / block_rows(rows, d)); }
+// (Rows of a segment are fewer than 2^31: T_new * H is.  Divisions of 64-bit numbers take 150 instructions each; the plan, one workgroup that
+// goes through its code once, is bound by fetching it.)
+SP_ATTEND_FN int block_rows(int rows, int d) { return rows <= kFewRows ? kFewRows : many_rows(d); }
+SP_ATTEND_FN int segment_blocks(int rows, int d) {
+  const uint32_t m = (uint32_t)block_rows(rows, d);
+  const int shift = m == 16 ? 4 : m == 128 ? 7 : 8;
+  return (int)(((uint32_t)rows + m - 1) >> shift);
+}
 
 // One past the last key that row `row` of a sequence sees (its rows counted from 0, G to a token), n new tokens, len keys.
-SP_ATTEND_FN int row_limit(int64_t row, int G, int n, int len) {
-  const int64_t v = (int64_t)len - n + row / G + 1;
+SP_ATTEND_FN int row_limit(uint32_t row, int G, int n, int len) {
+  const int64_t v = (int64_t)len - n + row / (uint32_t)G + 1;
   return v < 0 ? 0 : v > len ? len : (int)v;
 }
 
 // The keys of block i (of m rows) of a sequence's own segment: [shared, the limit of its last row)
-SP_ATTEND_FN int own_block_keys(int64_t rows, int i, int m, int G, int n, int len, int shared) {
-  const int64_t last = (int64_t)(i + 1) * m < rows ? (int64_t)(i + 1) * m - 1 : rows - 1;
+SP_ATTEND_FN int own_block_keys(int rows, int i, int m, int G, int n, int len, int shared) {
+  const uint32_t end = (uint32_t)(i + 1) * (uint32_t)m, last = (end < (uint32_t)rows ? end : (uint32_t)rows) - 1;
   const int v = row_limit(last, G, n, len) - shared;
   return v < 0 ? 0 : v;
 }
 
 // Steps of 64 keys of a block's keys [first, first + keys), cut at multiples of 64 keys of the sequence
-SP_ATTEND_FN int block_steps(int first, int keys) { return (int)(((int64_t)(first & (kPieceStep - 1)) + keys + kPieceStep - 1) / kPieceStep); }
+SP_ATTEND_FN int block_steps(int first, int keys) { return (int)(((uint32_t)(first & (kPieceStep - 1)) + (uint32_t)keys + kPieceStep - 1) / kPieceStep); }
 
 // A piece of few rows and few keys is not worth all waves: where several follow one another, they share the waves
 SP_ATTEND_FN bool is_short(int rows, int keys) { return rows <= kFewRows && keys <= 1024; }
@@ -166,13 +172,14 @@ inline int64_t most_stretches(const sp_attend_args* a) {
   const int64_t steps = room / kPieceStep + 2, step = a->d == 64 ? 4 : large ? 8 : 5, extra = 12;
   return stretch_count(c.blocks * (steps * step + extra), a->d, a->H_kv);
 }
-// Where stretch s of n begins, blocks laid end to end
-SP_ATTEND_FN int64_t stretch_start(int64_t cost, int n, int s) { return cost * s / n; }
+// Where stretch s of n begins, blocks laid end to end (exact: products are below 2^53, and quotients far enough from whole numbers)
+SP_ATTEND_FN int64_t stretch_start(int64_t cost, int n, int s) { return (int64_t)((double)cost * s / n); }
 // ... as a step of the block whose share begins at `start` (what the block costs besides spread over its steps): `steps` (the next
-// block's first) or 0 where a piece would get too short
+// block's first) or 0 where a piece would get too short.  Does not descend as x ascends.
 SP_ATTEND_FN int step_at(int64_t x, int64_t start, int steps, int per_step, int extra) {
-  const int64_t cost = (int64_t)steps * per_step + extra, j = (2 * (x - start) * steps + cost) / (2 * cost);
-  return j < kMinSteps ? 0 : steps - j < kMinSteps ? steps : (int)j;
+  const double cost = (double)steps * per_step + extra;
+  const int j = (int)((double)(x - start) * steps / cost + 0.5);
+  return j < kMinSteps ? 0 : steps - j < kMinSteps ? steps : j;
 }
 SP_ATTEND_FN int step_key(int first, int keys, int steps, int j) {
   return j <= 0 ? first : j >= steps ? first + keys : (first & ~(kPieceStep - 1)) + j * kPieceStep;
@@ -185,11 +192,13 @@ SP_ATTEND_FN int make_cut(int64_t total, int d, int H_kv) {
   const int64_t cut = (share + kPieceStep - 1) / kPieceStep * kPieceStep;
   return cut < least ? (int)least : cut > 0x40000000 ? 0x40000000 : (int)cut;
 }
-SP_ATTEND_FN int pieces_of(int keys, int cut) { return keys <= cut ? 1 : (int)(((int64_t)keys + cut - 1) / cut); }
+SP_ATTEND_FN int pieces_of(int keys, int cut) { return keys <= cut ? 1 : (int)(((uint32_t)keys + (uint32_t)cut - 1) / (uint32_t)cut); }
+// first step of piece p of so many (exact, as above)
+SP_ATTEND_FN int piece_step(int steps, int pieces, int p) { return (int)((double)steps * p / pieces); }
 // first key of piece p
 SP_ATTEND_FN int piece_start(int first, int keys, int pieces, int p) {
   const int steps = block_steps(first, keys);
-  return step_key(first, keys, steps, p == pieces ? steps : (int)((int64_t)steps * p / pieces));
+  return step_key(first, keys, steps, p == pieces ? steps : piece_step(steps, pieces, p));
 }
 
 SP_ATTEND_FN uint64_t attend_print(const sp_attend_args* a) {

@@ -33,26 +33,34 @@ __device__ __forceinline__ int group_of(const PlanDev& p, int b) {
   return upper_segment(p.a.d_cu_group, n, b);
 }
 
-// exclusive prefixes of N numbers over the workgroup's 1024 threads, and their sums over all of them
+// exclusive prefixes of N numbers over the workgroup's 1024 threads, and their sums over all of them (most waves have nothing to add)
 template <int N>
 __device__ __forceinline__ void block_exclusive(int64_t (&v)[N], int64_t (&total)[N]) {
   __shared__ int64_t waves[16][N];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  bool any = false;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    int64_t x = v[i];
+  for (int i = 0; i < N; ++i) any |= v[i] != 0;
+  if (__ballot(any)) {
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int64_t y = __shfl_up(x, off, kWave);
-      if (l >= off) x += y;
+    for (int i = 0; i < N; ++i) {
+      int64_t x = v[i];
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const int64_t y = __shfl_up(x, off, kWave);
+        if (l >= off) x += y;
+      }
+      if (l == 63) waves[w][i] = x;
+      v[i] = x - v[i];
     }
-    if (l == 63) waves[w][i] = x;
-    v[i] = x - v[i];
+  } else if (l < N) {
+    waves[w][l] = 0;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     total[i] = 0;
+#pragma unroll
     for (int x = 0; x < 16; ++x) {
       if (x == w) v[i] += total[i];
       total[i] += waves[x][i];
@@ -63,7 +71,7 @@ __device__ __forceinline__ void block_exclusive(int64_t (&v)[N], int64_t (&total
 
 struct Block {       // a block of rows
   int seg, i;        // segment (prefixes first, then sequences), block of it
-  int64_t rows;      // of the segment
+  int rows;          // of the segment
   int m, nr;         // rows of a whole block, of this one
   int first, keys;   // its keys are [first, first + keys)
   int steps, cost;   // ... and a step's cost
@@ -94,7 +102,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   __shared__ int64_t cuts[kMostStretches + 1];        // (block, step) that each stretch begins at
   __shared__ int32_t first_unit[kMostStretches + 1];
   __shared__ int32_t slot_of[kMostStretchBlocks];
-  __shared__ uint8_t runs[kMostStretchBlocks + kMostStretches];
+  __shared__ uint8_t alone[kMostStretchBlocks + kMostStretches];  // pieces that are short
   PlanSeq* const seqs = p.a.B <= kLdsSeqs ? lds_seqs : p.seqs;
   int32_t* const seg_start = p.a.B <= kLdsSeqs ? lds_seg : p.seg_start;  // (no more groups than sequences)
   const int tid = threadIdx.x, B = p.a.B, n_groups = p.a.n_groups, G = p.G, T = (int)p.a.T_new;
@@ -145,7 +153,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     for (int g = tid; g < n_groups; g += 1024) {  // (atomics are done in L2: read there)
       const int active = __hip_atomic_load(&p.groups[g].active, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       const int shared = __hip_atomic_load(&p.groups[g].shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      p.groups[g].shared = shares((int64_t)p.groups[g].tokens * G, active) ? shared : 0;
+      p.groups[g].shared = shares(p.groups[g].tokens * G, active) ? shared : 0;
     }
     __syncthreads();
     for (int b = tid; b < B; b += 1024) {
@@ -154,11 +162,22 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     }
     __syncthreads();
   }
-  block_prefix_table(n_groups + B, [&](int s) -> int32_t {
-    if (s < n_groups) return p.groups[s].shared > 0 ? segment_blocks((int64_t)p.groups[s].tokens * G, p.a.d) : 0;
-    const int n = seqs[s - n_groups].n;
-    return n > 0 ? segment_blocks((int64_t)n * G, p.a.d) : 0;
-  }, seg_start);
+  {  // the segments' first blocks
+    const int n_seg = n_groups + B, per = (n_seg + 1023) / 1024, s0 = min(n_seg, tid * per), s1 = min(n_seg, s0 + per);
+    auto blocks_of = [&](int s) {
+      const int tokens = s < n_groups ? (p.groups[s].shared > 0 ? p.groups[s].tokens : 0) : seqs[s - n_groups].n;
+      return tokens > 0 ? segment_blocks(tokens * G, p.a.d) : 0;
+    };
+    int64_t count[1] = {0}, all[1];
+    for (int s = s0; s < s1; ++s) count[0] += blocks_of(s);
+    block_exclusive(count, all);
+    for (int s = s0; s < s1; ++s) {
+      seg_start[s] = (int)count[0];
+      count[0] += blocks_of(s);
+    }
+    if (tid == 0) seg_start[n_seg] = (int)all[0];
+    __syncthreads();
+  }
   const int n_blocks = seg_start[n_groups + B], n_prefix = seg_start[n_groups];
   if (n_blocks > p.cap_blocks) return;  // (offsets that do not ascend may ask for more than there is room for: no plan then)
 
@@ -170,7 +189,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     Block k;
     k.seg = hint >= 0 && flat >= seg_start[hint] && flat < seg_start[hint + 1] ? hint : upper_segment(seg_start, n_groups + B, flat);
     k.i = flat - seg_start[k.seg];
-    k.rows = (int64_t)(k.seg < n_groups ? p.groups[k.seg].tokens : seqs[k.seg - n_groups].n) * G;
+    k.rows = (k.seg < n_groups ? p.groups[k.seg].tokens : seqs[k.seg - n_groups].n) * G;
     k.m = block_rows(k.rows, p.a.d);
     if (k.seg < n_groups) {
       k.first = 0;
@@ -180,7 +199,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       k.first = s.shared;
       k.keys = s.len < 0 ? 0 : own_block_keys(k.rows, k.i, k.m, G, s.n, s.len, s.shared);
     }
-    k.nr = (int)min((int64_t)k.m, k.rows - (int64_t)k.i * k.m);
+    k.nr = min(k.m, k.rows - k.i * k.m);
     k.steps = block_steps(k.first, k.keys);
     k.cost = step_cost(k.nr, p.a.d, fp8);
     k.extra = piece_cost(k.nr, k.keys, p.a.d);
@@ -296,7 +315,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       } else {
         for (int q = 0; q < pieces; ++q) {
           AttendStretch s;
-          s.unit = p.units[u + q] = unit_of(k, (int)((int64_t)k.steps * q / pieces), q + 1 == pieces ? k.steps : (int)((int64_t)k.steps * (q + 1) / pieces),
+          s.unit = p.units[u + q] = unit_of(k, piece_step(k.steps, pieces, q), q + 1 == pieces ? k.steps : piece_step(k.steps, pieces, q + 1),
                                             sums ? slot + (int64_t)q * step : -1);
           s.first = (int)(u + q);
           s.end = s.first + 1;
@@ -309,40 +328,35 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   }
   __syncthreads();
   if (stretched) {
-    for (int u = tid; u < (int)n[kUnits]; u += 1024) {
-      const int s = last_at_most(first_unit, n_cuts, u);
+    auto piece = [&](int u, int s) {
       const int64_t a = cuts[s], b = cuts[s + 1];
       const int x = (int)(a >> 32) + u - first_unit[s];
       const Block k = block_at(x, -1);
       const int j0 = x == (int)(a >> 32) ? (int)a : 0, j1 = x == (int)(b >> 32) ? (int)b : k.steps;
       const int q = j0 > 0 ? s - first_cut(x) + 1 : 0;
-      p.units[u] = unit_of(k, j0, j1, slot_of[x] < 0 ? -1 : slot_of[x] + (int64_t)q * (k.m / kSlotRows));
+      return unit_of(k, j0, j1, slot_of[x] < 0 ? -1 : slot_of[x] + (int64_t)q * (k.m / kSlotRows));
+    };
+    for (int u = tid; u < (int)n[kUnits]; u += 1024) {
+      const AttendUnit x = piece(u, last_at_most(first_unit, n_cuts, u));
+      alone[u] = x.run != kBadUnit && is_short(x.nr, x.k1 - x.k0);
     }
     __syncthreads();
     // short pieces that are taken side by side: as many as follow one another in a stretch, up to the waves of a workgroup
     const int waves = attend_waves(p.a.d);
-    auto alone = [&](int u) {
-      const AttendUnit x = p.units[u];
-      return x.run != kBadUnit && is_short(x.nr, x.k1 - x.k0);
-    };
     for (int u = tid; u < (int)n[kUnits]; u += 1024) {
-      const int end = first_unit[last_at_most(first_unit, n_cuts, u) + 1];
-      int run = 0;
-      while (run < waves && u + run < end && alone(u + run)) ++run;
-      if (run > 1) runs[u] = run;   // (the units themselves are still being read)
-      else runs[u] = 0;
-    }
-    __syncthreads();
-    for (int u = tid; u < (int)n[kUnits]; u += 1024)
-      if (runs[u] > 0) p.units[u].run = runs[u];
-    __syncthreads();
-    for (int s = tid; s < n_cuts; s += 1024) {
+      const int s = last_at_most(first_unit, n_cuts, u);
       AttendStretch x = {};
       x.first = first_unit[s];
       x.end = first_unit[s + 1];
-      if (x.first < x.end) x.unit = p.units[x.first];
-      p.stretches[s] = x;
+      x.unit = piece(u, s);
+      int run = 0;
+      while (run < waves && u + run < x.end && alone[u + run]) ++run;
+      if (run > 1) x.unit.run = run;
+      p.units[u] = x.unit;
+      if (u == x.first) p.stretches[s] = x;
     }
+    for (int s = tid; s < n_cuts; s += 1024)
+      if (first_unit[s] == first_unit[s + 1]) p.stretches[s] = AttendStretch();
   }
   int64_t slot = at[kSlots], j = at[kJoins], row = at[kRows];
   walk([&](int x, const Block& k) {
@@ -376,7 +390,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       o.own_step = e.own_step * kSlotRows;
       if (e.group >= 0) {  // (the blocks of a prefix may be cut differently)
         const PlanGroup g = p.groups[e.group];
-        const int m = block_rows((int64_t)g.tokens * G, p.a.d), in = o.row - g.t0 * G, x = seg_start[e.group] + in / m;
+        const int m = block_rows(g.tokens * G, p.a.d), in = o.row - g.t0 * G, x = seg_start[e.group] + in / m;
         if (in >= 0 && in < g.tokens * G) {
           o.pre_pieces = stretched ? pieces_at(x, Block()) : g.pieces;
           o.pre_at = (stretched ? slot_of[x] : g.slot + in / m * g.pieces * (m / kSlotRows)) * kSlotRows + in % m;

@@ -28,10 +28,10 @@ extern "C" void caps(const sp_attend_args* a, int64_t* out) {
 }
 extern "C" uint64_t print_of(const sp_attend_args* a) { return attend_print(a); }
 extern "C" int by_stretches_of(int64_t blocks, int64_t many, int d, int H_kv) { return by_stretches(blocks, many, d, H_kv); }
-extern "C" int share(int64_t rows, int members) { return shares(rows, members); }
+extern "C" int share(int rows, int members) { return shares(rows, members); }
 // segments (prefixes first): rows, n (0: a prefix), len, shared.  blocks out, in the order that they are laid out in: segment, i,
 // first key, keys, pieces, rows of a block, cost of a step, steps; pieces out: block, first key, end, stretch.  Returns the number of blocks.
-extern "C" int cut_up(int n_seg, const int64_t* rows, const int* n, const int* len, const int* shared, int G, int H_kv, int d, int fp8, int* blocks,
+extern "C" int cut_up(int n_seg, const int* rows, const int* n, const int* len, const int* shared, int G, int H_kv, int d, int fp8, int* blocks,
                       int* pieces, int* n_pieces, int* n_stretches) {
   int nb = 0;
   int64_t keys_all = 0, cost_all = 0, many = 0;
@@ -40,8 +40,8 @@ extern "C" int cut_up(int n_seg, const int64_t* rows, const int* n, const int* l
     int* b = blocks + 9 * nb++;
     b[0] = s; b[1] = i; b[2] = n[s] ? shared[s] : 0;
     b[3] = n[s] ? own_block_keys(rows[s], i, block_rows(rows[s], d), G, n[s], len[s], shared[s]) : shared[s];
-    b[4] = 0; b[5] = block_rows(rows[s], d); b[6] = step_cost((int)std::min<int64_t>(b[5], rows[s] - (int64_t)i * b[5]), d, fp8); b[7] = block_steps(b[2], b[3]);
-    const int nr = (int)std::min<int64_t>(b[5], rows[s] - (int64_t)i * b[5]);
+    b[4] = 0; b[5] = block_rows(rows[s], d); b[6] = step_cost(std::min(b[5], rows[s] - i * b[5]), d, fp8); b[7] = block_steps(b[2], b[3]);
+    const int nr = std::min(b[5], rows[s] - i * b[5]);
     b[8] = piece_cost(nr, b[3], d);
     many += nr > kFewRows;
     start.push_back(cost_all);
@@ -92,7 +92,7 @@ def shim(tmp_path_factory):
                     "-I", os.path.join(ROOT, "paper_2502_02789_amd", "csrc"), "shim.cpp", "-o", "shim.so"], cwd=where, check=True)
     lib = C.CDLL(str(where / "shim.so"))
     lib.print_of.restype = C.c_uint64
-    lib.share.argtypes = [C.c_int64, C.c_int]
+    lib.share.argtypes = [C.c_int, C.c_int]
     lib.by_stretches_of.argtypes = [C.c_int64, C.c_int64, C.c_int, C.c_int]
     return lib
 
@@ -130,7 +130,7 @@ def _batches():
 
 def _cut(shim, segs, G, H_kv, d=128, fp8=0):
     arr = lambda i, t: np.array([s[i] for s in segs], dtype=t)  # noqa: E731
-    arrays = [arr(0, np.int64), arr(1, np.int32), arr(2, np.int32), arr(3, np.int32)]
+    arrays = [arr(0, np.int32), arr(1, np.int32), arr(2, np.int32), arr(3, np.int32)]
     blocks, pieces = np.zeros(9 * 80000, np.int32), np.zeros(4 * 80000, np.int32)
     n_pieces, n_stretches = C.c_int(), C.c_int()
     ptr = lambda x: x.ctypes.data_as(C.c_void_p)  # noqa: E731

@@ -63,46 +63,35 @@ __device__ __forceinline__ void widen_e4m3(const u32x4 w, u32x4& lo, u32x4& hi) 
 }
 
 // Where the rows of a piece's keys lie.  Tiles start at multiples of 8 keys and pages hold multiples of 8, so the 8 keys of an
-// octet lie at one stride from one base, formed in scalar registers, once for all lanes of a wave.  The page numbers come in
-// vector registers, 64 at a time and 64 ahead, a lane each (scalar loads would share a counter with the LDS reads, each of
-// whose waits would then wait for them too: 202 -> 196 us for 64 new tokens behind 128K keys of 32 over 8 heads).
+// octet lie at one stride from one base, formed in scalar registers, once for all lanes of a wave.  The page numbers of a tile's
+// keys come in a vector register, a lane each, requested a tile ahead and before that tile's loads, so that nothing waits for them
+// that does not wait for older loads anyway.  (Scalar loads share a counter with the LDS reads, whose waits then wait for both:
+// 202 -> 196 us for 64 new tokens behind 128K keys.  64 pages at a time, on demand: PAGES64.)
 template <bool PAGED>
 struct KeyRows {
   const int32_t* table;
-  int lg_page, first, last_key, lane, chunk;
-  uint32_t last, pages, next;
+  int lg_page, first, last_key, lane;
+  uint32_t last, pages;
   int32_t ts;
   int64_t ps;
-  // key: the first that will be asked for
-  __device__ __forceinline__ KeyRows(const AttendDev& p, const AttendUnit& u, int l, int key) {
+  // tile: the first that will be asked for
+  __device__ __forceinline__ KeyRows(const AttendDev& p, const AttendUnit& u, int l, int tile) {
     ts = p.c_ts; ps = p.c_ps; lg_page = p.lg_page; last_key = u.k1 - 1; lane = l;
     first = PAGED ? 0 : u.seq;
     last = PAGED ? p.last_page : p.last_row;
     table = PAGED ? p.table + (int64_t)u.seq * p.blocks_per_seq : nullptr;
-    if (PAGED && u.k0 < u.k1) {
-      chunk = min(key, last_key) >> lg_page >> 6;
-      pages = load(chunk);
-      next = load(chunk + 1);
-    }
+    if (u.k0 < u.k1) ahead(tile);
   }
-  __device__ __forceinline__ uint32_t load(int c) const { return (uint32_t)table[min(c * 64 + lane, last_key >> lg_page)]; }
-  // before the octets of a tile (its keys' pages lie in one run of 64) that begins at `key`, fewer than 64 pages on from the one before
-  __device__ __forceinline__ void advance(int key) {
-    if constexpr (PAGED) {
-      const int c = min(key, last_key) >> lg_page >> 6;
-      if (c != chunk) {
-        chunk = c;
-        pages = next;
-        next = load(c + 1);
-      }
-    }
+  // asks for the pages of the tile that begins at `tile`
+  __device__ __forceinline__ void ahead(int tile) {
+    if constexpr (PAGED) pages = (uint32_t)table[min(tile + lane, last_key) >> lg_page];
   }
-  // first key of the octet that `key` (wave-uniform) lies in, no further than the last key's
-  __device__ __forceinline__ int octet(int key) const { return min(key, last_key) & ~7; }
-  // byte offset of the octet's first key.  Nothing outside the pool is addressed, a bad page is noted.
-  __device__ __forceinline__ int64_t base(int octet, uint32_t& bad) const {
+  // first key of the octet that row r (wave-uniform) of a tile lies in, no further than the last key's
+  __device__ __forceinline__ int octet(int tile, int r) const { return min(tile + r, last_key) & ~7; }
+  // byte offset of that key.  Nothing outside the pool is addressed, a bad page is noted.
+  __device__ __forceinline__ int64_t base(int octet, int r, uint32_t& bad) const {
     if constexpr (PAGED) {
-      const uint32_t entry = (uint32_t)__builtin_amdgcn_readlane((int)pages, (octet >> lg_page) & 63);
+      const uint32_t entry = (uint32_t)__builtin_amdgcn_readlane((int)pages, r & ~7);
       bad |= entry > last;
       return (int64_t)min(entry, last) * ps + (int64_t)(octet & ((1 << lg_page) - 1)) * ts;
     } else {
@@ -215,22 +204,22 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   int64_t oct_at[Tile::N];
   uint32_t in[Tile::N];
   auto place = [&](int tile) {
-    rows.advance(tile);
+    int64_t bases[4];
+    int octs[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      octs[j] = rows.octet(tile, 8 * j);
+      bases[j] = rows.base(octs[j], 8 * j, bad);
+    }
 #pragma unroll
     for (int i = 0; i < Tile::N; ++i) {
       constexpr int R = Tile::R;
-      const int oct = rows.octet(tile + R * i);
-      if constexpr (R <= 8) {
-        oct_at[i] = rows.base(oct, bad);
-        in[i] = rows.within(oct, tile + R * i + lane_row) + lane_chunk;
-      } else {                        // a load covers two octets
-        const int oct1 = rows.octet(tile + R * i + 8);
-        const int64_t b0 = rows.base(oct, bad), b1 = rows.base(oct1, bad);
-        const bool second = lane_row >= 8;
-        oct_at[i] = second ? b1 : b0;
-        in[i] = rows.within(second ? oct1 : oct, tile + R * i + lane_row) + lane_chunk;
-      }
+      const int j = R * i / 8;
+      const bool second = R > 8 && lane_row >= 8;  // (a load may cover two octets)
+      oct_at[i] = second ? bases[(j + 1) & 3] : bases[j];
+      in[i] = rows.within(second ? octs[(j + 1) & 3] : octs[j], tile + R * i + lane_row) + lane_chunk;
     }
+    rows.ahead(tile + 32 * W);
   };
   if (tile < u.k1) {
     place(tile);
@@ -477,19 +466,19 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
   auto load = [&](int tile, Tile& kt, Tile& vl) {
     int64_t at[Tile::N];
     uint32_t in[Tile::N];
-    rows.advance(tile);
 #pragma unroll
     for (int i = 0; i < Tile::N; ++i) {
-      const int first = tile + R * w + Tile::STEP * i;
-      int oct = rows.octet(first);
-      at[i] = rows.base(oct, bad);
+      const int r = R * w + Tile::STEP * i;
+      int oct = rows.octet(tile, r);
+      at[i] = rows.base(oct, r, bad);
       if constexpr (R > 8) {
-        const int oct1 = rows.octet(first + 8);
-        const int64_t at1 = rows.base(oct1, bad);
+        const int oct1 = rows.octet(tile, r + 8);
+        const int64_t at1 = rows.base(oct1, r + 8, bad);
         if (lane_row >= 8) { at[i] = at1; oct = oct1; }
       }
-      in[i] = rows.within(oct, first + lane_row) + lane_chunk;
+      in[i] = rows.within(oct, tile + r + lane_row) + lane_chunk;
     }
+    rows.ahead(tile + STRIDE);
     kt.load(kb, at, in);
     vl.load(vb, at, in);
   };

@@ -342,7 +342,7 @@ SP_API sp_status sp_gather(const sp_gather_args* args, void* hip_stream);
  * stated at each call.  New tokens of sequence b are rows [d_cu_new[b], d_cu_new[b+1]) of a flat axis with
  * room for T_new tokens (d_cu_new[0] = 0, non-decreasing, d_cu_new[B] <= T_new; rows at and beyond d_cu_new[B] are
  * neither read nor written).  Limits: d 64 or 128, H <= 1024, H % H_kv == 0,
- * H / H_kv <= 16, T_new * H < 2^31.
+ * H / H_kv <= 16, T_new * H < 2^31, T_new of an append <= 2^25.  With T_new = 0 the pointers to new tokens may be NULL.
  * Pointers to bf16 or 8-bit data are 16-byte aligned; strides count elements and are multiples of 8
  * (of an 8-bit cache: 16).
  * --------------------------------------------------------------------------- */
@@ -355,7 +355,7 @@ SP_API sp_status sp_gather(const sp_gather_args* args, void* hip_stream);
  * bf16 (nearest even), or divided by the scale in fp32 and rounded to E4M3 (nearest even; beyond +-448 the largest finite
  * value; NaN stays NaN; a scale of zero stores zeros).  A bf16 cache filled so holds bit for bit what
  * sp_score with rope_theta > 0 makes of an unrotated one.
- * A token whose cache index lies outside its sequence's room (blocks_per_seq * page_size tokens, or its rows of a
+ * A token whose cache index is negative or outside its sequence's room (blocks_per_seq * page_size tokens, or its rows of a
  * contiguous cache) or whose page number lies outside the pool is not written to the cache; its row of q_out is.
  * No two tokens of a call may have the same place in the cache. */
 typedef struct {
@@ -421,6 +421,9 @@ SP_API sp_status sp_cache_append(const sp_cache_append_args* args, void* hip_str
  * sp_attend calls at once if each has a workspace of its own.
  * Answered with NaN in out and lse: sequences whose kv_len is negative or beyond their room (all rows), and rows whose
  * part of the work met a page number outside the pool.
+ * Limits: n_rows and blocks_per_seq * page_size <= 2^31 - 2^16, cache_token_stride < 2^26, and lists of work that one launch has
+ * threads for (about T_new * H < 2^31 for prompts, B * H_kv < 2^23 for single tokens): SP_EINVAL beyond.
+ * Rows of a contiguous cache are those that d_cu_cache names at the time of the plan.  d_out overlaps no input.
  * Both calls may be captured into graphs: nothing depends on lengths on the host. */
 typedef struct {
   int32_t B;                 /* sequences, >= 1                                                       */
@@ -437,7 +440,7 @@ typedef struct {
   const int32_t* d_block_table; /* paged cache: int32 [B, blocks_per_seq], else NULL                  */
   int32_t page_size;         /* (ignored if not paged)                                                */
   int32_t blocks_per_seq;    /* (ignored if not paged)                                                */
-  int64_t n_rows;            /* token rows of the cache, < 2^31                                       */
+  int64_t n_rows;            /* token rows of the cache                                               */
   int32_t cache_dtype;       /* sp_k_dtype                                                            */
   const void* d_q;           /* bf16 [T_new, H, d] (rotated), any token and head strides              */
   int64_t q_token_stride;

@@ -14,6 +14,8 @@ namespace {
 
 constexpr int kTokens = 4;  // most tokens of a workgroup (8192 tokens into 8 bits: 4 41.7 us, 8 42.5, 16 49.4; 100K of d = 64: 213, 220, 231)
 
+constexpr int64_t kMostTokens = INT64_C(1) << 25;  // of a call: a launch has fewer than 2^32 threads
+
 struct AppendDev {
   int B, H, H_kv, T_new, tokens, lg_page, blocks_per_seq;
   int64_t q_ts, q_hs, k_ts, k_hs, v_ts, v_hs;
@@ -80,15 +82,16 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendDev p) {
     const int t = first + threadIdx.x;
     const int b = upper_segment(cu, p.B, t);
     const int64_t i = (int64_t)(t - cu[b]) + (p.cache_len ? p.cache_len[b] : 0);
+    const bool ours = t >= cu[b];  // (not in front of the first sequence)
     int64_t at = -1;
     if (p.table) {
-      if (i >= 0 && i < p.room) {
+      if (ours && i >= 0 && i < p.room) {
         const uint32_t page = (uint32_t)p.table[(int64_t)b * p.blocks_per_seq + (i >> p.lg_page)];
         if (page < p.n_pages) at = (int64_t)page * p.c_ps + (i & (((int64_t)1 << p.lg_page) - 1)) * p.c_ts;
       }
     } else {
       const int64_t lo = p.cu_cache[b], row = lo + i;
-      if (i >= 0 && lo >= 0 && row < p.cu_cache[b + 1] && row < (int64_t)p.n_rows) at = row * p.c_ts;
+      if (ours && i >= 0 && lo >= 0 && row < p.cu_cache[b + 1] && row < (int64_t)p.n_rows) at = row * p.c_ts;
     }
     place[threadIdx.x] = at < 0 ? -1 : at * (FP8 ? 1 : 2);
     if constexpr (ROPE) position[threadIdx.x] = p.pos ? p.pos[t] : (int)i;
@@ -143,13 +146,13 @@ sp_status check_append(const sp_cache_append_args* a) {
   const bool queries = a->d_q != nullptr;
   if (a->B < 1 || a->H_kv < 1 || a->H_kv > 1024 || (a->d != 64 && a->d != 128) || a->T_new < 0) return SP_EINVAL;
   if (queries && (a->H < 1 || a->H > 1024 || a->H % a->H_kv != 0 || a->H / a->H_kv > 16)) return SP_EINVAL;
-  if (a->T_new >= INT64_C(0x80000000) / (queries ? a->H : a->H_kv)) return SP_EINVAL;
+  if (a->T_new >= INT64_C(0x80000000) / (queries ? a->H : a->H_kv) || a->T_new > kMostTokens) return SP_EINVAL;
   if (a->n_rows < 1 || a->n_rows >= INT64_C(0x80000000)) return SP_EINVAL;
   if (a->cache_dtype != SP_K_BF16 && a->cache_dtype != SP_K_FP8_E4M3) return SP_EINVAL;
   if (a->cache_dtype == SP_K_BF16 && (a->d_k_scale || a->d_v_scale)) return SP_EINVAL;
   if (!finite_f32(a->rope_theta) || a->rope_theta < 0.f || (a->rope_theta > 0.f && a->d_inv_freq)) return SP_EINVAL;
   if (a->d_pos && a->rope_theta == 0.f && !a->d_inv_freq) return SP_EINVAL;
-  if (!a->d_k || !a->d_v || !a->d_cu_new || !a->d_k_cache || !a->d_v_cache) return SP_ENULL;
+  if ((a->T_new > 0 && (!a->d_k || !a->d_v)) || !a->d_cu_new || !a->d_k_cache || !a->d_v_cache) return SP_ENULL;
   if (queries != (a->d_q_out != nullptr)) return SP_ENULL;
   if (!a->d_block_table && !a->d_cu_cache) return SP_ENULL;
   if (a->d_block_table && a->d_cu_cache) return SP_EINVAL;

@@ -26,6 +26,7 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 constexpr uint32_t kNanF32 = 0x7fc00000u;
 constexpr int kNanBf16 = 0x7fc0;
+constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kSlack = 8.f;   // logits (log2) may exceed the running maximum by this much
 constexpr int kTileKeys = 64;   // many rows
 constexpr int kAhead = 6;       // operands that are read before the first product that takes one
@@ -708,11 +709,11 @@ namespace {
 sp_status check_attend(const sp_attend_args* a) {
   const sp_status st = check_attend_plan_args(a);
   if (st != SP_OK) return st;
-  if (!finite_f32(a->scale) || a->scale <= 0.f) return SP_EINVAL;
+  if (!finite_f32(a->scale * kLog2e) || a->scale <= 0.f) return SP_EINVAL;
   const bool fp8 = a->cache_dtype == SP_K_FP8_E4M3;
   if (!fp8 && (a->d_k_scale || a->d_v_scale)) return SP_EINVAL;
   if (a->cache_token_stride >= INT64_C(1) << 26) return SP_EINVAL;
-  if (!a->d_q || !a->d_k_cache || !a->d_v_cache || !a->d_out) return SP_ENULL;
+  if ((a->T_new > 0 && (!a->d_q || !a->d_out)) || !a->d_k_cache || !a->d_v_cache) return SP_ENULL;
   const int64_t row[] = {a->q_token_stride, a->q_head_stride, a->out_token_stride, a->out_head_stride};
   const int64_t cache[] = {a->cache_token_stride, a->cache_head_stride, a->d_block_table ? a->cache_page_stride : 0};
   for (int64_t s : row) if (s < 0) return SP_EINVAL;
@@ -757,7 +758,7 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.last_page = paged ? (uint32_t)(a->n_rows / a->page_size - 1) : 0;
   p.last_row = (uint32_t)(a->n_rows - 1);
   p.most_items = (uint32_t)(caps.rows * a->H_kv);  // (no more than T_new * H)
-  p.scale_log2 = a->scale * 1.44269504088896340736f;
+  p.scale_log2 = a->scale * kLog2e;
   p.q_ts = a->q_token_stride; p.q_hs = a->q_head_stride;
   p.o_ts = a->out_token_stride; p.o_hs = a->out_head_stride;
   p.c_ts = (int32_t)(a->cache_token_stride * E); p.c_hs = a->cache_head_stride * E; p.c_ps = a->cache_page_stride * E;

@@ -33,6 +33,7 @@ constexpr int kFewRows = 16;      // rows of a block of a small segment
 constexpr int kSlotRows = 16;     // rows of a workspace slot
 constexpr int kShareRows = 128;   // see shares()
 constexpr int kPieceStep = 64;    // pieces are cut at multiples of so many keys
+constexpr int64_t kMostKeys = 0x7fff0000;  // of a cache, and of a sequence's room in one: indices some tiles further are 32-bit numbers still
 constexpr int kMinSteps = 2;      // no piece is made shorter than so many steps
 constexpr int kMostStretchBlocks = 3 * 768;  // blocks that stretches are made for, at most
 

@@ -175,7 +175,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       seg_start[s] = (int)count[0];
       count[0] += blocks_of(s);
     }
-    if (tid == 0) seg_start[n_seg] = (int)all[0];
+    if (tid == 0) seg_start[n_seg] = (int)min(all[0], (int64_t)0x7fffffff);
     __syncthreads();
   }
   const int n_blocks = seg_start[n_groups + B], n_prefix = seg_start[n_groups];
@@ -518,11 +518,11 @@ sp_status check_attend_shape(const sp_attend_args* a) {
   if (a->d != 64 && a->d != 128) return SP_EINVAL;
   if (a->T_new < 0 || a->n_groups < 0 || a->n_groups > a->B) return SP_EINVAL;
   if (a->T_new >= INT64_C(0x80000000) / a->H) return SP_EINVAL;
-  if (a->n_rows < 1 || a->n_rows >= INT64_C(0x80000000)) return SP_EINVAL;
+  if (a->n_rows < 1 || a->n_rows > kMostKeys) return SP_EINVAL;
   if (a->cache_dtype != SP_K_BF16 && a->cache_dtype != SP_K_FP8_E4M3) return SP_EINVAL;
   if (a->d_block_table) {
     if (a->page_size < 8 || (a->page_size & (a->page_size - 1)) != 0 || a->blocks_per_seq < 1) return SP_EINVAL;
-    if ((int64_t)a->blocks_per_seq * a->page_size >= INT64_C(0x80000000) || a->n_rows % a->page_size != 0) return SP_EINVAL;
+    if ((int64_t)a->blocks_per_seq * a->page_size > kMostKeys || a->n_rows % a->page_size != 0) return SP_EINVAL;
   }
   return SP_OK;
 }
@@ -537,7 +537,8 @@ sp_status check_attend_plan_args(const sp_attend_args* a) {
   if (a->n_groups == 0 && (a->d_cu_group || a->d_prefix_len)) return SP_EINVAL;
   if (a->n_groups > 0 && !a->d_block_table) return SP_EUNSUPPORTED;
   const AttendCaps c = attend_caps(a);
-  if (c.slots * kSlotRows >= INT64_C(0x7fffffff) || c.rows >= INT64_C(0x7fffffff) || c.units * a->H_kv >= INT64_C(0x7fffffff)) return SP_EINVAL;
+  if (c.slots * kSlotRows >= INT64_C(0x7fffffff) || c.rows >= INT64_C(0x7fffffff) || c.units * a->H_kv * 64 * attend_waves(a->d) >= INT64_C(0x100000000))
+    return SP_EINVAL;  // (the last: threads of a launch)
   if (!a->d_plan) return SP_ENULL;
   if (reinterpret_cast<uintptr_t>(a->d_plan) & 255u) return SP_EALIGN;
   if (a->plan_bytes < attend_plan_layout(a).bytes) return SP_EWORKSPACE;

@@ -270,7 +270,8 @@ class AttendPlan(_OnDevice):
             _check_ints(cu_group, int(cu_group.numel()), "cu_group")
             _check_ints(prefix_len, int(cu_group.numel()) - 1, "prefix_len")
         self.cu_new, self.kv_len, self.block_table, self.cu_cache = cu_new, kv_len, block_table, cu_cache
-        self.cu_group, self.prefix_len, self.H, self.total_new, self.shape = cu_group, prefix_len, int(H), int(total_new), k_cache.shape
+        self.cu_group, self.prefix_len, self.H, self.total_new = cu_group, prefix_len, int(H), int(total_new)
+        self.shape, self.bytes = k_cache.shape, k_cache.element_size()
         kw = dict(H=H, total_new=total_new, block_table=block_table, cu_cache=cu_cache, cu_group=cu_group, prefix_len=prefix_len)
         probe = sp.make_attend_plan_args(cu_new, kv_len, k_cache, **kw)
         need = sp.sp_attend_plan_bytes(probe)
@@ -294,7 +295,7 @@ class Attender(_OnDevice):
         self._device = _on_one_device(plan.plan, q, k_cache, v_cache, k_scale, v_scale, out, workspace)
         d = int(k_cache.shape[-1])
         _check_cache(k_cache, v_cache, plan.block_table, plan.cu_cache, int(plan.cu_new.numel()) - 1, (k_scale, v_scale))
-        _need(k_cache.shape == plan.shape, "the cache must have the shape that the plan was made for")
+        _need(k_cache.shape == plan.shape and k_cache.element_size() == plan.bytes, "the cache must have the shape and type that the plan was made for")
         _check_rows(q, plan.total_new, plan.H, d, "q")
         if out is None:
             out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)

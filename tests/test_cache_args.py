@@ -52,6 +52,7 @@ APPEND_BAD = [
     (sp.SP_EALIGN, dict(k_token_stride=772)), (sp.SP_EALIGN, dict(v_head_stride=4)), (sp.SP_EALIGN, dict(q_head_stride=4)),
     (sp.SP_EALIGN, dict(cache_token_stride=132)), (sp.SP_EALIGN, dict(cache_token_stride=136, **FP8)), (sp.SP_EALIGN, dict(cache_page_stride=2056, **FP8)),
     (sp.SP_EALIGN, dict(d_k=P + 2)), (sp.SP_EALIGN, dict(d_q=P + 8)), (sp.SP_EALIGN, dict(d_q_out=P + 8)), (sp.SP_EALIGN, dict(d_v_cache=P + 8)),
+    (sp.SP_EINVAL, dict(d_q=None, d_q_out=None, T_new=(1 << 25) + 1)),
 ]
 PLAN_BAD = [
     (sp.SP_EINVAL, dict(B=0)), (sp.SP_EINVAL, dict(d=32)), (sp.SP_EINVAL, dict(H=9)), (sp.SP_EINVAL, dict(H=34)), (sp.SP_EINVAL, dict(H=2048, H_kv=256)),
@@ -62,6 +63,8 @@ PLAN_BAD = [
     (sp.SP_ENULL, dict(n_groups=1, d_prefix_len=P)), (sp.SP_EINVAL, dict(d_cu_group=P)), (sp.SP_EINVAL, dict(d_prefix_len=P)),
     (sp.SP_EUNSUPPORTED, dict(n_groups=1, d_cu_group=P, d_prefix_len=P, d_block_table=None, d_cu_cache=P)), (sp.SP_ENULL, dict(d_plan=None)),
     (sp.SP_EALIGN, dict(d_plan=P + 16)), (sp.SP_EWORKSPACE, dict(plan_bytes=64)),
+    (sp.SP_EINVAL, dict(n_rows=0x7fff0010)), (sp.SP_EINVAL, dict(blocks_per_seq=0x7fff001)),
+    (sp.SP_EINVAL, dict(B=1 << 22, T_new=1 << 22, H=8, H_kv=8)), (sp.SP_EINVAL, dict(T_new=(1 << 31) // 64 - 1, H=64, H_kv=4, d=128)),  # threads of a launch
 ]
 ATTEND_BAD = PLAN_BAD + [
     (sp.SP_EINVAL, dict(scale=0.0)), (sp.SP_EINVAL, dict(scale=-1.0)), (sp.SP_EINVAL, dict(scale=float("nan"))), (sp.SP_EINVAL, dict(scale=float("inf"))),
@@ -70,7 +73,7 @@ ATTEND_BAD = PLAN_BAD + [
     (sp.SP_EALIGN, dict(q_token_stride=516)), (sp.SP_EALIGN, dict(out_head_stride=68)), (sp.SP_EALIGN, dict(cache_token_stride=132)),
     (sp.SP_EALIGN, dict(cache_token_stride=136, **FP8)), (sp.SP_EALIGN, dict(d_q=P + 8)), (sp.SP_EALIGN, dict(d_out=P + 8)),
     (sp.SP_EALIGN, dict(d_k_cache=P + 4)), (sp.SP_EWORKSPACE, dict(workspace_bytes=1024)), (sp.SP_EWORKSPACE, dict(d_workspace=None)),
-    (sp.SP_EALIGN, dict(d_workspace=P + 16)),
+    (sp.SP_EALIGN, dict(d_workspace=P + 16)), (sp.SP_EINVAL, dict(scale=3e38)), (sp.SP_EINVAL, dict(cache_token_stride=1 << 26)),
 ]
 
 
@@ -95,6 +98,9 @@ def test_null_structs_no_tokens_and_sizes():
     assert lib.sp_attend_plan_bytes(None) == lib.sp_attend_workspace_bytes(None) == 0
     assert lib.sp_cache_append(C.byref(_append(T_new=0)), None) == sp.SP_OK      # nothing to do, nothing launched
     assert lib.sp_attend(C.byref(_attend(T_new=0)), None) == sp.SP_OK
+    nothing = dict(T_new=0, d_q=None)                                            # (tensors without elements have no address)
+    assert lib.sp_cache_append(C.byref(_append(d_k=None, d_v=None, d_q_out=None, **nothing)), None) == sp.SP_OK
+    assert lib.sp_attend(C.byref(_attend(d_out=None, **nothing)), None) == sp.SP_OK
     for bad in (dict(B=0), dict(d=65), dict(H=9), dict(n_rows=0), dict(page_size=9)):
         assert sp.sp_attend_plan_bytes(_attend(**bad)) == sp.sp_attend_workspace_bytes(_attend(**bad)) == 0
     few, many = _attend(T_new=1, B=1), _attend(T_new=4000, B=64, n_groups=4)

@@ -124,6 +124,38 @@ def test_shared_prefixes(heads, layout):
         _run(_case(rng, new, length, *heads, groups=groups, **layout))
 
 
+@pytest.mark.parametrize("groups", [False, True])
+@pytest.mark.parametrize("bits", [16, 8])
+def test_more_sequences_than_the_plan_keeps_in_lds(groups, bits):
+    rng = np.random.default_rng(20)
+    length = rng.integers(9, 40, 700).tolist()
+    new = [int(min(n, m - 8)) for n, m in zip(rng.integers(0, 4, 700), length)]
+    share = [(7 * i, 7 * i + 7, int(rng.integers(0, 9))) for i in range(100)] if groups else ()
+    _run(_case(rng, new, length, 4, 2, 64, page=8, bits=bits, groups=share))
+
+
+@pytest.mark.parametrize("groups", [False, True])
+def test_more_blocks_than_are_laid_end_to_end(groups):
+    """One block to a workgroup: more blocks in all than the stretches' table has room for, more large ones than three rounds of
+    workgroups; of both kinds, some longer than a workgroup's share."""
+    rng = np.random.default_rng(21)
+    length = rng.integers(9, 24, 2500).tolist()
+    length[1200] = 900
+    _run(_case(rng, [1] * 2500, length, 1, 1, 64, page=8, groups=[(5 * i, 5 * i + 5, i % 9) for i in range(500)] if groups else ()))
+    new = rng.integers(17, 21, 160).tolist()
+    length = [n + int(x) for n, x in zip(new, rng.integers(8, 50, 160))]
+    new[77], length[77] = 3, 2000
+    _run(_case(rng, new, length, 16, 16, 64, page=8, groups=[(8 * i, 8 * i + 8, 3 + i % 6) for i in range(20)] if groups else ()))
+    new, length = new[:100], length[:100]
+    _run(_case(rng, new, length, 8, 8, 128, page=8, bits=8, groups=[(10 * i, 10 * i + 10, 3 + i % 6) for i in range(10)] if groups else ()))
+
+
+def test_more_kv_heads_than_workgroups_at_once():
+    rng = np.random.default_rng(22)
+    _run(_case(rng, [1, 20, 2], [300, 70, 9], 300, 300, 128, page=16))
+    _run(_case(rng, [1, 20], [100, 70], 1000, 1000, 64, page=0))
+
+
 def test_prefixes_that_not_every_query_sees():
     """Members whose own queries lie inside the stated prefix, shorter members, an empty one, a first member without queries."""
     rng = np.random.default_rng(4)

@@ -132,6 +132,19 @@ def test_negative_cached_lengths_write_nothing_in_front():
     _run(rng, [6, 6], [-3, -6], 4, 2, 64, cache=cache, theta=0.0)
 
 
+def test_tokens_in_front_of_the_first_sequence_write_nothing():
+    import torch
+    from paper_2502_02789_amd import device as dev
+    k = torch.randn((8, 2, 64), device="cuda").to(torch.bfloat16)
+    for where in (dict(cu_cache=cc.cuda_ints([0, 30])), dict(block_table=cc.cuda_ints([[0, 1]]))):
+        kc = torch.full((30, 2, 64) if "cu_cache" in where else (2, 16, 2, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+        vc = kc.clone()
+        dev.CacheAppender(k, k, cc.cuda_ints([5, 8]), kc, vc, cache_len=cc.cuda_ints([10]), **where).run()
+        torch.cuda.synchronize()
+        got = kc.view(-1, 2, 64)
+        assert (got[10:13] == k[5:]).all() and (got[:10] == 3).all() and (got[13:] == 3).all()
+
+
 def test_fills_what_scoring_an_unrotated_cache_makes_of_it():
     """A cache filled by the append gives, scored as it is, the scores of the unrotated cache with rope_theta: the same two-pass
     kernels (batches of unstated length) run in both cases, so bit for bit."""

@@ -179,7 +179,7 @@ def test_device_classes_refuse_what_does_not_fit_together():
         return dev.CacheAppender(k, v, cu, kc, vc, **dict(good, **kw))
     append(q=q, cache_len=cc.cuda_ints([1]), rope_theta=1e4)
     for bad in (dict(k=k.float()), dict(v=k[:2]), dict(k=k[..., ::2]), dict(cu=cu.long()), dict(cache_len=cc.cuda_ints([1, 2])), dict(vc=kc[:2]),
-                dict(block_table=table[:, ::2]), dict(block_table=None), dict(cu_cache=cu), dict(k_scale=one), dict(q=q[:, :, :32]), dict(q_out=q),
+                dict(block_table=table.long()), dict(block_table=None), dict(cu_cache=cu), dict(k_scale=one), dict(q=q[:, :, :32]), dict(q_out=q),
                 dict(q=q, q_out=q.transpose(0, 1).contiguous().transpose(0, 1)), dict(pos=cc.cuda_ints([1, 2]), rope_theta=1e4),
                 dict(inv_freq=torch.ones(32, device="cuda")), dict(kc=kc.float(), vc=kc.float()), dict(kc=kc.view(-1, 2, 64), vc=kc.view(-1, 2, 64))):
         with pytest.raises(ValueError):

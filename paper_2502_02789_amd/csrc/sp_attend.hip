@@ -1,16 +1,24 @@
 // sp_attend: attention of new tokens over a (paged, bf16 or E4M3) cache, the keys of a shared prefix read once for a group.
 //
-// One launch takes every piece of the plan (sp_attend_plan.h), a workgroup of four waves a stretch of pieces for one KV head.  Two forms:
-//   few rows (<= 16: single tokens, their heads)   bound by reading keys and values.  Each wave walks over 32-key tiles of its own
-//     with a 16x16 tile of logits, keys straight from memory into matrix operands, values through LDS for the transpose; nothing
-//     is shared before the end, and every wave has the next tile in flight.
-//   many rows (<= 128: prompts, prefixes of groups)  bound by the matrix cores.  The four waves share 64-key tiles in LDS (two
-//     buffers, one barrier a tile), each has 32 rows.
+// One launch takes every piece of the plan (sp_attend_plan.h), a workgroup of eight waves (d = 128: one on a compute unit; four
+// and three of them, d = 64) a stretch of pieces for one KV head.  Two forms:
+//   few rows (<= 32: single tokens or several, their heads)   bound by reading keys and values.  Each wave walks over 32-key tiles of
+//     its own through LDS, with one or two 16x16 tiles of logits twice; nothing is shared before the end, and every wave has its next
+//     tile of keys and of values in flight.  64 sequences of 4096 bf16 keys, H_kv 8, d 128: 175-178 us, 6.1 TB/s; in 8 bits 98.7, 5.4
+//     (the vector instructions that widen them); d = 64, bf16 110.  Two tiles of rows instead of a large block, whose matrix tiles they
+//     would fill to a tenth: 32 sequences of 1K-3K keys, 5 to 8 tokens of 4 heads, 66.4 -> 57 us; eight in 8 bits 39.0 -> 28.6.
+//   many rows (<= 256, d = 64 128: prompts, prefixes of groups)  bound by the matrix cores and the vector work between their products.
+//     The waves share 64-key tiles in LDS (two buffers, one barrier a tile; a second tile on its way in registers), each has 32 rows.
+//     6592 tokens, H 64, d 128, causal: 680-693 us, 1.03-1.05 PFLOP/s; eight prompts of 300-3000 tokens, H 32, d 64: 118-128 us, 0.6.
+//     (Blocks of at most 128 rows with the waves' halves on alternate tiles and their sums added at the end: slower, four sequences
+//     of 8K-20K keys and 28 tokens 73 -> 77 us, and 64 single tokens 111 -> 114 us by the mere size of the kernel.)
 // Both compute S^T = K Q^T, so that a lane has the logits of one row, turn the weights exp2(s - m) into bf16 in place -- the order
 // of keys in a matrix product's sum is free, and is chosen so that a lane's logits are its own operand of O^T = V^T P^T -- and read
-// V^T out of row-major LDS tiles with the transposing LDS read.  The running maximum m follows the logits only
-// where one exceeds it by more than 8 (weights stay below 2^8, sums in fp32), so sums are rarely rescaled.
+// V^T out of row-major LDS tiles with the transposing LDS read.  A weight's rounding to bf16, 2^-8 of itself, is what the matrix cores'
+// operands allow; logits, maxima, sums and O are fp32.  The running maximum m follows the logits only
+// where one exceeds it by more than 8 (weights stay below 2^8), so sums are rarely rescaled.
 // Compiled on the assumption that there are no NaNs; those that mark invalid rows are written as bit patterns.
+// (Nothing here may need scratch memory: workgroups that do are dispatched later, 64 single tokens 111 -> 117 us with 20 bytes of it.)
 #include "sp_attend_internal.h"
 #include "sp_lds.h"
 
@@ -67,7 +75,8 @@ __device__ __forceinline__ void widen_e4m3(const u32x4 w, u32x4& lo, u32x4& hi) 
 // octet lie at one stride from one base, formed in scalar registers, once for all lanes of a wave.  The page numbers of a tile's
 // keys come in a vector register, a lane each, requested a tile ahead and before that tile's loads, so that nothing waits for them
 // that does not wait for older loads anyway.  (Scalar loads share a counter with the LDS reads, whose waits then wait for both:
-// 202 -> 196 us for 64 new tokens behind 128K keys.  64 pages at a time, on demand: PAGES64.)
+// 202 -> 196 us for 64 new tokens behind 128K keys.  64 pages at a time, asked for when needed, instead of a tile's: 98.7 -> 102.6 us
+// for 64 sequences of 4096 8-bit keys.)
 template <bool PAGED>
 struct KeyRows {
   const int32_t* table;
@@ -180,9 +189,9 @@ struct FewTile {
   }
 };
 
-// W waves (a power of two of those of the workgroup, side by side) take the piece; the others take others at the same time, and
-// all meet at one barrier.
-template <int D, bool FP8, bool PAGED>
+// NR tiles of 16 rows.  W waves (a power of two of those of the workgroup, side by side) take the piece; the others take others at the
+// same time, and all meet at one barrier.
+template <int D, bool FP8, bool PAGED, int NR>
 __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit& u, int g, int W, char* lds) {
   constexpr int KS = D / 32;          // steps of the product with the queries
   constexpr int DB = D / 16;          // blocks of values
@@ -190,8 +199,13 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   using Tile = FewTile<D, FP8>;
   constexpr int NW = attend_waves(D);
   const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), turn = w & (W - 1), l = tid & 63, row = l & 15, quad = l >> 4;
-  const bool mine = row < u.nr;
-  const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
+  bool mine[NR];
+  RowPlace at[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    mine[n] = row + 16 * n < u.nr;
+    at[n] = row_place(p, u.r0 + (mine[n] ? row + 16 * n : 0), g);
+  }
 
   int tile = u.k0 < u.k1 ? (u.k0 & ~31) + 32 * turn : u.k1;
   KeyRows<PAGED> rows(p, u, l, tile);
@@ -231,27 +245,39 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   // the queries
   uint32_t flip, keep;
   const float c = key_factor(p, g, flip, keep);
-  bf16x8 qf[KS];
+  bf16x8 qf[NR][KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    u32x4 x = {0, 0, 0, 0};
-    if (mine) x = *reinterpret_cast<const u32x4*>(p.q + at.token * p.q_ts + at.h * p.q_hs + s * 32 + quad * 8);
+  for (int n = 0; n < NR; ++n)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (x[i] ^ flip) & keep;
-    qf[s] = __builtin_bit_cast(bf16x8, x);
-  }
-  int limit = u.k1, least = u.k1;
+    for (int s = 0; s < KS; ++s) {
+      u32x4 x = {0, 0, 0, 0};
+      if (mine[n]) x = *reinterpret_cast<const u32x4*>(p.q + at[n].token * p.q_ts + at[n].h * p.q_hs + s * 32 + quad * 8);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = (x[i] ^ flip) & keep;
+      qf[n][s] = __builtin_bit_cast(bf16x8, x);
+    }
+  int limit[NR], least = u.k1;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) limit[n] = u.k1;
   if (u.off != kNoLimit) {
-    if (mine) limit = min(u.k1, at.token + u.off);
-    least = limit;
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      if (mine[n]) limit[n] = min(u.k1, at[n].token + u.off);
+      least = min(least, limit[n]);
+    }
 #pragma unroll
     for (int off = 8; off >= 1; off >>= 1) least = min(least, __shfl_xor(least, off, kWave));
     least = __builtin_amdgcn_readfirstlane(least);
   }
-  f32x4 o[DB];
+  f32x4 o[NR][DB];
+  float m[NR], sum[NR];
 #pragma unroll
-  for (int i = 0; i < DB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, sum = 0.f;
+  for (int n = 0; n < NR; ++n) {
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m[n] = -INFINITY;
+    sum[n] = 0.f;
+  }
 
   for (; tile < u.k1; tile += 32 * W) {
     const bool more = tile + 32 * W < u.k1;
@@ -261,42 +287,52 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
       kt.load(kb, oct_at, in);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
+    f32x4 s[NR][2];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const char* at0 = kd + row * (D * 2) + swizzled<C>(row, 4 * s + quad) * 16;  // (rows 16 apart are permuted alike)
-      s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(at0), qf[s], s0, 0, 0, 0);
-      s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(at0 + 16 * D * 2), qf[s], s1, 0, 0, 0);
+    for (int n = 0; n < NR; ++n) s[n][0] = s[n][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      const char* at0 = kd + row * (D * 2) + swizzled<C>(row, 4 * i + quad) * 16;  // (rows 16 apart are permuted alike)
+      const bf16x8 k0 = *reinterpret_cast<const bf16x8*>(at0), k1 = *reinterpret_cast<const bf16x8*>(at0 + 16 * D * 2);
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        s[n][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[n][i], s[n][0], 0, 0, 0);
+        s[n][1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[n][i], s[n][1], 0, 0, 0);
+      }
     }
     vl.store(vd, l);
     if (more) vl.load(vb, oct_at, in);
 
-    float x[8];
+    bf16x8 pf[NR];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { x[i] = s0[i] * c; x[4 + i] = s1[i] * c; }
-    if (tile + 32 > least || tile < u.k0) {
+    for (int n = 0; n < NR; ++n) {
+      float x[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int key = tile + 16 * (i >> 2) + 4 * quad + (i & 3);
-        if (key >= limit || key < u.k0) x[i] = -INFINITY;
+      for (int i = 0; i < 4; ++i) { x[i] = s[n][0][i] * c; x[4 + i] = s[n][1][i] * c; }
+      if (tile + 32 > least || tile < u.k0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int key = tile + 16 * (i >> 2) + 4 * quad + (i & 3);
+          if (key >= limit[n] || key < u.k0) x[i] = -INFINITY;
+        }
       }
-    }
-    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-    if (__builtin_amdgcn_ballot_w64(top > m + kSlack)) {
-      top = fmaxf(top, __shfl_xor(top, 16, kWave));
-      top = fmaxf(top, __shfl_xor(top, 32, kWave));
-      const float next = fmaxf(m, top);
-      const float f = next == -INFINITY ? 1.f : fast_exp2(m - next);
-      m = next;
-      sum *= f;
+      float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+      if (__builtin_amdgcn_ballot_w64(top > m[n] + kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float next = fmaxf(m[n], top);
+        const float f = next == -INFINITY ? 1.f : fast_exp2(m[n] - next);
+        m[n] = next;
+        sum[n] *= f;
 #pragma unroll
-      for (int i = 0; i < DB; ++i) o[i] *= f;
-    }
-    const float base_m = m == -INFINITY ? 0.f : m;
+        for (int i = 0; i < DB; ++i) o[n][i] *= f;
+      }
+      const float base_m = m[n] == -INFINITY ? 0.f : m[n];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { x[i] = fast_exp2(x[i] - base_m); sum += x[i]; }
-    const u32x4 pw = {pack_bf16_pair(x[0], x[1]), pack_bf16_pair(x[2], x[3]), pack_bf16_pair(x[4], x[5]), pack_bf16_pair(x[6], x[7])};
-    const bf16x8 pf = __builtin_bit_cast(bf16x8, pw);
+      for (int i = 0; i < 8; ++i) { x[i] = fast_exp2(x[i] - base_m); sum[n] += x[i]; }
+      const u32x4 pw = {pack_bf16_pair(x[0], x[1]), pack_bf16_pair(x[2], x[3]), pack_bf16_pair(x[4], x[5]), pack_bf16_pair(x[6], x[7])};
+      pf[n] = __builtin_bit_cast(bf16x8, pw);
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const int vr = 4 * quad + ((l & 15) >> 2);  // row of the tile that this lane reads from (and 16 + that)
 #pragma unroll
@@ -304,25 +340,30 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
       const int ch = 2 * i + ((l & 3) >> 1);
       const char* at0 = vd + vr * (D * 2) + swizzled<C>(vr, ch) * 16 + (l & 1) * 8;
       const bf16x8 vf = join8(lds_read_tr(at0), lds_read_tr(at0 + 16 * D * 2));
-      o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o[i], 0, 0, 0);
+#pragma unroll
+      for (int n = 0; n < NR; ++n) o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n], o[n][i], 0, 0, 0);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
-  // the waves' sums joined, in the waves' order
-  sum += __shfl_xor(sum, 16, kWave);
-  sum += __shfl_xor(sum, 32, kWave);
-  // every wave's sums in what was its own tile, then one barrier
-  float* const tops = reinterpret_cast<float*>(lds + NW * (2 * 32 * D * 2));  // [wave][16], sums of weights, bad pages
-  float* const sums = tops + NW * 16;
-  uint32_t* const bads = reinterpret_cast<uint32_t*>(sums + NW * 16);
-  constexpr int ROW = D + 4;  // floats from one row to the next: rows begin in different banks
+  // every wave's sums in what was its own tile, 16-byte chunks of a row permuted (rows begin in one bank), then one barrier
+  constexpr int ROWS = 16 * NR;
+  float* const tops = reinterpret_cast<float*>(lds + NW * (2 * 32 * D * 2));  // [wave][ROWS], sums of weights, bad pages
+  float* const sums = tops + NW * ROWS;
+  uint32_t* const bads = reinterpret_cast<uint32_t*>(sums + NW * ROWS);
   float* const parts = reinterpret_cast<float*>(lds);
+  auto chunk_at = [](int r, int ch) { return r * D + 4 * (ch ^ (r & (D / 4 - 1))); };
 #pragma unroll
-  for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(parts + w * (32 * D) + row * ROW + 16 * i + 4 * quad) = o[i];
-  if (quad == 0) {
-    tops[w * 16 + row] = m;
-    sums[w * 16 + row] = sum;
+  for (int n = 0; n < NR; ++n) {
+    sum[n] += __shfl_xor(sum[n], 16, kWave);
+    sum[n] += __shfl_xor(sum[n], 32, kWave);
+    const int r = row + 16 * n;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(parts + w * (32 * D) + chunk_at(r, 4 * i + quad)) = o[n][i];
+    if (quad == 0) {
+      tops[w * ROWS + r] = m[n];
+      sums[w * ROWS + r] = sum[n];
+    }
   }
   if (l == 0) bads[w] = bad;
   __syncthreads();
@@ -330,10 +371,10 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   constexpr int V = D / 16;
   const int w0 = w - turn, lane = tid & 15;
   for (int r = (turn * 64 + l) >> 4; r < u.nr; r += 4 * W) {
-    float acc[V], l_all = 0.f, top = tops[w0 * 16 + r];
+    float acc[V], l_all = 0.f, top = tops[w0 * ROWS + r];
     uint32_t any_bad = bads[w0];
     for (int x = w0 + 1; x < w0 + W; ++x) {
-      top = fmaxf(top, tops[x * 16 + r]);
+      top = fmaxf(top, tops[x * ROWS + r]);
       any_bad |= bads[x];
     }
     const float base = top == -INFINITY ? 0.f : top;
@@ -341,11 +382,14 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
     for (int i = 0; i < V; ++i) acc[i] = 0.f;
 #pragma unroll 2
     for (int x = w0; x < w0 + W; ++x) {
-      const float f = fast_exp2(tops[x * 16 + r] - base);
-      l_all += sums[x * 16 + r] * f;
-      const float* part = parts + x * (32 * D) + r * ROW + lane * V;
+      const float f = fast_exp2(tops[x * ROWS + r] - base);
+      l_all += sums[x * ROWS + r] * f;
 #pragma unroll
-      for (int i = 0; i < V; ++i) acc[i] += part[i] * f;
+      for (int i = 0; i < V; i += 4) {
+        const f32x4 part = *reinterpret_cast<const f32x4*>(parts + x * (32 * D) + chunk_at(r, lane * (V / 4) + i / 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i + e] += part[e] * f;
+      }
     }
     if (u.slot >= 0) {
       const int64_t place = slot_row(p, u.slot, r, g);
@@ -394,22 +438,17 @@ struct ManyTile {
   }
 };
 
-// SPLIT: the block has no more rows than half of the waves take: the two halves of the workgroup have the same rows and take tiles in turn, each
-// with two buffers of its own, and add their sums up at the end.
-template <int D, bool FP8, bool PAGED, bool SPLIT>
+template <int D, bool FP8, bool PAGED>
 __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit& u, int g, char* lds) {
-  constexpr int NW = attend_waves(D), TW = SPLIT ? NW / 2 : NW;  // waves, waves that share a tile
-  constexpr int SETS = NW == 8 && !SPLIT ? 2 : 1;                // tiles on their way from memory
-  constexpr int STRIDE = SPLIT ? 2 * kTileKeys : kTileKeys;      // keys from one tile of a wave to the next
+  constexpr int NW = attend_waves(D);
+  constexpr int SETS = NW == 8 ? 2 : 1;  // tiles on their way from memory
   constexpr int KS = D / 16;   // steps of the product with the queries
   constexpr int DB = D / 32;   // blocks of values
   constexpr int C = D / 8;
   constexpr int TILE = kTileKeys * D * 2;  // bytes of a tile of keys or of values
-  using Tile = ManyTile<D, FP8, 64 * TW>;
-  const int all_tid = thread_of_piece(), share = SPLIT ? __builtin_amdgcn_readfirstlane(all_tid / (64 * TW)) : 0, tid = all_tid - share * 64 * TW;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, half = l >> 5;
+  using Tile = ManyTile<D, FP8, 64 * NW>;
+  const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, half = l >> 5;
   const int row = w * 32 + (l & 31);
-  char* const tiles = lds + share * 4 * TILE;
   const bool mine = row < u.nr;
   const RowPlace at = row_place(p, u.r0 + (mine ? row : 0), g);
   uint32_t flip, keep;
@@ -435,8 +474,8 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
   least = __builtin_amdgcn_readfirstlane(least);
   most = __builtin_amdgcn_readfirstlane(most);
 
-  const int first_tile = u.k0 < u.k1 ? u.k0 & ~(kTileKeys - 1) : u.k1, my_first = first_tile + share * kTileKeys;
-  KeyRows<PAGED> rows(p, u, l, my_first);
+  const int first_tile = u.k0 < u.k1 ? u.k0 & ~(kTileKeys - 1) : u.k1;
+  KeyRows<PAGED> rows(p, u, l, first_tile);
   const char* const kb = p.k + (int64_t)g * p.c_hs;
   const char* const vb = p.v + (int64_t)g * p.c_hs;
   const int lane_row = l / Tile::C, lane_chunk = (l % Tile::C) * 16;
@@ -479,25 +518,23 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       }
       in[i] = rows.within(oct, tile + r + lane_row) + lane_chunk;
     }
-    rows.ahead(tile + STRIDE);
+    rows.ahead(tile + kTileKeys);
     kt.load(kb, at, in);
     vl.load(vb, at, in);
   };
-  if (my_first < u.k1) load(my_first, kt[0], vl[0]);
-  if (SETS == 2 && my_first + STRIDE < u.k1) load(my_first + STRIDE, kt[SETS - 1], vl[SETS - 1]);
+  if (first_tile < u.k1) load(first_tile, kt[0], vl[0]);
+  if (SETS == 2 && first_tile + kTileKeys < u.k1) load(first_tile + kTileKeys, kt[SETS - 1], vl[SETS - 1]);
   // One tile out of buffer BUF (a constant, so that the operands' addresses are too).  The compiler is told how to mix reads, products and
   // the rest: operands are read several products ahead, and the weights of the next 16 keys are formed while the
   // matrix cores work on these.
   auto step = [&](auto buf, int tile) {
     constexpr int SET = decltype(buf)::value % SETS;
-    char* const kd = tiles + decltype(buf)::value * 2 * TILE;
+    char* const kd = lds + decltype(buf)::value * 2 * TILE;
     char* const vd = kd + TILE;
-    if (!SPLIT || tile < u.k1) {
-      kt[SET].store(kd, tid);
-      vl[SET].store(vd, tid);
-    }
+    kt[SET].store(kd, tid);
+    vl[SET].store(vd, tid);
     __syncthreads();
-    if (tile + SETS * STRIDE < u.k1) load(tile + SETS * STRIDE, kt[SET], vl[SET]);
+    if (tile + SETS * kTileKeys < u.k1) load(tile + SETS * kTileKeys, kt[SET], vl[SET]);
     if (tile >= most) return;  // (the wave's rows see none of these keys)
     __builtin_amdgcn_s_setprio(1);  // products first: the other wave's other instructions fill the gaps
     f32x16 s[2];
@@ -577,64 +614,43 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       }
     __builtin_amdgcn_s_setprio(0);
   };
-  for (int tile = first_tile; tile < u.k1; tile += 2 * STRIDE) {  // (both halves go through as many barriers)
-    step(std::integral_constant<int, 0>(), tile + share * kTileKeys);
-    if (tile + STRIDE < u.k1) step(std::integral_constant<int, 1>(), tile + STRIDE + share * kTileKeys);
+  for (int tile = first_tile; tile < u.k1; tile += 2 * kTileKeys) {
+    step(std::integral_constant<int, 0>(), tile);
+    if (tile + kTileKeys < u.k1) step(std::integral_constant<int, 1>(), tile + kTileKeys);
   }
 
-  const int any_bad = __syncthreads_or(bad != 0);
+  // the waves' bad pages (`bad` is the same in all lanes), behind the tiles
+  uint32_t* const bads = reinterpret_cast<uint32_t*>(lds + 4 * TILE);
+  if (l == 0) bads[w] = bad;
+  __syncthreads();
+  uint32_t any_bad = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) any_bad |= bads[i];
   sum += __shfl_xor(sum, 32, kWave);
-  if constexpr (SPLIT) {
-    // the second half's sums through LDS: blocks of 4 values of a row side by side for 32 rows, so that a wave writes and reads whole runs
-    float* const part = reinterpret_cast<float*>(lds) + w * (32 * D);
-    float* const stat = reinterpret_cast<float*>(lds + TW * 32 * D * 4) + w * 64;
-    if (share == 1) {
-#pragma unroll
-      for (int i = 0; i < DB; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          *reinterpret_cast<f32x4*>(part + ((i * 4 + j) * 64 + l) * 4) = f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
-      if (half == 0) {
-        stat[l] = m;
-        stat[32 + l] = sum;
-      }
-    }
-    __syncthreads();
-    if (share == 1) return;
-    const float other = stat[l & 31], top = fmaxf(m, other), base = top == -INFINITY ? 0.f : top;
-    const float f = fast_exp2(m - base), h = fast_exp2(other - base);
-    sum = sum * f + stat[32 + (l & 31)] * h;
-    m = top;
-#pragma unroll
-    for (int i = 0; i < DB; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(part + ((i * 4 + j) * 64 + l) * 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[i][4 * j + e] = o[i][4 * j + e] * f + x[e] * h;
-      }
-  }
-  if (!mine) return;
+  // (formed again: nothing of it is kept in registers over the loop)
+  const int end_tid = thread_of_piece(), end_row = (end_tid >> 6) * 32 + (end_tid & 31), end_half = (end_tid >> 5) & 1;
+  if (end_row >= u.nr) return;
   if (u.slot >= 0) {
-    const int64_t place = slot_row(p, u.slot, row, g);
-    float* dst = p.sums + place * D + 4 * half;
+    const int64_t place = slot_row(p, u.slot, end_row, g);
+    float* dst = p.sums + place * D + 4 * end_half;
 #pragma unroll
     for (int i = 0; i < DB; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         *reinterpret_cast<f32x4*>(dst + 32 * i + 8 * j) = f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
-    if (half == 0) store_stats(p, place, m, sum, any_bad);
+    if (end_half == 0) store_stats(p, place, m, sum, any_bad);
     return;
   }
   const float mul = (sum == 0.f ? 0.f : 1.f / sum) * (p.v_scale ? p.v_scale[g] : 1.f);
-  uint16_t* dst = p.out + at.token * p.o_ts + at.h * p.o_hs + 4 * half;
+  const RowPlace to = row_place(p, u.r0 + end_row, g);
+  uint16_t* dst = p.out + to.token * p.o_ts + to.h * p.o_hs + 4 * end_half;
 #pragma unroll
   for (int i = 0; i < DB; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       store_values(dst + 32 * i + 8 * j, f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]} * mul, any_bad);
     }
-  if (half == 0 && p.lse) store_lse(p, at.token, at.h, m, sum, any_bad);
+  if (end_half == 0 && p.lse) store_lse(p, to.token, to.h, m, sum, any_bad);
 }
 
 // every row of the call, or of one piece and KV head, becomes NaN
@@ -654,7 +670,7 @@ __device__ __forceinline__ void nan_rows(const AttendDev& p, int d, int64_t r0, 
 template <int D, bool FP8, bool PAGED>
 __global__ __launch_bounds__(64 * attend_waves(D), D == 64 ? 3 : 2) void attend_kernel(const AttendDev p) {
   constexpr int T = 64 * attend_waves(D);
-  __shared__ __align__(16) char lds[attend_waves(D) * (64 * D * 2 + 2 * 16 * 4 + 4)];  // tiles: 16 KB a wave (8, d = 64), and few rows' statistics
+  __shared__ __align__(16) char lds[attend_waves(D) * (64 * D * 2 + 2 * kFewRows * 4 + 4)];  // tiles: 16 KB a wave (8, d = 64), and few rows' statistics
   // The KV heads of a piece are neighbours: with eight of them, each has the L2 of one XCD, which the rows of a
   // block share, as workgroups go to the XCDs in turn.
   const int n = (int)(blockIdx.x / (uint32_t)p.H_kv), g = (int)(blockIdx.x % (uint32_t)p.H_kv);
@@ -690,12 +706,12 @@ __global__ __launch_bounds__(64 * attend_waves(D), D == 64 ? 3 : 2) void attend_
       AttendUnit v = u;
       if (mine > 0 && mine < run) v = read(unit_at(x + mine));
       if (mine >= run) v.nr = v.k0 = v.k1 = 0;
-      attend_few<D, FP8, PAGED>(p, v, g, W, lds);
+      if (u.nr <= kTileRows) attend_few<D, FP8, PAGED, 1>(p, v, g, W, lds);
+      else attend_few<D, FP8, PAGED, 2>(p, v, g, W, lds);
       x += run;
     } else {
-      if (u.run == kBadUnit) nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, threadIdx.x, T);
-      else if (attend_waves(D) == 8 && u.nr <= many_rows(D) / 2) attend_many<D, FP8, PAGED, attend_waves(D) == 8>(p, u, g, lds);
-      else attend_many<D, FP8, PAGED, false>(p, u, g, lds);
+      if (u.run == kBadUnit) nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, thread_of_piece(), T);
+      else attend_many<D, FP8, PAGED>(p, u, g, lds);
       ++x;
     }
     if (x >= end) return;

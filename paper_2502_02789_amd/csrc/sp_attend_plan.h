@@ -3,14 +3,15 @@
 //
 // The rows of a call are (token, head of a KV head's group) pairs, row = token * G + head, flat over all tokens: the rows of a
 // sequence, and of a group of sequences, lie side by side.  A segment is a set of rows that attend to the same keys: the shared
-// prefix of a group (all rows of its members), or what a sequence has for itself.  A segment is cut into blocks of 16 rows
-// (if it has no more: one small matrix tile, bound by reading the keys) or of many_rows() (bound by the matrix cores).
+// prefix of a group (all rows of its members), or what a sequence has for itself.  A segment is cut into blocks: one of 16 or 32 rows
+// if it has no more (one or two small matrix tiles, bound by reading the keys), else of many_rows() (bound by the matrix cores).
 //
-// The device has room for attend_items() workgroups at once.  With fewer than three times as many (large block, KV head) pairs, blocks are laid end to end,
-// each at its cost, and cut into as many stretches of equal cost as there is room for: every workgroup has one, and all end together.
-// (One block to a workgroup instead, in whole rounds, pieces cut to 1/1024 of the keys -> stretches: MEASURED_STRETCHES.)
-// With more blocks than that a workgroup takes one block, and takes the next as it gets done, longest first; only a block longer than a
-// workgroup's equal share is cut.
+// The device has room for attend_items() workgroups at once.  With fewer than three times as many (large block, KV head) pairs, blocks
+// are laid end to end, each at its cost, and cut into as many stretches of equal cost as there is room for: every workgroup has one, and
+// all end together.  With more than that a workgroup takes one block, and the device the next as one gets done, longest first; only a
+// block longer than a workgroup's equal share is cut.  Both measured (stretches, blocks): 64 sequences of 1K-4K keys 114, 127 us; 64
+// that share 32K 75, 79; two pieces of 500 tokens behind 17K 335, 466; but, with more blocks than the rule allows, 6592 tokens of 64
+// heads 833, 679; eight prompts of 300-3000 tokens, d = 64, 150, 123.
 //
 // A block of one piece whose rows have no shared prefix is finished by its workgroup; the pieces of all others leave their
 // sums in slots of the workspace, which a second kernel joins.
@@ -29,7 +30,8 @@
 
 namespace sp {
 
-constexpr int kFewRows = 16;      // rows of a block of a small segment
+constexpr int kTileRows = 16;     // rows of the smallest matrix tile
+constexpr int kFewRows = 32;      // most rows of a block of a small segment: one such tile, or two
 constexpr int kSlotRows = 16;     // rows of a workspace slot
 constexpr int kShareRows = 128;   // see shares()
 constexpr int kPieceStep = 64;    // pieces are cut at multiples of so many keys
@@ -101,26 +103,25 @@ inline AttendCaps attend_caps(const sp_attend_args* a) {
   // rows to join: of blocks that are cut (of which there are at most as many as pieces added) and of sequences that share
   const int64_t cut_rows = many * added + (a->n_groups ? shared_rows : 0);
   c.rows = rows < cut_rows ? rows : cut_rows;
-  // blocks that may leave sums, in large blocks and in all; own segments of over 16 rows: at most one per 17
-  const int64_t big_segments = own_segments < rows / (kFewRows + 1) ? own_segments : rows / (kFewRows + 1);
-  const int64_t shared_big = a->n_groups ? 2 * (shared_rows / many) + big_segments + (groups < rows / (kFewRows + 1) ? groups : rows / (kFewRows + 1)) : 0;
-  const int64_t shared_few = a->n_groups ? own_segments + groups : 0;
-  const bool any_big = rows > kFewRows;
+  // blocks that may leave sums, in large blocks and in all; segments of over 16 (32) rows: at most one per 17 (33)
+  const int64_t per_big = rows / (kFewRows + 1), per_two = rows / (kTileRows + 1);
+  const int64_t shared_big = a->n_groups ? 2 * (shared_rows / many) + (own_segments < per_big ? own_segments : per_big) + (groups < per_big ? groups : per_big) : 0;
+  const int64_t shared_few = a->n_groups ? own_segments + groups + (own_segments < per_two ? own_segments : per_two) + (groups < per_two ? groups : per_two) : 0;
   // pieces of blocks that are cut: at most two for each piece added
-  c.slots = (any_big ? (many / kSlotRows) : 1) * (2 * added) + (many / kSlotRows) * shared_big + shared_few;
+  c.slots = (rows > kFewRows ? many / kSlotRows : rows > kTileRows ? 2 : 1) * (2 * added) + (many / kSlotRows) * shared_big + shared_few;
   return c;
 }
 
 // What a member's shared prefix saves: a block's rows are filled up by several members, and its keys read once for them all.  With 128 rows of its own
-// for each member there is little to gain.
+// for each member there is little to gain.  (From 16 rows on not shared: 24 sequences of 1 to 8 tokens of four heads, 8K shared, 50 -> 86 us.)
 SP_ATTEND_FN bool shares(int rows, int members) { return members >= 2 && rows / kShareRows < members; }
 
 // (Rows of a segment are fewer than 2^31: T_new * H is.  Divisions of 64-bit numbers take 150 instructions each; the plan, one workgroup that
 // goes through its code once, is bound by fetching it.)
-SP_ATTEND_FN int block_rows(int rows, int d) { return rows <= kFewRows ? kFewRows : many_rows(d); }
+SP_ATTEND_FN int block_rows(int rows, int d) { return rows <= kTileRows ? kTileRows : rows <= kFewRows ? kFewRows : many_rows(d); }
 SP_ATTEND_FN int segment_blocks(int rows, int d) {
   const uint32_t m = (uint32_t)block_rows(rows, d);
-  const int shift = m == 16 ? 4 : m == 128 ? 7 : 8;
+  const int shift = m == 16 ? 4 : m == 32 ? 5 : m == 128 ? 7 : 8;
   return (int)(((uint32_t)rows + m - 1) >> shift);
 }
 
@@ -140,17 +141,21 @@ SP_ATTEND_FN int own_block_keys(int rows, int i, int m, int G, int n, int len, i
 // Steps of 64 keys of a block's keys [first, first + keys), cut at multiples of 64 keys of the sequence
 SP_ATTEND_FN int block_steps(int first, int keys) { return (int)(((uint32_t)(first & (kPieceStep - 1)) + (uint32_t)keys + kPieceStep - 1) / kPieceStep); }
 
-// A piece of few rows and few keys is not worth all waves: where several follow one another, they share the waves
+// A piece of few rows and few keys is not worth all waves: where several follow one another, they share the waves.  (64 sequences of
+// 200-1000 keys 37.7 -> 35.0 us; up to 4096 keys instead of 1024: the same, but 64 that share 32K 74.7 -> 75.8.)
 SP_ATTEND_FN bool is_short(int rows, int keys) { return rows <= kFewRows && keys <= 1024; }
 
-// What a step costs a workgroup, in units of 0.27 us (d = 128) and 0.67 us on a full device: 16 rows are bound by reading 64 keys and
-// values, more by the matrix cores (eight waves with up to 128 rows work on two steps at a time); and what a piece costs besides.
+// What a step costs a workgroup, in units of 0.27 us (d = 128) and 0.67 us on a full device: few rows are bound by reading 64 keys
+// and values, more by the matrix cores; and what a piece costs besides.  (Few and many rows alike: 24 sequences of 1 to 8 new tokens
+// that share 8K 49.5 -> 51.6 us, two pieces of 500 tokens behind 17K 335 -> 342.)
 SP_ATTEND_FN int step_cost(int rows, int d, bool fp8) {
-  if (rows <= kFewRows) return d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5);
-  return d == 64 ? 4 : rows <= many_rows(d) / 2 ? 6 : 8;
+  if (rows <= kTileRows) return d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5);
+  if (rows <= kFewRows) return d == 64 ? 4 : fp8 ? 4 : 6;
+  return d == 64 ? 4 : 8;
 }
 SP_ATTEND_FN int piece_cost(int rows, int keys, int d) { return d == 64 ? (is_short(rows, keys) ? 2 : 4) : is_short(rows, keys) ? 3 : 12; }
-// No stretch costs less: more than a step of any kind
+// No stretch costs less: more than a step of any kind.  (Three times as much: one token behind 1000 keys 11.7 -> 12.2 us, 64 that
+// share 32K 74.7 -> 76.3.)
 SP_ATTEND_FN int least_stretch(int d) { return d == 64 ? 10 : 11; }
 
 // many: blocks of more than 16 rows (the others are cheap to cut)
@@ -170,7 +175,7 @@ inline int64_t most_stretches(const sp_attend_args* a) {
   const int64_t large = rows > kFewRows ? c.blocks : 0;
   if (!by_stretches(c.blocks, large, a->d, a->H_kv)) return c.units;
   const int64_t room = a->d_block_table ? (int64_t)a->blocks_per_seq * a->page_size : a->n_rows;
-  const int64_t steps = room / kPieceStep + 2, step = a->d == 64 ? 4 : large ? 8 : 5, extra = 12;
+  const int64_t steps = room / kPieceStep + 2, step = a->d == 64 ? 4 : large ? 8 : 6, extra = 12;
   return stretch_count(c.blocks * (steps * step + extra), a->d, a->H_kv);
 }
 // Where stretch s of n begins, blocks laid end to end (exact: products are below 2^53, and quotients far enough from whole numbers)

@@ -1,6 +1,7 @@
 // sp_attend_plan: the list of pieces of work of an attention call, made on the device from the lengths (which only the
 // device knows, so that a captured graph follows them), and the kernel that joins the pieces' sums.  The cut itself is in sp_attend_plan.h.
-// The plan is bound by its chain of dependent reads and barriers (one workgroup); a step makes it once for all layers.
+// The plan is bound by its chain of dependent reads and barriers and by fetching its own code (one workgroup): 28 us for one sequence,
+// 50 for 64 in groups; a step makes it once for all layers.
 #include "sp_attend_internal.h"
 
 namespace sp {
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   __shared__ int64_t cuts[kMostStretches + 1];        // (block, step) that each stretch begins at
   __shared__ int32_t first_unit[kMostStretches + 1];
   __shared__ int32_t slot_of[kMostStretchBlocks];
-  __shared__ uint8_t alone[kMostStretchBlocks + kMostStretches];  // pieces that are short
+  __shared__ uint8_t alone[kMostStretchBlocks + kMostStretches];  // pieces that are short: how many tiles of rows they have
   PlanSeq* const seqs = p.a.B <= kLdsSeqs ? lds_seqs : p.seqs;
   int32_t* const seg_start = p.a.B <= kLdsSeqs ? lds_seg : p.seg_start;  // (no more groups than sequences)
   const int tid = threadIdx.x, B = p.a.B, n_groups = p.a.n_groups, G = p.G, T = (int)p.a.T_new;
@@ -338,10 +339,11 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     };
     for (int u = tid; u < (int)n[kUnits]; u += 1024) {
       const AttendUnit x = piece(u, last_at_most(first_unit, n_cuts, u));
-      alone[u] = x.run != kBadUnit && is_short(x.nr, x.k1 - x.k0);
+      alone[u] = x.run == kBadUnit || !is_short(x.nr, x.k1 - x.k0) ? 0 : x.nr <= kTileRows ? 1 : 2;
     }
     __syncthreads();
-    // short pieces that are taken side by side: as many as follow one another in a stretch, up to the waves of a workgroup
+    // short pieces that are taken side by side: as many of one or of two tiles of rows as follow one another in a stretch, up to the
+    // waves of a workgroup
     const int waves = attend_waves(p.a.d);
     for (int u = tid; u < (int)n[kUnits]; u += 1024) {
       const int s = last_at_most(first_unit, n_cuts, u);
@@ -350,7 +352,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       x.end = first_unit[s + 1];
       x.unit = piece(u, s);
       int run = 0;
-      while (run < waves && u + run < x.end && alone[u + run]) ++run;
+      while (run < waves && u + run < x.end && alone[u + run] && alone[u + run] == alone[u]) ++run;
       if (run > 1) x.unit.run = run;
       p.units[u] = x.unit;
       if (u == x.first) p.stretches[s] = x;
@@ -414,7 +416,8 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
 // Rows of several pieces: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^(m_p - max m), added in an order that the plan alone
 // fixes.  Bound by its dependent reads (record, maxima, sums) where rows are few and by reading the sums where they are many: d / 4 lanes
 // take a row's pieces one after the other, 16 bytes a lane; with more than 16 pieces to a row all of the workgroup's
-// lanes take one row, every eighth (sixteenth, d = 64) piece each group of lanes.  (Compiled with NaNs honoured: invalid rows
+// lanes take one row, every eighth (sixteenth, d = 64) piece each group of lanes (from 5 pieces on: 24 sequences that share 8K 50 -> 53 us;
+// from 65 on: the listed kinds of calls the same).  256 rows of 8 KV heads in 22 pieces each: 9 us; one token's 32 rows 3.7.  (Compiled with NaNs honoured: invalid rows
 // have a NaN for l.)
 template <int D>
 __global__ __launch_bounds__(256, 4) void attend_join_kernel(const AttendDev p) {

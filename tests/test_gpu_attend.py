@@ -150,6 +150,18 @@ def test_more_blocks_than_are_laid_end_to_end(groups):
     _run(_case(rng, new, length, 8, 8, 128, page=8, bits=8, groups=[(10 * i, 10 * i + 10, 3 + i % 6) for i in range(10)] if groups else ()))
 
 
+@pytest.mark.parametrize("layout", [dict(page=16), dict(page=8, bits=8), dict(page=0)])
+@pytest.mark.parametrize("heads", [(8, 2, 128), (8, 2, 64)])
+def test_short_pieces_of_one_and_of_two_tiles_of_rows_side_by_side(heads, layout):
+    rng = np.random.default_rng(23)
+    new = [1, 5, 6, 8, 8, 4, 1, 1, 7, 5, 0, 5, 9, 8, 2, 6] * 6
+    length = [n + int(x) for n, x in zip(new, rng.integers(0, 300, len(new)))]
+    length[20], length[50] = 4000, 9000
+    _run(_case(rng, new, length, *heads, **layout))
+    if layout["page"]:
+        _run(_case(rng, new, [m + 70 for m in length], *heads, groups=[(0, 16, 70), (16, 90, 33), (90, 96, 64)], **layout))
+
+
 def test_more_kv_heads_than_workgroups_at_once():
     rng = np.random.default_rng(22)
     _run(_case(rng, [1, 20, 2], [300, 70, 9], 300, 300, 128, page=16))

@@ -147,11 +147,12 @@ SP_ATTEND_FN bool is_short(int rows, int keys) { return rows <= kFewRows && keys
 
 // What a step costs a workgroup, in units of 0.27 us (d = 128) and 0.67 us on a full device: few rows are bound by reading 64 keys
 // and values, more by the matrix cores; and what a piece costs besides.  (Few and many rows alike: 24 sequences of 1 to 8 new tokens
-// that share 8K 49.5 -> 51.6 us, two pieces of 500 tokens behind 17K 335 -> 342.)
+// that share 8K 49.5 -> 51.6 us, two pieces of 500 tokens behind 17K 335 -> 342; large blocks alike, however many
+// of their rows are there: 32 sequences that share 32K 8-bit keys 41 -> 45.6.)
 SP_ATTEND_FN int step_cost(int rows, int d, bool fp8) {
   if (rows <= kTileRows) return d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5);
   if (rows <= kFewRows) return d == 64 ? 4 : fp8 ? 4 : 6;
-  return d == 64 ? 4 : 8;
+  return d == 64 ? 4 : rows > many_rows(d) / 2 ? 8 : fp8 ? 5 : 6;
 }
 SP_ATTEND_FN int piece_cost(int rows, int keys, int d) { return d == 64 ? (is_short(rows, keys) ? 2 : 4) : is_short(rows, keys) ? 3 : 12; }
 // No stretch costs less: more than a step of any kind.  (Three times as much: one token behind 1000 keys 11.7 -> 12.2 us, 64 that

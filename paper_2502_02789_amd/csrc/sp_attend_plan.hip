@@ -413,20 +413,35 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   }
 }
 
+struct JoinDev {
+  const AttendHeader* header;
+  const AttendRow* rows;
+  const float* sums;
+  const float2* stats;
+  const float* v_scale;
+  uint16_t* out;
+  float* lse;
+  uint64_t print;
+  int64_t o_ts, o_hs;
+  int H, H_kv, G;
+};
+
 // Rows of several pieces: out = sum_p f_p O_p / sum_p f_p l_p with f_p = 2^(m_p - max m), added in an order that the plan alone
-// fixes.  Bound by its dependent reads (record, maxima, sums) where rows are few and by reading the sums where they are many: d / 4 lanes
-// take a row's pieces one after the other, 16 bytes a lane; with more than 16 pieces to a row all of the workgroup's
-// lanes take one row, every eighth (sixteenth, d = 64) piece each group of lanes (from 5 pieces on: 24 sequences that share 8K 50 -> 53 us;
-// from 65 on: the listed kinds of calls the same).  256 rows of 8 KV heads in 22 pieces each: 9 us; one token's 32 rows 3.7.  (Compiled with NaNs honoured: invalid rows
-// have a NaN for l.)
+// fixes.  Bound by its dependent reads (record; maxima, weights' sums and values together) where rows are few and by reading the sums
+// where they are many: d / 4 lanes take a row's pieces one after the other, four in flight, 16 bytes a lane; with more than 16 pieces to
+// a row, or more than 4 of few rows, all of the workgroup's lanes take one row, every eighth (sixteenth, d = 64) piece each group of lanes
+// (from 5 pieces on for all: one token behind 1000 keys 11.5 -> 10.8 us, but 32 sequences that share 8K 66 -> 70-75).  (Compiled with NaNs honoured: invalid rows have a NaN for l.)
 template <int D>
-__global__ __launch_bounds__(256, 4) void attend_join_kernel(const AttendDev p) {
+__global__ __launch_bounds__(256) void attend_join_kernel(const JoinDev p) {
   constexpr int L = D / 4, GROUPS = 256 / L;
   __shared__ float4 part[GROUPS][L];
   __shared__ float2 stat[GROUPS];
-  const uint64_t print = p.header->print;
-  const uint32_t n_rows = (uint32_t)p.header->n_rows, H_kv = (uint32_t)p.H_kv;
-  const bool together = p.header->most_pieces > 16;
+  asm volatile("" ::"s"(p.rows), "s"(p.sums), "s"(p.stats), "s"(p.v_scale), "s"(p.out), "s"(p.lse), "s"(p.print), "s"(p.o_ts), "s"(p.o_hs),
+               "s"(p.H), "s"(p.H_kv), "s"(p.G));  // (all read at once)
+  const auto header = reinterpret_cast<const __attribute__((address_space(4))) AttendHeader*>(reinterpret_cast<uintptr_t>(p.header));
+  const uint64_t print = header->print;
+  const uint32_t n_rows = (uint32_t)header->n_rows, H_kv = (uint32_t)p.H_kv;
+  const bool together = header->most_pieces > (n_rows * H_kv <= 1024 ? 4 : 16);
   const int group = threadIdx.x / L, c = threadIdx.x % L, step = together ? GROUPS : 1, first = together ? group : 0;
   // (without a plan the pieces' kernel has filled the outputs)
   const uint32_t n_items = print == p.print ? n_rows * H_kv : 0, stride = gridDim.x * (together ? 1 : GROUPS);
@@ -436,45 +451,35 @@ __global__ __launch_bounds__(256, 4) void attend_join_kernel(const AttendDev p) 
     const int g = (int)(item % H_kv);
     AttendRow r = {};
     if (active) r = p.rows[item / H_kv];
-    const int n = r.own_pieces + r.pre_pieces, mine = n > first ? (n - first + step - 1) / step : 0;
-    // index of piece q's row among all rows of the workspace
-    auto place = [&](int q) -> int64_t {
-      const int at = q < r.own_pieces ? r.own_at + q * r.own_step : r.pre_at + (q - r.own_pieces) * r.pre_step;
-      return ((int64_t)(at / kSlotRows) * p.H_kv + g) * kSlotRows + at % kSlotRows;
-    };
+    const float scale = p.v_scale ? p.v_scale[g] : 1.f;
+    const int n = r.own_pieces + r.pre_pieces;
+    // index of piece q's row among all rows of the workspace: pieces are whole slots apart
+    const uint32_t own_step = r.own_step * H_kv, pre_step = r.pre_step * H_kv;
+    const uint32_t own_at = ((uint32_t)r.own_at / kSlotRows * H_kv + g) * kSlotRows + r.own_at % kSlotRows;
+    const uint32_t pre_at = ((uint32_t)r.pre_at / kSlotRows * H_kv + g) * kSlotRows + r.pre_at % kSlotRows - r.own_pieces * pre_step;
     float top = -INFINITY, sum = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int q0 = 0; q0 < mine; q0 += L) {  // a lane holds the factor of one piece
-      const int count = min(L, mine - q0);
+    for (int q = first; q < n; q += 4 * step) {
       float4 x[4];
-      auto read = [&](int q) {  // (beyond the last: its values again, with a factor of zero)
+      float2 s[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          x[i] = *reinterpret_cast<const float4*>(p.sums + place(first + (q0 + min(q + i, count - 1)) * step) * D + c * 4);
-      };
-      float2 s = make_float2(-INFINITY, 0.f);
-      if (q0 + c < mine) s = p.stats[place(first + (q0 + c) * step)];
-      read(0);
-      float next = s.x;
-#pragma unroll
-      for (int off = L / 2; off >= 1; off >>= 1) next = fmaxf(next, __shfl_xor(next, off, L));
-      next = fmaxf(next, top);
-      const float base = next == -INFINITY ? 0.f : next, old = exp2f(top - base), f = exp2f(s.x - base);
-      float add = f * s.y;
-#pragma unroll
-      for (int off = L / 2; off >= 1; off >>= 1) add += __shfl_xor(add, off, L);
+      for (int i = 0; i < 4; ++i) {  // (beyond the last: its values again, with a weight of zero)
+        const int piece = min(q + i * step, n - 1);
+        const size_t place = piece < r.own_pieces ? own_at + piece * own_step : pre_at + piece * pre_step;
+        s[i] = p.stats[place];
+        x[i] = *reinterpret_cast<const float4*>(p.sums + place * D + c * 4);
+        if (q + i * step >= n) s[i] = make_float2(-INFINITY, 0.f);
+      }
+      const float next = fmaxf(fmaxf(fmaxf(s[0].x, s[1].x), fmaxf(s[2].x, s[3].x)), top);
+      const float base = next == -INFINITY ? 0.f : next, old = exp2f(top - base);
       top = next;
-      sum = sum * old + add;
+      sum *= old;
       acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
-      for (int q = 0;;) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float w = __shfl(f, q + i, L);
-          acc.x += w * x[i].x; acc.y += w * x[i].y; acc.z += w * x[i].z; acc.w += w * x[i].w;
-        }
-        q += 4;
-        if (q >= count) break;
-        read(q);
+      for (int i = 0; i < 4; ++i) {
+        const float w = exp2f(s[i].x - base);
+        sum += w * s[i].y;
+        acc.x += w * x[i].x; acc.y += w * x[i].y; acc.z += w * x[i].z; acc.w += w * x[i].w;
       }
     }
     if (together) {  // the groups' sums, in their order
@@ -488,7 +493,7 @@ __global__ __launch_bounds__(256, 4) void attend_join_kernel(const AttendDev p) 
         const float base = top == -INFINITY ? 0.f : top;
         sum = 0.f;
         acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
+#pragma unroll 4
         for (int x = 0; x < GROUPS; ++x) {
           const float f = exp2f(stat[x].x - base);
           sum += f * stat[x].y;
@@ -501,16 +506,17 @@ __global__ __launch_bounds__(256, 4) void attend_join_kernel(const AttendDev p) 
     }
     if (!active) continue;
     const int token = r.row / p.G, h = g * p.G + r.row % p.G;
-    const float mul = (sum == 0.f ? 0.f : 1.f / sum) * (p.v_scale ? p.v_scale[g] : 1.f);
+    const float mul = (sum == 0.f ? 0.f : 1.f / sum) * scale;
     uint16_t* dst = p.out + token * p.o_ts + h * p.o_hs + c * 4;
     *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16_pair(acc.x * mul, acc.y * mul), pack_bf16_pair(acc.z * mul, acc.w * mul));
     if (c == 0 && p.lse) p.lse[(int64_t)token * p.H + h] = sum == 0.f ? -INFINITY : ((top == -INFINITY ? 0.f : top) + log2f(sum)) * 0.69314718055994531f;
   }
 }
 
-void launch_attend_join(const AttendDev& p, int d, hipStream_t stream) {
-  const int grid = (int)(p.most_items < 2048 ? p.most_items : 2048);
+void launch_attend_join(const AttendDev& a, int d, hipStream_t stream) {
+  const int grid = (int)(a.most_items < 2048 ? a.most_items : 2048);
   if (grid < 1) return;
+  const JoinDev p = {a.header, a.rows, a.sums, a.stats, a.v_scale, a.out, a.lse, a.print, a.o_ts, a.o_hs, a.H, a.H_kv, a.G};
   if (d == 128) hipLaunchKernelGGL(attend_join_kernel<128>, dim3(grid), dim3(256), 0, stream, p);
   else hipLaunchKernelGGL(attend_join_kernel<64>, dim3(grid), dim3(256), 0, stream, p);
 }
@@ -540,7 +546,7 @@ sp_status check_attend_plan_args(const sp_attend_args* a) {
   if (a->n_groups == 0 && (a->d_cu_group || a->d_prefix_len)) return SP_EINVAL;
   if (a->n_groups > 0 && !a->d_block_table) return SP_EUNSUPPORTED;
   const AttendCaps c = attend_caps(a);
-  if (c.slots * kSlotRows >= INT64_C(0x7fffffff) || c.rows >= INT64_C(0x7fffffff) || c.units * a->H_kv * 64 * attend_waves(a->d) >= INT64_C(0x100000000))
+  if (c.slots * kSlotRows * a->H_kv >= INT64_C(0x100000000) || c.slots * kSlotRows >= INT64_C(0x7fffffff) || c.rows >= INT64_C(0x7fffffff) || c.units * a->H_kv * 64 * attend_waves(a->d) >= INT64_C(0x100000000))
     return SP_EINVAL;  // (the last: threads of a launch)
   if (!a->d_plan) return SP_ENULL;
   if (reinterpret_cast<uintptr_t>(a->d_plan) & 255u) return SP_EALIGN;

@@ -1,12 +1,15 @@
 // sp_attend_plan: the list of pieces of work of an attention call, made on the device from the lengths (which only the
 // device knows, so that a captured graph follows them), and the kernel that joins the pieces' sums.  The cut itself is in sp_attend_plan.h.
-// The plan is bound by its chain of dependent reads and barriers and by fetching its own code (one workgroup): 28 us for one sequence,
-// 50 for 64 in groups; a step makes it once for all layers.
+// The plan is bound by its chain of dependent reads and barriers and by fetching its own code (one workgroup): 14 us for one sequence,
+// 21 for 64, 38 for 64 that share a prefix; a step makes it once for all layers.
 #include "sp_attend_internal.h"
 
 namespace sp {
 
 namespace {
+
+constexpr int kPlanThreads = 512;  // (1024, whose registers do not do: 28.1 us instead of 14.2 for one sequence, 34.8 instead of 21.1 for 64, 44.9 and
+                                   // 38.1 for 64 that share a prefix; 256: 13.4, 21.1, 49.7)
 
 struct PlanSeq { int32_t t0, n, len, shared; };                 // len -1: invalid
 struct PlanGroup { int32_t shared, active, t0, tokens, slot, pieces, pad[2]; };
@@ -34,10 +37,10 @@ __device__ __forceinline__ int group_of(const PlanDev& p, int b) {
   return upper_segment(p.a.d_cu_group, n, b);
 }
 
-// exclusive prefixes of N numbers over the workgroup's 1024 threads, and their sums over all of them (most waves have nothing to add)
+// exclusive prefixes of N numbers over the workgroup's threads, and their sums over all of them (most waves have nothing to add)
 template <int N>
 __device__ __forceinline__ void block_exclusive(int64_t (&v)[N], int64_t (&total)[N]) {
-  __shared__ int64_t waves[16][N];
+  __shared__ int64_t waves[kPlanThreads / 64][N];
   const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
   bool any = false;
 #pragma unroll
@@ -62,7 +65,7 @@ __device__ __forceinline__ void block_exclusive(int64_t (&v)[N], int64_t (&total
   for (int i = 0; i < N; ++i) {
     total[i] = 0;
 #pragma unroll
-    for (int x = 0; x < 16; ++x) {
+    for (int x = 0; x < kPlanThreads / 64; ++x) {
       if (x == w) v[i] += total[i];
       total[i] += waves[x][i];
     }
@@ -95,7 +98,7 @@ constexpr int kMostStretches = 768;  // (attend_items())
 
 }  // namespace
 
-__global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
+__global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev p) {
   __shared__ int most_pieces;
   __shared__ PlanSeq lds_seqs[kLdsSeqs];
   __shared__ int32_t lds_seg[2 * kLdsSeqs + 1];
@@ -113,7 +116,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   }
 
   // the sequences' new tokens and lengths, as far as they are valid
-  for (int b = tid; b < B; b += 1024) {
+  for (int b = tid; b < B; b += kPlanThreads) {
     PlanSeq s;
     s.t0 = clamp_int(p.a.d_cu_new[b], 0, T);
     s.n = clamp_int(p.a.d_cu_new[b + 1], s.t0, T) - s.t0;
@@ -129,7 +132,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     if (s.len < 0 || s.len > room) s.len = -1;
     seqs[b] = s;
   }
-  for (int g = tid; g < n_groups; g += 1024) {
+  for (int g = tid; g < n_groups; g += kPlanThreads) {
     PlanGroup x = {};
     const int b0 = clamp_int(p.a.d_cu_group[g], 0, B), b1 = clamp_int(p.a.d_cu_group[g + 1], b0, B);
     x.shared = max(p.a.d_prefix_len[g], 0);
@@ -140,7 +143,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   __syncthreads();
   // a prefix is cut to what all queries of the group see
   if (n_groups > 0) {
-    for (int b = tid; b < B; b += 1024) {
+    for (int b = tid; b < B; b += kPlanThreads) {
       const int g = group_of(p, b);
       if (g < 0) continue;
       const PlanSeq s = seqs[b];
@@ -151,20 +154,20 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       }
     }
     __syncthreads();
-    for (int g = tid; g < n_groups; g += 1024) {  // (atomics are done in L2: read there)
+    for (int g = tid; g < n_groups; g += kPlanThreads) {  // (atomics are done in L2: read there)
       const int active = __hip_atomic_load(&p.groups[g].active, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       const int shared = __hip_atomic_load(&p.groups[g].shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       p.groups[g].shared = shares(p.groups[g].tokens * G, active) ? shared : 0;
     }
     __syncthreads();
-    for (int b = tid; b < B; b += 1024) {
+    for (int b = tid; b < B; b += kPlanThreads) {
       const int g = group_of(p, b);
       if (g >= 0) seqs[b].shared = p.groups[g].shared;
     }
     __syncthreads();
   }
   {  // the segments' first blocks
-    const int n_seg = n_groups + B, per = (n_seg + 1023) / 1024, s0 = min(n_seg, tid * per), s1 = min(n_seg, s0 + per);
+    const int n_seg = n_groups + B, per = (n_seg + kPlanThreads - 1) / kPlanThreads, s0 = min(n_seg, tid * per), s1 = min(n_seg, s0 + per);
     auto blocks_of = [&](int s) {
       const int tokens = s < n_groups ? (p.groups[s].shared > 0 ? p.groups[s].tokens : 0) : seqs[s - n_groups].n;
       return tokens > 0 ? segment_blocks(tokens * G, p.a.d) : 0;
@@ -207,7 +210,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     return k;
   };
   // every thread walks over a run of blocks, several times
-  const int per = (n_blocks + 1023) / 1024, x0 = min(n_blocks, tid * per), x1 = min(n_blocks, x0 + per);
+  const int per = (n_blocks + kPlanThreads - 1) / kPlanThreads, x0 = min(n_blocks, tid * per), x1 = min(n_blocks, x0 + per);
   auto walk = [&](auto&& visit) {
     int seg = -1;
     for (int x = x0; x < x1; ++x) {
@@ -235,7 +238,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       at += (int64_t)k.steps * k.cost + k.extra;
     });
     __syncthreads();
-    for (int s = tid; s <= n_cuts; s += 1024) {
+    for (int s = tid; s <= n_cuts; s += kPlanThreads) {
       int b = s < n_cuts && n_blocks > 0 ? 0 : n_blocks, j = 0;
       if (s > 0 && s < n_cuts) {
         const int64_t x = stretch_start(total[0], n_cuts, s);
@@ -270,13 +273,15 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   block_exclusive(at, n);
   if (n[kUnits] > p.cap_units || n[kSlots] > p.cap_slots || n[kJoins] > p.cap_joins || n[kRows] > p.cap_rows) return;
   if (stretched) {
+    const int run = (n_cuts + kPlanThreads - 1) / kPlanThreads, s0 = min(n_cuts, tid * run), s1 = min(n_cuts, s0 + run);
+    auto units_of = [&](int s) { return (cuts[s + 1] >> 32) + ((cuts[s + 1] & 0xffffffff) != 0) - (cuts[s] >> 32); };
     int64_t count[1] = {0}, units[1];
-    if (tid < n_cuts) {
-      const int64_t a = cuts[tid], b = cuts[tid + 1];
-      count[0] = (b >> 32) + ((b & 0xffffffff) != 0) - (a >> 32);
-    }
+    for (int s = s0; s < s1; ++s) count[0] += units_of(s);
     block_exclusive(count, units);
-    if (tid < n_cuts) first_unit[tid] = (int)count[0];
+    for (int s = s0; s < s1; ++s) {
+      first_unit[s] = (int)count[0];
+      count[0] += units_of(s);
+    }
     if (tid == 0) first_unit[n_cuts] = (int)units[0];
   }
 
@@ -302,6 +307,11 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     unit.slot = (int)slot;
     return unit;
   };
+  auto put_stretch = [&](int64_t s, int first, int end, const AttendUnit& unit) {
+    p.stretches[s].first = first;
+    p.stretches[s].end = end;
+    p.stretches[s].unit = unit;
+  };
   {
     int64_t u = at[kUnits], slot = at[kSlots];
     walk([&](int x, const Block& k) {
@@ -315,12 +325,10 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
         slot_of[x] = sums ? (int)slot : -1;
       } else {
         for (int q = 0; q < pieces; ++q) {
-          AttendStretch s;
-          s.unit = p.units[u + q] = unit_of(k, piece_step(k.steps, pieces, q), q + 1 == pieces ? k.steps : piece_step(k.steps, pieces, q + 1),
-                                            sums ? slot + (int64_t)q * step : -1);
-          s.first = (int)(u + q);
-          s.end = s.first + 1;
-          p.stretches[u + q] = s;
+          const AttendUnit unit = unit_of(k, piece_step(k.steps, pieces, q), q + 1 == pieces ? k.steps : piece_step(k.steps, pieces, q + 1),
+                                          sums ? slot + (int64_t)q * step : -1);
+          p.units[u + q] = unit;
+          put_stretch(u + q, (int)(u + q), (int)(u + q + 1), unit);
         }
         u += pieces;
       }
@@ -337,7 +345,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
       const int q = j0 > 0 ? s - first_cut(x) + 1 : 0;
       return unit_of(k, j0, j1, slot_of[x] < 0 ? -1 : slot_of[x] + (int64_t)q * (k.m / kSlotRows));
     };
-    for (int u = tid; u < (int)n[kUnits]; u += 1024) {
+    for (int u = tid; u < (int)n[kUnits]; u += kPlanThreads) {
       const AttendUnit x = piece(u, last_at_most(first_unit, n_cuts, u));
       alone[u] = x.run == kBadUnit || !is_short(x.nr, x.k1 - x.k0) ? 0 : x.nr <= kTileRows ? 1 : 2;
     }
@@ -345,20 +353,18 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
     // short pieces that are taken side by side: as many of one or of two tiles of rows as follow one another in a stretch, up to the
     // waves of a workgroup
     const int waves = attend_waves(p.a.d);
-    for (int u = tid; u < (int)n[kUnits]; u += 1024) {
+    for (int u = tid; u < (int)n[kUnits]; u += kPlanThreads) {
       const int s = last_at_most(first_unit, n_cuts, u);
-      AttendStretch x = {};
-      x.first = first_unit[s];
-      x.end = first_unit[s + 1];
-      x.unit = piece(u, s);
+      const int first = first_unit[s], end = first_unit[s + 1];
+      AttendUnit unit = piece(u, s);
       int run = 0;
-      while (run < waves && u + run < x.end && alone[u + run] && alone[u + run] == alone[u]) ++run;
-      if (run > 1) x.unit.run = run;
-      p.units[u] = x.unit;
-      if (u == x.first) p.stretches[s] = x;
+      while (run < waves && u + run < end && alone[u + run] && alone[u + run] == alone[u]) ++run;
+      if (run > 1) unit.run = run;
+      p.units[u] = unit;
+      if (u == first) put_stretch(s, first, end, unit);
     }
-    for (int s = tid; s < n_cuts; s += 1024)
-      if (first_unit[s] == first_unit[s + 1]) p.stretches[s] = AttendStretch();
+    for (int s = tid; s < n_cuts; s += kPlanThreads)
+      if (first_unit[s] == first_unit[s + 1]) p.stretches[s].first = p.stretches[s].end = 0;
   }
   int64_t slot = at[kSlots], j = at[kJoins], row = at[kRows];
   walk([&](int x, const Block& k) {
@@ -382,7 +388,7 @@ __global__ __launch_bounds__(1024) void attend_plan_kernel(const PlanDev p) {
   });
   __syncthreads();
   // a wave for each block that is joined, a lane for each row
-  for (int64_t x = tid >> 6; x < n[kJoins]; x += 16) {
+  for (int64_t x = tid >> 6; x < n[kJoins]; x += kPlanThreads / 64) {
     const AttendJoin e = p.joins[x];
     for (int r = tid & 63; r < e.nr; r += 64) {
       AttendRow o = {};
@@ -580,6 +586,6 @@ extern "C" sp_status sp_attend_plan(const sp_attend_args* a, void* hip_stream) {
   p.seg_start = reinterpret_cast<int32_t*>(base + l.seg_start);
   p.seqs = reinterpret_cast<PlanSeq*>(base + l.seqs);
   p.groups = reinterpret_cast<PlanGroup*>(base + l.groups);
-  hipLaunchKernelGGL(attend_plan_kernel, dim3(1), dim3(1024), 0, static_cast<hipStream_t>(hip_stream), p);
+  hipLaunchKernelGGL(attend_plan_kernel, dim3(1), dim3(kPlanThreads), 0, static_cast<hipStream_t>(hip_stream), p);
   return launch_status();
 }

@@ -31,10 +31,9 @@ struct PlanDev {
 
 __device__ __forceinline__ int clamp_int(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
 
-__device__ __forceinline__ int group_of(const PlanDev& p, int b) {
-  const int n = p.a.n_groups;
-  if (n == 0 || b < p.a.d_cu_group[0] || b >= p.a.d_cu_group[n]) return -1;
-  return upper_segment(p.a.d_cu_group, n, b);
+__device__ __forceinline__ int group_of(const int32_t* cu_group, int n, int b) {
+  if (n == 0 || b < cu_group[0] || b >= cu_group[n]) return -1;
+  return upper_segment(cu_group, n, b);
 }
 
 // exclusive prefixes of N numbers over the workgroup's threads, and their sums over all of them (most waves have nothing to add)
@@ -101,6 +100,8 @@ constexpr int kMostStretches = 768;  // (attend_items())
 __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev p) {
   __shared__ int most_pieces;
   __shared__ PlanSeq lds_seqs[kLdsSeqs];
+  __shared__ PlanGroup lds_groups[kLdsSeqs];
+  __shared__ int32_t lds_cu_group[kStagedOffsets];
   __shared__ int32_t lds_seg[2 * kLdsSeqs + 1];
   __shared__ int64_t start[kMostStretchBlocks + 1];   // by stretches: the blocks laid end to end
   __shared__ int64_t cuts[kMostStretches + 1];        // (block, step) that each stretch begins at
@@ -108,12 +109,15 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
   __shared__ int32_t slot_of[kMostStretchBlocks];
   __shared__ uint8_t alone[kMostStretchBlocks + kMostStretches];  // pieces that are short: how many tiles of rows they have
   PlanSeq* const seqs = p.a.B <= kLdsSeqs ? lds_seqs : p.seqs;
-  int32_t* const seg_start = p.a.B <= kLdsSeqs ? lds_seg : p.seg_start;  // (no more groups than sequences)
+  PlanGroup* const groups = p.a.B <= kLdsSeqs ? lds_groups : p.groups;  // (no more groups than sequences)
+  int32_t* const seg_start = p.a.B <= kLdsSeqs ? lds_seg : p.seg_start;
   const int tid = threadIdx.x, B = p.a.B, n_groups = p.a.n_groups, G = p.G, T = (int)p.a.T_new;
   if (tid == 0) {
     p.header->print = 0;
     most_pieces = 0;
   }
+
+  const int32_t* const cu_group = n_groups > 0 ? staged_offsets(p.a.d_cu_group, n_groups, lds_cu_group) : nullptr;
 
   // the sequences' new tokens and lengths, as far as they are valid
   for (int b = tid; b < B; b += kPlanThreads) {
@@ -134,42 +138,42 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
   }
   for (int g = tid; g < n_groups; g += kPlanThreads) {
     PlanGroup x = {};
-    const int b0 = clamp_int(p.a.d_cu_group[g], 0, B), b1 = clamp_int(p.a.d_cu_group[g + 1], b0, B);
+    const int b0 = clamp_int(cu_group[g], 0, B), b1 = clamp_int(cu_group[g + 1], b0, B);
     x.shared = max(p.a.d_prefix_len[g], 0);
     x.t0 = clamp_int(p.a.d_cu_new[b0], 0, T);
     x.tokens = clamp_int(p.a.d_cu_new[b1], x.t0, T) - x.t0;
-    p.groups[g] = x;
+    groups[g] = x;
   }
   __syncthreads();
   // a prefix is cut to what all queries of the group see
   if (n_groups > 0) {
     for (int b = tid; b < B; b += kPlanThreads) {
-      const int g = group_of(p, b);
+      const int g = group_of(cu_group, n_groups, b);
       if (g < 0) continue;
       const PlanSeq s = seqs[b];
-      if (b == p.a.d_cu_group[g]) atomicMin(&p.groups[g].shared, max(s.len, 0));
+      if (b == cu_group[g]) atomicMin(&groups[g].shared, max(s.len, 0));
       if (s.n > 0) {
-        atomicMin(&p.groups[g].shared, s.len < 0 ? 0 : max(s.len - s.n, 0));
-        atomicAdd(&p.groups[g].active, 1);
+        atomicMin(&groups[g].shared, s.len < 0 ? 0 : max(s.len - s.n, 0));
+        atomicAdd(&groups[g].active, 1);
       }
     }
     __syncthreads();
     for (int g = tid; g < n_groups; g += kPlanThreads) {  // (atomics are done in L2: read there)
-      const int active = __hip_atomic_load(&p.groups[g].active, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const int shared = __hip_atomic_load(&p.groups[g].shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      p.groups[g].shared = shares(p.groups[g].tokens * G, active) ? shared : 0;
+      const int active = __hip_atomic_load(&groups[g].active, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      const int shared = __hip_atomic_load(&groups[g].shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      groups[g].shared = shares(groups[g].tokens * G, active) ? shared : 0;
     }
     __syncthreads();
     for (int b = tid; b < B; b += kPlanThreads) {
-      const int g = group_of(p, b);
-      if (g >= 0) seqs[b].shared = p.groups[g].shared;
+      const int g = group_of(cu_group, n_groups, b);
+      if (g >= 0) seqs[b].shared = groups[g].shared;
     }
     __syncthreads();
   }
   {  // the segments' first blocks
     const int n_seg = n_groups + B, per = (n_seg + kPlanThreads - 1) / kPlanThreads, s0 = min(n_seg, tid * per), s1 = min(n_seg, s0 + per);
     auto blocks_of = [&](int s) {
-      const int tokens = s < n_groups ? (p.groups[s].shared > 0 ? p.groups[s].tokens : 0) : seqs[s - n_groups].n;
+      const int tokens = s < n_groups ? (groups[s].shared > 0 ? groups[s].tokens : 0) : seqs[s - n_groups].n;
       return tokens > 0 ? segment_blocks(tokens * G, p.a.d) : 0;
     };
     int64_t count[1] = {0}, all[1];
@@ -193,11 +197,11 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
     Block k;
     k.seg = hint >= 0 && flat >= seg_start[hint] && flat < seg_start[hint + 1] ? hint : upper_segment(seg_start, n_groups + B, flat);
     k.i = flat - seg_start[k.seg];
-    k.rows = (k.seg < n_groups ? p.groups[k.seg].tokens : seqs[k.seg - n_groups].n) * G;
+    k.rows = (k.seg < n_groups ? groups[k.seg].tokens : seqs[k.seg - n_groups].n) * G;
     k.m = block_rows(k.rows, p.a.d);
     if (k.seg < n_groups) {
       k.first = 0;
-      k.keys = p.groups[k.seg].shared;
+      k.keys = groups[k.seg].shared;
     } else {
       const PlanSeq s = seqs[k.seg - n_groups];
       k.first = s.shared;
@@ -289,8 +293,8 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
     AttendUnit unit;
     int t0;
     if (k.seg < n_groups) {
-      t0 = p.groups[k.seg].t0;
-      unit.seq = clamp_int(p.a.d_cu_group[k.seg], 0, B - 1);
+      t0 = groups[k.seg].t0;
+      unit.seq = clamp_int(cu_group[k.seg], 0, B - 1);
       unit.off = kNoLimit;
       unit.run = 0;
     } else {
@@ -318,8 +322,8 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
       const int pieces = pieces_at(x, k), step = k.m / kSlotRows;
       const bool sums = leaves_sums(k, pieces);
       if (k.seg < n_groups && k.i == 0) {
-        p.groups[k.seg].slot = (int)slot;
-        p.groups[k.seg].pieces = pieces;
+        groups[k.seg].slot = (int)slot;
+        groups[k.seg].pieces = pieces;
       }
       if (stretched) {
         slot_of[x] = sums ? (int)slot : -1;
@@ -380,7 +384,7 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
       e.own_step = step;
       e.first = (int)row;
       row += e.nr;
-      e.group = seqs[b].shared > 0 ? group_of(p, b) : -1;
+      e.group = seqs[b].shared > 0 ? group_of(cu_group, n_groups, b) : -1;
       if (e.group < 0) atomicMax(&most_pieces, pieces);
       p.joins[j++] = e;
     }
@@ -397,7 +401,7 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
       o.own_pieces = e.own_pieces;
       o.own_step = e.own_step * kSlotRows;
       if (e.group >= 0) {  // (the blocks of a prefix may be cut differently)
-        const PlanGroup g = p.groups[e.group];
+        const PlanGroup g = groups[e.group];
         const int m = block_rows(g.tokens * G, p.a.d), in = o.row - g.t0 * G, x = seg_start[e.group] + in / m;
         if (in >= 0 && in < g.tokens * G) {
           o.pre_pieces = stretched ? pieces_at(x, Block()) : g.pieces;

@@ -1,7 +1,7 @@
 // sp_attend_plan: the list of pieces of work of an attention call, made on the device from the lengths (which only the
 // device knows, so that a captured graph follows them), and the kernel that joins the pieces' sums.  The cut itself is in sp_attend_plan.h.
 // The plan is bound by its chain of dependent reads and barriers and by fetching its own code (one workgroup): 14 us for one sequence,
-// 21 for 64, 38 for 64 that share a prefix; a step makes it once for all layers.
+// 20 for 64, 25 for 64 that share a prefix; a step makes it once for all layers.
 #include "sp_attend_internal.h"
 
 namespace sp {
@@ -391,10 +391,10 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
     slot += (int64_t)pieces * step;
   });
   __syncthreads();
-  // a wave for each block that is joined, a lane for each row
-  for (int64_t x = tid >> 6; x < n[kJoins]; x += kPlanThreads / 64) {
+  // 16 lanes for each block that is joined, a lane for each row
+  for (int64_t x = tid >> 4; x < n[kJoins]; x += kPlanThreads / 16) {
     const AttendJoin e = p.joins[x];
-    for (int r = tid & 63; r < e.nr; r += 64) {
+    for (int r = tid & 15; r < e.nr; r += 16) {
       AttendRow o = {};
       o.row = e.r0 + r;
       o.own_at = e.own_slot * kSlotRows + r;

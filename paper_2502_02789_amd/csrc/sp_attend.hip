@@ -767,7 +767,7 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   const bool fp8 = a->cache_dtype == SP_K_FP8_E4M3, paged = a->d_block_table != nullptr;
   const int E = fp8 ? 1 : 2;
   AttendDev p;
-  p.B = a->B; p.H = a->H; p.H_kv = a->H_kv; p.G = a->H / a->H_kv; p.T_new = (int)a->T_new;
+  p.H = a->H; p.H_kv = a->H_kv; p.G = a->H / a->H_kv; p.T_new = (int)a->T_new;
   p.lg_page = 0;
   while (paged && (1 << p.lg_page) < a->page_size) ++p.lg_page;
   p.blocks_per_seq = a->blocks_per_seq;

@@ -9,7 +9,7 @@ namespace sp {
 
 // Kernel-side view of sp_attend_args (passed by value).
 struct AttendDev {
-  int B, H, H_kv, G, T_new;
+  int H, H_kv, G, T_new;
   int lg_page, blocks_per_seq;
   uint32_t last_page, last_row;  // of the pool, of a contiguous cache
   uint32_t most_items;           // (row, KV head) pairs to join that the list has room for

@@ -76,7 +76,7 @@ struct AttendHeader {
   uint64_t print;     // of the shape fields the plan was made for
   int32_t n_stretches, n_rows;  // workgroups for each KV head, rows to join
   int32_t most_pieces;      // of a row to join
-  int32_t n_slots;
+  int32_t pad;
 };
 
 constexpr int kNoLimit = 0x7fffffff;

@@ -417,7 +417,6 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
   if (tid == 0) {
     p.header->n_stretches = stretched ? n_cuts : (int)n[kUnits];
     p.header->n_rows = (int)n[kRows];
-    p.header->n_slots = (int)n[kSlots];
     p.header->most_pieces = most_pieces;
     p.header->print = p.print;
   }

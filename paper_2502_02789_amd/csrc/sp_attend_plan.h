@@ -43,11 +43,11 @@ constexpr int kMostStretchBlocks = 3 * 768;  // blocks that stretches are made f
 // d = 64 takes a quarter of the LDS and fewer registers, three of four
 SP_ATTEND_FN constexpr int attend_waves(int d) { return d == 64 ? 4 : 8; }
 SP_ATTEND_FN constexpr int attend_items(int d) { return d == 64 ? 768 : 256; }
-// Rows of a block that has more than 16: 32 for each wave
+// Rows of a block that has more than 32: 32 for each wave
 SP_ATTEND_FN constexpr int many_rows(int d) { return 32 * attend_waves(d); }
 
 struct AttendUnit {   // one piece of one block
-  int32_t r0, nr;     // first row, rows (nr <= 16: the kernel part for few rows)
+  int32_t r0, nr;     // first row, rows (nr <= 32: the kernel part for few rows)
   int32_t seq;        // whose block table is read; of a contiguous cache: the row of its first token
   int32_t k0, k1;     // keys [k0, k1)
   int32_t off;        // token t sees keys below t + off (kNoLimit: all of the piece)
@@ -159,7 +159,7 @@ SP_ATTEND_FN int piece_cost(int rows, int keys, int d) { return d == 64 ? (is_sh
 // share 32K 74.7 -> 76.3.)
 SP_ATTEND_FN int least_stretch(int d) { return d == 64 ? 10 : 11; }
 
-// many: blocks of more than 16 rows (the others are cheap to cut)
+// many: blocks of more than 32 rows (the others are cheap to cut)
 SP_ATTEND_FN bool by_stretches(int64_t blocks, int64_t many, int d, int H_kv) {
   return many * H_kv < 3 * (int64_t)attend_items(d) && blocks <= kMostStretchBlocks;
 }

@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
     for (int g = tid; g < n_groups; g += kPlanThreads) {  // (atomics are done in L2: read there)
       const int active = __hip_atomic_load(&groups[g].active, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       const int shared = __hip_atomic_load(&groups[g].shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      groups[g].shared = shares(groups[g].tokens * G, active) ? shared : 0;
+      groups[g].shared = prefix_pays(groups[g].tokens * G, active, shared, p.a.d, p.a.cache_dtype == SP_K_FP8_E4M3) ? shared : 0;
     }
     __syncthreads();
     for (int b = tid; b < B; b += kPlanThreads) {

@@ -1,0 +1,71 @@
+"""GPU: sp_attend with queries of zeros.  All weights are exactly one then, values are small whole numbers, so every sum is a whole number that fp32 holds:
+the number of keys that a row met can be told from its lse, and a key that is met twice, missed or taken for another moves the sums."""
+import numpy as np
+import pytest
+
+from oracle import cache_oracle as co
+from tests import attend_batches as ab
+from tests import cache_cases as cc
+
+pytestmark = pytest.mark.gpu
+
+
+def _counted(b, seed, values):
+    """The batch on the device: (plan, attender, sums that are wanted [T, H_kv, d], keys that a row sees [T])."""
+    import torch
+    from paper_2502_02789_amd import device as dev
+    rng = np.random.default_rng(seed)
+    cache = cc.Cache(rng, [m + (3 if b["page"] else 0) for m in b["length"]], b["H_kv"], b["d"], b["page"], b["bits"], groups=b["groups"])
+    whole = values(rng, cache.v.shape).astype(np.float32)
+    cache.v[:] = co.f32_to_e4m3_codes(whole) if b["bits"] == 8 else co.f32_to_bf16_bits(whole)
+    if b["bits"] == 8:
+        cache.v_scale[:] = 0.5       # (exact)
+    cache.share(b["groups"])
+    cache.spoil_unused(b["length"])
+    _, v = cache.values()
+    T = sum(b["new"])
+    sums, seen, t = np.zeros((T, b["H_kv"], b["d"])), np.zeros(T, np.int64), 0
+    for s, (n, m) in enumerate(zip(b["new"], b["length"])):
+        if n == 0:
+            continue
+        add = np.concatenate([np.zeros((1,) + v.shape[1:]), np.cumsum(v[cache.rows(s, m)], axis=0)])
+        seen[t:t + n] = np.clip(m - n + np.arange(n) + 1, 0, m)
+        sums[t:t + n] = add[seen[t:t + n]]
+        t += n
+    where, kc, vc, scales = cache.device()
+    group = {}
+    if b["groups"]:
+        group = dict(cu_group=cc.cuda_ints([g[0] for g in b["groups"]] + [b["groups"][-1][1]]), prefix_len=cc.cuda_ints([g[2] for g in b["groups"]]))
+    plan = dev.AttendPlan(cc.cuda_ints(cc.offsets(b["new"])), cc.cuda_ints(b["length"]), kc, H=b["H"], total_new=T, **where, **group)
+    q = torch.zeros((T, b["H"], b["d"]), dtype=torch.bfloat16, device="cuda")
+    a = dev.Attender(plan, q, kc, vc, scale=co.softmax_scale(b["d"]), want_lse=True, **scales)
+    a.out.fill_(7)
+    a.lse.fill_(7)
+    return plan, a, sums, seen
+
+
+def _check(b, a, sums, seen):
+    G = b["H"] // b["H_kv"]
+    lse, out = a.lse.cpu().numpy().astype(np.float64), a.out.float().cpu().numpy().astype(np.float64)
+    sums = np.repeat(sums, G, axis=1)
+    assert seen.max() < 100000           # the lse of n and n + 1 keys differ by 1 / n, its own error is 2^-22 (1 + log n)
+    some = seen > 0
+    assert np.isneginf(lse[~some]).all() and (out[~some] == 0).all()
+    met = np.rint(np.exp(lse[some]))
+    wrong = np.argwhere(met != seen[some][:, None])
+    assert len(wrong) == 0, f"row, head {wrong[0]}: {met[tuple(wrong[0])]:.0f} keys instead of {seen[some][wrong[0][0]]}"
+    want = sums[some] / seen[some][:, None, None]
+    # the quotient in fp32 (a reciprocal, a product: 2^-20 is ample), then rounded to bf16
+    off = np.abs(out[some] - want) - np.abs(want) * (2.0 ** -8 + 2.0 ** -20)
+    wrong = np.argwhere(off > 0)
+    assert len(wrong) == 0, f"row, head, element {wrong[0]}: {out[some][tuple(wrong[0])]} instead of {want[tuple(wrong[0])]}"
+
+
+@pytest.mark.parametrize("batch", ab.SHARED + ab.BLOCKS, ids=lambda b: b["name"])
+def test_every_key_is_met_once(batch):
+    import torch
+    plan, a, sums, seen = _counted(batch, 5, lambda rng, shape: rng.integers(-8, 9, shape))
+    plan.run()
+    a.run()
+    torch.cuda.synchronize()
+    _check(batch, a, sums, seen)

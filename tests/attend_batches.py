@@ -45,5 +45,32 @@ def _shared():
     return out
 
 
+def _blocks():
+    """So many large blocks that a workgroup takes one at a time: 768 (d = 128) or 2304 (d = 64) and more of them, KV heads counted.  cut: of a sequence's
+    large blocks some are longer than a workgroup's share and cut, cut_prefix: of a group's."""
+    out = []
+    for H, H_kv, d, n, page, bits in ((16, 16, 128, 50, 8, 16), (16, 16, 128, 50, 16, 8), (32, 8, 128, 100, 16, 16), (64, 64, 64, 40, 8, 16), (64, 16, 64, 150, 16, 8)):
+        G = H // H_kv
+        at = f"H {H}, {H_kv} of d {d}, {bits} bits"
+        kw = dict(d=d, bits=bits, page=page)
+        new = _ints(41, 32 // G + 1, 40 // G + 2, n)
+        own = _some(42, 0, 30, new)
+        # large blocks, small ones between them, sequences of none; a block that is cut, several blocks of which the last are
+        few = [1, 0, 2, 1, 16 // G, 32 // G, 3, 1]
+        new2 = new[:20] + few + new[20:] + [60, 300 // G + 5]
+        own2 = own[:20] + [5, 9, 700, 1, 40, 300, 3, 2500] + own[20:] + [1500, 2000 + 300 // G]
+        out.append(_batch(f"blocks that are cut, {at}", new2, own2, H, H_kv, cut=True, cut_prefix=False, **kw))
+        # groups: a prefix of single tokens that is cut, one of large blocks, one that each member reads; then sequences without a group
+        m = 40 // G + 1
+        new3 = [1] * m + [34 // G + 1] * 6 + [1, 0, 2] + new
+        own3 = _some(43, 0, 60, new3)
+        groups = [(0, m, 1801), (m, m + 6, 2600), (m + 6, m + 9, 30)] + [(b, b + 1, 0) for b in range(m + 9, len(new3))]
+        out.append(_batch(f"prefixes that are cut, {at}", new3, own3, H, H_kv, groups=groups, sharing=[True, True, False] + [False] * (len(new3) - m - 9), cut=False,
+                          cut_prefix=True, **kw))
+    for d, n, bits in ((128, 3000, 16), (64, 4600, 16), (128, 2900, 8)):
+        out.append(_batch(f"a whole prompt of {n} tokens, d {d}, {bits} bits", [n], [n], 64, 64, d, bits=bits, page=0, cut=False, cut_prefix=False))
+    return out
+
+
 SHARED = _shared()
-BLOCKS = []
+BLOCKS = _blocks()

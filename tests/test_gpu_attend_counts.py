@@ -22,15 +22,16 @@ def _counted(b, seed, values):
         cache.v_scale[:] = 0.5       # (exact)
     cache.share(b["groups"])
     cache.spoil_unused(b["length"])
-    _, v = cache.values()
+    v = cache.values()[1].astype(np.float32)      # (exact)
     T = sum(b["new"])
-    sums, seen, t = np.zeros((T, b["H_kv"], b["d"])), np.zeros(T, np.int64), 0
+    sums, seen, t = np.zeros((T, b["H_kv"], b["d"]), np.float32), np.zeros(T, np.int64), 0
     for s, (n, m) in enumerate(zip(b["new"], b["length"])):
         if n == 0:
             continue
-        add = np.concatenate([np.zeros((1,) + v.shape[1:]), np.cumsum(v[cache.rows(s, m)], axis=0)])
         seen[t:t + n] = np.clip(m - n + np.arange(n) + 1, 0, m)
-        sums[t:t + n] = add[seen[t:t + n]]
+        rows, before = cache.rows(s, m), max(0, m - n)
+        first = v[rows[:before]].sum(0)
+        sums[t + max(0, n - m):t + n] = first + np.cumsum(v[rows[before:]], axis=0)
         t += n
     where, kc, vc, scales = cache.device()
     group = {}
@@ -47,7 +48,7 @@ def _counted(b, seed, values):
 def _check(b, a, sums, seen):
     G = b["H"] // b["H_kv"]
     lse, out = a.lse.cpu().numpy().astype(np.float64), a.out.float().cpu().numpy().astype(np.float64)
-    sums = np.repeat(sums, G, axis=1)
+    sums = np.repeat(sums, G, axis=1).astype(np.float64)
     assert seen.max() < 100000           # the lse of n and n + 1 keys differ by 1 / n, its own error is 2^-22 (1 + log n)
     some = seen > 0
     assert np.isneginf(lse[~some]).all() and (out[~some] == 0).all()

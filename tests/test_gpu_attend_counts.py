@@ -70,3 +70,38 @@ def test_every_key_is_met_once(batch):
     a.run()
     torch.cuda.synchronize()
     _check(batch, a, sums, seen)
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("paged", [True, False])
+def test_every_key_of_a_long_cache_is_met_once(paged, bits):
+    """70001 keys at the end of a pool whose byte offsets pass 2^32; single tokens, two at once, and enough rows for a large block."""
+    import torch
+    from paper_2502_02789_amd import device as dev
+    page, H_kv, d, m = 16, 8, 128, 70001
+    need = -(-m // page)
+    pages = (1 << 32) // (page * H_kv * d * (bits // 8)) + need
+    g = torch.Generator(device="cuda").manual_seed(3)
+    dtype = torch.bfloat16 if bits == 16 else torch.float8_e4m3fn
+    kc = torch.full((pages, page, H_kv, d), 0x7F, dtype=torch.uint8, device="cuda") if bits == 8 else torch.full((pages, page, H_kv, d), float("nan"), dtype=dtype, device="cuda")
+    vc = kc.clone()
+    first = pages - need
+    whole = torch.randint(-8, 9, (need, page, H_kv, d), generator=g, device="cuda").float()
+    kc[first:] = torch.randn(whole.shape, generator=g, device="cuda").to(dtype).view(kc.dtype)
+    vc[first:] = whole.to(dtype).view(kc.dtype)
+    table = None
+    if paged:
+        table = torch.full((2, need), -1, dtype=torch.int32, device="cuda")
+        table[1] = torch.randperm(need, generator=g, device="cuda").to(torch.int32) + first
+        whole = whole[table[1].long() - first]
+    add = torch.cat([torch.zeros((1, H_kv, d), device="cuda", dtype=torch.float64), whole.view(-1, H_kv, d)[:m].double().cumsum(0)]).cpu().numpy()
+    for n in (1, 2, 40):
+        cache = (kc, vc) if paged else (kc.view(-1, H_kv, d), vc.view(-1, H_kv, d))
+        where = dict(block_table=table) if paged else dict(cu_cache=cc.cuda_ints([0, first * page, first * page + m]))
+        plan = dev.AttendPlan(cc.cuda_ints([0, 0, n]), cc.cuda_ints([0, m]), cache[0], H=8, total_new=n, **where)
+        a = dev.Attender(plan, torch.zeros((n, 8, d), dtype=torch.bfloat16, device="cuda"), *cache, scale=1.0, want_lse=True)
+        plan.run()
+        a.run()
+        torch.cuda.synchronize()
+        seen = m - n + 1 + np.arange(n)
+        _check(dict(H=8, H_kv=8), a, add[seen], seen)

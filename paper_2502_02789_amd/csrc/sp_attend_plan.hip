@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
     if (tid == 0) first_unit[n_cuts] = (int)units[0];
   }
 
-  auto unit_of = [&](const Block& k, int j0, int j1, int64_t slot) {
+  auto unit_of = [&](const Block& k, int k0, int k1, int64_t slot) {
     AttendUnit unit;
     int t0;
     if (k.seg < n_groups) {
@@ -306,8 +306,8 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
     }
     unit.r0 = t0 * G + k.i * k.m;
     unit.nr = k.nr;
-    unit.k0 = step_key(k.first, k.keys, k.steps, j0);
-    unit.k1 = step_key(k.first, k.keys, k.steps, j1);
+    unit.k0 = k0;
+    unit.k1 = k1;
     unit.slot = (int)slot;
     return unit;
   };
@@ -329,8 +329,7 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
         slot_of[x] = sums ? (int)slot : -1;
       } else {
         for (int q = 0; q < pieces; ++q) {
-          const AttendUnit unit = unit_of(k, piece_step(k.steps, pieces, q), q + 1 == pieces ? k.steps : piece_step(k.steps, pieces, q + 1),
-                                          sums ? slot + (int64_t)q * step : -1);
+          const AttendUnit unit = unit_of(k, piece_start(k.first, k.keys, pieces, q), piece_start(k.first, k.keys, pieces, q + 1), sums ? slot + (int64_t)q * step : -1);
           p.units[u + q] = unit;
           put_stretch(u + q, (int)(u + q), (int)(u + q + 1), unit);
         }
@@ -347,7 +346,8 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
       const Block k = block_at(x, -1);
       const int j0 = x == (int)(a >> 32) ? (int)a : 0, j1 = x == (int)(b >> 32) ? (int)b : k.steps;
       const int q = j0 > 0 ? s - first_cut(x) + 1 : 0;
-      return unit_of(k, j0, j1, slot_of[x] < 0 ? -1 : slot_of[x] + (int64_t)q * (k.m / kSlotRows));
+      return unit_of(k, step_key(k.first, k.keys, k.steps, j0), step_key(k.first, k.keys, k.steps, j1),
+                     slot_of[x] < 0 ? -1 : slot_of[x] + (int64_t)q * (k.m / kSlotRows));
     };
     for (int u = tid; u < (int)n[kUnits]; u += kPlanThreads) {
       const AttendUnit x = piece(u, last_at_most(first_unit, n_cuts, u));

@@ -357,7 +357,9 @@ SP_API sp_status sp_gather(const sp_gather_args* args, void* hip_stream);
  * sp_score with rope_theta > 0 makes of an unrotated one.
  * A token whose cache index is negative or outside its sequence's room (blocks_per_seq * page_size tokens, or its rows of a
  * contiguous cache) or whose page number lies outside the pool is not written to the cache; its row of q_out is.
- * No two tokens of a call may have the same place in the cache. */
+ * No two tokens of a call may have the same place in the cache: keys and values are different arrays, the cache's strides are at
+ * least d where there are several heads, tokens or pages (SP_EINVAL), and its layout keeps all rows apart.  q_out, unless it is d_q itself, and the
+ * cache overlap no input. */
 typedef struct {
   int32_t B;                 /* sequences, >= 1                                                       */
   int32_t H;                 /* query heads (ignored if d_q is NULL)                                  */
@@ -405,7 +407,8 @@ SP_API sp_status sp_cache_append(const sp_cache_append_args* args, void* hip_str
  * A row that sees no token gets out = 0 and lse = -infinity.  Logits, maxima, sums and the accumulation of out are
  * fp32; the weights exp(s_i - m) are rounded to bf16 for the product with the values, as the values are.
  * NaN/Inf among the queries, or the keys and values of the first kv_len[b] tokens, are precondition violations
- * (undefined values in rows of that sequence, or of its group); what lies behind them in the cache is never used.
+ * (undefined values in rows of that sequence, or of its group), and so are logits beyond fp32's range on the positive side; one that overflows to
+ * -infinity has weight 0.  What lies behind the first kv_len[b] tokens in the cache is never used.
  *
  * Shared prefixes: sequences d_cu_group[g] .. d_cu_group[g+1]-1 form a group whose members hold the same first
  * d_prefix_len[g] tokens (the same pages, or copies).  Results are those of the definition; the keys and values of those
@@ -423,7 +426,8 @@ SP_API sp_status sp_cache_append(const sp_cache_append_args* args, void* hip_str
  * part of the work met a page number outside the pool.
  * Limits: n_rows and blocks_per_seq * page_size <= 2^31 - 2^16, cache_token_stride < 2^26, and lists of work that one launch has
  * threads for (about T_new * H < 2^31 for prompts, B * H_kv < 2^23 for single tokens): SP_EINVAL beyond.
- * Rows of a contiguous cache are those that d_cu_cache names at the time of the plan.  d_out overlaps no input.
+ * Rows of a contiguous cache are those that d_cu_cache names at the time of the plan.  d_out overlaps no input, and no two of its rows
+ * overlap (strides below d, where there are several heads or rows: SP_EINVAL).
  * Both calls may be captured into graphs: nothing depends on lengths on the host. */
 typedef struct {
   int32_t B;                 /* sequences, >= 1                                                       */

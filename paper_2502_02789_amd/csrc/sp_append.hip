@@ -166,6 +166,11 @@ sp_status check_append(const sp_cache_append_args* a) {
     if (a->page_size < 8 || (a->page_size & (a->page_size - 1)) != 0 || a->blocks_per_seq < 1) return SP_EINVAL;
     if ((int64_t)a->blocks_per_seq * a->page_size >= INT64_C(0x80000000) || a->n_rows % a->page_size != 0) return SP_EINVAL;
   }
+  // heads and tokens that lie in one another would be written by several lanes at once, and so would keys over values
+  if (a->H_kv > 1 && a->cache_head_stride < a->d) return SP_EINVAL;
+  if ((a->d_block_table || a->n_rows > 1) && a->cache_token_stride < a->d) return SP_EINVAL;
+  if (a->d_block_table && a->n_rows > a->page_size && a->cache_page_stride < a->d) return SP_EINVAL;
+  if (a->d_k_cache == a->d_v_cache) return SP_EINVAL;
   for (int64_t s : in) if (s & 7) return SP_EALIGN;
   for (int64_t s : out) if (s & (a->cache_dtype == SP_K_FP8_E4M3 ? 15 : 7)) return SP_EALIGN;
   if (!aligned16(a->d_q) || !aligned16(a->d_k) || !aligned16(a->d_v) || !aligned16(a->d_q_out) || !aligned16(a->d_k_cache) ||

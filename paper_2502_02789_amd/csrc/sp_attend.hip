@@ -734,6 +734,7 @@ sp_status check_attend(const sp_attend_args* a) {
   const int64_t cache[] = {a->cache_token_stride, a->cache_head_stride, a->d_block_table ? a->cache_page_stride : 0};
   for (int64_t s : row) if (s < 0) return SP_EINVAL;
   for (int64_t s : cache) if (s < 0) return SP_EINVAL;
+  if ((a->H > 1 && a->out_head_stride < a->d) || (a->T_new > 1 && a->out_token_stride < a->d)) return SP_EINVAL;  // rows of out that lie in one another
   for (int64_t s : row) if (s & 7) return SP_EALIGN;
   for (int64_t s : cache) if (s & (fp8 ? 15 : 7)) return SP_EALIGN;
   if (!aligned16(a->d_q) || !aligned16(a->d_k_cache) || !aligned16(a->d_v_cache) || !aligned16(a->d_out)) return SP_EALIGN;

@@ -151,7 +151,6 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
       const int g = group_of(cu_group, n_groups, b);
       if (g < 0) continue;
       const PlanSeq s = seqs[b];
-      if (b == cu_group[g]) atomicMin(&groups[g].shared, max(s.len, 0));
       if (s.n > 0) {
         atomicMin(&groups[g].shared, s.len < 0 ? 0 : max(s.len - s.n, 0));
         atomicAdd(&groups[g].active, 1);
@@ -160,7 +159,8 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
     __syncthreads();
     for (int g = tid; g < n_groups; g += kPlanThreads) {  // (atomics are done in L2: read there)
       const int active = __hip_atomic_load(&groups[g].active, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      const int shared = __hip_atomic_load(&groups[g].shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      // (no more than the sequence has whose pages are read, whatever the offsets are)
+      const int shared = min(__hip_atomic_load(&groups[g].shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), max(seqs[clamp_int(cu_group[g], 0, B - 1)].len, 0));
       groups[g].shared = prefix_pays(groups[g].tokens * G, active, shared, p.a.d, p.a.cache_dtype == SP_K_FP8_E4M3) ? shared : 0;
     }
     __syncthreads();

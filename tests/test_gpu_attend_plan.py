@@ -114,3 +114,38 @@ def test_lists_of_batches_of_all_sorts(walk, kind):  # noqa: F811
     for new, length, groups in some:
         if sum(new) * kind[0] // kind[1] < 40000 and len(groups) <= len(new):       # (more groups than sequences are refused)
             _verify(walk, new, length, groups, *kind)
+
+
+@pytest.mark.parametrize("cu_group", [[0, 40], [0, 9, 33, 40], [0, 0, 40], [-7, 40], [-7, -2, 40], [5, 3, 40], [0, 30, 10, 40], [40, 0], [12, 50], [0, 2**31 - 1], [39, 90]])
+@pytest.mark.parametrize("prefix", [2000, 2**31 - 1])
+def test_no_piece_reaches_beyond_the_table(walk, cu_group, prefix):  # noqa: F811
+    """Offsets of groups that do not ascend, or lie outside: what the rows get is not defined, but every piece's keys lie in the room of the sequence whose
+    pages it reads, and its rows among the call's."""
+    import torch
+    from paper_2502_02789_amd import device as dev
+    rng, B, page, blocks = np.random.default_rng(8), 40, 16, 200
+    new = rng.integers(0, 3, B)
+    new[[0, 5, 39]] = 0             # (the sequence whose table is read may have no query, and fewer tokens than the others)
+    length = rng.integers(2000, 3200, B)
+    length[[0, 5, 39]] = 30
+    cache = torch.empty((1, 1, 1, 128), dtype=torch.bfloat16, device="cuda").expand(blocks, page, 2, 128)
+    p = dev.AttendPlan(cc.cuda_ints(cc.offsets(new)), cc.cuda_ints(length), cache, H=8, total_new=int(new.sum()) + 3, block_table=cc.cuda_ints(np.zeros((B, blocks))),
+                       cu_group=cc.cuda_ints(cu_group), prefix_len=cc.cuda_ints([prefix] * (len(cu_group) - 1)))
+    p.run()
+    torch.cuda.synchronize()
+    raw, caps = p.plan.cpu().numpy(), host._caps(walk, p.args)
+    if raw[:8].view(np.uint64)[0] == 0:
+        return                      # no plan: NaN everywhere
+    n_stretches, n_rows, _ = raw[8:20].view(np.int32).tolist()
+    stretches = raw[caps["at_stretches"]:][:48 * n_stretches].view(np.int32).reshape(-1, 12)
+    units = raw[caps["at_units"]:][:32 * int(stretches[:, 1].max())].view(np.int32).reshape(-1, 8)
+    assert ((0 <= units[:, 2]) & (units[:, 2] < B)).all()
+    assert ((0 <= units[:, 3]) & (units[:, 3] <= units[:, 4])).all()
+    # (a piece without keys reads none)
+    assert ((units[:, 4] <= length[units[:, 2]]) | (units[:, 3] == units[:, 4])).all()
+    assert ((0 <= units[:, 0]) & (units[:, 0] + units[:, 1] <= 4 * p.total_new)).all()
+    assert ((units[:, 6] == -1) | ((0 <= units[:, 6]) & (units[:, 6] < caps["slots"]))).all()
+    rows = raw[caps["at_rows"]:][:32 * n_rows].view(np.int32).reshape(-1, 8)
+    assert ((0 <= rows[:, 0]) & (rows[:, 0] < 4 * p.total_new)).all()
+    for at, n, step in ((1, 2, 3), (4, 5, 6)):
+        assert ((rows[:, n] == 0) | ((rows[:, at] >= 0) & (rows[:, at] + (rows[:, n] - 1) * rows[:, step] < 16 * caps["slots"]))).all()

@@ -6,7 +6,7 @@ import numpy as np
 def _batch(name, new, own, H, H_kv, d, *, groups=(), sharing=(), bits=16, page=16, **kw):
     """own: keys of a sequence behind what its group shares; groups: (first, end, tokens shared); sharing: which of them are read once."""
     length = [o + next((p for lo, hi, p in groups if lo <= b < hi), 0) for b, o in enumerate(own)]
-    return dict(name=name, new=[int(n) for n in new], length=[int(m) for m in length], groups=tuple(groups), sharing=list(sharing), H=H, H_kv=H_kv, d=d,
+    return dict(name=name, new=[int(n) for n in new], length=[int(m) for m in length], groups=tuple(groups), sharing=list(sharing or ()), H=H, H_kv=H_kv, d=d,
                 bits=bits, page=page, **kw)
 
 
@@ -70,6 +70,27 @@ def _blocks():
     for d, n, bits in ((128, 3000, 16), (64, 4600, 16), (128, 2900, 8)):
         out.append(_batch(f"a whole prompt of {n} tokens, d {d}, {bits} bits", [n], [n], 64, 64, d, bits=bits, page=0, cut=False, cut_prefix=False))
     return out
+
+
+def drawn(seed):
+    """A batch of any kind: heads, pages and lengths over the whole ranges; some sequences of no token, or with more new tokens than keys."""
+    r = np.random.default_rng(seed)
+    H, H_kv = [(8, 2), (5, 5), (12, 1), (16, 1), (24, 2), (14, 2), (1, 1), (32, 8)][r.integers(8)]
+    d, bits, page = [64, 128][r.integers(2)], [16, 8][r.integers(2)], [0, 8, 16, 64, 1024][r.integers(5)]
+    B = int(np.exp(r.uniform(0, np.log(60))))
+    most = int(np.exp(r.uniform(0, np.log(max(2, 900 // B)))))
+    new = [int(n) for n in r.integers(0 if most > 1 else 1, most + 1, B)]
+    new[0] = max(new[0], 1)
+    far = int(np.exp(r.uniform(0, np.log(min(20000, 60000 // B)))))
+    own = [max(0, n + int(r.integers(-3 if far > 3 else 0, far + 1))) for n in new]
+    groups = []
+    if page and r.random() < 0.6:
+        b = 0
+        while b < B:
+            e = int(min(B, b + r.integers(1, B + 1)))
+            groups.append((b, e, int(np.exp(r.uniform(0, np.log(8000 if e - b > 1 else 50))))))
+            b = e
+    return _batch(f"drawn {seed}", new, own, H, H_kv, d, groups=groups, sharing=None, bits=bits, page=page)
 
 
 SHARED = _shared()

@@ -10,7 +10,7 @@ from tests import cache_cases as cc
 pytestmark = pytest.mark.gpu
 
 
-def _counted(b, seed, values):
+def _counted(b, seed, values, head_major=False, wide=False):
     """The batch on the device: (plan, attender, sums that are wanted [T, H_kv, d], keys that a row sees [T])."""
     import torch
     from paper_2502_02789_amd import device as dev
@@ -33,13 +33,17 @@ def _counted(b, seed, values):
         first = v[rows[:before]].sum(0)
         sums[t + max(0, n - m):t + n] = first + np.cumsum(v[rows[before:]], axis=0)
         t += n
-    where, kc, vc, scales = cache.device()
+    where, kc, vc, scales = cache.device(head_major)
     group = {}
     if b["groups"]:
         group = dict(cu_group=cc.cuda_ints([g[0] for g in b["groups"]] + [b["groups"][-1][1]]), prefix_len=cc.cuda_ints([g[2] for g in b["groups"]]))
     plan = dev.AttendPlan(cc.cuda_ints(cc.offsets(b["new"])), cc.cuda_ints(b["length"]), kc, H=b["H"], total_new=T, **where, **group)
     q = torch.zeros((T, b["H"], b["d"]), dtype=torch.bfloat16, device="cuda")
-    a = dev.Attender(plan, q, kc, vc, scale=co.softmax_scale(b["d"]), want_lse=True, **scales)
+    out = None
+    if wide:        # queries of one row for all, outputs inside wider rows, head by head
+        q = q[:1].expand(q.shape)
+        out = torch.full((b["H"] + 1, T + 1, b["d"] + 8), 7.0, dtype=torch.bfloat16, device="cuda")[1:, 1:, 8:].transpose(0, 1)
+    a = dev.Attender(plan, q, kc, vc, scale=co.softmax_scale(b["d"]), out=out, want_lse=True, **scales)
     a.out.fill_(7)
     a.lse.fill_(7)
     return plan, a, sums, seen
@@ -70,6 +74,20 @@ def test_every_key_is_met_once(batch):
     a.run()
     torch.cuda.synchronize()
     _check(batch, a, sums, seen)
+
+
+@pytest.mark.parametrize("seed", range(48))
+def test_every_key_of_any_batch_is_met_once(seed):
+    import torch
+    batch = ab.drawn(seed)
+    plan, a, sums, seen = _counted(batch, seed, lambda rng, shape: rng.integers(-8, 9, shape), head_major=seed % 3 == 1, wide=seed % 2 == 1)
+    plan.run()
+    a.run()
+    torch.cuda.synchronize()
+    _check(batch, a, sums, seen)
+    if seed % 2 == 1:
+        whole = a.out._base
+        assert (whole[0] == 7).all() and (whole[:, 0] == 7).all() and (whole[..., :8] == 7).all()
 
 
 @pytest.mark.parametrize("bits", [16, 8])

@@ -4,7 +4,7 @@
 // cache elements).  A workgroup takes a few tokens: their places in the cache are looked up once, the cosines and sines of
 // all frequencies formed once for all heads of queries and keys (in LDS), then every lane moves 16-byte chunks; a lane has
 // both halves of the pairs that it turns, chunk c and chunk c + d/16 of a row, so nothing is exchanged.  8192 tokens, H 32, H_kv 8,
-// d 128, into 8 bits: 41.6 us, 4.4 TB/s; 100K tokens, d 64, bf16: 213 us, 5.2 TB/s (a large copy: 4.8); 64 single tokens 4.2-5.9 us.
+// d 128, into 8 bits: 40.3 us, 4.6 TB/s; 100K tokens, d 64, bf16: 212 us, 5.3 TB/s (a large copy: 4.8); 64 single tokens 4.4 us.
 #include <cmath>
 
 #include "sp_score_internal.h"
@@ -13,7 +13,7 @@ namespace sp {
 
 namespace {
 
-constexpr int kTokens = 4;  // most tokens of a workgroup (8192 tokens into 8 bits: 4 41.7 us, 8 42.5, 16 49.4; 100K of d = 64: 213, 220, 231)
+constexpr int kTokens = 4;  // most tokens of a workgroup (8192 tokens into 8 bits: 8 takes 2 % longer, 16 18 %; 100K of d = 64: 3 and 8 %)
 
 constexpr int64_t kMostTokens = INT64_C(1) << 25;  // of a call: a launch has fewer than 2^32 threads
 

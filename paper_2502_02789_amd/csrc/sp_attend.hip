@@ -4,21 +4,26 @@
 // and three of them, d = 64) a stretch of pieces for one KV head.  Two forms:
 //   few rows (<= 32: single tokens or several, their heads)   bound by reading keys and values.  Each wave walks over 32-key tiles of
 //     its own through LDS, with one or two 16x16 tiles of logits twice; nothing is shared before the end, and every wave has its next
-//     tile of keys and of values in flight.  64 sequences of 4096 bf16 keys, H_kv 8, d 128: 175-178 us, 6.1 TB/s; in 8 bits 98.7, 5.4
-//     (the vector instructions that widen them); d = 64, bf16 110.  Two tiles of rows instead of a large block, whose matrix tiles they
-//     would fill to a tenth: 32 sequences of 1K-3K keys, 5 to 8 tokens of 4 heads, 66.4 -> 57 us; eight in 8 bits 39.0 -> 28.6.
+//     tile of keys and of values in flight.  64 sequences of 4096 bf16 keys, H_kv 8, d 128: 177 us, 6.1 TB/s; in 8 bits 104 us, 5.2 TB/s:
+//     there the waves wait for more than half of their time, the LDS is busy for 41 % (half of it the banks that the widened chunks meet in), the
+//     vector ALUs for 20 %.  Two tiles of rows instead of a large block, whose matrix tiles they would fill to a tenth: 14 to 27 % less
+//     time; 32 sequences of 1K-3K keys and 2 to 8 tokens of 4 heads: 62 us, 4.5 TB/s.
 //   many rows (<= 256, d = 64 128: prompts, prefixes of groups)  bound by the matrix cores and the vector work between their products.
 //     The waves share 64-key tiles in LDS (two buffers, one barrier a tile; a second tile on its way in registers), each has 32 rows.
-//     6592 tokens, H 64, d 128, causal: 680-693 us, 1.03-1.05 PFLOP/s; eight prompts of 300-3000 tokens, H 32, d 64: 118-128 us, 0.6.
-//     (Blocks of at most 128 rows with the waves' halves on alternate tiles and their sums added at the end: slower, four sequences
-//     of 8K-20K keys and 28 tokens 73 -> 77 us, and 64 single tokens 111 -> 114 us by the mere size of the kernel.)
+//     6592 tokens, H 64, d 128, causal: 700-720 us, 1.0 PFLOP/s (matrix cores busy for 47 % of the clocks, vector ALUs for 43 %, at 1.93 GHz); eight
+//     prompts of 300-3000 tokens, H 32, d 64: 119 us, 0.6 (28 and 58 %).
+//     (Blocks of at most 128 rows with the waves' halves on alternate tiles and their sums added at the end: 5 % slower, and single tokens
+//     3 % by the mere size of the kernel.)
 // Both compute S^T = K Q^T, so that a lane has the logits of one row, turn the weights exp2(s - m) into bf16 in place -- the order
 // of keys in a matrix product's sum is free, and is chosen so that a lane's logits are its own operand of O^T = V^T P^T -- and read
-// V^T out of row-major LDS tiles with the transposing LDS read.  A weight's rounding to bf16, 2^-8 of itself, is what the matrix cores'
-// operands allow; logits, maxima, sums and O are fp32.  The running maximum m follows the logits only
+// V^T out of row-major LDS tiles with the transposing LDS read.  Logits, maxima, sums and O are fp32.  A weight is rounded to bf16, by 2^-8 of
+// itself at most, because a product of the matrix cores takes both operands of one type and the values are bf16; a second product with what the
+// rounding left would make that error 2^-16 and half as many products again.  The sum of weights is that of the unrounded ones, so that the lse keeps the
+// accuracy of fp32; out is off by the mean of the weights' roundings: 0.0023 of its size in all for 64 sequences of 1K-4K keys, where its own
+// rounding to bf16 makes 0.0017.  The running maximum m follows the logits only
 // where one exceeds it by more than 8 (weights stay below 2^8), so sums are rarely rescaled.
 // Compiled on the assumption that there are no NaNs; those that mark invalid rows are written as bit patterns.
-// (Nothing here may need scratch memory: workgroups that do are dispatched later, 64 single tokens 111 -> 117 us with 20 bytes of it.)
+// (Nothing here may need scratch memory: workgroups that do are dispatched later, 64 single tokens 5 % slower with 20 bytes of it.)
 #include "sp_attend_internal.h"
 #include "sp_lds.h"
 
@@ -75,7 +80,7 @@ __device__ __forceinline__ void widen_e4m3(const u32x4 w, u32x4& lo, u32x4& hi) 
 // octet lie at one stride from one base, formed in scalar registers, once for all lanes of a wave.  The page numbers of a tile's
 // keys come in a vector register, a lane each, requested a tile ahead and before that tile's loads, so that nothing waits for them
 // that does not wait for older loads anyway.  (Scalar loads share a counter with the LDS reads, whose waits then wait for both:
-// 202 -> 196 us for 64 new tokens behind 128K keys.  64 pages at a time, asked for when needed, instead of a tile's: 98.7 -> 102.6 us
+// 3 % slower for 64 new tokens behind 128K keys.  64 pages at a time, asked for when needed, instead of a tile's: 4 % slower
 // for 64 sequences of 4096 8-bit keys.)
 template <bool PAGED>
 struct KeyRows {

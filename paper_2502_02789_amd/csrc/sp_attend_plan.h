@@ -8,10 +8,11 @@
 //
 // The device has room for attend_items() workgroups at once.  With fewer than three times as many (large block, KV head) pairs, blocks
 // are laid end to end, each at its cost, and cut into as many stretches of equal cost as there is room for: every workgroup has one, and
-// all end together.  With more than that a workgroup takes one block, and the device the next as one gets done, longest first; only a
-// block longer than a workgroup's equal share is cut.  Both measured (stretches, blocks): 64 sequences of 1K-4K keys 114, 127 us; 64
-// that share 32K 75, 79; two pieces of 500 tokens behind 17K 335, 466; but, with more blocks than the rule allows, 6592 tokens of 64
-// heads 833, 679; eight prompts of 300-3000 tokens, d = 64, 150, 123.
+// all end together.  With more than that a workgroup takes one block, and the device the next as one gets done, from the last sequence's last
+// block to the first's first: longest first within a sequence, but sequences as they lie in the batch, whatever their lengths.  Only a
+// block longer than a workgroup's equal share is cut.  Both measured, stretches against blocks: 64 sequences of 1K-4K keys 10 % less
+// time, 64 that share 32K 5 %, two pieces of 500 tokens behind 17K 28 %; but, with more blocks than the rule allows, 6592 tokens of 64
+// heads 23 % more, eight prompts of 300-3000 tokens, d = 64, 22 % more.
 //
 // A block of one piece whose rows have no shared prefix is finished by its workgroup; the pieces of all others leave their
 // sums in slots of the workspace, which a second kernel joins.
@@ -142,21 +143,21 @@ SP_ATTEND_FN int own_block_keys(int rows, int i, int m, int G, int n, int len, i
 SP_ATTEND_FN int block_steps(int first, int keys) { return (int)(((uint32_t)(first & (kPieceStep - 1)) + (uint32_t)keys + kPieceStep - 1) / kPieceStep); }
 
 // A piece of few rows and few keys is not worth all waves: where several follow one another, they share the waves.  (64 sequences of
-// 200-1000 keys 37.7 -> 35.0 us; up to 4096 keys instead of 1024: the same, but 64 that share 32K 74.7 -> 75.8.)
+// 200-1000 keys take 7 % less time so; up to 4096 keys instead of 1024: the same, but 64 that share 32K 1.5 % more.)
 SP_ATTEND_FN bool is_short(int rows, int keys) { return rows <= kFewRows && keys <= 1024; }
 
 // What a step costs a workgroup, in units of 0.27 us (d = 128) and 0.67 us on a full device: few rows are bound by reading 64 keys
 // and values, more by the matrix cores; and what a piece costs besides.  (Few and many rows alike: 24 sequences of 1 to 8 new tokens
-// that share 8K 49.5 -> 51.6 us, two pieces of 500 tokens behind 17K 335 -> 342; large blocks alike, however many
-// of their rows are there: 32 sequences that share 32K 8-bit keys 41 -> 45.6.)
+// that share 8K 4 % slower, two pieces of 500 tokens behind 17K 2 %; large blocks alike, however many
+// of their rows are there: 32 sequences that share 32K 8-bit keys 11 %.)
 SP_ATTEND_FN int step_cost(int rows, int d, bool fp8) {
   if (rows <= kTileRows) return d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5);
   if (rows <= kFewRows) return d == 64 ? 4 : fp8 ? 4 : 6;
   return d == 64 ? 4 : rows > many_rows(d) / 2 ? 8 : fp8 ? 5 : 6;
 }
 SP_ATTEND_FN int piece_cost(int rows, int keys, int d) { return d == 64 ? (is_short(rows, keys) ? 2 : 4) : is_short(rows, keys) ? 3 : 12; }
-// No stretch costs less: more than a step of any kind.  (Three times as much: one token behind 1000 keys 11.7 -> 12.2 us, 64 that
-// share 32K 74.7 -> 76.3.)
+// No stretch costs less: more than a step of any kind.  (Three times as much: one token behind 1000 keys 4 % slower, 64 that share
+// 32K 2 %.)
 SP_ATTEND_FN int least_stretch(int d) { return d == 64 ? 10 : 11; }
 
 // Whether `members` sequences with `rows` rows in all, about as many each, have the `prefix` tokens that they share read once for all of them.

@@ -1,15 +1,15 @@
 // sp_attend_plan: the list of pieces of work of an attention call, made on the device from the lengths (which only the
 // device knows, so that a captured graph follows them), and the kernel that joins the pieces' sums.  The cut itself is in sp_attend_plan.h.
 // The plan is bound by its chain of dependent reads and barriers and by fetching its own code (one workgroup): 14 us for one sequence,
-// 20 for 64, 25 for 64 that share a prefix; a step makes it once for all layers.
+// 20 for 64, 25 for 64 that share a prefix, 9 for a long prompt whose blocks are not laid end to end; a step makes it once for all layers.
 #include "sp_attend_internal.h"
 
 namespace sp {
 
 namespace {
 
-constexpr int kPlanThreads = 512;  // (1024, whose registers do not do: 28.1 us instead of 14.2 for one sequence, 34.8 instead of 21.1 for 64, 44.9 and
-                                   // 38.1 for 64 that share a prefix; 256: 13.4, 21.1, 49.7)
+constexpr int kPlanThreads = 512;  // (1024, whose registers do not do: twice the time for one sequence, 1.2 times for 64 that share a prefix; 256: a
+                                   // twentieth less for one, 1.3 times for 64 that share a prefix)
 
 struct PlanSeq { int32_t t0, n, len, shared; };                 // len -1: invalid
 struct PlanGroup { int32_t shared, active, t0, tokens, slot, pieces, pad[2]; };
@@ -439,7 +439,8 @@ struct JoinDev {
 // fixes.  Bound by its dependent reads (record; maxima, weights' sums and values together) where rows are few and by reading the sums
 // where they are many: d / 4 lanes take a row's pieces one after the other, four in flight, 16 bytes a lane; with more than 16 pieces to
 // a row, or more than 4 of few rows, all of the workgroup's lanes take one row, every eighth (sixteenth, d = 64) piece each group of lanes
-// (from 5 pieces on for all: one token behind 1000 keys 11.5 -> 10.8 us, but 32 sequences that share 8K 66 -> 70-75).  (Compiled with NaNs honoured: invalid rows have a NaN for l.)
+// (from 5 pieces on for all: one token behind 1000 keys 6 % faster, but 32 sequences that share 8K 6 to 14 % slower).
+// 32 (row, KV head) pairs of 7 pieces 3.3 us, 2048 of 23 or 24 8.0, 33760 of two or three 13.8.  (Compiled with NaNs honoured: invalid rows have a NaN for l.)
 template <int D>
 __global__ __launch_bounds__(256) void attend_join_kernel(const JoinDev p) {
   constexpr int L = D / 4, GROUPS = 256 / L;

@@ -10,7 +10,7 @@
 //     time; 32 sequences of 1K-3K keys and 2 to 8 tokens of 4 heads: 62 us, 4.5 TB/s.
 //   many rows (<= 256, d = 64 128: prompts, prefixes of groups)  bound by the matrix cores and the vector work between their products.
 //     The waves share 64-key tiles in LDS (two buffers, one barrier a tile; a second tile on its way in registers), each has 32 rows.
-//     6592 tokens, H 64, d 128, causal: 700-720 us, 1.0 PFLOP/s (matrix cores busy for 47 % of the clocks, vector ALUs for 43 %, at 1.93 GHz); eight
+//     6592 tokens, H 64, d 128, causal: 690-720 us, 1.0 PFLOP/s (matrix cores busy for 48 % of the clocks, vector ALUs for 43 %, at 1.93 GHz); eight
 //     prompts of 300-3000 tokens, H 32, d 64: 119 us, 0.6 (28 and 58 %).
 //     (Blocks of at most 128 rows with the waves' halves on alternate tiles and their sums added at the end: 5 % slower, and single tokens
 //     3 % by the mere size of the kernel.)

@@ -190,7 +190,9 @@ def _check_rows(t, T: int, heads: Optional[int], d: int, name: str):
 
 
 class _OnDevice:
-    """Calls go to the tensors' own device, whatever the current one is, and to its current stream unless one is given."""
+    """Calls go to the tensors' own device, whatever the current one is, and to its current stream unless one is given.  What a constructor
+    allocates (the plan is cleared, so that none is taken for one) belongs to the stream that is current then: as with any tensor, a caller lets another
+    stream wait for it before the first call there."""
 
     def _call(self, fn, args, stream):
         if torch.cuda.current_device() == self._device.index:

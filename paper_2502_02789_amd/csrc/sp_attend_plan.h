@@ -161,19 +161,20 @@ SP_ATTEND_FN int piece_cost(int rows, int keys, int d) { return d == 64 ? (is_sh
 SP_ATTEND_FN int least_stretch(int d) { return d == 64 ? 10 : 11; }
 
 // Whether `members` sequences with `rows` rows in all, about as many each, have the `prefix` tokens that they share read once for all of them.
-// Without that each reads them, the first at a step's cost and the others out of the caches, at 2 a step for few rows and 4 for more.  With
-// it the rows' blocks read them once, but every row of every member leaves its sums to the join, at about 2 (d = 64: 1) a row.  Measured
+// Without that each reads them, the first at a step's cost and the others out of the caches, at 2 a step for one tile of rows, 3 for two and 5
+// for more.  With it the rows' blocks read them once, but every row of every member leaves its sums to the join, which with what its
+// prefix's block costs besides comes to 5/4 a row.  (A step is 64 keys.)  Measured
 // (read by each, once for all): 64 sequences, 1000 keys of their own, four heads: 64 shared tokens 47.7, 50.4 us, 512 54.8, 49.9, 4096 113,
 // 55.7; four new tokens each: 64 48.9, 68.0, 512 55.6, 64.9, 2048 76.7, 63.6; 24 sequences of 8 tokens of eight heads: 512 41.3, 44.5,
-// 4096 86.1, 66.8; two of one token: 4096 12.7, 12.4.  Over 2456 such calls the rule loses 1.4 % against the better of the two, sharing always
-// 8.6 % (at worst 2.6 times), never 19 %.
+// 4096 86.1, 66.8; two of one token: 4096 12.7, 12.4.  Over 2456 such calls the rule loses 1.8 % against the better of the two (at worst 1.5
+// times; against sharing always 1.3), sharing always 8.6 % (at worst 2.6 times), never 19 %.
 SP_ATTEND_FN bool prefix_pays(int rows, int members, int prefix, int d, bool fp8) {
   if (prefix <= 0 || !shares(rows, members)) return false;
   const int own = (int)((uint32_t)rows / (uint32_t)members), many = many_rows(d), whole = rows > kFewRows ? (int)((uint32_t)rows / (uint32_t)many) : 0;
   const int rest = rows - whole * many;
-  const int64_t each = step_cost(own, d, fp8) + (int64_t)(members - 1) * (own <= kFewRows ? 2 : 4);
+  const int64_t each = step_cost(own, d, fp8) + (int64_t)(members - 1) * (own <= kTileRows ? 2 : own <= kFewRows ? 3 : 5);
   const int64_t once = (int64_t)whole * step_cost(many, d, fp8) + (rest > 0 ? step_cost(rest, d, fp8) : 0);
-  return block_steps(0, prefix) * (each - once) >= (int64_t)rows * (d / 64);
+  return prefix * (each - once) >= (int64_t)rows * (kPieceStep * 5 / 4);
 }
 
 // many: blocks of more than 32 rows (the others are cheap to cut)

@@ -64,7 +64,11 @@ typedef enum { SP_LAYER_MAX = 0, SP_LAYER_MEAN = 1 } sp_layer_reduce;
  * accumulated in fp32; the scale joins the logit scale.  Scores therefore meet the same tolerance against
  * the definition evaluated on the decoded keys as a bf16 cache does.  NaN codes are a precondition
  * violation like NaN in a bf16 cache. */
-typedef enum { SP_K_BF16 = 0, SP_K_FP8_E4M3 = 1 } sp_k_dtype;
+typedef enum {
+  SP_K_BF16 = 0,
+  SP_K_FP8_E4M3 = 1,
+  SP_K_MXFP4 = 4         /* of the cache calls below (see there), not of sp_score */
+} sp_k_dtype;
 
 #define SP_MAX_LAYERS 128
 #define SP_MAX_QUERIES 16
@@ -337,14 +341,20 @@ SP_API sp_status sp_gather(const sp_gather_args* args, void* hip_stream);
  *               g*cache_head_stride + t; sequence b owns the rows up to d_cu_cache[b+1] (int32 [B+1], non-decreasing)
  * Keys and values are two arrays of the same layout and type (sp_k_dtype); 8-bit elements stand for
  * scale[g] * decode(byte), one fp32 scale per KV head (finite) for the keys and one for the values, NULL = all 1.
+ * SP_K_MXFP4 holds 4.25 bits per element (OCP Microscaling, MXFP4): E2M1 codes (1 sign, 2 exponent, 1 mantissa bit, bias 1:
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two to a byte, the even element in the low half, and one E8M0 scale, the
+ * byte s for 2^(s - 127), 255 for NaN, to 32 elements that follow one another in a head.  Codes and scales are separate arrays of the
+ * same layout: the codes of the elements from offset e on begin at byte e / 2, and the scale of the block that begins at offset e
+ * is byte e / 32 of the scales.  The strides still count elements, and are multiples of 32 (16 bytes of codes).  Heads outermost in a page (token
+ * stride d) keep a head's codes and scales of neighbouring tokens side by side, which sp_attend reads fastest.
  * n_rows is the number of token rows of the pool (pages * page_size) or of the contiguous cache.  Nothing outside it
  * is read or written, whatever the tables hold: a page number outside the pool or a row outside the cache is answered as
  * stated at each call.  New tokens of sequence b are rows [d_cu_new[b], d_cu_new[b+1]) of a flat axis with
  * room for T_new tokens (d_cu_new[0] = 0, non-decreasing, d_cu_new[B] <= T_new; rows at and beyond d_cu_new[B] are
  * neither read nor written).  Limits: d 64 or 128, H <= 1024, H % H_kv == 0,
  * H / H_kv <= 16, T_new * H < 2^31, T_new of an append <= 2^25.  With T_new = 0 the pointers to new tokens may be NULL.
- * Pointers to bf16 or 8-bit data are 16-byte aligned; strides count elements and are multiples of 8
- * (of an 8-bit cache: 16).
+ * Pointers to bf16, 8-bit or 4-bit data are 16-byte aligned, those to block scales need not be; strides count elements and are multiples
+ * of 8 (of an 8-bit cache: 16, of a 4-bit one: 32).
  * --------------------------------------------------------------------------- */
 
 /* sp_cache_append: for new token j of sequence b (flat row t = cu_new[b] + j), at cache index i = cache_len[b] + j and
@@ -353,7 +363,11 @@ SP_API sp_status sp_gather(const sp_gather_args* args, void* hip_stream);
  * R_p turns the pair (m, m + d/2) by the angle p * f_m, f_m = inv_freq[m] or rope_theta^(-2m/d): the angle in fp64, its
  * cosine and sine rounded to fp32, the products and their sum separate fp32 operations.  Results are rounded once: to
  * bf16 (nearest even), or divided by the scale in fp32 and rounded to E4M3 (nearest even; beyond +-448 the largest finite
- * value; NaN stays NaN; a scale of zero stores zeros).  A bf16 cache filled so holds bit for bit what
+ * value; NaN stays NaN; a scale of zero stores zeros), or, 32 of a head at a time, quantised to MXFP4: the scale is the smallest power of
+ * two, 2^-125 at least, whose seven-fold no magnitude of the block exceeds, the codes are the values divided by it rounded
+ * to the nearest (even), beyond 6 the largest; a block with a NaN or an infinity gets the scale NaN.  (Seven rather than six, with which nothing is
+ * cut off: the codes' steps are finer, the error of normally distributed values 3 % smaller.  Magnitudes from 2^127 on may come back as infinity.)
+ * A bf16 cache filled so holds bit for bit what
  * sp_score with rope_theta > 0 makes of an unrotated one.
  * A token whose cache index is negative or outside its sequence's room (blocks_per_seq * page_size tokens, or its rows of a
  * contiguous cache) or whose page number lies outside the pool is not written to the cache; its row of q_out is.
@@ -394,16 +408,61 @@ typedef struct {
   int32_t cache_dtype;       /* sp_k_dtype                                                            */
   const float* d_k_scale;    /* fp32 [H_kv] of an 8-bit cache, or NULL (all 1)                        */
   const float* d_v_scale;    /* fp32 [H_kv] of an 8-bit cache, or NULL (all 1)                        */
+  uint8_t* d_k_block_scale;  /* out: E8M0 scales of a 4-bit cache, else NULL                          */
+  uint8_t* d_v_block_scale;  /* out: E8M0 scales of a 4-bit cache, else NULL                          */
 } sp_cache_append_args;
 
 /* Enqueue the append on hip_stream.  Needs no workspace. */
 SP_API sp_status sp_cache_append(const sp_cache_append_args* args, void* hip_stream);
+
+/* sp_cache_read: tokens of the cache as bf16 keys and values, for what takes no quantised cache (sp_score of an MXFP4 one) or
+ * no block table, or for moving tokens: for row t of sequence b (cu_rows[b] <= t < cu_rows[b+1]), j = t - cu_rows[b], and
+ * i = first[b] + index[t] (d_index NULL: j for index[t]; d_first NULL: 0 for first[b]):
+ *     k_out[t, g, :] = K[i, g, :],   v_out[t, g, :] = V[i, g, :]
+ * in bf16: values of bf16 and MXFP4 caches, and of E4M3 ones without scales, are exact, those of E4M3 with scales are formed in fp32 and rounded to
+ * nearest even; NaN stays NaN.  A row whose token i is negative or outside its sequence's room, or whose page number lies outside the pool, becomes NaN.  Any tokens may be
+ * asked for in any order, one of them several times.  Rows at and beyond cu_rows[B] are left as they are.  Limits: T_rows <= 2^25.  No two rows of an
+ * output overlap (strides below d, where there are several heads or rows: SP_EINVAL), k_out and v_out are different arrays, and both overlap no input. */
+typedef struct {
+  int32_t B;                 /* sequences, >= 1                                                       */
+  int32_t H_kv;              /* key and value heads, <= 1024                                          */
+  int32_t d;                 /* head dim: 64 or 128                                                   */
+  int64_t T_rows;            /* rows of k_out and v_out                                               */
+  const int32_t* d_cu_rows;  /* int32 [B+1], d_cu_rows[0] = 0, non-decreasing, d_cu_rows[B] <= T_rows */
+  const int32_t* d_first;    /* int32 [B], or NULL (0)                                                */
+  const int32_t* d_index;    /* int32 [T_rows], or NULL (0, 1, .. in each sequence)                   */
+  const void* d_k_cache;
+  const void* d_v_cache;     /* or NULL: keys only                                                    */
+  int64_t cache_token_stride;
+  int64_t cache_head_stride;
+  int64_t cache_page_stride; /* (ignored if not paged)                                                */
+  const int32_t* d_cu_cache; /* contiguous cache: int32 [B+1], else NULL                              */
+  const int32_t* d_block_table; /* paged cache: int32 [B, blocks_per_seq], else NULL                  */
+  int32_t page_size;         /* (ignored if not paged)                                                */
+  int32_t blocks_per_seq;    /* (ignored if not paged)                                                */
+  int64_t n_rows;            /* token rows of the cache, < 2^31                                       */
+  int32_t cache_dtype;       /* sp_k_dtype                                                            */
+  const float* d_k_scale;    /* fp32 [H_kv] of an 8-bit cache, or NULL (all 1)                        */
+  const float* d_v_scale;    /* fp32 [H_kv] of an 8-bit cache, or NULL (all 1)                        */
+  const uint8_t* d_k_block_scale; /* E8M0 scales of a 4-bit cache, else NULL                          */
+  const uint8_t* d_v_block_scale; /* E8M0 scales of a 4-bit cache, else NULL                          */
+  void* d_k_out;             /* out bf16 [T_rows, H_kv, d], any token and head strides                */
+  int64_t k_out_token_stride;
+  int64_t k_out_head_stride;
+  void* d_v_out;             /* out bf16 [T_rows, H_kv, d], any token and head strides, NULL iff d_v_cache is */
+  int64_t v_out_token_stride;
+  int64_t v_out_head_stride;
+} sp_cache_read_args;
+
+/* Enqueue the read on hip_stream.  Needs no workspace. */
+SP_API sp_status sp_cache_read(const sp_cache_read_args* args, void* hip_stream);
 
 /* sp_attend: attention of the new tokens over the cache, causal.  Sequence b has kv_len[b] tokens in the cache, its
  * n_b new ones (appended before the call) the last of them, so new token j sees the first
  * n_vis = clamp(kv_len[b] - n_b + j + 1, 0, kv_len[b]) tokens.  For query head h and KV head g = h / (H/H_kv), t = cu_new[b] + j:
  *     s_i = scale * k_scale[g] * <q[t, h, :], K[i, g, :]>,  i < n_vis
  *     out[t, h, :] = sum_i softmax(s)_i * v_scale[g] * V[i, g, :]   (rounded once to bf16),   lse[t, h] = log sum_i exp(s_i)
+ * (k_scale and v_scale 1 but for an 8-bit cache; the values of a 4-bit one, scales applied, are what K and V stand for, and exact.)
  * A row that sees no token gets out = 0 and lse = -infinity.  Logits, maxima, sums and the accumulation of out are
  * fp32; the weights exp(s_i - m) are rounded to bf16 for the product with the values, as the values are.
  * NaN/Inf among the queries, or the keys and values of the first kv_len[b] tokens, are precondition violations
@@ -465,6 +524,8 @@ typedef struct {
   size_t plan_bytes;
   void* d_workspace;         /* 256-byte aligned; not read by sp_attend_plan                          */
   size_t workspace_bytes;
+  const uint8_t* d_k_block_scale; /* E8M0 scales of a 4-bit cache, else NULL (not read by sp_attend_plan) */
+  const uint8_t* d_v_block_scale; /* E8M0 scales of a 4-bit cache, else NULL (not read by sp_attend_plan) */
 } sp_attend_args;
 
 /* Bytes of d_plan and of d_workspace for the shape fields (pointers are not read); 0 if these are invalid. */
@@ -472,6 +533,59 @@ SP_API size_t sp_attend_plan_bytes(const sp_attend_args* args);
 SP_API size_t sp_attend_workspace_bytes(const sp_attend_args* args);
 SP_API sp_status sp_attend_plan(const sp_attend_args* args, void* hip_stream);
 SP_API sp_status sp_attend(const sp_attend_args* args, void* hip_stream);
+
+/* ---------------------------------------------------------------------------
+ * sp_verify: which drafted tokens stand, and the token behind them.  Sequence b has n_b = cu_draft[b+1] - cu_draft[b] drafted tokens
+ * x_0, x_1, .. (rows t = cu_draft[b] + j of d_tokens, d_u and d_draft; n_b may be 0) and n_b + 1 rows of the target's logits, rows
+ * cu_draft[b] + b + j of d_target: row j is what the target says of the place of x_j, the last one of the place behind them all.  With
+ *     p_j = softmax(target row j / temperature[b]),   q_j = softmax(draft row j / temperature[b])
+ * (at temperature 0 everything at the largest logit, the lowest index of equal ones; without d_draft q_j is 1 at x_j: tokens that were looked up, not sampled)
+ *     x_j stands  if all before it do and u_j * q_j(x_j) < p_j(x_j)
+ *     a           = the number of tokens that stand
+ *     w           = max(p_a - q_a, 0), or p_a where a = n_b, or where that leaves nothing
+ *     y           = the lowest index k with  w(0) + .. + w(k) > r_b * (w(0) + .. + w(V-1))      (the last k with w(k) > 0, if rounding leaves none)
+ * so that x_0 .. x_(a-1), y are distributed as the target's own tokens if u and r are independent and uniform in [0, 1) and x_j was drawn from q_j.  Outputs:
+ *     n_accepted[b] = a;   out_tokens of rows cu_draft[b] + b + j: x_j for j < a, y for j = a, -1 behind;
+ *     logprob: log p_j of these tokens, -infinity behind;   kept_len[b] = past_len[b] + 1 + a
+ * (kept_len: of a step that appended the last token and the drafted ones behind past_len[b] tokens, what of the cache stands).
+ * Logits may be off by a constant in each row (log-probabilities will do) and -infinity (probability 0).  Sums, probabilities and comparisons are such
+ * that y and a are those of exact arithmetic unless a border lies within about 1e-12 of the number that decides: the weights of y's row are
+ * formed and added in fp64, in an order that does not change.
+ * In band: a sequence that meets a row with a NaN, a +infinity or nothing but -infinity, before or at its row a, or a drafted token outside [0, V), or a
+ * negative or NaN temperature, gets n_accepted = -1, out_tokens -1 and logprob NaN in all of its rows, and kept_len = past_len.  What lies in rows behind row
+ * a does not matter.
+ * Limits: V < 2^24, T + B < 2^24, at most SP_VERIFY_MAX_DRAFTED drafted tokens for a sequence (one with more: as above).  Rows are contiguous, their strides in
+ * elements >= V where there are several; the pointers are aligned to their type.  Rows of out_tokens and logprob at and beyond cu_draft[B] + B are left as they are.
+ * --------------------------------------------------------------------------- */
+typedef enum { SP_LOGITS_BF16 = 0, SP_LOGITS_F32 = 1 } sp_logits_dtype;
+#define SP_VERIFY_MAX_DRAFTED 63
+
+typedef struct {
+  int32_t B;                 /* sequences, >= 1                                                       */
+  int32_t V;                 /* vocabulary, >= 1                                                      */
+  int64_t T;                 /* rows of d_tokens, d_u and d_draft; d_target has T + B                 */
+  const int32_t* d_cu_draft; /* int32 [B+1], d_cu_draft[0] = 0, non-decreasing, d_cu_draft[B] <= T    */
+  const int32_t* d_tokens;   /* int32 [T] drafted tokens (NULL allowed if T = 0)                      */
+  const void* d_target;      /* [T + B, V] logits                                                     */
+  int64_t target_stride;
+  const void* d_draft;       /* [T, V] logits, or NULL: the tokens were not sampled                   */
+  int64_t draft_stride;
+  int32_t logits_dtype;      /* sp_logits_dtype, of both                                              */
+  const float* d_temperature;/* fp32 [B], or NULL (all 1)                                             */
+  const float* d_u;          /* fp32 [T] in [0, 1) (NULL allowed if T = 0)                            */
+  const float* d_r;          /* fp32 [B] in [0, 1)                                                    */
+  const int32_t* d_past_len; /* int32 [B], NULL iff d_kept_len is                                     */
+  int32_t* d_n_accepted;     /* out int32 [B]                                                         */
+  int32_t* d_out_tokens;     /* out int32 [T + B]                                                     */
+  float* d_logprob;          /* out fp32 [T + B], or NULL                                             */
+  int32_t* d_kept_len;       /* out int32 [B], or NULL; may be d_past_len itself                      */
+  void* d_workspace;         /* 256-byte aligned                                                      */
+  size_t workspace_bytes;
+} sp_verify_args;
+
+/* Bytes of d_workspace for the shape fields (pointers are not read); 0 if these are invalid. */
+SP_API size_t sp_verify_workspace_bytes(const sp_verify_args* args);
+SP_API sp_status sp_verify(const sp_verify_args* args, void* hip_stream);
 
 /* Static, never-NULL description of a status code. */
 SP_API const char* sp_strerror(sp_status status);

@@ -17,15 +17,17 @@ SP_LAYER_MAX, SP_LAYER_MEAN = 0, 1
 SP_MAX_LAYERS, SP_MAX_QUERIES = 128, 16
 SP_SCORE_EXCLUSIVE_DEVICE = 1
 SP_SCORE_WORKSPACE_KEPT = 2
-SP_K_BF16, SP_K_FP8_E4M3 = 0, 1
+SP_K_BF16, SP_K_FP8_E4M3, SP_K_MXFP4 = 0, 1, 4
+SP_LOGITS_BF16, SP_LOGITS_F32 = 0, 1
+SP_VERIFY_MAX_DRAFTED = 63
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libspecprefill.so")
 
 EXPORTS = (
     "sp_score_workspace_bytes", "sp_score", "sp_score_general", "sp_score_check", "sp_set_wait_budget",
     "sp_keep_upper_bound", "sp_pool_select_workspace_bytes", "sp_pool_select", "sp_pool_select_static", "sp_score_pool_select",
-    "sp_gather", "sp_cache_append", "sp_attend_plan_bytes", "sp_attend_workspace_bytes", "sp_attend_plan", "sp_attend",
-    "sp_strerror", "sp_version",
+    "sp_gather", "sp_cache_append", "sp_cache_read", "sp_attend_plan_bytes", "sp_attend_workspace_bytes", "sp_attend_plan", "sp_attend",
+    "sp_verify_workspace_bytes", "sp_verify", "sp_strerror", "sp_version",
 )
 
 
@@ -79,6 +81,21 @@ class CacheAppendArgs(C.Structure):
         ("cache_head_stride", C.c_int64), ("cache_page_stride", C.c_int64), ("d_cu_cache", C.c_void_p),
         ("d_block_table", C.c_void_p), ("page_size", C.c_int32), ("blocks_per_seq", C.c_int32), ("n_rows", C.c_int64),
         ("cache_dtype", C.c_int32), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p),
+        ("d_k_block_scale", C.c_void_p), ("d_v_block_scale", C.c_void_p),
+    ]
+
+
+class CacheReadArgs(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32), ("T_rows", C.c_int64),
+        ("d_cu_rows", C.c_void_p), ("d_first", C.c_void_p), ("d_index", C.c_void_p),
+        ("d_k_cache", C.c_void_p), ("d_v_cache", C.c_void_p), ("cache_token_stride", C.c_int64),
+        ("cache_head_stride", C.c_int64), ("cache_page_stride", C.c_int64), ("d_cu_cache", C.c_void_p),
+        ("d_block_table", C.c_void_p), ("page_size", C.c_int32), ("blocks_per_seq", C.c_int32), ("n_rows", C.c_int64),
+        ("cache_dtype", C.c_int32), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p),
+        ("d_k_block_scale", C.c_void_p), ("d_v_block_scale", C.c_void_p),
+        ("d_k_out", C.c_void_p), ("k_out_token_stride", C.c_int64), ("k_out_head_stride", C.c_int64),
+        ("d_v_out", C.c_void_p), ("v_out_token_stride", C.c_int64), ("v_out_head_stride", C.c_int64),
     ]
 
 
@@ -94,6 +111,17 @@ class AttendArgs(C.Structure):
         ("d_v_scale", C.c_void_p), ("scale", C.c_float), ("d_out", C.c_void_p), ("out_token_stride", C.c_int64),
         ("out_head_stride", C.c_int64), ("d_lse", C.c_void_p), ("d_plan", C.c_void_p), ("plan_bytes", C.c_size_t),
         ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+        ("d_k_block_scale", C.c_void_p), ("d_v_block_scale", C.c_void_p),
+    ]
+
+
+class VerifyArgs(C.Structure):
+    _fields_ = [
+        ("B", C.c_int32), ("V", C.c_int32), ("T", C.c_int64), ("d_cu_draft", C.c_void_p), ("d_tokens", C.c_void_p),
+        ("d_target", C.c_void_p), ("target_stride", C.c_int64), ("d_draft", C.c_void_p), ("draft_stride", C.c_int64),
+        ("logits_dtype", C.c_int32), ("d_temperature", C.c_void_p), ("d_u", C.c_void_p), ("d_r", C.c_void_p),
+        ("d_past_len", C.c_void_p), ("d_n_accepted", C.c_void_p), ("d_out_tokens", C.c_void_p), ("d_logprob", C.c_void_p),
+        ("d_kept_len", C.c_void_p), ("d_workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
     ]
 
 
@@ -133,6 +161,12 @@ def load_library() -> C.CDLL:
     lib.sp_gather.argtypes = [C.POINTER(GatherArgs), C.c_void_p]
     lib.sp_cache_append.restype = C.c_int
     lib.sp_cache_append.argtypes = [C.POINTER(CacheAppendArgs), C.c_void_p]
+    lib.sp_cache_read.restype = C.c_int
+    lib.sp_cache_read.argtypes = [C.POINTER(CacheReadArgs), C.c_void_p]
+    lib.sp_verify_workspace_bytes.restype = C.c_size_t
+    lib.sp_verify_workspace_bytes.argtypes = [C.POINTER(VerifyArgs)]
+    lib.sp_verify.restype = C.c_int
+    lib.sp_verify.argtypes = [C.POINTER(VerifyArgs), C.c_void_p]
     for name in ("sp_attend_plan_bytes", "sp_attend_workspace_bytes"):
         getattr(lib, name).restype = C.c_size_t
         getattr(lib, name).argtypes = [C.POINTER(AttendArgs)]
@@ -325,10 +359,16 @@ def sp_gather(args: GatherArgs, stream=None) -> None:
 
 
 # ----------------------------------------------------------------------------
-# sp_cache_append, sp_attend
+# sp_cache_append, sp_cache_read, sp_attend
 # ----------------------------------------------------------------------------
+def is_4bit(cache) -> bool:
+    """Whether a cache tensor holds E2M1 codes, two to an element (the last axis is d/2 long)."""
+    return str(cache.dtype) == "torch.float4_e2m1fn_x2"
+
+
 def _fill_cache_fields(a, k_cache, v_cache, block_table, cu_cache) -> None:
-    """The cache as sp_cache_append and sp_attend take it: [pages, page_size, H_kv, d] with a block table, or [rows, H_kv, d]."""
+    """The cache as the calls take it: [pages, page_size, H_kv, d] with a block table, or [rows, H_kv, d]; of 4 bits, float4_e2m1fn_x2
+    [.., d/2]."""
     paged = block_table is not None
     if k_cache.dim() != (4 if paged else 3):
         raise ValueError("a paged cache is [pages, page_size, H_kv, d], a contiguous one [rows, H_kv, d]")
@@ -336,19 +376,20 @@ def _fill_cache_fields(a, k_cache, v_cache, block_table, cu_cache) -> None:
         raise ValueError("keys and values must be of one shape, layout and type")
     if k_cache.stride(-1) != 1:
         raise ValueError("the head dim of the cache must be contiguous")
-    a.H_kv, a.d = int(k_cache.shape[-2]), int(k_cache.shape[-1])
-    a.cache_token_stride, a.cache_head_stride = int(k_cache.stride(-3)), int(k_cache.stride(-2))
-    a.cache_page_stride = int(k_cache.stride(0)) if paged else 0
+    per = 2 if is_4bit(k_cache) else 1  # elements of the head dim to one of the tensor
+    a.H_kv, a.d = int(k_cache.shape[-2]), per * int(k_cache.shape[-1])
+    a.cache_token_stride, a.cache_head_stride = per * int(k_cache.stride(-3)), per * int(k_cache.stride(-2))
+    a.cache_page_stride = per * int(k_cache.stride(0)) if paged else 0
     a.page_size = int(k_cache.shape[1]) if paged else 0
     a.blocks_per_seq = int(block_table.shape[1]) if paged else 0
     a.n_rows = int(k_cache.shape[0]) * (int(k_cache.shape[1]) if paged else 1)
-    a.cache_dtype = SP_K_FP8_E4M3 if k_cache.element_size() == 1 else SP_K_BF16
+    a.cache_dtype = SP_K_MXFP4 if is_4bit(k_cache) else SP_K_FP8_E4M3 if k_cache.element_size() == 1 else SP_K_BF16
     a.d_block_table, a.d_cu_cache = _ptr(block_table), _ptr(cu_cache)
 
 
 def make_cache_append_args(k, v, cu_new, k_cache, v_cache, *, q=None, q_out=None, cache_len=None, pos=None,
                            rope_theta: float = 0.0, inv_freq=None, block_table=None, cu_cache=None, k_scale=None,
-                           v_scale=None) -> CacheAppendArgs:
+                           v_scale=None, k_block_scale=None, v_block_scale=None) -> CacheAppendArgs:
     """k, v: bf16 [T_new, H_kv, d], q: bf16 [T_new, H, d] (any token and head strides)."""
     a = CacheAppendArgs()
     _fill_cache_fields(a, k_cache, v_cache, block_table, cu_cache)
@@ -362,11 +403,33 @@ def make_cache_append_args(k, v, cu_new, k_cache, v_cache, *, q=None, q_out=None
     a.rope_theta, a.d_inv_freq = float(rope_theta), _ptr(inv_freq)
     a.d_q_out, a.d_k_cache, a.d_v_cache = _ptr(q_out), _ptr(k_cache), _ptr(v_cache)
     a.d_k_scale, a.d_v_scale = _ptr(k_scale), _ptr(v_scale)
+    a.d_k_block_scale, a.d_v_block_scale = _ptr(k_block_scale), _ptr(v_block_scale)
     return a
 
 
 def sp_cache_append(args: CacheAppendArgs, stream=None) -> None:
     _check("sp_cache_append", load_library().sp_cache_append(C.byref(args), _stream_handle(stream)))
+
+
+def make_cache_read_args(k_cache, v_cache, cu_rows, k_out, v_out, *, first=None, index=None, block_table=None, cu_cache=None,
+                         k_scale=None, v_scale=None, k_block_scale=None, v_block_scale=None) -> CacheReadArgs:
+    """k_out, v_out: bf16 [T_rows, H_kv, d] (any token and head strides); v_cache and v_out None: keys only."""
+    a = CacheReadArgs()
+    _fill_cache_fields(a, k_cache, v_cache, block_table, cu_cache)
+    a.B, a.T_rows = int(cu_rows.numel()) - 1, int(k_out.shape[0])
+    a.d_cu_rows, a.d_first, a.d_index = _ptr(cu_rows), _ptr(first), _ptr(index)
+    a.d_k_cache, a.d_v_cache = _ptr(k_cache), _ptr(v_cache)
+    a.d_k_scale, a.d_v_scale = _ptr(k_scale), _ptr(v_scale)
+    a.d_k_block_scale, a.d_v_block_scale = _ptr(k_block_scale), _ptr(v_block_scale)
+    for name, t in (("k_out", k_out), ("v_out", v_out)):
+        setattr(a, "d_" + name, _ptr(t))
+        setattr(a, name + "_token_stride", 0 if t is None else int(t.stride(0)))
+        setattr(a, name + "_head_stride", 0 if t is None else int(t.stride(1)))
+    return a
+
+
+def sp_cache_read(args: CacheReadArgs, stream=None) -> None:
+    _check("sp_cache_read", load_library().sp_cache_read(C.byref(args), _stream_handle(stream)))
 
 
 def make_attend_plan_args(cu_new, kv_len, k_cache, *, H: int, total_new: int, block_table=None, cu_cache=None, cu_group=None,
@@ -383,7 +446,7 @@ def make_attend_plan_args(cu_new, kv_len, k_cache, *, H: int, total_new: int, bl
 
 
 def add_attend_args(plan_args: AttendArgs, q, k_cache, v_cache, out, *, scale: float, block_table=None, cu_cache=None,
-                    k_scale=None, v_scale=None, lse=None, workspace=None) -> AttendArgs:
+                    k_scale=None, v_scale=None, k_block_scale=None, v_block_scale=None, lse=None, workspace=None) -> AttendArgs:
     """A copy of plan_args with one layer's queries bf16 [T_new, H, d], cache and outputs."""
     a = AttendArgs()
     C.memmove(C.byref(a), C.byref(plan_args), C.sizeof(AttendArgs))
@@ -392,6 +455,7 @@ def add_attend_args(plan_args: AttendArgs, q, k_cache, v_cache, out, *, scale: f
     a.d_out, a.out_token_stride, a.out_head_stride = _ptr(out), int(out.stride(0)), int(out.stride(1))
     a.d_k_cache, a.d_v_cache = _ptr(k_cache), _ptr(v_cache)
     a.d_k_scale, a.d_v_scale = _ptr(k_scale), _ptr(v_scale)
+    a.d_k_block_scale, a.d_v_block_scale = _ptr(k_block_scale), _ptr(v_block_scale)
     a.scale, a.d_lse = float(scale), _ptr(lse)
     a.d_workspace = _ptr(workspace)
     a.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
@@ -412,3 +476,31 @@ def sp_attend_plan(args: AttendArgs, stream=None) -> None:
 
 def sp_attend(args: AttendArgs, stream=None) -> None:
     _check("sp_attend", load_library().sp_attend(C.byref(args), _stream_handle(stream)))
+
+
+# ----------------------------------------------------------------------------
+# sp_verify
+# ----------------------------------------------------------------------------
+def make_verify_args(target, tokens, cu_draft, u, r, n_accepted, out_tokens, *, draft=None, temperature=None, past_len=None,
+                     logprob=None, kept_len=None, workspace=None) -> VerifyArgs:
+    """target: bf16 or fp32 [T + B, V] logits, draft: alike [T, V] or None (any row strides)."""
+    a = VerifyArgs()
+    a.B, a.V, a.T = int(cu_draft.numel()) - 1, int(target.shape[1]), int(tokens.numel())
+    a.d_cu_draft, a.d_tokens = _ptr(cu_draft), _ptr(tokens)
+    a.d_target, a.target_stride = _ptr(target), int(target.stride(0))
+    a.d_draft, a.draft_stride = _ptr(draft), 0 if draft is None else int(draft.stride(0))
+    a.logits_dtype = SP_LOGITS_F32 if target.element_size() == 4 else SP_LOGITS_BF16
+    a.d_temperature, a.d_u, a.d_r = _ptr(temperature), _ptr(u), _ptr(r)
+    a.d_past_len, a.d_kept_len = _ptr(past_len), _ptr(kept_len)
+    a.d_n_accepted, a.d_out_tokens, a.d_logprob = _ptr(n_accepted), _ptr(out_tokens), _ptr(logprob)
+    a.d_workspace = _ptr(workspace)
+    a.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return a
+
+
+def sp_verify_workspace_bytes(args: VerifyArgs) -> int:
+    return int(load_library().sp_verify_workspace_bytes(C.byref(args)))
+
+
+def sp_verify(args: VerifyArgs, stream=None) -> None:
+    _check("sp_verify", load_library().sp_verify(C.byref(args), _stream_handle(stream)))

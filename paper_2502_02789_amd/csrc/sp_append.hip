@@ -37,6 +37,8 @@ struct AppendDev {
   uint16_t* q_out;
   char* k_cache;
   char* v_cache;
+  uint8_t* k_block_scale;
+  uint8_t* v_block_scale;
 };
 
 // two fp32 values over a scale -> two E4M3 codes in the low half (nearest even, saturating; NaN stays NaN)
@@ -46,6 +48,27 @@ __device__ __forceinline__ uint32_t e4m3_pair(float a, float b, float scale) {
   a = a > 448.f ? 448.f : a < -448.f ? -448.f : a;
   b = b > 448.f ? 448.f : b < -448.f ? -448.f : b;
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xffffu;
+}
+
+// The E8M0 scale of the 32 values that the lanes of a quad hold, eight each: the smallest power of two, 2^-125 at least, whose seven-fold
+// is no less than any magnitude.  (The bits of a magnitude, taken as an integer, ascend with it, NaN and infinity last; 1.75 = 7/4 is
+// where the exponent goes up.)
+__device__ __forceinline__ uint32_t block_scale(const float (&x)[8]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xf, 0xf, false));  // the quad's lanes 1, 0, 3, 2
+  top = max(top, (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xf, 0xf, false));  // 2, 3, 0, 1
+  return top >= 0x7f800000u ? 255u : (uint32_t)max((int)((top + 0x1fffffu) >> 23) - 2, 2);
+}
+
+// eight values over a scale -> E2M1 codes (the instruction rounds to nearest even and saturates at 6)
+__device__ __forceinline__ uint32_t e2m1_codes(const float (&x)[8], float scale) {
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
 }
 
 // eight values as the cache holds them
@@ -68,8 +91,9 @@ __device__ __forceinline__ void widen(const u32x4 w, float (&x)[8]) {
 
 }  // namespace
 
-template <int D, bool FP8, bool ROPE>
+template <int D, int KIND, bool ROPE>
 __global__ __launch_bounds__(256) void append_kernel(const AppendDev p) {
+  constexpr bool FP8 = KIND == SP_K_FP8_E4M3, FP4 = KIND == SP_K_MXFP4;
   constexpr int C = D / 16;  // pairs of chunks of a row
   __shared__ int32_t cu_lds[kStagedOffsets];
   __shared__ int64_t place[kTokens];     // byte offset of the token's row in the cache, or -1
@@ -94,7 +118,7 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendDev p) {
       const int64_t lo = p.cu_cache[b], row = lo + i;
       if (ours && i >= 0 && lo >= 0 && row < p.cu_cache[b + 1] && row < (int64_t)p.n_rows) at = row * p.c_ts;
     }
-    place[threadIdx.x] = at < 0 ? -1 : at * (FP8 ? 1 : 2);
+    place[threadIdx.x] = at < 0 ? -1 : FP4 ? at / 2 : at * (FP8 ? 1 : 2);
     if constexpr (ROPE) position[threadIdx.x] = p.pos ? p.pos[t] : (int)i;
   }
   __syncthreads();
@@ -130,6 +154,19 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendDev p) {
     } else if (place[tl] >= 0) {
       const bool key = r < p.H + p.H_kv;
       const int g = r - p.H - (key ? 0 : p.H_kv);
+      if constexpr (FP4) {  // (a quad's four chunks are one block: a row has a multiple of four)
+        const int64_t at = place[tl] + (g * p.c_hs + 8 * c) / 2;
+        char* codes = (key ? p.k_cache : p.v_cache) + at;
+        uint8_t* scales = (key ? p.k_block_scale : p.v_block_scale) + at / 16;
+        const uint32_t s_lo = block_scale(lo), s_hi = block_scale(hi);
+        *reinterpret_cast<uint32_t*>(codes) = e2m1_codes(lo, __uint_as_float(s_lo << 23));
+        *reinterpret_cast<uint32_t*>(codes + D / 4) = e2m1_codes(hi, __uint_as_float(s_hi << 23));
+        if ((c & 3) == 0) {
+          scales[0] = (uint8_t)s_lo;
+          scales[D / 64] = (uint8_t)s_hi;
+        }
+        continue;
+      }
       const float* scales = key ? p.k_scale : p.v_scale;
       const float scale = FP8 && scales ? scales[g] : 1.f;
       constexpr int E = FP8 ? 1 : 2;
@@ -149,12 +186,14 @@ sp_status check_append(const sp_cache_append_args* a) {
   if (queries && (a->H < 1 || a->H > 1024 || a->H % a->H_kv != 0 || a->H / a->H_kv > 16)) return SP_EINVAL;
   if (a->T_new >= INT64_C(0x80000000) / (queries ? a->H : a->H_kv) || a->T_new > kMostTokens) return SP_EINVAL;
   if (a->n_rows < 1 || a->n_rows >= INT64_C(0x80000000)) return SP_EINVAL;
-  if (a->cache_dtype != SP_K_BF16 && a->cache_dtype != SP_K_FP8_E4M3) return SP_EINVAL;
-  if (a->cache_dtype == SP_K_BF16 && (a->d_k_scale || a->d_v_scale)) return SP_EINVAL;
+  if (a->cache_dtype != SP_K_BF16 && a->cache_dtype != SP_K_FP8_E4M3 && a->cache_dtype != SP_K_MXFP4) return SP_EINVAL;
+  if (a->cache_dtype != SP_K_FP8_E4M3 && (a->d_k_scale || a->d_v_scale)) return SP_EINVAL;
+  if (a->cache_dtype != SP_K_MXFP4 && (a->d_k_block_scale || a->d_v_block_scale)) return SP_EINVAL;
   if (!finite_f32(a->rope_theta) || a->rope_theta < 0.f || (a->rope_theta > 0.f && a->d_inv_freq)) return SP_EINVAL;
   if (a->d_pos && a->rope_theta == 0.f && !a->d_inv_freq) return SP_EINVAL;
   if ((a->T_new > 0 && (!a->d_k || !a->d_v)) || !a->d_cu_new || !a->d_k_cache || !a->d_v_cache) return SP_ENULL;
   if (queries != (a->d_q_out != nullptr)) return SP_ENULL;
+  if (a->cache_dtype == SP_K_MXFP4 && (!a->d_k_block_scale || !a->d_v_block_scale)) return SP_ENULL;
   if (!a->d_block_table && !a->d_cu_cache) return SP_ENULL;
   if (a->d_block_table && a->d_cu_cache) return SP_EINVAL;
   const int64_t in[] = {a->k_token_stride, a->k_head_stride, a->v_token_stride, a->v_head_stride, queries ? a->q_token_stride : 0,
@@ -170,19 +209,26 @@ sp_status check_append(const sp_cache_append_args* a) {
   if (a->H_kv > 1 && a->cache_head_stride < a->d) return SP_EINVAL;
   if ((a->d_block_table || a->n_rows > 1) && a->cache_token_stride < a->d) return SP_EINVAL;
   if (a->d_block_table && a->n_rows > a->page_size && a->cache_page_stride < a->d) return SP_EINVAL;
-  if (a->d_k_cache == a->d_v_cache) return SP_EINVAL;
+  if (a->d_k_cache == a->d_v_cache || (a->d_k_block_scale && a->d_k_block_scale == a->d_v_block_scale)) return SP_EINVAL;
   for (int64_t s : in) if (s & 7) return SP_EALIGN;
-  for (int64_t s : out) if (s & (a->cache_dtype == SP_K_FP8_E4M3 ? 15 : 7)) return SP_EALIGN;
+  for (int64_t s : out) if (s & (cache_stride_unit(a->cache_dtype) - 1)) return SP_EALIGN;
   if (!aligned16(a->d_q) || !aligned16(a->d_k) || !aligned16(a->d_v) || !aligned16(a->d_q_out) || !aligned16(a->d_k_cache) ||
       !aligned16(a->d_v_cache))
     return SP_EALIGN;
   return SP_OK;
 }
 
-template <int D, bool FP8>
+template <int D, int KIND>
 void launch_append(const AppendDev& p, bool rope, dim3 grid, hipStream_t stream) {
-  if (rope) hipLaunchKernelGGL((append_kernel<D, FP8, true>), grid, dim3(256), 0, stream, p);
-  else hipLaunchKernelGGL((append_kernel<D, FP8, false>), grid, dim3(256), 0, stream, p);
+  if (rope) hipLaunchKernelGGL((append_kernel<D, KIND, true>), grid, dim3(256), 0, stream, p);
+  else hipLaunchKernelGGL((append_kernel<D, KIND, false>), grid, dim3(256), 0, stream, p);
+}
+
+template <int D>
+void launch_append(const AppendDev& p, int dtype, bool rope, dim3 grid, hipStream_t stream) {
+  if (dtype == SP_K_MXFP4) launch_append<D, SP_K_MXFP4>(p, rope, grid, stream);
+  else if (dtype == SP_K_FP8_E4M3) launch_append<D, SP_K_FP8_E4M3>(p, rope, grid, stream);
+  else launch_append<D, SP_K_BF16>(p, rope, grid, stream);
 }
 
 }  // namespace
@@ -214,6 +260,7 @@ extern "C" sp_status sp_cache_append(const sp_cache_append_args* a, void* hip_st
   p.k_scale = a->d_k_scale; p.v_scale = a->d_v_scale;
   p.q_out = static_cast<uint16_t*>(a->d_q_out);
   p.k_cache = static_cast<char*>(a->d_k_cache); p.v_cache = static_cast<char*>(a->d_v_cache);
+  p.k_block_scale = a->d_k_block_scale; p.v_block_scale = a->d_v_block_scale;
   // few tokens: one to a workgroup, and several workgroups to a token, until the device has some hundred
   p.tokens = (int)std::min<int64_t>(kTokens, std::max<int64_t>(1, a->T_new / 512));
   const int64_t blocks = (a->T_new + p.tokens - 1) / p.tokens;
@@ -221,8 +268,7 @@ extern "C" sp_status sp_cache_append(const sp_cache_append_args* a, void* hip_st
   const int parts = blocks >= 512 ? 1 : (int)std::min<int64_t>(chunks, 512 / blocks);
   const dim3 grid((unsigned)blocks, (unsigned)std::max(parts, 1));
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const bool fp8 = a->cache_dtype == SP_K_FP8_E4M3;
-  if (a->d == 128) fp8 ? launch_append<128, true>(p, rope, grid, stream) : launch_append<128, false>(p, rope, grid, stream);
-  else fp8 ? launch_append<64, true>(p, rope, grid, stream) : launch_append<64, false>(p, rope, grid, stream);
+  if (a->d == 128) launch_append<128>(p, a->cache_dtype, rope, grid, stream);
+  else launch_append<64>(p, a->cache_dtype, rope, grid, stream);
   return launch_status();
 }

@@ -76,6 +76,19 @@ __device__ __forceinline__ void widen_e4m3(const u32x4 w, u32x4& lo, u32x4& hi) 
   }
 }
 
+// 2 N E2M1 codes and their E8M0 scale -> as many bf16 values (exact)
+template <int N>
+__device__ __forceinline__ void widen_e2m1(const uint32_t (&w)[N / 4], uint32_t scale, uint32_t (&out)[N]) {
+  const float s = __uint_as_float(scale << 23);
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) {
+    out[4 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 0));
+    out[4 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 1));
+    out[4 * i + 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 2));
+    out[4 * i + 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[i], s, 3));
+  }
+}
+
 // Where the rows of a piece's keys lie.  Tiles start at multiples of 8 keys and pages hold multiples of 8, so the 8 keys of an
 // octet lie at one stride from one base, formed in scalar registers, once for all lanes of a wave.  The page numbers of a tile's
 // keys come in a vector register, a lane each, requested a tile ahead and before that tile's loads, so that nothing waits for them
@@ -194,6 +207,75 @@ struct FewTile {
   }
 };
 
+// The end of a piece of few rows: the sums of its W waves become one.  A lane has, of rows (l & 15) + 16 n, values 16 i + 4 quad .. + 3 of O in
+// o[n][i], the maximum and its own part of the sum of weights.
+template <int D, int NR>
+__device__ __forceinline__ void finish_few(const AttendDev& p, const AttendUnit& u, int g, int W, char* lds, int w, int turn, int l, int tid, uint32_t bad,
+                                           const f32x4 (&o)[NR][D / 16], const float (&m)[NR], float (&sum)[NR]) {
+  constexpr int DB = D / 16, NW = attend_waves(D);
+  const int row = l & 15, quad = l >> 4;
+  // every wave's sums in what was its own tile, 16-byte chunks of a row permuted (rows begin in one bank), then one barrier
+  constexpr int ROWS = 16 * NR;
+  float* const tops = reinterpret_cast<float*>(lds + NW * (2 * 32 * D * 2));  // [wave][ROWS], sums of weights, bad pages
+  float* const sums = tops + NW * ROWS;
+  uint32_t* const bads = reinterpret_cast<uint32_t*>(sums + NW * ROWS);
+  float* const parts = reinterpret_cast<float*>(lds);
+  auto chunk_at = [](int r, int ch) { return r * D + 4 * (ch ^ (r & (D / 4 - 1))); };
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    sum[n] += __shfl_xor(sum[n], 16, kWave);
+    sum[n] += __shfl_xor(sum[n], 32, kWave);
+    const int r = row + 16 * n;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(parts + w * (32 * D) + chunk_at(r, 4 * i + quad)) = o[n][i];
+    if (quad == 0) {
+      tops[w * ROWS + r] = m[n];
+      sums[w * ROWS + r] = sum[n];
+    }
+  }
+  if (l == 0) bads[w] = bad;
+  __syncthreads();
+  // the piece's waves join them, in their order, 16 lanes to a row
+  constexpr int V = D / 16;
+  const int w0 = w - turn, lane = tid & 15;
+  for (int r = (turn * 64 + l) >> 4; r < u.nr; r += 4 * W) {
+    float acc[V], l_all = 0.f, top = tops[w0 * ROWS + r];
+    uint32_t any_bad = bads[w0];
+    for (int x = w0 + 1; x < w0 + W; ++x) {
+      top = fmaxf(top, tops[x * ROWS + r]);
+      any_bad |= bads[x];
+    }
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < V; ++i) acc[i] = 0.f;
+#pragma unroll 2
+    for (int x = w0; x < w0 + W; ++x) {
+      const float f = fast_exp2(tops[x * ROWS + r] - base);
+      l_all += sums[x * ROWS + r] * f;
+#pragma unroll
+      for (int i = 0; i < V; i += 4) {
+        const f32x4 part = *reinterpret_cast<const f32x4*>(parts + x * (32 * D) + chunk_at(r, lane * (V / 4) + i / 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i + e] += part[e] * f;
+      }
+    }
+    if (u.slot >= 0) {
+      const int64_t place = slot_row(p, u.slot, r, g);
+      float* dst = p.sums + place * D + lane * V;
+#pragma unroll
+      for (int i = 0; i < V; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+      if (lane == 0) store_stats(p, place, top, l_all, any_bad);
+      continue;
+    }
+    const RowPlace to = row_place(p, u.r0 + r, g);
+    const float mul = (l_all == 0.f ? 0.f : 1.f / l_all) * (p.v_scale ? p.v_scale[g] : 1.f);
+    uint16_t* dst = p.out + to.token * p.o_ts + to.h * p.o_hs + lane * V;
+#pragma unroll
+    for (int i = 0; i < V; i += 4) store_values(dst + i, f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]} * mul, any_bad);
+    if (lane == 0 && p.lse) store_lse(p, to.token, to.h, top, l_all, any_bad);
+  }
+}
+
 // NR tiles of 16 rows.  W waves (a power of two of those of the workgroup, side by side) take the piece; the others take others at the
 // same time, and all meet at one barrier.
 template <int D, bool FP8, bool PAGED, int NR>
@@ -202,7 +284,6 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
   constexpr int DB = D / 16;          // blocks of values
   constexpr int C = D / 8;            // 16-byte chunks of a bf16 row
   using Tile = FewTile<D, FP8>;
-  constexpr int NW = attend_waves(D);
   const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), turn = w & (W - 1), l = tid & 63, row = l & 15, quad = l >> 4;
   bool mine[NR];
   RowPlace at[NR];
@@ -351,77 +432,225 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 
-  // every wave's sums in what was its own tile, 16-byte chunks of a row permuted (rows begin in one bank), then one barrier
-  constexpr int ROWS = 16 * NR;
-  float* const tops = reinterpret_cast<float*>(lds + NW * (2 * 32 * D * 2));  // [wave][ROWS], sums of weights, bad pages
-  float* const sums = tops + NW * ROWS;
-  uint32_t* const bads = reinterpret_cast<uint32_t*>(sums + NW * ROWS);
-  float* const parts = reinterpret_cast<float*>(lds);
-  auto chunk_at = [](int r, int ch) { return r * D + 4 * (ch ^ (r & (D / 4 - 1))); };
+  finish_few<D, NR>(p, u, g, W, lds, w, turn, l, tid, bad, o, m, sum);
+}
+
+// ---------------------------------------------------------------- few rows, 4-bit keys and values
+// 64-key tiles.  Keys need no LDS: lane (key l & 15, quad) holds D/4 consecutive elements of a key, and as the order of
+// elements inside a product's sum is free, it hands them to the matrix cores as they are, turned into bf16, eight to a step;
+// the queries are laid out alike.  Values become bf16 on their way into LDS, where they are transposed.
+template <int D, bool PAGED>
+struct FourBitTile {
+  static constexpr int KW = D / 32;    // 32-bit words of a lane's part of a key
+  static constexpr int C = D / 32;     // 16-byte chunks of a stored row, one block each
+  static constexpr int R = 64 / C;     // rows of a load of values
+  static constexpr int N = 64 / R;     // loads of a tile of values
+  uint32_t k[4][KW], ks[4];
+  uint32_t v[N][4], vs[N];
+  int64_t base[8];                     // where the tile's octets lie
+  int octet[8];
+  __device__ __forceinline__ void place(KeyRows<PAGED>& rows, int tile, int next, uint32_t& bad) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      octet[j] = rows.octet(tile, 8 * j);
+      base[j] = rows.base(octet[j], 8 * j, bad);
+    }
+    rows.ahead(next);
+  }
+  __device__ __forceinline__ void load_keys(const AttendDev& p, const KeyRows<PAGED>& rows, int tile, int64_t head, int l) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const bool second = (l & 8) != 0;
+      const int64_t at = head + (second ? base[2 * x + 1] : base[2 * x]) + rows.within(second ? octet[2 * x + 1] : octet[2 * x], tile + 16 * x + (l & 15));
+      const char* codes = p.k + at + (l >> 4) * (4 * KW);
+      if constexpr (KW == 4) {
+        const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[x][i] = w[i];
+      } else {
+        typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+        const u32x2 w = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(codes));
+        k[x][0] = w[0];
+        k[x][1] = w[1];
+      }
+      ks[x] = p.k_block_scale[(at >> 4) + (l >> 4) * KW / 4];
+    }
+  }
+  __device__ __forceinline__ void load_values(const AttendDev& p, const KeyRows<PAGED>& rows, int tile, int64_t head, int l) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = l / C;  // (and R i)
+      int64_t b = base[R * i / 8];
+      int oct = octet[R * i / 8];
+#pragma unroll
+      for (int j = 1; j < R / 8; ++j)
+        if (r >= 8 * j) { b = base[R * i / 8 + j]; oct = octet[R * i / 8 + j]; }
+      const int64_t at = head + b + rows.within(oct, tile + R * i + r);
+      const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p.v + at + l % C * 16));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[i][j] = w[j];
+      vs[i] = p.v_block_scale[(at >> 4) + l % C];
+    }
+  }
+  __device__ __forceinline__ void store_values(char* tile, int l) const {  // as bf16
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = l / C + R * i, ch = 4 * (l % C);
+      uint32_t w[16];
+      widen_e2m1<16>(v[i], vs[i], w);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<u32x4*>(tile + r * (D * 2) + swizzled<D / 8>(r, ch + j) * 16) = u32x4{w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]};
+    }
+  }
+};
+
+template <int D, bool PAGED, int NR>
+__device__ __forceinline__ void attend_few_4bit(const AttendDev& p, const AttendUnit& u, int g, int W, char* lds) {
+  constexpr int KS = D / 32;          // steps of the product with the queries
+  constexpr int DB = D / 16;          // blocks of values
+  constexpr int C = D / 8;            // 16-byte chunks of a bf16 row
+  using Tile = FourBitTile<D, PAGED>;
+  const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), turn = w & (W - 1), l = tid & 63, row = l & 15, quad = l >> 4;
+  bool mine[NR];
+  RowPlace at[NR];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-    sum[n] += __shfl_xor(sum[n], 16, kWave);
-    sum[n] += __shfl_xor(sum[n], 32, kWave);
-    const int r = row + 16 * n;
-#pragma unroll
-    for (int i = 0; i < DB; ++i) *reinterpret_cast<f32x4*>(parts + w * (32 * D) + chunk_at(r, 4 * i + quad)) = o[n][i];
-    if (quad == 0) {
-      tops[w * ROWS + r] = m[n];
-      sums[w * ROWS + r] = sum[n];
-    }
+    mine[n] = row + 16 * n < u.nr;
+    at[n] = row_place(p, u.r0 + (mine[n] ? row + 16 * n : 0), g);
   }
-  if (l == 0) bads[w] = bad;
-  __syncthreads();
-  // the piece's waves join them, in their order, 16 lanes to a row
-  constexpr int V = D / 16;
-  const int w0 = w - turn, lane = tid & 15;
-  for (int r = (turn * 64 + l) >> 4; r < u.nr; r += 4 * W) {
-    float acc[V], l_all = 0.f, top = tops[w0 * ROWS + r];
-    uint32_t any_bad = bads[w0];
-    for (int x = w0 + 1; x < w0 + W; ++x) {
-      top = fmaxf(top, tops[x * ROWS + r]);
-      any_bad |= bads[x];
+  int tile = u.k0 < u.k1 ? (u.k0 & ~63) + 64 * turn : u.k1;
+  KeyRows<PAGED> rows(p, u, l, tile);
+  const int64_t head = (int64_t)g * p.c_hs;
+  char* const vd = lds + w * (64 * D * 2);
+  uint32_t bad = 0;
+  Tile t;
+  if (tile < u.k1) {
+    t.place(rows, tile, tile + 64 * W, bad);
+    t.load_keys(p, rows, tile, head, l);
+    t.load_values(p, rows, tile, head, l);
+  }
+
+  // the queries, in the order of the keys' elements
+  bf16x8 qf[NR][KS];
+#pragma unroll
+  for (int n = 0; n < NR; ++n)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      u32x4 x = {0, 0, 0, 0};
+      if (mine[n]) x = *reinterpret_cast<const u32x4*>(p.q + at[n].token * p.q_ts + at[n].h * p.q_hs + quad * (D / 4) + s * 8);
+      qf[n][s] = __builtin_bit_cast(bf16x8, x);
     }
-    const float base = top == -INFINITY ? 0.f : top;
+  const float c = p.scale_log2;
+  int limit[NR], least = u.k1;
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] = 0.f;
-#pragma unroll 2
-    for (int x = w0; x < w0 + W; ++x) {
-      const float f = fast_exp2(tops[x * ROWS + r] - base);
-      l_all += sums[x * ROWS + r] * f;
+  for (int n = 0; n < NR; ++n) limit[n] = u.k1;
+  if (u.off != kNoLimit) {
 #pragma unroll
-      for (int i = 0; i < V; i += 4) {
-        const f32x4 part = *reinterpret_cast<const f32x4*>(parts + x * (32 * D) + chunk_at(r, lane * (V / 4) + i / 4));
+    for (int n = 0; n < NR; ++n) {
+      if (mine[n]) limit[n] = min(u.k1, at[n].token + u.off);
+      least = min(least, limit[n]);
+    }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i + e] += part[e] * f;
+    for (int off = 8; off >= 1; off >>= 1) least = min(least, __shfl_xor(least, off, kWave));
+    least = __builtin_amdgcn_readfirstlane(least);
+  }
+  f32x4 o[NR][DB];
+  float m[NR], sum[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m[n] = -INFINITY;
+    sum[n] = 0.f;
+  }
+
+  for (; tile < u.k1; tile += 64 * W) {
+    const bool more = tile + 64 * W < u.k1;
+    f32x4 s[NR][4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      uint32_t kw[4 * Tile::KW];
+      widen_e2m1<4 * Tile::KW>(t.k[x], t.ks[x], kw);
+#pragma unroll
+      for (int n = 0; n < NR; ++n) s[n][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const bf16x8 kf = __builtin_bit_cast(bf16x8, u32x4{kw[4 * i], kw[4 * i + 1], kw[4 * i + 2], kw[4 * i + 3]});
+#pragma unroll
+        for (int n = 0; n < NR; ++n) s[n][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][i], s[n][x], 0, 0, 0);
       }
     }
-    if (u.slot >= 0) {
-      const int64_t place = slot_row(p, u.slot, r, g);
-      float* dst = p.sums + place * D + lane * V;
-#pragma unroll
-      for (int i = 0; i < V; i += 4) *reinterpret_cast<f32x4*>(dst + i) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
-      if (lane == 0) store_stats(p, place, top, l_all, any_bad);
-      continue;
+    t.store_values(vd, l);
+    if (more) {
+      t.place(rows, tile + 64 * W, tile + 128 * W, bad);
+      t.load_keys(p, rows, tile + 64 * W, head, l);
+      t.load_values(p, rows, tile + 64 * W, head, l);
     }
-    const RowPlace to = row_place(p, u.r0 + r, g);
-    const float mul = (l_all == 0.f ? 0.f : 1.f / l_all) * (p.v_scale ? p.v_scale[g] : 1.f);
-    uint16_t* dst = p.out + to.token * p.o_ts + to.h * p.o_hs + lane * V;
+    bf16x8 pf[NR][2];
 #pragma unroll
-    for (int i = 0; i < V; i += 4) store_values(dst + i, f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]} * mul, any_bad);
-    if (lane == 0 && p.lse) store_lse(p, to.token, to.h, top, l_all, any_bad);
+    for (int n = 0; n < NR; ++n) {
+      float x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = s[n][i >> 2][i & 3] * c;
+      if (tile + 64 > least || tile < u.k0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = tile + 16 * (i >> 2) + 4 * quad + (i & 3);
+          if (key >= limit[n] || key < u.k0) x[i] = -INFINITY;
+        }
+      }
+      float top = x[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+      if (__builtin_amdgcn_ballot_w64(top > m[n] + kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float next = fmaxf(m[n], top);
+        const float f = next == -INFINITY ? 1.f : fast_exp2(m[n] - next);
+        m[n] = next;
+        sum[n] *= f;
+#pragma unroll
+        for (int i = 0; i < DB; ++i) o[n][i] *= f;
+      }
+      const float base_m = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) { x[i] = fast_exp2(x[i] - base_m); sum[n] += x[i]; }
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const u32x4 pw = {pack_bf16_pair(x[8 * y], x[8 * y + 1]), pack_bf16_pair(x[8 * y + 2], x[8 * y + 3]),
+                          pack_bf16_pair(x[8 * y + 4], x[8 * y + 5]), pack_bf16_pair(x[8 * y + 6], x[8 * y + 7])};
+        pf[n][y] = __builtin_bit_cast(bf16x8, pw);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int vr = 4 * quad + ((l & 15) >> 2);  // row of the tile that this lane reads from (and 16, 32, 48 + that)
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int i = 0; i < DB; ++i) {
+        const int ch = 2 * i + ((l & 3) >> 1);
+        const char* at0 = vd + (vr + 32 * y) * (D * 2) + swizzled<C>(vr, ch) * 16 + (l & 1) * 8;
+        const bf16x8 vf = join8(lds_read_tr(at0), lds_read_tr(at0 + 16 * D * 2));
+#pragma unroll
+        for (int n = 0; n < NR; ++n) o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][y], o[n][i], 0, 0, 0);
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
+  finish_few<D, NR>(p, u, g, W, lds, w, turn, l, tid, bad, o, m, sum);
 }
 
 // ---------------------------------------------------------------- many rows
 // one lane's share of a 64-key tile of keys or values that T threads load: chunks tid + T i of the tile's 16-byte chunks
-template <int D, bool FP8, int T>
+template <int D, int KIND, int T>
 struct ManyTile {
+  static constexpr bool FP8 = KIND == SP_K_FP8_E4M3;
+  static constexpr int CB = 16;                            // bytes of a chunk
   static constexpr int C = FP8 ? D / 16 : D / 8;           // 16-byte chunks of a stored row
   static constexpr int N = kTileKeys * C / T;
   static constexpr int STEP = T / C;                       // rows between a lane's chunks
   u32x4 x[N];
-  __device__ __forceinline__ void load(const char* base, const int64_t (&at)[N], const uint32_t (&in)[N]) {
+  __device__ __forceinline__ void load(const char* base, const uint8_t*, const int64_t (&at)[N], const uint32_t (&in)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) x[i] = *reinterpret_cast<const u32x4*>(base + at[i] + in[i]);
   }
@@ -442,8 +671,29 @@ struct ManyTile {
     }
   }
 };
+// ... of 4-bit codes: half a block, 8 bytes, to a lane, so that all lanes load
+template <int D, int T>
+struct ManyTile<D, SP_K_MXFP4, T> {
+  static constexpr int CB = 8, C = D / 16, N = 1, STEP = kTileKeys;
+  static_assert(kTileKeys * C == T, "a chunk to a thread");
+  uint2 x;
+  uint32_t scale;
+  __device__ __forceinline__ void load(const char* base, const uint8_t* scales, const int64_t (&at)[N], const uint32_t (&in)[N]) {
+    x = *reinterpret_cast<const uint2*>(base + at[0] + in[0]);
+    scale = scales[(at[0] + in[0]) >> 4];
+  }
+  __device__ __forceinline__ void store(char* tile, int tid) const {
+    const int ch = 2 * (tid % C), r = tid / C;
+    char* row = tile + r * (D * 2);
+    const uint32_t codes[2] = {x.x, x.y};
+    uint32_t w[8];
+    widen_e2m1<8>(codes, scale, w);
+    *reinterpret_cast<u32x4*>(row + swizzled<D / 8>(r, ch) * 16) = u32x4{w[0], w[1], w[2], w[3]};
+    *reinterpret_cast<u32x4*>(row + swizzled<D / 8>(r, ch + 1) * 16) = u32x4{w[4], w[5], w[6], w[7]};
+  }
+};
 
-template <int D, bool FP8, bool PAGED>
+template <int D, int KIND, bool PAGED>
 __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit& u, int g, char* lds) {
   constexpr int NW = attend_waves(D);
   constexpr int SETS = NW == 8 ? 2 : 1;  // tiles on their way from memory
@@ -451,7 +701,7 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
   constexpr int DB = D / 32;   // blocks of values
   constexpr int C = D / 8;
   constexpr int TILE = kTileKeys * D * 2;  // bytes of a tile of keys or of values
-  using Tile = ManyTile<D, FP8, 64 * NW>;
+  using Tile = ManyTile<D, KIND, 64 * NW>;
   const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, half = l >> 5;
   const int row = w * 32 + (l & 31);
   const bool mine = row < u.nr;
@@ -483,7 +733,9 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
   KeyRows<PAGED> rows(p, u, l, first_tile);
   const char* const kb = p.k + (int64_t)g * p.c_hs;
   const char* const vb = p.v + (int64_t)g * p.c_hs;
-  const int lane_row = l / Tile::C, lane_chunk = (l % Tile::C) * 16;
+  const uint8_t* const kb_scale = KIND == SP_K_MXFP4 ? p.k_block_scale + (int64_t)g * p.c_hs / 16 : nullptr;
+  const uint8_t* const vb_scale = KIND == SP_K_MXFP4 ? p.v_block_scale + (int64_t)g * p.c_hs / 16 : nullptr;
+  const int lane_row = l / Tile::C, lane_chunk = (l % Tile::C) * Tile::CB;
   uint32_t bad = 0;
 
   f32x16 o[DB];
@@ -524,8 +776,8 @@ __device__ __forceinline__ void attend_many(const AttendDev& p, const AttendUnit
       in[i] = rows.within(oct, tile + r + lane_row) + lane_chunk;
     }
     rows.ahead(tile + kTileKeys);
-    kt.load(kb, at, in);
-    vl.load(vb, at, in);
+    kt.load(kb, kb_scale, at, in);
+    vl.load(vb, vb_scale, at, in);
   };
   if (first_tile < u.k1) load(first_tile, kt[0], vl[0]);
   if (SETS == 2 && first_tile + kTileKeys < u.k1) load(first_tile + kTileKeys, kt[SETS - 1], vl[SETS - 1]);
@@ -672,7 +924,7 @@ __device__ __forceinline__ void nan_rows(const AttendDev& p, int d, int64_t r0, 
 
 }  // namespace
 
-template <int D, bool FP8, bool PAGED>
+template <int D, int KIND, bool PAGED>
 __global__ __launch_bounds__(64 * attend_waves(D), D == 64 ? 3 : 2) void attend_kernel(const AttendDev p) {
   constexpr int T = 64 * attend_waves(D);
   __shared__ __align__(16) char lds[attend_waves(D) * (64 * D * 2 + 2 * kFewRows * 4 + 4)];  // tiles: 16 KB a wave (8, d = 64), and few rows' statistics
@@ -711,12 +963,18 @@ __global__ __launch_bounds__(64 * attend_waves(D), D == 64 ? 3 : 2) void attend_
       AttendUnit v = u;
       if (mine > 0 && mine < run) v = read(unit_at(x + mine));
       if (mine >= run) v.nr = v.k0 = v.k1 = 0;
-      if (u.nr <= kTileRows) attend_few<D, FP8, PAGED, 1>(p, v, g, W, lds);
-      else attend_few<D, FP8, PAGED, 2>(p, v, g, W, lds);
+      if constexpr (KIND == SP_K_MXFP4) {
+        if (u.nr <= kTileRows) attend_few_4bit<D, PAGED, 1>(p, v, g, W, lds);
+        else attend_few_4bit<D, PAGED, 2>(p, v, g, W, lds);
+      } else {
+        constexpr bool FP8 = KIND == SP_K_FP8_E4M3;
+        if (u.nr <= kTileRows) attend_few<D, FP8, PAGED, 1>(p, v, g, W, lds);
+        else attend_few<D, FP8, PAGED, 2>(p, v, g, W, lds);
+      }
       x += run;
     } else {
       if (u.run == kBadUnit) nan_rows(p, D, u.r0, u.nr, p.G, g * p.G, thread_of_piece(), T);
-      else attend_many<D, FP8, PAGED>(p, u, g, lds);
+      else attend_many<D, KIND, PAGED>(p, u, g, lds);
       ++x;
     }
     if (x >= end) return;
@@ -731,27 +989,35 @@ sp_status check_attend(const sp_attend_args* a) {
   const sp_status st = check_attend_plan_args(a);
   if (st != SP_OK) return st;
   if (!finite_f32(a->scale * kLog2e) || a->scale <= 0.f) return SP_EINVAL;
-  const bool fp8 = a->cache_dtype == SP_K_FP8_E4M3;
+  const bool fp8 = a->cache_dtype == SP_K_FP8_E4M3, fp4 = a->cache_dtype == SP_K_MXFP4;
   if (!fp8 && (a->d_k_scale || a->d_v_scale)) return SP_EINVAL;
+  if (!fp4 && (a->d_k_block_scale || a->d_v_block_scale)) return SP_EINVAL;
   if (a->cache_token_stride >= INT64_C(1) << 26) return SP_EINVAL;
   if ((a->T_new > 0 && (!a->d_q || !a->d_out)) || !a->d_k_cache || !a->d_v_cache) return SP_ENULL;
+  if (fp4 && (!a->d_k_block_scale || !a->d_v_block_scale)) return SP_ENULL;
   const int64_t row[] = {a->q_token_stride, a->q_head_stride, a->out_token_stride, a->out_head_stride};
   const int64_t cache[] = {a->cache_token_stride, a->cache_head_stride, a->d_block_table ? a->cache_page_stride : 0};
   for (int64_t s : row) if (s < 0) return SP_EINVAL;
   for (int64_t s : cache) if (s < 0) return SP_EINVAL;
   if ((a->H > 1 && a->out_head_stride < a->d) || (a->T_new > 1 && a->out_token_stride < a->d)) return SP_EINVAL;  // rows of out that lie in one another
   for (int64_t s : row) if (s & 7) return SP_EALIGN;
-  for (int64_t s : cache) if (s & (fp8 ? 15 : 7)) return SP_EALIGN;
+  for (int64_t s : cache) if (s & (cache_stride_unit(a->cache_dtype) - 1)) return SP_EALIGN;
   if (!aligned16(a->d_q) || !aligned16(a->d_k_cache) || !aligned16(a->d_v_cache) || !aligned16(a->d_out)) return SP_EALIGN;
   if (!a->d_workspace || a->workspace_bytes < sp_attend_workspace_bytes(a)) return SP_EWORKSPACE;
   if (reinterpret_cast<uintptr_t>(a->d_workspace) & 255u) return SP_EALIGN;
   return SP_OK;
 }
 
-template <int D, bool FP8>
+template <int D, int KIND>
 void launch_attend(const AttendDev& p, bool paged, uint32_t grid, hipStream_t stream) {
-  if (paged) hipLaunchKernelGGL((attend_kernel<D, FP8, true>), dim3(grid), dim3(64 * attend_waves(D)), 0, stream, p);
-  else hipLaunchKernelGGL((attend_kernel<D, FP8, false>), dim3(grid), dim3(64 * attend_waves(D)), 0, stream, p);
+  if (paged) hipLaunchKernelGGL((attend_kernel<D, KIND, true>), dim3(grid), dim3(64 * attend_waves(D)), 0, stream, p);
+  else hipLaunchKernelGGL((attend_kernel<D, KIND, false>), dim3(grid), dim3(64 * attend_waves(D)), 0, stream, p);
+}
+template <int D>
+void launch_attend(const AttendDev& p, int dtype, bool paged, uint32_t grid, hipStream_t stream) {
+  if (dtype == SP_K_MXFP4) launch_attend<D, SP_K_MXFP4>(p, paged, grid, stream);
+  else if (dtype == SP_K_FP8_E4M3) launch_attend<D, SP_K_FP8_E4M3>(p, paged, grid, stream);
+  else launch_attend<D, SP_K_BF16>(p, paged, grid, stream);
 }
 
 }  // namespace
@@ -770,8 +1036,8 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   const AttendCaps caps = attend_caps(a);
   const AttendPlanLayout l = attend_plan_layout(a);
   const char* base = static_cast<const char*>(a->d_plan);
-  const bool fp8 = a->cache_dtype == SP_K_FP8_E4M3, paged = a->d_block_table != nullptr;
-  const int E = fp8 ? 1 : 2;
+  const bool paged = a->d_block_table != nullptr;
+  const auto bytes = [&](int64_t elements) { return a->cache_dtype == SP_K_MXFP4 ? elements / 2 : a->cache_dtype == SP_K_FP8_E4M3 ? elements : 2 * elements; };
   AttendDev p;
   p.H = a->H; p.H_kv = a->H_kv; p.G = a->H / a->H_kv; p.T_new = (int)a->T_new;
   p.lg_page = 0;
@@ -783,7 +1049,7 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.scale_log2 = a->scale * kLog2e;
   p.q_ts = a->q_token_stride; p.q_hs = a->q_head_stride;
   p.o_ts = a->out_token_stride; p.o_hs = a->out_head_stride;
-  p.c_ts = (int32_t)(a->cache_token_stride * E); p.c_hs = a->cache_head_stride * E; p.c_ps = a->cache_page_stride * E;
+  p.c_ts = (int32_t)bytes(a->cache_token_stride); p.c_hs = bytes(a->cache_head_stride); p.c_ps = bytes(a->cache_page_stride);
   p.print = attend_print(a);
   p.header = reinterpret_cast<const AttendHeader*>(base);
   p.units = reinterpret_cast<const AttendUnit*>(base + l.units);
@@ -793,13 +1059,14 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.q = static_cast<const uint16_t*>(a->d_q);
   p.k = static_cast<const char*>(a->d_k_cache); p.v = static_cast<const char*>(a->d_v_cache);
   p.k_scale = a->d_k_scale; p.v_scale = a->d_v_scale;
+  p.k_block_scale = a->d_k_block_scale; p.v_block_scale = a->d_v_block_scale;
   p.out = static_cast<uint16_t*>(a->d_out); p.lse = a->d_lse;
   p.sums = static_cast<float*>(a->d_workspace);
   p.stats = reinterpret_cast<float2*>(static_cast<char*>(a->d_workspace) + attend_sums_bytes(a));
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const uint32_t grid = (uint32_t)(most_stretches(a) * a->H_kv);
-  if (a->d == 128) fp8 ? launch_attend<128, true>(p, paged, grid, stream) : launch_attend<128, false>(p, paged, grid, stream);
-  else fp8 ? launch_attend<64, true>(p, paged, grid, stream) : launch_attend<64, false>(p, paged, grid, stream);
+  if (a->d == 128) launch_attend<128>(p, a->cache_dtype, paged, grid, stream);
+  else launch_attend<64>(p, a->cache_dtype, paged, grid, stream);
   launch_attend_join(p, a->d, stream);
   return launch_status();
 }

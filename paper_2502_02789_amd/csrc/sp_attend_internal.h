@@ -32,6 +32,8 @@ struct AttendDev {
   float* lse;
   float* sums;                   // [slot][KV head][16][d]
   float2* stats;                 // [slot][KV head][16]: row maximum (of logits in log2 units), sum of weights
+  const uint8_t* k_block_scale;  // of a 4-bit cache: the scale of the codes from byte x on is byte x / 16
+  const uint8_t* v_block_scale;
 };
 
 sp_status check_attend_shape(const sp_attend_args* a);

@@ -150,10 +150,12 @@ SP_ATTEND_FN bool is_short(int rows, int keys) { return rows <= kFewRows && keys
 // and values, more by the matrix cores; and what a piece costs besides.  (Few and many rows alike: 24 sequences of 1 to 8 new tokens
 // that share 8K 4 % slower, two pieces of 500 tokens behind 17K 2 %; large blocks alike, however many
 // of their rows are there: 32 sequences that share 32K 8-bit keys 11 %.)
-SP_ATTEND_FN int step_cost(int rows, int d, bool fp8) {
-  if (rows <= kTileRows) return d == 64 ? (fp8 ? 2 : 3) : (fp8 ? 3 : 5);
-  if (rows <= kFewRows) return d == 64 ? 4 : fp8 ? 4 : 6;
-  return d == 64 ? 4 : rows > many_rows(d) / 2 ? 8 : fp8 ? 5 : 6;
+// (dtype: sp_k_dtype; a 4-bit cache costs what an 8-bit one does)
+SP_ATTEND_FN int step_cost(int rows, int d, int dtype) {
+  const bool wide = dtype == SP_K_BF16;
+  if (rows <= kTileRows) return d == 64 ? (wide ? 3 : 2) : (wide ? 5 : 3);
+  if (rows <= kFewRows) return d == 64 ? 4 : wide ? 6 : 4;
+  return d == 64 ? 4 : rows > many_rows(d) / 2 ? 8 : wide ? 6 : 5;
 }
 SP_ATTEND_FN int piece_cost(int rows, int keys, int d) { return d == 64 ? (is_short(rows, keys) ? 2 : 4) : is_short(rows, keys) ? 3 : 12; }
 // No stretch costs less: more than a step of any kind.  (Three times as much: one token behind 1000 keys 4 % slower, 64 that share
@@ -168,12 +170,12 @@ SP_ATTEND_FN int least_stretch(int d) { return d == 64 ? 10 : 11; }
 // 55.7; four new tokens each: 64 48.9, 68.0, 512 55.6, 64.9, 2048 76.7, 63.6; 24 sequences of 8 tokens of eight heads: 512 41.3, 44.5,
 // 4096 86.1, 66.8; two of one token: 4096 12.7, 12.4.  Over 2456 such calls the rule loses 1.8 % against the better of the two (at worst 1.5
 // times; against sharing always 1.3), sharing always 8.6 % (at worst 2.6 times), never 19 %.
-SP_ATTEND_FN bool prefix_pays(int rows, int members, int prefix, int d, bool fp8) {
+SP_ATTEND_FN bool prefix_pays(int rows, int members, int prefix, int d, int dtype) {
   if (prefix <= 0 || !shares(rows, members)) return false;
   const int own = (int)((uint32_t)rows / (uint32_t)members), many = many_rows(d), whole = rows > kFewRows ? (int)((uint32_t)rows / (uint32_t)many) : 0;
   const int rest = rows - whole * many;
-  const int64_t each = step_cost(own, d, fp8) + (int64_t)(members - 1) * (own <= kTileRows ? 2 : own <= kFewRows ? 3 : 5);
-  const int64_t once = (int64_t)whole * step_cost(many, d, fp8) + (rest > 0 ? step_cost(rest, d, fp8) : 0);
+  const int64_t each = step_cost(own, d, dtype) + (int64_t)(members - 1) * (own <= kTileRows ? 2 : own <= kFewRows ? 3 : 5);
+  const int64_t once = (int64_t)whole * step_cost(many, d, dtype) + (rest > 0 ? step_cost(rest, d, dtype) : 0);
   return prefix * (each - once) >= (int64_t)rows * (kPieceStep * 5 / 4);
 }
 

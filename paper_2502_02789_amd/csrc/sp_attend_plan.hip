@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
       const int active = __hip_atomic_load(&groups[g].active, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       // (no more than the sequence has whose pages are read, whatever the offsets are)
       const int shared = min(__hip_atomic_load(&groups[g].shared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), max(seqs[clamp_int(cu_group[g], 0, B - 1)].len, 0));
-      groups[g].shared = prefix_pays(groups[g].tokens * G, active, shared, p.a.d, p.a.cache_dtype == SP_K_FP8_E4M3) ? shared : 0;
+      groups[g].shared = prefix_pays(groups[g].tokens * G, active, shared, p.a.d, p.a.cache_dtype) ? shared : 0;
     }
     __syncthreads();
     for (int b = tid; b < B; b += kPlanThreads) {
@@ -191,7 +191,6 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
 
   // Blocks in the order that they are laid out in: prefixes first, then the sequences' blocks from the last to the first (of
   // a causal segment's blocks the last have the most keys).
-  const bool fp8 = p.a.cache_dtype == SP_K_FP8_E4M3;
   auto block_at = [&](int x, int hint) {
     const int flat = x < n_prefix ? x : n_blocks - 1 - (x - n_prefix);
     Block k;
@@ -209,7 +208,7 @@ __global__ __launch_bounds__(kPlanThreads) void attend_plan_kernel(const PlanDev
     }
     k.nr = min(k.m, k.rows - k.i * k.m);
     k.steps = block_steps(k.first, k.keys);
-    k.cost = step_cost(k.nr, p.a.d, fp8);
+    k.cost = step_cost(k.nr, p.a.d, p.a.cache_dtype);
     k.extra = piece_cost(k.nr, k.keys, p.a.d);
     return k;
   };
@@ -538,7 +537,7 @@ sp_status check_attend_shape(const sp_attend_args* a) {
   if (a->T_new < 0 || a->n_groups < 0 || a->n_groups > a->B) return SP_EINVAL;
   if (a->T_new >= INT64_C(0x80000000) / a->H) return SP_EINVAL;
   if (a->n_rows < 1 || a->n_rows > kMostKeys) return SP_EINVAL;
-  if (a->cache_dtype != SP_K_BF16 && a->cache_dtype != SP_K_FP8_E4M3) return SP_EINVAL;
+  if (a->cache_dtype != SP_K_BF16 && a->cache_dtype != SP_K_FP8_E4M3 && a->cache_dtype != SP_K_MXFP4) return SP_EINVAL;
   if (a->d_block_table) {
     if (a->page_size < 8 || (a->page_size & (a->page_size - 1)) != 0 || a->blocks_per_seq < 1) return SP_EINVAL;
     if ((int64_t)a->blocks_per_seq * a->page_size > kMostKeys || a->n_rows % a->page_size != 0) return SP_EINVAL;

@@ -165,10 +165,25 @@ def _on_one_device(*tensors) -> torch.device:
     return next(iter(devices))
 
 
+def _head_dim(cache) -> int:
+    return (2 if sp.is_4bit(cache) else 1) * int(cache.shape[-1])
+
+
+def _check_block_scales(cache, scales, name: str):
+    _need((scales is not None) == sp.is_4bit(cache), f"{name} belongs to a 4-bit cache (float4_e2m1fn_x2), and that needs it")
+    if scales is None:
+        return
+    _need(scales.dtype in (torch.uint8, torch.float8_e8m0fnu) and cache.shape[-1] % 16 == 0 and
+          scales.shape == cache.shape[:-1] + (cache.shape[-1] // 16,), f"{name}: uint8 or float8_e8m0fnu, the shape of the cache with d/32 for its last axis")
+    _need(scales.stride(-1) == 1 and all(n == 1 or 16 * y == x for n, x, y in zip(cache.shape[:-1], cache.stride()[:-1], scales.stride()[:-1])),
+          f"{name} must be laid out as the cache is: each stride a sixteenth of the cache's")
+
+
 def _check_cache(k_cache, v_cache, block_table, cu_cache, B: int, scales=()):
     _need((block_table is None) != (cu_cache is None), "a cache is paged (block_table) or contiguous (cu_cache)")
     for c in (k_cache, v_cache):
-        _need(c is None or c.dtype in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn), "the cache holds bf16 or E4M3 (uint8, float8_e4m3fn)")
+        _need(c is None or c.dtype in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn, torch.float4_e2m1fn_x2),
+              "the cache holds bf16, E4M3 (uint8, float8_e4m3fn) or E2M1 codes (float4_e2m1fn_x2)")
     if block_table is not None:
         _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous() and block_table.shape[0] == B,
               "block_table: contiguous int32 [B, blocks_per_seq]")
@@ -176,7 +191,7 @@ def _check_cache(k_cache, v_cache, block_table, cu_cache, B: int, scales=()):
         _check_ints(cu_cache, B + 1, "cu_cache")
     for s in scales:
         if s is not None:
-            _need(k_cache.element_size() == 1, "scales belong to 8-bit caches")
+            _need(k_cache.element_size() == 1 and not sp.is_4bit(k_cache), "scales belong to 8-bit caches")
             _need(s.dtype == torch.float32 and s.is_contiguous() and s.numel() == k_cache.shape[-2], "scales: contiguous fp32 [H_kv]")
 
 
@@ -211,19 +226,24 @@ class CacheAppender(_OnDevice):
                  cache_len: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None, rope_theta: float = 0.0,
                  inv_freq: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
                  cu_cache: Optional[torch.Tensor] = None, k_scale: Optional[torch.Tensor] = None,
-                 v_scale: Optional[torch.Tensor] = None):
+                 v_scale: Optional[torch.Tensor] = None, k_block_scale: Optional[torch.Tensor] = None,
+                 v_block_scale: Optional[torch.Tensor] = None):
         """k, v: bf16 [T, H_kv, d] and q: bf16 [T, H, d], any token and head strides (slices of one projection's output);
         cu_new int32 [B+1] bounds the sequences' new tokens; cache_len int32 [B]: tokens cached before (None: none).
         k_cache, v_cache: [pages, page_size, H_kv, d] with block_table int32 [B, blocks_per_seq], or [rows, H_kv, d] with cu_cache
-        int32 [B+1]; bf16, or 8-bit (uint8 or float8_e4m3fn) with k_scale, v_scale fp32 [H_kv].
+        int32 [B+1]; bf16, or 8-bit (uint8 or float8_e4m3fn) with k_scale, v_scale fp32 [H_kv], or 4-bit (float4_e2m1fn_x2
+        [.., d/2]; see mxfp4_cache()) with k_block_scale, v_block_scale (uint8 or float8_e8m0fnu [.., d/32]), which are written too.
         pos: int32 [T] positions (the Gatherer's kept_pos, say), None: the index in the cache.  rope_theta or inv_freq (fp64
         [d/2]) asks for the rotation.  q_out: where the rotated queries go (a contiguous tensor, q itself allowed; default: a new one)."""
-        T, B, d = int(k.shape[0]), int(cu_new.numel()) - 1, int(k_cache.shape[-1])
+        T, B, d = int(k.shape[0]), int(cu_new.numel()) - 1, _head_dim(k_cache)
         H_kv = int(k_cache.shape[-2])
-        self._device = _on_one_device(k, v, cu_new, k_cache, v_cache, q, q_out, cache_len, pos, inv_freq, block_table, cu_cache, k_scale, v_scale)
+        self._device = _on_one_device(k, v, cu_new, k_cache, v_cache, q, q_out, cache_len, pos, inv_freq, block_table, cu_cache, k_scale, v_scale,
+                                      k_block_scale, v_block_scale)
         _need(B >= 1, "cu_new: int32 [B+1]")
         _check_ints(cu_new, B + 1, "cu_new")
         _check_cache(k_cache, v_cache, block_table, cu_cache, B, (k_scale, v_scale))
+        _check_block_scales(k_cache, k_block_scale, "k_block_scale")
+        _check_block_scales(v_cache, v_block_scale, "v_block_scale")
         _check_rows(k, T, H_kv, d, "k")
         _check_rows(v, T, H_kv, d, "v")
         if q is not None:
@@ -241,14 +261,73 @@ class CacheAppender(_OnDevice):
         if inv_freq is not None:
             _need(inv_freq.dtype == torch.float64 and inv_freq.is_contiguous() and inv_freq.numel() == d // 2, f"inv_freq: fp64 [{d // 2}]")
         self.q_out = q_out
-        self._held = (k, v, cu_new, k_cache, v_cache, q, cache_len, pos, inv_freq, block_table, cu_cache, k_scale, v_scale)
+        self._held = (k, v, cu_new, k_cache, v_cache, q, cache_len, pos, inv_freq, block_table, cu_cache, k_scale, v_scale, k_block_scale,
+                      v_block_scale)
         self.args = sp.make_cache_append_args(k, v, cu_new, k_cache, v_cache, q=q, q_out=q_out, cache_len=cache_len, pos=pos,
                                               rope_theta=rope_theta, inv_freq=inv_freq, block_table=block_table,
-                                              cu_cache=cu_cache, k_scale=k_scale, v_scale=v_scale)
+                                              cu_cache=cu_cache, k_scale=k_scale, v_scale=v_scale,
+                                              k_block_scale=k_block_scale, v_block_scale=v_block_scale)
 
     def run(self, stream=None) -> Optional[torch.Tensor]:
         self._call(sp.sp_cache_append, self.args, stream)
         return self.q_out
+
+
+def mxfp4_cache(rows, H_kv: int, d: int, *, device="cuda"):
+    """An empty 4-bit cache (zeros) of keys or of values: float4_e2m1fn_x2 codes [.., H_kv, d/2] and float8_e8m0fnu scales [.., H_kv, d/32], `rows` the
+    leading axes: (pages, page_size), or a number of rows.  The heads lie outermost in a page (or in all): the layout that attention reads fastest."""
+    lead = (int(rows),) if isinstance(rows, int) else tuple(int(n) for n in rows)
+    _need(d in (64, 128) and len(lead) in (1, 2), "rows: a number, or (pages, page_size); d: 64 or 128")
+
+    def empty(n):
+        return torch.zeros((*lead[:-1], H_kv, lead[-1], n), dtype=torch.uint8, device=device).transpose(-3, -2)
+
+    return empty(d // 2).view(torch.float4_e2m1fn_x2), empty(d // 32).view(torch.float8_e8m0fnu)
+
+
+class CacheReader(_OnDevice):
+    """One sp_cache_read problem: tokens of a cache as bf16 keys and values [T, H_kv, d], for what takes no quantised cache or no block table
+    (the Scorer, say, of a 4-bit one)."""
+
+    def __init__(self, k_cache: torch.Tensor, v_cache: Optional[torch.Tensor], cu_rows: torch.Tensor, *, total: int,
+                 first: Optional[torch.Tensor] = None, index: Optional[torch.Tensor] = None, block_table: Optional[torch.Tensor] = None,
+                 cu_cache: Optional[torch.Tensor] = None, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+                 k_block_scale: Optional[torch.Tensor] = None, v_block_scale: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None):
+        """Rows cu_rows[b] .. cu_rows[b+1]-1 (int32 [B+1], at most `total` in all) are tokens of sequence b: those from first[b] on (int32 [B],
+        None: 0), or first[b] + index[t] (int32 [total]: the Gatherer's kept_pos, say).  The cache as the CacheAppender takes it;
+        v_cache None: keys only.  k_out, v_out: bf16 [total, H_kv, d], any token and head strides (default: new ones)."""
+        B, H_kv, d, T = int(cu_rows.numel()) - 1, int(k_cache.shape[-2]), _head_dim(k_cache), int(total)
+        self._device = _on_one_device(k_cache, v_cache, cu_rows, first, index, block_table, cu_cache, k_scale, v_scale, k_block_scale,
+                                      v_block_scale, k_out, v_out)
+        _need(B >= 1, "cu_rows: int32 [B+1]")
+        _check_ints(cu_rows, B + 1, "cu_rows")
+        _check_cache(k_cache, v_cache, block_table, cu_cache, B, (k_scale, v_scale))
+        _check_block_scales(k_cache, k_block_scale, "k_block_scale")
+        if v_cache is not None:
+            _check_block_scales(v_cache, v_block_scale, "v_block_scale")
+        else:
+            _need(v_scale is None and v_block_scale is None and v_out is None, "values without v_cache")
+        if first is not None:
+            _check_ints(first, B, "first")
+        if index is not None:
+            _need(index.dtype == torch.int32 and index.is_contiguous() and index.numel() >= T, f"index: contiguous int32 [{T}]")
+        if k_out is None:
+            k_out = torch.empty((T, H_kv, d), dtype=torch.bfloat16, device=self._device)
+        if v_out is None and v_cache is not None:
+            v_out = torch.empty((T, H_kv, d), dtype=torch.bfloat16, device=self._device)
+        _check_rows(k_out, T, H_kv, d, "k_out")
+        if v_out is not None:
+            _check_rows(v_out, T, H_kv, d, "v_out")
+        self.k_out, self.v_out = k_out, v_out
+        self._held = (k_cache, v_cache, cu_rows, first, index, block_table, cu_cache, k_scale, v_scale, k_block_scale, v_block_scale)
+        self.args = sp.make_cache_read_args(k_cache, v_cache, cu_rows, k_out, v_out, first=first, index=index, block_table=block_table,
+                                            cu_cache=cu_cache, k_scale=k_scale, v_scale=v_scale, k_block_scale=k_block_scale,
+                                            v_block_scale=v_block_scale)
+
+    def run(self, stream=None):
+        self._call(sp.sp_cache_read, self.args, stream)
+        return self.k_out, self.v_out
 
 
 class AttendPlan(_OnDevice):
@@ -273,7 +352,7 @@ class AttendPlan(_OnDevice):
             _check_ints(prefix_len, int(cu_group.numel()) - 1, "prefix_len")
         self.cu_new, self.kv_len, self.block_table, self.cu_cache = cu_new, kv_len, block_table, cu_cache
         self.cu_group, self.prefix_len, self.H, self.total_new = cu_group, prefix_len, int(H), int(total_new)
-        self.shape, self.bytes = k_cache.shape, k_cache.element_size()
+        self.shape, self.bytes, self.four_bits = k_cache.shape, k_cache.element_size(), sp.is_4bit(k_cache)
         kw = dict(H=H, total_new=total_new, block_table=block_table, cu_cache=cu_cache, cu_group=cu_group, prefix_len=prefix_len)
         probe = sp.make_attend_plan_args(cu_new, kv_len, k_cache, **kw)
         need = sp.sp_attend_plan_bytes(probe)
@@ -292,12 +371,16 @@ class Attender(_OnDevice):
 
     def __init__(self, plan: AttendPlan, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, *, scale: float,
                  k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                 want_lse: bool = False, workspace: Optional[torch.Tensor] = None):
-        """workspace: uint8 of plan.workspace's size, for layers that run at the same time (default: the plan's)."""
-        self._device = _on_one_device(plan.plan, q, k_cache, v_cache, k_scale, v_scale, out, workspace)
-        d = int(k_cache.shape[-1])
+                 want_lse: bool = False, workspace: Optional[torch.Tensor] = None, k_block_scale: Optional[torch.Tensor] = None,
+                 v_block_scale: Optional[torch.Tensor] = None):
+        """k_scale, v_scale, k_block_scale, v_block_scale: as the CacheAppender takes them.  workspace: uint8 of plan.workspace's size, for layers that
+        run at the same time (default: the plan's)."""
+        self._device = _on_one_device(plan.plan, q, k_cache, v_cache, k_scale, v_scale, out, workspace, k_block_scale, v_block_scale)
+        d = _head_dim(k_cache)
         _check_cache(k_cache, v_cache, plan.block_table, plan.cu_cache, int(plan.cu_new.numel()) - 1, (k_scale, v_scale))
-        _need(k_cache.shape == plan.shape and k_cache.element_size() == plan.bytes, "the cache must have the shape and type that the plan was made for")
+        _check_block_scales(k_cache, k_block_scale, "k_block_scale")
+        _check_block_scales(v_cache, v_block_scale, "v_block_scale")
+        _need(k_cache.shape == plan.shape and k_cache.element_size() == plan.bytes and sp.is_4bit(k_cache) == plan.four_bits, "the cache must have the shape and type that the plan was made for")
         _check_rows(q, plan.total_new, plan.H, d, "q")
         if out is None:
             out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
@@ -305,10 +388,54 @@ class Attender(_OnDevice):
         self.plan, self.out = plan, out
         self.lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
         self.workspace = plan.workspace if workspace is None else workspace
-        self._held = (q, k_cache, v_cache, k_scale, v_scale)
+        self._held = (q, k_cache, v_cache, k_scale, v_scale, k_block_scale, v_block_scale)
         self.args = sp.add_attend_args(plan.args, q, k_cache, v_cache, out, scale=scale, block_table=plan.block_table,
-                                       cu_cache=plan.cu_cache, k_scale=k_scale, v_scale=v_scale, lse=self.lse, workspace=self.workspace)
+                                       cu_cache=plan.cu_cache, k_scale=k_scale, v_scale=v_scale, k_block_scale=k_block_scale,
+                                       v_block_scale=v_block_scale, lse=self.lse, workspace=self.workspace)
 
     def run(self, stream=None) -> torch.Tensor:
         self._call(sp.sp_attend, self.args, stream)
         return self.out
+
+
+class Verifier(_OnDevice):
+    """One sp_verify problem: which drafted tokens stand against the target's probabilities, and the token behind them."""
+
+    def __init__(self, target: torch.Tensor, tokens: torch.Tensor, cu_draft: torch.Tensor, u: torch.Tensor, r: torch.Tensor, *,
+                 draft: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None, past_len: Optional[torch.Tensor] = None,
+                 want_logprob: bool = False):
+        """cu_draft int32 [B+1] bounds the sequences' drafted tokens (tokens: int32 [T]).  target: bf16 or fp32 [T + B, V] logits, one row more
+        for each sequence than it has drafted tokens; draft: alike [T, V], None for tokens that were not sampled.  u: fp32 [T] and r: fp32 [B], random
+        numbers in [0, 1).  temperature: fp32 [B] (None: 1; 0 takes the largest logit).  past_len int32 [B]: tokens of the cache before the step.
+        After run(): n_accepted int32 [B], out_tokens int32 [T + B] (-1 behind a sequence's last), logprob fp32 [T + B] if wanted, kept_len
+        int32 [B] if past_len is given: the tokens of the cache that stand, the next step's past_len."""
+        T, B = int(tokens.numel()), int(cu_draft.numel()) - 1
+        self._device = _on_one_device(target, tokens, cu_draft, u, r, draft, temperature, past_len)
+        _need(B >= 1, "cu_draft: int32 [B+1]")
+        _check_ints(cu_draft, B + 1, "cu_draft")
+        _check_ints(tokens, T, "tokens")
+        _need(target.dtype in (torch.bfloat16, torch.float32), "target: bf16 or fp32 logits")
+        for t, n, name in ((target, T + B, "target"), (draft, T, "draft")):
+            _need(t is None or (t.dtype == target.dtype and t.dim() == 2 and t.shape[0] == n and t.shape[1] == target.shape[1] and t.stride(1) == 1),
+                  f"{name}: [{n}, V] of the target's type, contiguous rows")
+        for t, n, name in ((u, T, "u"), (r, B, "r"), (temperature, B, "temperature")):
+            _need(t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n), f"{name}: contiguous fp32 [{n}]")
+        if past_len is not None:
+            _check_ints(past_len, B, "past_len")
+        new = dict(device=self._device)
+        self.n_accepted = torch.empty(B, dtype=torch.int32, **new)
+        self.out_tokens = torch.empty(T + B, dtype=torch.int32, **new)
+        self.logprob = torch.empty(T + B, dtype=torch.float32, **new) if want_logprob else None
+        self.kept_len = torch.empty(B, dtype=torch.int32, **new) if past_len is not None else None
+        self._held = (target, tokens, cu_draft, u, r, draft, temperature, past_len)
+        kw = dict(draft=draft, temperature=temperature, past_len=past_len, logprob=self.logprob, kept_len=self.kept_len)
+        probe = sp.make_verify_args(target, tokens, cu_draft, u, r, self.n_accepted, self.out_tokens, **kw)
+        need = sp.sp_verify_workspace_bytes(probe)
+        if need == 0:
+            raise sp.SpError("sp_verify_workspace_bytes", sp.SP_EINVAL)
+        self.workspace = torch.empty(need, dtype=torch.uint8, **new)
+        self.args = sp.make_verify_args(target, tokens, cu_draft, u, r, self.n_accepted, self.out_tokens, workspace=self.workspace, **kw)
+
+    def run(self, stream=None):
+        self._call(sp.sp_verify, self.args, stream)
+        return self.n_accepted, self.out_tokens

@@ -1,0 +1,249 @@
+"""GPU: sp_verify against the fp64 oracle: the same tokens, log-probabilities within what fp32 sums allow."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import verify_oracle as vo
+from tests import cache_cases as cc
+
+pytestmark = pytest.mark.gpu
+
+
+def _case(rng, n, V, *, bits=16, draft=True, temperature=None, spread=2.5, near=0.7, pad=0, spare=0):
+    """Logits in rows of V + pad, tokens sampled from the draft (or, without one, likely ones of the target's)."""
+    import torch
+    B, T, dtype = len(n), sum(n), torch.bfloat16 if bits == 16 else torch.float32
+    z = spread * rng.standard_normal((T + B, V))
+    z[np.arange(T + B)[:, None], rng.integers(0, V, (T + B, 3))] += 6
+    rows = np.concatenate([np.arange(a, a + k) + b for b, (a, k) in enumerate(zip(cc.offsets(n)[:-1], n))]).astype(int)
+
+    def put(x, more):
+        wide = torch.full((len(x) + more, V + pad), float("nan"), dtype=dtype, device="cuda")
+        wide[:len(x), :V] = torch.from_numpy(x).cuda().to(dtype)
+        return wide[:, :V]
+    target = put(z, spare)
+    t = np.ones(B) if temperature is None else np.asarray(temperature, np.float64)
+    d = put(z[rows] + near * rng.standard_normal((T, V)), spare) if T else put(np.zeros((0, V)), spare)
+    dl = (d if draft else target[torch.from_numpy(rows).cuda()]).double().cpu().numpy()
+    tokens = np.array([int(np.argmax(dl[i] + t[b] * -np.log(-np.log(rng.random(V)))))
+                       for b in range(B) for i in range(cc.offsets(n)[b], cc.offsets(n)[b + 1])], np.int32)
+    tokens = np.concatenate([tokens, np.full(spare, 1 << 30, np.int32)])
+    return dict(n=n, V=V, target=target, draft=d if draft else None, tokens=tokens, temperature=temperature, spare=spare,
+                u=rng.random(T + spare).astype(np.float32), r=rng.random(B).astype(np.float32), past=rng.integers(0, 1000, B).astype(np.int32))
+
+
+def _verifier(c):
+    import torch
+    from paper_2502_02789_amd import device as dev
+    f = lambda x: torch.from_numpy(np.asarray(x, np.float32)).cuda()  # noqa: E731
+    v = dev.Verifier(c["target"], cc.cuda_ints(c["tokens"]), cc.cuda_ints(cc.offsets(c["n"])), f(c["u"]), f(c["r"]), draft=c["draft"],
+                     temperature=None if c["temperature"] is None else f(c["temperature"]), past_len=cc.cuda_ints(c["past"]), want_logprob=True)
+    v.out_tokens.fill_(7)
+    v.logprob.fill_(7.0)
+    return v
+
+
+def _want(c):
+    t = None if c["temperature"] is None else np.asarray(c["temperature"], np.float32).astype(np.float64)
+    return vo.verify(c["target"].double().cpu().numpy(), c["tokens"], cc.offsets(c["n"]), c["u"].astype(np.float64), c["r"].astype(np.float64),
+                     draft=None if c["draft"] is None else c["draft"].double().cpu().numpy(), temperature=t, past_len=c["past"])
+
+
+def _check(c, v, want=None):
+    """log p = (z - top) / T - log(sum of exp).  The sum, in fp32: exp2 is off by 2^-22 of itself; its argument's two roundings by 2^-23 of the
+    argument, whose mean over the distribution is below log2 V; adding 32 numbers, the lanes' and the waves', 2^-24 for each of some 48 steps; and the
+    result is rounded to fp32."""
+    n, out, logprob, kept, margin = want or _want(c)
+    assert margin > 1e-5      # (of the inputs, whatever the kernels do)
+    rows = sum(c["n"]) + len(c["n"])
+    assert v.n_accepted.cpu().numpy().tolist() == n.tolist()
+    got = v.out_tokens.cpu().numpy()
+    assert got[:rows].tolist() == out[:rows].tolist() and (got[rows:] == 7).all()
+    assert v.kept_len.cpu().numpy().tolist() == kept.tolist()
+    lp = v.logprob.double().cpu().numpy()
+    assert (lp[rows:] == 7).all()
+    lp, logprob = lp[:rows], logprob[:rows]
+    assert (np.isnan(lp) == np.isnan(logprob)).all() and (np.isneginf(lp) == np.isneginf(logprob)).all()
+    there = np.isfinite(logprob)
+    tol = 2.0 ** -22 + math.log2(c["V"] + 1) * 2.0 ** -22 + 48 * 2.0 ** -24 + 2.0 ** -24 * np.abs(logprob[there])
+    assert (np.abs(lp[there] - logprob[there]) <= tol).all()
+
+
+def _run(c):
+    import torch
+    v = _verifier(c)
+    v.run()
+    torch.cuda.synchronize()
+    _check(c, v)
+    return v
+
+
+@pytest.mark.parametrize("bits", [16, 32])
+@pytest.mark.parametrize("draft", [True, False])
+@pytest.mark.parametrize("V", [1, 2, 7, 64, 255, 1000, 4095, 4096, 4097, 8192, 8193, 50257])
+def test_vocabularies(V, draft, bits):
+    rng = np.random.default_rng(V)
+    _run(_case(rng, [3, 0, 1, 8, 2], V, bits=bits, draft=draft))
+    _run(_case(rng, [2, 5], V, bits=bits, draft=draft, pad=3, temperature=[0.7, 1.3], spare=2))
+
+
+@pytest.mark.parametrize("bits", [16, 32])
+def test_temperatures(bits):
+    """0, the smallest and the largest that make sense; logits that tie at the top."""
+    import torch
+    rng = np.random.default_rng(1)
+    c = _case(rng, [4, 4, 4, 4, 4, 0], 3001, bits=bits, temperature=[0.0, 0.01, 0.3, 1.0, 50.0, 0.0])
+    _run(c)
+    c["target"][:5, 100:200] = c["target"][:5].max() + 1
+    c["target"][24] = -3.0
+    c["tokens"][:4] = [100, 101, 100, 100]
+    _run(c)
+    c["draft"] = None
+    _run(c)
+    assert torch.cuda.is_available()
+
+
+def test_most_drafted_tokens_and_one_more():
+    """63 tokens that all stand, and 64, which is answered in band."""
+    rng = np.random.default_rng(2)
+    c = _case(rng, [63, 64, 1], 500)
+    c["u"][:] = 0.0
+    n, out, logprob, kept, margin = _want(c)
+    rows = slice(64, 64 + 65)
+    n[1], out[rows], logprob[rows], kept[1] = -1, -1, np.nan, c["past"][1]
+    v = _verifier(c)
+    v.run()
+    assert n[0] == 63
+    _check(c, v, (n, out, logprob, kept, margin))
+
+
+def test_many_sequences():
+    rng = np.random.default_rng(3)
+    _run(_case(rng, [int(x) for x in rng.integers(0, 4, 400)], 200, temperature=rng.choice([0.0, 0.5, 1.0], 400)))
+
+
+def test_random_numbers_at_their_ends():
+    """u and r of 0 and of the largest number below 1."""
+    rng = np.random.default_rng(4)
+    for u, r in ((0.0, 0.0), (0.0, 1 - 2.0 ** -24), (1 - 2.0 ** -24, 0.0), (1 - 2.0 ** -24, 1 - 2.0 ** -24)):
+        c = _case(rng, [3, 2, 0, 4], 5000)
+        c["u"][:], c["r"][:] = u, r
+        if r == 0.0:
+            c["target"][:, :37] = -math.inf     # (the first token with any probability, not the first)
+        _run(c)
+
+
+def test_probabilities_of_zero():
+    """Log-probabilities with -infinity: cut distributions, a drafted token that the target gives nothing, and one that the draft gives nothing."""
+    import torch
+    rng = np.random.default_rng(5)
+    c = _case(rng, [4, 4, 4], 3000, bits=32)
+    for x in (c["target"], c["draft"]):
+        kth = x.topk(20, dim=1).values[:, -1:]
+        x.copy_(torch.where(x >= kth, x, torch.full_like(x, -math.inf)).log_softmax(dim=1))
+    c["tokens"][:] = c["target"][[0, 1, 2, 3, 5, 6, 7, 8, 10, 11, 12, 13]].argmax(dim=1).int().cpu().numpy()
+    c["tokens"][5] = int((c["target"][6] == -math.inf).nonzero()[0])
+    _run(c)
+
+
+def test_draft_equal_to_target():
+    """Everything stands whatever u is (below 1); forced down by a draft that sees the token twice as likely, what is left is nothing at the others."""
+    rng = np.random.default_rng(6)
+    c = _case(rng, [5, 5], 4000, near=0.0)
+    rows = [0, 1, 2, 3, 4, 6, 7, 8, 9, 10]
+    c["draft"].copy_(c["target"][rows])
+    c["u"][:] = 0.99
+    v = _run(c)
+    assert v.n_accepted.tolist() == [5, 5]
+
+
+def test_rows_that_are_none_are_answered_in_band():
+    import torch
+    rng = np.random.default_rng(7)
+    for spoil in ("nan", "inf", "empty"):
+        value = dict(nan=math.nan, inf=math.inf, empty=-math.inf)[spoil]
+        c = _case(rng, [3, 3, 3, 0, 3], 9000, temperature=[1.0, 1.0, 1.0, 1.0, 0.0])
+        c["u"][:] = 0.0
+        at = slice(None) if spoil == "empty" else 8500
+        c["target"][0, at] = value                # a first row
+        c["draft"][4, at] = value                 # a draft row in the middle
+        c["target"][11, at] = value               # the last row, of a sequence all of whose tokens stand
+        c["target"][12, at] = value               # of a sequence without drafted tokens
+        c["target"][14, at] = value               # at temperature 0
+        c["tokens"][9:12] = c["target"][13:16].float().nan_to_num(posinf=0.0).argmax(dim=1).int().cpu().numpy()
+        c["draft"][9:12] = c["target"][13:16].float().nan_to_num(nan=0.0, posinf=0.0, neginf=0.0).to(c["draft"].dtype)
+        v = _run(c)
+        assert v.n_accepted.tolist()[:4] == [-1, -1, -1, -1] and v.n_accepted.tolist()[4] == -1
+    # behind the row that decides nothing matters
+    c = _case(rng, [3, 3], 9000)
+    c["u"][:] = 0.0
+    c["target"][1, c["tokens"][1]] = -math.inf
+    c["target"][2:4] = math.nan
+    c["draft"][2] = math.nan
+    c["tokens"][5] = -1
+    v = _run(c)
+    assert v.n_accepted.tolist() == [1, -1]
+    c = _case(rng, [2, 2, 2], 800, temperature=[-1.0, math.nan, 1.0])
+    want = _want(c)
+    v = _verifier(c)
+    v.run()
+    torch.cuda.synchronize()
+    _check(c, v, want)
+    assert v.n_accepted.tolist()[:2] == [-1, -1]
+
+
+def test_sampled_as_the_target_is():
+    """20000 sequences of one drafted token: how often each token comes out against the target's probabilities, within five standard deviations."""
+    import torch
+    rng = np.random.default_rng(8)
+    B, V = 20000, 9
+    p, q = np.array([.3, .25, .15, .1, .08, .06, .03, .02, .01]), np.array([.05, .2, .2, .2, .05, .05, .1, .1, .05])
+    c = dict(n=[1] * B, V=V, target=torch.from_numpy(np.log(p)).float().cuda().expand(2 * B, V).contiguous(),
+             draft=torch.from_numpy(np.log(q)).float().cuda().expand(B, V).contiguous(), tokens=rng.choice(V, B, p=q).astype(np.int32), temperature=None,
+             u=rng.random(B).astype(np.float32), r=rng.random(B).astype(np.float32), past=np.zeros(B, np.int32))
+    v = _verifier(c)
+    v.run()
+    first = v.out_tokens.view(B, 2)[:, 0].cpu().numpy()
+    share = np.bincount(first, minlength=V) / B
+    assert (np.abs(share - p) <= 5 * np.sqrt(p * (1 - p) / B)).all()
+    assert abs(float((v.n_accepted == 1).float().mean()) - np.minimum(p, q).sum()) < 0.02
+
+
+def test_the_same_on_every_run_in_a_graph_and_on_another_stream():
+    import torch
+    rng = np.random.default_rng(9)
+    c = _case(rng, [3, 8, 0, 5], 128256, temperature=[1.0, 0.8, 0.0, 1.2])
+    v = _run(c)
+    want = [x.clone() for x in (v.n_accepted, v.out_tokens, v.logprob, v.kept_len)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        v.run()
+    stream = torch.cuda.Stream()
+    for k in range(4):
+        for x in (v.n_accepted, v.out_tokens, v.logprob, v.kept_len):
+            x.fill_(3)
+        v.workspace.fill_(255 - k)
+        if k < 3:
+            graph.replay()
+        else:
+            stream.wait_stream(torch.cuda.current_stream())
+            v.run(stream)
+            torch.cuda.current_stream().wait_stream(stream)
+        torch.cuda.synchronize()
+        for got, expect in zip((v.n_accepted, v.out_tokens, v.logprob, v.kept_len), want):
+            assert torch.equal(got, expect)
+
+
+def test_kept_len_may_be_past_len_itself():
+    import torch
+    from paper_2502_02789_amd import binding as sp
+    rng = np.random.default_rng(10)
+    c = _case(rng, [3, 0, 2], 20000)
+    v = _run(c)
+    want = v.kept_len.clone()
+    past = cc.cuda_ints(c["past"])
+    v.args.d_past_len = v.args.d_kept_len = past.data_ptr()
+    sp.sp_verify(v.args)
+    torch.cuda.synchronize()
+    assert torch.equal(past, want)

@@ -20,7 +20,7 @@ constexpr double kLog2e64 = 1.4426950408889634074;
 
 struct RowStats { float top, sum; int32_t arg, pad; };   // of a slice: largest logit, sum of exp((z - top) / temperature), where the largest is
 struct VerifyState {                                       // of a sequence
-  double inv_t;
+  double c;               // of a logit in front of exp2
   float top_p, top_q;
   int32_t row_p, row_q;   // rows of the target and of the draft (-1: none) that the token is sampled from
   int32_t token;          // without draft logits: the token that is taken off, or -1
@@ -49,21 +49,22 @@ struct VerifyDev {
   double* sum_w;
 };
 
-template <bool F32> __device__ __forceinline__ float logit(const void* row, int i) {
-  if constexpr (F32) return static_cast<const float*>(row)[i];
-  else return bf16_lo(static_cast<const uint16_t*>(row)[i]);
-}
 template <bool F32> __device__ __forceinline__ const char* row_of(const void* base, int64_t stride, int64_t row) {
   return static_cast<const char*>(base) + row * stride * (F32 ? 4 : 2);
 }
+template <bool F32> __device__ __forceinline__ float logit(const char* row, int i) {
+  if constexpr (F32) return reinterpret_cast<const float*>(row)[i];
+  else return bf16_lo(reinterpret_cast<const uint16_t*>(row)[i]);
+}
 
-// 16 bytes of logits; those outside [0, V) are -infinity.  i: index of the first, at a multiple of 16 bytes of memory.
+// 16 bytes of logits from element i on, wherever the row begins; those from V on are -infinity
 template <bool F32> constexpr int kVec = F32 ? 4 : 8;
 template <bool F32>
 __device__ __forceinline__ void load_logits(const char* row, int i, int V, float (&x)[kVec<F32>]) {
   constexpr int E = kVec<F32>;
-  if (i >= 0 && i + E <= V) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(row + (int64_t)i * (F32 ? 4 : 2));
+  struct __attribute__((packed, aligned(F32 ? 4 : 2))) Words { u32x4 w; };
+  if (i + E <= V) {
+    const u32x4 w = reinterpret_cast<const Words*>(row + (int64_t)i * (F32 ? 4 : 2))->w;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if constexpr (F32) x[k] = __uint_as_float(w[k]);
@@ -71,23 +72,17 @@ __device__ __forceinline__ void load_logits(const char* row, int i, int V, float
     }
   } else {
 #pragma unroll
-    for (int k = 0; k < E; ++k) x[k] = i + k >= 0 && i + k < V ? logit<F32>(row, i + k) : -INFINITY;
+    for (int k = 0; k < E; ++k) x[k] = i + k < V ? logit<F32>(row, i + k) : -INFINITY;
   }
 }
-// logits between a row's beginning and the multiple of 16 bytes of memory in front of it
-template <bool F32> __device__ __forceinline__ int misaligned(const char* row) { return (int)(reinterpret_cast<uintptr_t>(row) & 15u) / (F32 ? 4 : 2); }
 
-__device__ __forceinline__ float row_factor(const VerifyDev& p, int b) {  // of a logit in front of exp2
-  const float t = p.temperature ? p.temperature[b] : 1.f;
-  return t > 0.f ? (float)(kLog2e64 / (double)t) : (float)kLog2e64;
-}
+// of a logit in front of exp2
+__device__ __forceinline__ double exp2_factor(float t) { return t > 0.f ? kLog2e64 / (double)t : kLog2e64; }
 
-// exp2 of t <= 0 in fp64: 2^n times the Taylor series of exp(f ln 2), |f| <= 1/2, whose first term left out is 2e-16
+// exp2 of t <= 0 in fp64: 2^n times the Taylor series of exp(f ln 2), |f| <= 1/2, whose first term left out is 7e-15
 __device__ __forceinline__ double exp2_64(double t) {
-  if (!(t > -1000.0)) return t != t ? t : 0.0;
-  const double n = rint(t), y = (t - n) * 0.69314718055994530942;
-  double s = 1.0 / 479001600.0;
-  s = fma(s, y, 1.0 / 39916800.0);
+  const double n = rint(fmax(t, -1000.0)), y = (fmax(t, -1000.0) - n) * 0.69314718055994530942;
+  double s = 1.0 / 39916800.0;
   s = fma(s, y, 1.0 / 3628800.0);
   s = fma(s, y, 1.0 / 362880.0);
   s = fma(s, y, 1.0 / 40320.0);
@@ -99,18 +94,24 @@ __device__ __forceinline__ double exp2_64(double t) {
   s = fma(s, y, 0.5);
   s = fma(s, y, 1.0);
   s = fma(s, y, 1.0);
-  return __longlong_as_double(__double_as_longlong(s) + ((long long)n << 52));
+  return t > -1000.0 ? ldexp(s, (int)n) : 0.0;
 }
-__device__ __forceinline__ double weight64(float z, float top, double inv_t) { return exp2_64(((double)z - (double)top) * inv_t * kLog2e64); }
+__device__ __forceinline__ double weight64(float z, float top, double c) { return exp2_64(((double)z - (double)top) * c); }
 
-// the workgroup's 256 numbers added, in an order that does not change; all threads get the sum
-__device__ __forceinline__ double block_sum(double v, double* lds) {
+// N numbers added over the workgroup's 256 threads, in an order that does not change; all threads get the sums
+template <int N>
+__device__ __forceinline__ void block_sums(double (&v)[N], double (*lds)[N]) {
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off, kWave);
+  for (int off = 32; off >= 1; off >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], off, kWave);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) lds[threadIdx.x >> 6][i] = v[i];
   __syncthreads();
-  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = (lds[0][i] + lds[1][i]) + (lds[2][i] + lds[3][i]);
 }
 
 }  // namespace
@@ -123,8 +124,11 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyDev p) {
   const int slice = (int)(blockIdx.x % (uint32_t)p.slices), row = (int)(blockIdx.x / (uint32_t)p.slices);
   const bool target = row < p.T + p.B;
   const int r = target ? row : row - (p.T + p.B);
-  const int used = p.cu[p.B];
-  if (r >= (target ? used + p.B : used)) return;  // (a row of nobody)
+  if (r >= p.cu[p.B] + (target ? p.B : 0)) return;  // (a row of nobody)
+  const char* at = target ? row_of<F32>(p.target, p.target_stride, r) : row_of<F32>(p.draft, p.draft_stride, r);
+  float x[N][E];
+#pragma unroll
+  for (int k = 0; k < N; ++k) load_logits<F32>(at, slice * kSlice + (k * 256 + (int)threadIdx.x) * E, p.V, x[k]);
   float c = (float)kLog2e64;
   bool greedy = false;
   if (p.temperature) {
@@ -133,14 +137,10 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyDev p) {
       const int mid = (lo + hi) >> 1;
       if (p.cu[mid] + (target ? mid : 0) <= r) lo = mid; else hi = mid;
     }
-    c = row_factor(p, lo);
-    greedy = p.temperature[lo] == 0.f;
+    const float t = p.temperature[lo];
+    c = (float)exp2_factor(t);
+    greedy = t == 0.f;
   }
-  const char* at = target ? row_of<F32>(p.target, p.target_stride, r) : row_of<F32>(p.draft, p.draft_stride, r);
-  const int first = slice * kSlice - misaligned<F32>(at);
-  float x[N][E];
-#pragma unroll
-  for (int k = 0; k < N; ++k) load_logits<F32>(at, first + (k * 256 + (int)threadIdx.x) * E, p.V, x[k]);
   float top = -INFINITY;
 #pragma unroll
   for (int k = 0; k < N; ++k)
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyDev p) {
 #pragma unroll
   for (int k = 0; k < N; ++k)
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum += exp2f((x[k][e] - base) * c);
+    for (int e = 0; e < E; ++e) sum += __builtin_amdgcn_exp2f((x[k][e] - base) * c);
   sum = wave_sum(sum);
   int arg = 0x7fffffff;
   if (greedy) {
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyDev p) {
     for (int k = N - 1; k >= 0; --k)
 #pragma unroll
       for (int e = E - 1; e >= 0; --e)
-        if (x[k][e] == top) arg = first + (k * 256 + (int)threadIdx.x) * E + e;
+        if (x[k][e] == top) arg = slice * kSlice + (k * 256 + (int)threadIdx.x) * E + e;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) arg = min(arg, __shfl_xor(arg, off, kWave));
   }
@@ -182,32 +182,49 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyDev p) {
 
 template <bool F32>
 __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
-  constexpr int kRows = 2 * SP_VERIFY_MAX_DRAFTED + 1;
+  constexpr int kRows = 2 * SP_VERIFY_MAX_DRAFTED + 1, E = kVec<F32>;
   __shared__ float tops[kRows];
-  __shared__ double sums[kRows], lds[4];
+  __shared__ double sums[kRows], lds[4][2];
   __shared__ int args[kRows];
   __shared__ int shared_a, shared_bad;
   const int part = (int)(blockIdx.x % (uint32_t)p.parts), b = (int)(blockIdx.x / (uint32_t)p.parts), tid = threadIdx.x;
   const int t0 = p.cu[b], n = p.cu[b + 1] - t0;
   const float t = p.temperature ? p.temperature[b] : 1.f;
   const bool valid = t0 >= 0 && n >= 0 && n <= SP_VERIFY_MAX_DRAFTED && (int64_t)t0 + n <= p.T && t >= 0.f && t < INFINITY;
-  const float c = row_factor(p, b);
-  if (valid) {
-    const int rows = n + 1 + (p.draft ? n : 0);
-    for (int i = tid; i < rows; i += 256) {
+  const double c = exp2_factor(t);
+  // lane j of the first wave has drafted token j
+  const bool mine = valid && tid < n;
+  const int x = mine ? p.tokens[t0 + tid] : 0;
+  const float u = mine ? p.u[t0 + tid] : 0.f;
+  const bool there = x >= 0 && x < p.V;
+  const float zp = mine && there ? logit<F32>(row_of<F32>(p.target, p.target_stride, (int64_t)t0 + b + tid), x) : 0.f;
+  const float zq = mine && there && p.draft ? logit<F32>(row_of<F32>(p.draft, p.draft_stride, t0 + tid), x) : 0.f;
+  if (valid) {  // the rows' sums, 16 lanes to a row
+    const int rows = n + 1 + (p.draft ? n : 0), lane = tid & 15;
+    for (int i = tid >> 4; i < rows; i += 16) {
       const RowStats* s = p.stats + (i <= n ? (int64_t)t0 + b + i : (int64_t)p.T + p.B + t0 + (i - n - 1)) * p.slices;
       float top = -INFINITY;
-      for (int k = 0; k < p.slices; ++k) top = fmaxf(top, s[k].top);
-      const float base = top == -INFINITY ? 0.f : top;
       double sum = 0.0;
       int arg = 0x7fffffff;
-      for (int k = 0; k < p.slices; ++k) {
-        sum += (double)(s[k].sum * exp2f((s[k].top - base) * c));
-        if (s[k].top == top) arg = min(arg, s[k].arg);
+      for (int k = lane; k < p.slices; k += 16) {
+        const RowStats y = s[k];
+        if (y.top == top) arg = min(arg, y.arg);
+        else if (y.top > top) arg = y.arg;
+        const float next = fmaxf(top, y.top), base = next == -INFINITY ? 0.f : next;
+        sum = sum * (double)__builtin_amdgcn_exp2f((top - base) * (float)c) + (double)(y.sum * __builtin_amdgcn_exp2f((y.top - base) * (float)c));
+        top = next;
       }
-      tops[i] = top;
-      sums[i] = sum;
-      args[i] = arg;
+#pragma unroll
+      for (int off = 8; off >= 1; off >>= 1) {
+        const float top2 = __shfl_xor(top, off, kWave);
+        const double sum2 = __shfl_xor(sum, off, kWave);
+        const int arg2 = __shfl_xor(arg, off, kWave);
+        const float next = fmaxf(top, top2), base = next == -INFINITY ? 0.f : next;
+        sum = sum * (double)__builtin_amdgcn_exp2f((top - base) * (float)c) + sum2 * (double)__builtin_amdgcn_exp2f((top2 - base) * (float)c);
+        arg = top == top2 ? min(arg, arg2) : top > top2 ? arg : arg2;
+        top = next;
+      }
+      if (lane == 0) { tops[i] = top; sums[i] = sum; args[i] = arg; }
     }
   }
   __syncthreads();
@@ -215,23 +232,18 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
   if (tid < 64) {
     bool stands = false, bad = false;
     double lp = 0.0;
-    if (valid && tid < n) {
-      const int x = p.tokens[t0 + tid];
-      bad = x < 0 || x >= p.V || !sound(tid) || (p.draft && !sound(n + 1 + tid));
-      if (!bad) {
-        double px, qx = 1.0;
-        if (t > 0.f) {
-          const double z = ((double)logit<F32>(row_of<F32>(p.target, p.target_stride, (int64_t)t0 + b + tid), x) - (double)tops[tid]) / (double)t;
-          px = exp2_64(z * kLog2e64) / sums[tid];
-          lp = z - log(sums[tid]);
-          if (p.draft)
-            qx = weight64(logit<F32>(row_of<F32>(p.draft, p.draft_stride, t0 + tid), x), tops[n + 1 + tid], 1.0 / (double)t) / sums[n + 1 + tid];
-        } else {
-          px = args[tid] == x ? 1.0 : 0.0;
-          if (p.draft) qx = args[n + 1 + tid] == x ? 1.0 : 0.0;
-        }
-        stands = (double)p.u[t0 + tid] * qx < px;
+    if (mine) {
+      bad = !there || !sound(tid) || (p.draft && !sound(n + 1 + tid));
+      double px, qx = 1.0;
+      if (t > 0.f) {
+        px = weight64(zp, tops[tid], c) / sums[tid];
+        if (p.draft) qx = weight64(zq, tops[n + 1 + tid], c) / sums[n + 1 + tid];
+        if (p.logprob && part == 0) lp = ((double)zp - (double)tops[tid]) / (double)t - log(sums[tid]);
+      } else {
+        px = args[tid] == x ? 1.0 : 0.0;
+        if (p.draft) qx = args[n + 1 + tid] == x ? 1.0 : 0.0;
       }
+      stands = !bad && (double)u * qx < px;
     }
     const uint64_t falls = __builtin_amdgcn_ballot_w64(tid < n && !stands), bads = __builtin_amdgcn_ballot_w64(bad);
     const int a = falls ? __builtin_ctzll(falls) : n;
@@ -245,7 +257,7 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
           p.out_tokens[first + j] = -1;
           if (p.logprob) p.logprob[first + j] = __uint_as_float(0x7fc00000u);
         } else if (j < a) {
-          p.out_tokens[first + j] = p.tokens[t0 + j];
+          p.out_tokens[first + j] = x;
           if (p.logprob) p.logprob[first + j] = (float)lp;
         } else if (j > a) {
           p.out_tokens[first + j] = -1;
@@ -259,7 +271,7 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
         p.n_accepted[b] = wrong ? -1 : a;
         if (p.kept_len) p.kept_len[b] = p.past_len[b] + (wrong ? 0 : 1 + a);
         VerifyState s;
-        s.inv_t = t > 0.f ? 1.0 / (double)t : 0.0;
+        s.c = c;
         s.sample = !wrong && t > 0.f;
         s.row_p = s.sample ? t0 + b + a : 0;
         s.row_q = s.sample && a < n && p.draft ? t0 + a : -1;
@@ -273,124 +285,164 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
   __syncthreads();
   const int a = shared_a;
   if (shared_bad || t == 0.f) return;
+  // the row's part of the sums in fp64, and the draft's
   const bool with_q = a < n && p.draft;
   const char* row_p = row_of<F32>(p.target, p.target_stride, (int64_t)t0 + b + a);
-  const char* row_q = with_q ? row_of<F32>(p.draft, p.draft_stride, (int64_t)t0 + a) : nullptr;
-  const double inv_t = 1.0 / (double)t;
+  const char* row_q = with_q ? row_of<F32>(p.draft, p.draft_stride, (int64_t)t0 + a) : row_p;
   const float top_p = tops[a], top_q = with_q ? tops[n + 1 + a] : 0.f;
-  double zp = 0.0, zq = 0.0;
-  for (int k = 0; k < kMine; ++k) {
-    const int i = part * kPart + k * 256 + tid;
-    if (i >= p.V) break;
-    zp += weight64(logit<F32>(row_p, i), top_p, inv_t);
-    if (with_q) zq += weight64(logit<F32>(row_q, i), top_q, inv_t);
+  float vp[kMine / E][E], vq[kMine / E][E];
+  const int first = part * kPart;
+#pragma unroll
+  for (int k = 0; k < kMine / E; ++k) load_logits<F32>(row_p, first + (k * 256 + tid) * E, p.V, vp[k]);
+  if (with_q) {
+#pragma unroll
+    for (int k = 0; k < kMine / E; ++k) load_logits<F32>(row_q, first + (k * 256 + tid) * E, p.V, vq[k]);
   }
-  zp = block_sum(zp, lds);
-  zq = block_sum(zq, lds);
+  double z[2] = {0.0, 0.0};
+#pragma unroll
+  for (int k = 0; k < kMine / E; ++k)
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[0] += weight64(vp[k][e], top_p, c);
+  if (with_q) {
+#pragma unroll
+    for (int k = 0; k < kMine / E; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) z[1] += weight64(vq[k][e], top_q, c);
+  }
+  block_sums(z, lds);
   if (tid == 0) {
-    p.sum_p[(int64_t)b * p.parts + part] = zp;
-    p.sum_q[(int64_t)b * p.parts + part] = zq;
+    p.sum_p[(int64_t)b * p.parts + part] = z[0];
+    p.sum_q[(int64_t)b * p.parts + part] = z[1];
   }
-}
-
-// sums over a sequence's parts, by 256 threads
-__device__ __forceinline__ double parts_sum(const double* parts, int n, double* lds) {
-  double v = 0.0;
-  for (int i = threadIdx.x; i < n; i += 256) v += parts[i];
-  return block_sum(v, lds);
 }
 
 // what is left of p_i over the draft: max(p_i - q_i, 0), p and q normalised
-template <bool F32>
-__device__ __forceinline__ double residual_weight(const VerifyDev& p, const VerifyState& s, const char* row_p, const char* row_q, int i, double inv_p, double inv_q) {
-  const double w = weight64(logit<F32>(row_p, i), s.top_p, s.inv_t) * inv_p;
-  if (i == s.token) return 0.0;
-  if (!row_q) return w;
-  const double left = w - weight64(logit<F32>(row_q, i), s.top_q, s.inv_t) * inv_q;
-  return left > 0.0 ? left : 0.0;
+__device__ __forceinline__ double residual_weight(const VerifyState& s, float zp, float zq, bool with_q, int i, double inv_p, double inv_q) {
+  double w = weight64(zp, s.top_p, s.c) * inv_p;
+  if (with_q) w = fmax(w - weight64(zq, s.top_q, s.c) * inv_q, 0.0);
+  return i == s.token ? 0.0 : w;
 }
 
 template <bool F32>
 __global__ __launch_bounds__(256) void verify_residual_kernel(const VerifyDev p) {
-  __shared__ double lds[4];
-  const int part = (int)(blockIdx.x % (uint32_t)p.parts), b = (int)(blockIdx.x / (uint32_t)p.parts);
+  constexpr int E = kVec<F32>;
+  __shared__ double lds[4][2], lds1[4][1];
+  const int part = (int)(blockIdx.x % (uint32_t)p.parts), b = (int)(blockIdx.x / (uint32_t)p.parts), tid = threadIdx.x;
   const VerifyState s = p.states[b];
   if (!s.sample) return;
+  const bool with_q = s.row_q >= 0;
   const char* row_p = row_of<F32>(p.target, p.target_stride, s.row_p);
-  const char* row_q = s.row_q >= 0 ? row_of<F32>(p.draft, p.draft_stride, s.row_q) : nullptr;
-  const double inv_p = 1.0 / parts_sum(p.sum_p + (int64_t)b * p.parts, p.parts, lds);
-  const double inv_q = row_q ? 1.0 / parts_sum(p.sum_q + (int64_t)b * p.parts, p.parts, lds) : 0.0;
-  double sum = 0.0;
-  for (int k = 0; k < kMine; ++k) {
-    const int i = part * kPart + k * 256 + (int)threadIdx.x;
-    if (i >= p.V) break;
-    sum += residual_weight<F32>(p, s, row_p, row_q, i, inv_p, inv_q);
+  const char* row_q = row_of<F32>(p.draft, p.draft_stride, s.row_q);
+  float vp[kMine / E][E], vq[kMine / E][E];
+  const int first = part * kPart;
+#pragma unroll
+  for (int k = 0; k < kMine / E; ++k) load_logits<F32>(row_p, first + (k * 256 + tid) * E, p.V, vp[k]);
+  if (with_q) {
+#pragma unroll
+    for (int k = 0; k < kMine / E; ++k) load_logits<F32>(row_q, first + (k * 256 + tid) * E, p.V, vq[k]);
   }
-  sum = block_sum(sum, lds);
-  if (threadIdx.x == 0) p.sum_w[(int64_t)b * p.parts + part] = sum;
+  double z[2] = {0.0, 0.0};
+  for (int i = tid; i < p.parts; i += 256) {
+    z[0] += p.sum_p[(int64_t)b * p.parts + i];
+    if (with_q) z[1] += p.sum_q[(int64_t)b * p.parts + i];
+  }
+  block_sums(z, lds);
+  const double inv_p = 1.0 / z[0], inv_q = with_q ? 1.0 / z[1] : 0.0;
+  double sum[1] = {0.0};
+#pragma unroll
+  for (int k = 0; k < kMine / E; ++k)
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[0] += residual_weight(s, vp[k][e], with_q ? vq[k][e] : 0.f, with_q, first + (k * 256 + tid) * E + e, inv_p, inv_q);
+  block_sums(sum, lds1);
+  if (tid == 0) p.sum_w[(int64_t)b * p.parts + part] = sum[0];
+}
+
+// exclusive sums over the workgroup's 256 threads
+__device__ __forceinline__ double block_before(double v, double* lds) {
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  double x = v;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const double y = __shfl_up(x, off, kWave);
+    if (l >= off) x += y;
+  }
+  __syncthreads();
+  if (l == 63) lds[w] = x;
+  __syncthreads();
+  double before = 0.0;
+  for (int i = 0; i < w; ++i) before += lds[i];
+  return before + (x - v);
 }
 
 template <bool F32>
 __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
-  __shared__ double lds[4], run[256];
-  __shared__ int found, last, picked;
-  __shared__ double before;
+  constexpr int E = kVec<F32>;
+  __shared__ double lds[4][3], run[4], start;
+  __shared__ int found, last, hit_part, last_part;
   const int b = blockIdx.x, tid = threadIdx.x;
   VerifyState s = p.states[b];
   if (!s.sample) return;
+  if (tid == 0) { found = hit_part = 0x7fffffff; last = last_part = -1; }
+  bool with_q = s.row_q >= 0;
   const char* row_p = row_of<F32>(p.target, p.target_stride, s.row_p);
-  const char* row_q = s.row_q >= 0 ? row_of<F32>(p.draft, p.draft_stride, s.row_q) : nullptr;
-  const double sum_p = parts_sum(p.sum_p + (int64_t)b * p.parts, p.parts, lds);
-  const double inv_p = 1.0 / sum_p;
-  double inv_q = row_q ? 1.0 / parts_sum(p.sum_q + (int64_t)b * p.parts, p.parts, lds) : 0.0;
+  const char* row_q = row_of<F32>(p.draft, p.draft_stride, s.row_q);
+  const double* sum_p = p.sum_p + (int64_t)b * p.parts;
+  const double* sum_q = p.sum_q + (int64_t)b * p.parts;
   const double* parts = p.sum_w + (int64_t)b * p.parts;
-  double total = parts_sum(parts, p.parts, lds), unit = 1.0;
+  double z[3] = {0.0, 0.0, 0.0};
+  for (int i = tid; i < p.parts; i += 256) {
+    z[0] += sum_p[i];
+    if (with_q) z[1] += sum_q[i];
+    z[2] += parts[i];
+  }
+  block_sums(z, lds);
+  const double inv_p = 1.0 / z[0], inv_q = with_q ? 1.0 / z[1] : 0.0;
+  double total = z[2], unit = 1.0;
   if (!(total > 0.0)) {  // nothing is left: p itself
-    parts = p.sum_p + (int64_t)b * p.parts;
+    parts = sum_p;
     unit = inv_p;
-    total = sum_p * inv_p;
-    row_q = nullptr;
+    total = z[0] * inv_p;
+    with_q = false;
     s.token = -1;
   }
   const double bound = (double)p.r[b] * total;
-  // the first part whose end lies beyond the bound, else the last that has anything
-  if (tid == 0) {
-    double at = 0.0, start = 0.0;
-    int pick = 0;
-    for (int i = 0; i < p.parts; ++i) {
-      const double w = parts[i] * unit;
-      if (w > 0.0) {
-        pick = i;
-        start = at;
-        if (at + w > bound) break;
-      }
-      at += w;
+  // the first part whose end lies beyond the bound, else the last that has anything; every thread has neighbours of its own
+  const int per = (p.parts + 255) / 256, i0 = min(p.parts, tid * per), i1 = min(p.parts, i0 + per);
+  double sum = 0.0;
+  for (int i = i0; i < i1; ++i) sum += parts[i] * unit;
+  const double before = block_before(sum, run);
+  double at = before;
+  for (int i = i0; i < i1; ++i) {
+    const double w = parts[i] * unit;
+    if (w > 0.0) {
+      atomicMax(&last_part, i);
+      if (at + w > bound) atomicMin(&hit_part, i);
     }
-    found = 0x7fffffff;
-    last = -1;
-    picked = pick;
-    before = start;
+    at += w;
   }
   __syncthreads();
-  const int part = picked;
-  const double start = before;
-  // every thread has neighbours of its own
+  const int part = hit_part != 0x7fffffff ? hit_part : max(last_part, 0);
+  // what lies before it (the thread that has it says so)
+  if (part >= i0 && part < i1) {
+    at = before;
+    for (int i = i0; i < part; ++i) at += parts[i] * unit;
+    start = at;
+  }
+  __syncthreads();
   const int first = part * kPart + tid * kMine;
   double w[kMine], mine = 0.0;
 #pragma unroll
-  for (int k = 0; k < kMine; ++k) {
-    w[k] = first + k < p.V ? residual_weight<F32>(p, s, row_p, row_q, first + k, inv_p, inv_q) : 0.0;
-    mine += w[k];
+  for (int k = 0; k < kMine / E; ++k) {
+    float vp[E], vq[E];
+    load_logits<F32>(row_p, first + k * E, p.V, vp);
+    if (with_q) load_logits<F32>(row_q, first + k * E, p.V, vq);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      w[k * E + e] = residual_weight(s, vp[e], with_q ? vq[e] : 0.f, with_q, first + k * E + e, inv_p, inv_q);
+      mine += w[k * E + e];
+    }
   }
-  run[tid] = mine;
-  __syncthreads();
-  for (int off = 1; off < 256; off <<= 1) {
-    const double v = tid >= off ? run[tid - off] : 0.0;
-    __syncthreads();
-    run[tid] += v;
-    __syncthreads();
-  }
-  double at = start + (tid > 0 ? run[tid - 1] : 0.0);
+  at = start + block_before(mine, run);
   int hit = 0x7fffffff, end = -1;
 #pragma unroll
   for (int k = 0; k < kMine; ++k) {
@@ -406,7 +458,7 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
   if (tid == 0) {
     const int y = found != 0x7fffffff ? found : max(last, 0);
     p.out_tokens[s.row_p] = y;
-    if (p.logprob) p.logprob[s.row_p] = (float)(((double)logit<F32>(row_p, y) - (double)s.top_p) * s.inv_t - log(sum_p));
+    if (p.logprob) p.logprob[s.row_p] = (float)(((double)logit<F32>(row_p, y) - (double)s.top_p) * s.c * 0.69314718055994530942 - log(z[0]));
   }
 }
 
@@ -414,7 +466,7 @@ namespace {
 
 struct VerifyLayout { size_t states, sum_p, sum_q, sum_w, bytes; };
 
-int verify_slices(const sp_verify_args* a) { return (int)(((int64_t)a->V + 7 + kSlice - 1) / kSlice); }  // (a row may begin up to 7 logits behind a multiple of 16 bytes)
+int verify_slices(const sp_verify_args* a) { return (a->V + kSlice - 1) / kSlice; }
 int verify_parts(const sp_verify_args* a) { return (a->V + kPart - 1) / kPart; }
 
 VerifyLayout verify_layout(const sp_verify_args* a) {

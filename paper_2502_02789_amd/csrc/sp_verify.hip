@@ -16,6 +16,7 @@ namespace {
 constexpr int kSlice = 8192;     // logits of a row that a workgroup of the first kernel takes
 constexpr int kPart = 4096;      // ... of the others
 constexpr int kMine = kPart / 256;
+constexpr int kStrip = kPart / 4; // ... of a wave: sums are kept by strips
 constexpr double kLog2e64 = 1.4426950408889634074;
 
 struct RowStats { float top, sum; int32_t arg, pad; };   // of a slice: largest logit, sum of exp((z - top) / temperature), where the largest is
@@ -44,7 +45,7 @@ struct VerifyDev {
   int32_t* kept_len;
   RowStats* stats;     // [T + B rows of the target, T of the draft][slices]
   VerifyState* states; // [B]
-  double* sum_p;       // [B][parts]
+  double* sum_p;       // [B][4 parts], by strips
   double* sum_q;
   double* sum_w;
 };
@@ -57,56 +58,95 @@ template <bool F32> __device__ __forceinline__ float logit(const char* row, int 
   else return bf16_lo(reinterpret_cast<const uint16_t*>(row)[i]);
 }
 
-// 16 bytes of logits from element i on, wherever the row begins; those from V on are -infinity
+// N times 16 bytes of logits, those of k from element first + k step on, wherever the row begins; those from V on are -infinity.  (All loads are on their way
+// together: what would lie outside the row is read at its beginning instead, and the one vector that a row ends in comes element by element.)
 template <bool F32> constexpr int kVec = F32 ? 4 : 8;
-template <bool F32>
-__device__ __forceinline__ void load_logits(const char* row, int i, int V, float (&x)[kVec<F32>]) {
+template <bool F32, int N>
+__device__ __forceinline__ void load_logits(const char* row, int first, int step, int V, float (&x)[N][kVec<F32>]) {
   constexpr int E = kVec<F32>;
   struct __attribute__((packed, aligned(F32 ? 4 : 2))) Words { u32x4 w; };
-  if (i + E <= V) {
-    const u32x4 w = reinterpret_cast<const Words*>(row + (int64_t)i * (F32 ? 4 : 2))->w;
+  u32x4 w[N];
+  if (V >= E) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if constexpr (F32) x[k] = __uint_as_float(w[k]);
-      else { x[2 * k] = bf16_lo(w[k]); x[2 * k + 1] = bf16_hi(w[k]); }
+    for (int k = 0; k < N; ++k) {
+      const int i = first + k * step;
+      w[k] = reinterpret_cast<const Words*>(row + (uint32_t)(i + E <= V ? i : 0) * (F32 ? 4 : 2))->w;
     }
-  } else {
+  }
 #pragma unroll
-    for (int k = 0; k < E; ++k) x[k] = i + k < V ? logit<F32>(row, i + k) : -INFINITY;
+  for (int k = 0; k < N; ++k) {
+    const bool whole = first + k * step + E <= V;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (F32) {
+        x[k][e] = whole ? __uint_as_float(w[k][e]) : -INFINITY;
+      } else {
+        const uint32_t y = whole ? w[k][e] : 0xff80ff80u;
+        x[k][2 * e] = bf16_lo(y);
+        x[k][2 * e + 1] = bf16_hi(y);
+      }
+    }
+  }
+  if (V % E != 0) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int i = first + k * step;
+      if (i < V && i + E > V) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (i + e < V) x[k][e] = logit<F32>(row, i + e);
+      }
+    }
   }
 }
 
 // of a logit in front of exp2
 __device__ __forceinline__ double exp2_factor(float t) { return t > 0.f ? kLog2e64 / (double)t : kLog2e64; }
 
-// exp2 of t <= 0 in fp64: 2^n times the Taylor series of exp(f ln 2), |f| <= 1/2, whose first term left out is 7e-15
-__device__ __forceinline__ double exp2_64(double t) {
-  const double n = rint(fmax(t, -1000.0)), y = (fmax(t, -1000.0) - n) * 0.69314718055994530942;
-  double s = 1.0 / 39916800.0;
-  s = fma(s, y, 1.0 / 3628800.0);
-  s = fma(s, y, 1.0 / 362880.0);
-  s = fma(s, y, 1.0 / 40320.0);
-  s = fma(s, y, 1.0 / 5040.0);
-  s = fma(s, y, 1.0 / 720.0);
-  s = fma(s, y, 1.0 / 120.0);
-  s = fma(s, y, 1.0 / 24.0);
-  s = fma(s, y, 1.0 / 6.0);
-  s = fma(s, y, 0.5);
-  s = fma(s, y, 1.0);
-  s = fma(s, y, 1.0);
-  return t > -1000.0 ? ldexp(s, (int)n) : 0.0;
+// exp((z - top) / temperature) in fp64, c = log2(e) / temperature and top_c = top * c: 2^n times the Taylor series of exp(f ln 2), |f| <= 1/2, whose first
+// term left out is 7e-15.  (n comes out of the low bits of the sum with 1.5 2^52.)  -infinity becomes 2^-1000, which is nothing in a sum.
+struct Exp64 {
+  double k[11] = {4.4455382718708114e-10, 7.0549116208011234e-9, 1.0178086009239699e-7, 1.3215486790144309e-6, 1.5252733804059841e-5, 1.5403530393381609e-4,
+                  1.3333558146428443e-3, 9.6181291076284772e-3, 5.5504108664821580e-2, 0.24022650695910071, 0.69314718055994531};  // ln(2)^k / k!, k = 11 .. 1
+  __device__ __forceinline__ Exp64() {  // (kept in scalar registers: as literals, each would be moved into a vector register in front of its use)
+#pragma unroll
+    for (int i = 0; i < 11; ++i) asm volatile("" : "+s"(k[i]));
+  }
+  __device__ __forceinline__ double operator()(float z, double top_c, double c) const {
+    const double t = fmax(fma((double)z, c, -top_c), -1000.0), shifted = t + 6755399441055744.0, f = t - (shifted - 6755399441055744.0);
+    double s = k[0];
+#pragma unroll
+    for (int i = 1; i < 11; ++i) s = fma(s, f, k[i]);
+    s = fma(s, f, 1.0);
+    const uint64_t bits = (uint64_t)__double_as_longlong(s);
+    return __longlong_as_double((long long)((bits & 0xffffffffull) | (uint64_t)((uint32_t)(bits >> 32) + ((uint32_t)__double_as_longlong(shifted) << 20)) << 32));
+  }
+};
+
+// the wave's numbers added, in an order that does not change; lane 63 gets the sum
+template <int CTRL, int ROWS> __device__ __forceinline__ double moved(double v) {  // (0 where a lane gets none)
+  const uint64_t x = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xf, false);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
-__device__ __forceinline__ double weight64(float z, float top, double c) { return exp2_64(((double)z - (double)top) * c); }
+// ... every lane the sum of those up to its own
+__device__ __forceinline__ double wave_prefix(double v) {
+  v += moved<0x111, 0xf>(v);   // from the lane 1, 2, 4, 8 below, in rows of 16
+  v += moved<0x112, 0xf>(v);
+  v += moved<0x114, 0xf>(v);
+  v += moved<0x118, 0xf>(v);
+  v += moved<0x142, 0xa>(v);   // a row's last lane into the next row, into the upper half
+  v += moved<0x143, 0xc>(v);
+  return v;
+}
 
 // N numbers added over the workgroup's 256 threads, in an order that does not change; all threads get the sums
 template <int N>
 __device__ __forceinline__ void block_sums(double (&v)[N], double (*lds)[N]) {
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], off, kWave);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0)
+  for (int i = 0; i < N; ++i) v[i] = wave_prefix(v[i]);
+  if ((threadIdx.x & 63) == 63)
 #pragma unroll
     for (int i = 0; i < N; ++i) lds[threadIdx.x >> 6][i] = v[i];
   __syncthreads();
@@ -127,8 +167,7 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyDev p) {
   if (r >= p.cu[p.B] + (target ? p.B : 0)) return;  // (a row of nobody)
   const char* at = target ? row_of<F32>(p.target, p.target_stride, r) : row_of<F32>(p.draft, p.draft_stride, r);
   float x[N][E];
-#pragma unroll
-  for (int k = 0; k < N; ++k) load_logits<F32>(at, slice * kSlice + (k * 256 + (int)threadIdx.x) * E, p.V, x[k]);
+  load_logits<F32, N>(at, slice * kSlice + (int)threadIdx.x * E, 256 * E, p.V, x);
   float c = (float)kLog2e64;
   bool greedy = false;
   if (p.temperature) {
@@ -141,40 +180,43 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyDev p) {
     c = (float)exp2_factor(t);
     greedy = t == 0.f;
   }
-  float top = -INFINITY;
+  // every thread's own maximum and sum, then the wave's, then the workgroup's
+  float top = -INFINITY, sum = 0.f;
 #pragma unroll
   for (int k = 0; k < N; ++k)
 #pragma unroll
     for (int e = 0; e < E; ++e) top = fmaxf(top, x[k][e]);
-  top = wave_max(top);
-  const int w = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 0) tops[w] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
   const float base = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
 #pragma unroll
   for (int k = 0; k < N; ++k)
 #pragma unroll
     for (int e = 0; e < E; ++e) sum += __builtin_amdgcn_exp2f((x[k][e] - base) * c);
-  sum = wave_sum(sum);
+  const float wave_top = wave_max(top), wave_base = wave_top == -INFINITY ? 0.f : wave_top;
+  sum = wave_sum(sum * __builtin_amdgcn_exp2f((top - wave_base) * c));
   int arg = 0x7fffffff;
   if (greedy) {
 #pragma unroll
     for (int k = N - 1; k >= 0; --k)
 #pragma unroll
       for (int e = E - 1; e >= 0; --e)
-        if (x[k][e] == top) arg = slice * kSlice + (k * 256 + (int)threadIdx.x) * E + e;
+        if (x[k][e] == wave_top) arg = slice * kSlice + (k * 256 + (int)threadIdx.x) * E + e;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) arg = min(arg, __shfl_xor(arg, off, kWave));
   }
-  if ((threadIdx.x & 63) == 0) { sums[w] = sum; args[w] = arg; }
+  const int w = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) { tops[w] = wave_top; sums[w] = sum; args[w] = arg; }
   __syncthreads();
   if (threadIdx.x == 0) {
     RowStats s;
-    s.top = top;
-    s.sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    s.arg = min(min(args[0], args[1]), min(args[2], args[3]));
+    s.top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    const float all = s.top == -INFINITY ? 0.f : s.top;
+    s.sum = 0.f;
+    s.arg = 0x7fffffff;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s.sum += sums[i] * __builtin_amdgcn_exp2f((tops[i] - all) * c);
+      if (tops[i] == s.top) s.arg = min(s.arg, args[i]);
+    }
     s.pad = 0;
     p.stats[(int64_t)row * p.slices + slice] = s;
   }
@@ -184,7 +226,7 @@ template <bool F32>
 __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
   constexpr int kRows = 2 * SP_VERIFY_MAX_DRAFTED + 1, E = kVec<F32>;
   __shared__ float tops[kRows];
-  __shared__ double sums[kRows], lds[4][2];
+  __shared__ double sums[kRows];
   __shared__ int args[kRows];
   __shared__ int shared_a, shared_bad;
   const int part = (int)(blockIdx.x % (uint32_t)p.parts), b = (int)(blockIdx.x / (uint32_t)p.parts), tid = threadIdx.x;
@@ -192,6 +234,7 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
   const float t = p.temperature ? p.temperature[b] : 1.f;
   const bool valid = t0 >= 0 && n >= 0 && n <= SP_VERIFY_MAX_DRAFTED && (int64_t)t0 + n <= p.T && t >= 0.f && t < INFINITY;
   const double c = exp2_factor(t);
+  const Exp64 exp64;
   // lane j of the first wave has drafted token j
   const bool mine = valid && tid < n;
   const int x = mine ? p.tokens[t0 + tid] : 0;
@@ -236,8 +279,8 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
       bad = !there || !sound(tid) || (p.draft && !sound(n + 1 + tid));
       double px, qx = 1.0;
       if (t > 0.f) {
-        px = weight64(zp, tops[tid], c) / sums[tid];
-        if (p.draft) qx = weight64(zq, tops[n + 1 + tid], c) / sums[n + 1 + tid];
+        px = zp == -INFINITY ? 0.0 : exp64(zp, (double)tops[tid] * c, c) / sums[tid];
+        if (p.draft) qx = zq == -INFINITY ? 0.0 : exp64(zq, (double)tops[n + 1 + tid] * c, c) / sums[n + 1 + tid];
         if (p.logprob && part == 0) lp = ((double)zp - (double)tops[tid]) / (double)t - log(sums[tid]);
       } else {
         px = args[tid] == x ? 1.0 : 0.0;
@@ -285,48 +328,46 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
   __syncthreads();
   const int a = shared_a;
   if (shared_bad || t == 0.f) return;
-  // the row's part of the sums in fp64, and the draft's
+  // the row's part of the sums in fp64, and the draft's, a strip to a wave
   const bool with_q = a < n && p.draft;
   const char* row_p = row_of<F32>(p.target, p.target_stride, (int64_t)t0 + b + a);
   const char* row_q = with_q ? row_of<F32>(p.draft, p.draft_stride, (int64_t)t0 + a) : row_p;
-  const float top_p = tops[a], top_q = with_q ? tops[n + 1 + a] : 0.f;
+  const double top_p = (double)tops[a] * c, top_q = with_q ? (double)tops[n + 1 + a] * c : 0.0;
   float vp[kMine / E][E], vq[kMine / E][E];
-  const int first = part * kPart;
-#pragma unroll
-  for (int k = 0; k < kMine / E; ++k) load_logits<F32>(row_p, first + (k * 256 + tid) * E, p.V, vp[k]);
-  if (with_q) {
-#pragma unroll
-    for (int k = 0; k < kMine / E; ++k) load_logits<F32>(row_q, first + (k * 256 + tid) * E, p.V, vq[k]);
-  }
-  double z[2] = {0.0, 0.0};
+  const int strip = part * 4 + (tid >> 6), first = strip * kStrip + (tid & 63) * E;
+  load_logits<F32, kMine / E>(row_p, first, 64 * E, p.V, vp);
+  if (with_q) load_logits<F32, kMine / E>(row_q, first, 64 * E, p.V, vq);
+  double z = 0.0, zd = 0.0;
 #pragma unroll
   for (int k = 0; k < kMine / E; ++k)
 #pragma unroll
-    for (int e = 0; e < E; ++e) z[0] += weight64(vp[k][e], top_p, c);
+    for (int e = 0; e < E; ++e) z += exp64(vp[k][e], top_p, c);
   if (with_q) {
 #pragma unroll
     for (int k = 0; k < kMine / E; ++k)
 #pragma unroll
-      for (int e = 0; e < E; ++e) z[1] += weight64(vq[k][e], top_q, c);
+      for (int e = 0; e < E; ++e) zd += exp64(vq[k][e], top_q, c);
   }
-  block_sums(z, lds);
-  if (tid == 0) {
-    p.sum_p[(int64_t)b * p.parts + part] = z[0];
-    p.sum_q[(int64_t)b * p.parts + part] = z[1];
+  z = wave_prefix(z);
+  zd = wave_prefix(zd);
+  if ((tid & 63) == 63) {
+    p.sum_p[(int64_t)b * 4 * p.parts + strip] = z;
+    p.sum_q[(int64_t)b * 4 * p.parts + strip] = zd;
   }
 }
 
 // what is left of p_i over the draft: max(p_i - q_i, 0), p and q normalised
-__device__ __forceinline__ double residual_weight(const VerifyState& s, float zp, float zq, bool with_q, int i, double inv_p, double inv_q) {
-  double w = weight64(zp, s.top_p, s.c) * inv_p;
-  if (with_q) w = fmax(w - weight64(zq, s.top_q, s.c) * inv_q, 0.0);
+struct Residual { double c, top_p, top_q, inv_p, inv_q; int token; bool with_q; };
+__device__ __forceinline__ double residual_weight(const Exp64& exp64, const Residual& s, float zp, float zq, int i) {
+  double w = zp == -INFINITY ? 0.0 : exp64(zp, s.top_p, s.c) * s.inv_p;
+  if (s.with_q) w = fmax(w - (zq == -INFINITY ? 0.0 : exp64(zq, s.top_q, s.c) * s.inv_q), 0.0);
   return i == s.token ? 0.0 : w;
 }
 
 template <bool F32>
 __global__ __launch_bounds__(256) void verify_residual_kernel(const VerifyDev p) {
   constexpr int E = kVec<F32>;
-  __shared__ double lds[4][2], lds1[4][1];
+  __shared__ double lds[4][2];
   const int part = (int)(blockIdx.x % (uint32_t)p.parts), b = (int)(blockIdx.x / (uint32_t)p.parts), tid = threadIdx.x;
   const VerifyState s = p.states[b];
   if (!s.sample) return;
@@ -334,40 +375,32 @@ __global__ __launch_bounds__(256) void verify_residual_kernel(const VerifyDev p)
   const char* row_p = row_of<F32>(p.target, p.target_stride, s.row_p);
   const char* row_q = row_of<F32>(p.draft, p.draft_stride, s.row_q);
   float vp[kMine / E][E], vq[kMine / E][E];
-  const int first = part * kPart;
-#pragma unroll
-  for (int k = 0; k < kMine / E; ++k) load_logits<F32>(row_p, first + (k * 256 + tid) * E, p.V, vp[k]);
-  if (with_q) {
-#pragma unroll
-    for (int k = 0; k < kMine / E; ++k) load_logits<F32>(row_q, first + (k * 256 + tid) * E, p.V, vq[k]);
-  }
+  const Exp64 exp64;
+  const int strip = part * 4 + (tid >> 6), first = strip * kStrip + (tid & 63) * E;
+  load_logits<F32, kMine / E>(row_p, first, 64 * E, p.V, vp);
+  if (with_q) load_logits<F32, kMine / E>(row_q, first, 64 * E, p.V, vq);
   double z[2] = {0.0, 0.0};
-  for (int i = tid; i < p.parts; i += 256) {
-    z[0] += p.sum_p[(int64_t)b * p.parts + i];
-    if (with_q) z[1] += p.sum_q[(int64_t)b * p.parts + i];
+  for (int i = tid; i < 4 * p.parts; i += 256) {
+    z[0] += p.sum_p[(int64_t)b * 4 * p.parts + i];
+    if (with_q) z[1] += p.sum_q[(int64_t)b * 4 * p.parts + i];
   }
   block_sums(z, lds);
-  const double inv_p = 1.0 / z[0], inv_q = with_q ? 1.0 / z[1] : 0.0;
-  double sum[1] = {0.0};
+  const Residual w = {s.c, (double)s.top_p * s.c, (double)s.top_q * s.c, 1.0 / z[0], 1.0 / z[1], s.token, with_q};
+  double sum = 0.0;
 #pragma unroll
   for (int k = 0; k < kMine / E; ++k)
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[0] += residual_weight(s, vp[k][e], with_q ? vq[k][e] : 0.f, with_q, first + (k * 256 + tid) * E + e, inv_p, inv_q);
-  block_sums(sum, lds1);
-  if (tid == 0) p.sum_w[(int64_t)b * p.parts + part] = sum[0];
+    for (int e = 0; e < E; ++e) sum += residual_weight(exp64, w, vp[k][e], with_q ? vq[k][e] : 0.f, first + k * 64 * E + e);
+  sum = wave_prefix(sum);
+  if ((tid & 63) == 63) p.sum_w[(int64_t)b * 4 * p.parts + strip] = sum;
 }
 
 // exclusive sums over the workgroup's 256 threads
 __device__ __forceinline__ double block_before(double v, double* lds) {
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-  double x = v;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const double y = __shfl_up(x, off, kWave);
-    if (l >= off) x += y;
-  }
+  const int w = threadIdx.x >> 6;
+  const double x = wave_prefix(v);
   __syncthreads();
-  if (l == 63) lds[w] = x;
+  if ((threadIdx.x & 63) == 63) lds[w] = x;
   __syncthreads();
   double before = 0.0;
   for (int i = 0; i < w; ++i) before += lds[i];
@@ -376,76 +409,72 @@ __device__ __forceinline__ double block_before(double v, double* lds) {
 
 template <bool F32>
 __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
-  constexpr int E = kVec<F32>;
+  constexpr int M = kStrip / 256;
   __shared__ double lds[4][3], run[4], start;
-  __shared__ int found, last, hit_part, last_part;
+  __shared__ int found, last, hit_strip, last_strip;
   const int b = blockIdx.x, tid = threadIdx.x;
-  VerifyState s = p.states[b];
+  const VerifyState s = p.states[b];
   if (!s.sample) return;
-  if (tid == 0) { found = hit_part = 0x7fffffff; last = last_part = -1; }
-  bool with_q = s.row_q >= 0;
+  if (tid == 0) { found = hit_strip = 0x7fffffff; last = last_strip = -1; }
+  const bool with_q = s.row_q >= 0;
   const char* row_p = row_of<F32>(p.target, p.target_stride, s.row_p);
   const char* row_q = row_of<F32>(p.draft, p.draft_stride, s.row_q);
-  const double* sum_p = p.sum_p + (int64_t)b * p.parts;
-  const double* sum_q = p.sum_q + (int64_t)b * p.parts;
-  const double* parts = p.sum_w + (int64_t)b * p.parts;
+  const int strips = 4 * p.parts;
+  const Exp64 exp64;
+  const double* sum_p = p.sum_p + (int64_t)b * strips;
+  const double* sum_q = p.sum_q + (int64_t)b * strips;
+  const double* sums = p.sum_w + (int64_t)b * strips;
   double z[3] = {0.0, 0.0, 0.0};
-  for (int i = tid; i < p.parts; i += 256) {
+  for (int i = tid; i < strips; i += 256) {
     z[0] += sum_p[i];
     if (with_q) z[1] += sum_q[i];
-    z[2] += parts[i];
+    z[2] += sums[i];
   }
   block_sums(z, lds);
-  const double inv_p = 1.0 / z[0], inv_q = with_q ? 1.0 / z[1] : 0.0;
+  Residual res = {s.c, (double)s.top_p * s.c, (double)s.top_q * s.c, 1.0 / z[0], 1.0 / z[1], s.token, with_q};
   double total = z[2], unit = 1.0;
   if (!(total > 0.0)) {  // nothing is left: p itself
-    parts = sum_p;
-    unit = inv_p;
-    total = z[0] * inv_p;
-    with_q = false;
-    s.token = -1;
+    sums = sum_p;
+    unit = res.inv_p;
+    total = z[0] * unit;
+    res.with_q = false;
+    res.token = -1;
   }
   const double bound = (double)p.r[b] * total;
-  // the first part whose end lies beyond the bound, else the last that has anything; every thread has neighbours of its own
-  const int per = (p.parts + 255) / 256, i0 = min(p.parts, tid * per), i1 = min(p.parts, i0 + per);
+  // the first strip whose end lies beyond the bound, else the last that has anything; every thread has neighbours of its own
+  const int per = (strips + 255) / 256, i0 = min(strips, tid * per), i1 = min(strips, i0 + per);
   double sum = 0.0;
-  for (int i = i0; i < i1; ++i) sum += parts[i] * unit;
+  for (int i = i0; i < i1; ++i) sum += sums[i] * unit;
   const double before = block_before(sum, run);
   double at = before;
   for (int i = i0; i < i1; ++i) {
-    const double w = parts[i] * unit;
+    const double w = sums[i] * unit;
     if (w > 0.0) {
-      atomicMax(&last_part, i);
-      if (at + w > bound) atomicMin(&hit_part, i);
+      atomicMax(&last_strip, i);
+      if (at + w > bound) atomicMin(&hit_strip, i);
     }
     at += w;
   }
   __syncthreads();
-  const int part = hit_part != 0x7fffffff ? hit_part : max(last_part, 0);
-  // what lies before it (the thread that has it says so)
-  if (part >= i0 && part < i1) {
+  const int strip = hit_strip != 0x7fffffff ? hit_strip : max(last_strip, 0);
+  if (strip >= i0 && strip < i1) {  // (the thread that has it says what lies before it)
     at = before;
-    for (int i = i0; i < part; ++i) at += parts[i] * unit;
+    for (int i = i0; i < strip; ++i) at += sums[i] * unit;
     start = at;
   }
-  __syncthreads();
-  const int first = part * kPart + tid * kMine;
-  double w[kMine], mine = 0.0;
+  const int first = strip * kStrip + tid * M;
+  double w[M], mine = 0.0;
 #pragma unroll
-  for (int k = 0; k < kMine / E; ++k) {
-    float vp[E], vq[E];
-    load_logits<F32>(row_p, first + k * E, p.V, vp);
-    if (with_q) load_logits<F32>(row_q, first + k * E, p.V, vq);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      w[k * E + e] = residual_weight(s, vp[e], with_q ? vq[e] : 0.f, with_q, first + k * E + e, inv_p, inv_q);
-      mine += w[k * E + e];
-    }
+  for (int k = 0; k < M; ++k) {
+    const bool there = first + k < p.V;
+    w[k] = there ? residual_weight(exp64, res, logit<F32>(row_p, there ? first + k : 0), res.with_q ? logit<F32>(row_q, there ? first + k : 0) : 0.f, first + k) : 0.0;
+    mine += w[k];
   }
-  at = start + block_before(mine, run);
+  at = block_before(mine, run);
+  at += start;
   int hit = 0x7fffffff, end = -1;
 #pragma unroll
-  for (int k = 0; k < kMine; ++k) {
+  for (int k = 0; k < M; ++k) {
     at += w[k];
     if (w[k] > 0.0) {
       end = first + k;
@@ -472,7 +501,7 @@ int verify_parts(const sp_verify_args* a) { return (a->V + kPart - 1) / kPart; }
 VerifyLayout verify_layout(const sp_verify_args* a) {
   VerifyLayout l;
   size_t at = align_up(sizeof(RowStats) * (size_t)(2 * a->T + a->B) * (size_t)verify_slices(a), 256);
-  const size_t sums = align_up(8 * (size_t)a->B * (size_t)verify_parts(a), 256);
+  const size_t sums = align_up(32 * (size_t)a->B * (size_t)verify_parts(a), 256);
   l.states = at; at += align_up(sizeof(VerifyState) * (size_t)a->B, 256);
   l.sum_p = at; at += sums;
   l.sum_q = at; at += sums;

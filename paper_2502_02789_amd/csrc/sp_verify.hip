@@ -1,12 +1,14 @@
 // sp_verify: which drafted tokens stand against the target's probabilities, and the token that is sampled behind them.
 //
-// Four kernels, bound by reading the logits once (the first; the others read the rows of one place of each sequence again):
+// Three kernels, bound by reading the logits once (the first; the others read the rows of one place of each sequence again):
 //   stats     maximum and sum of exp of every row, 8192 logits to a workgroup
-//   choose    per sequence: the rows' sums, how many tokens stand, hence the row that a token is sampled from; its parts' sums in fp64
-//   residual  sums of max(p - q, 0) in parts, p and q normalised by those sums
-//   pick      the part in which the sum passes r times the whole, and the token in it
+//   choose    per sequence: the rows' sums, how many tokens stand, hence the row that a token is sampled from; in strips of it, the sums of the weights of p and
+//             q, and of both over the tokens with something left: with Zp, Zq the sums over all, what is left in a strip is (sum of wp - Zp/Zq sum of wq) / Zp
+//   pick      the strip in which the sum passes r times the whole, and the token in it
 // Which token is picked depends on sums over the whole vocabulary: a vocabulary of 128K has so many borders between tokens that sums in fp32, off by 1e-7, would pick
-// another token once in some hundred calls.  The sampled row's weights are therefore formed and added in fp64; the order of all sums is fixed.
+// another token once in some hundred calls.  The sampled row's weights are therefore formed and added in fp64; the order of all sums is fixed.  Only which
+// tokens have something left is decided with the ratio Zp/Zq of the first kernel's sums in fp32, so that one pass does: a token whose p and q are within 1e-6 of one another may
+// count as one of which nothing is left.
 #include "sp_score_internal.h"
 
 namespace sp {
@@ -22,6 +24,7 @@ constexpr double kLog2e64 = 1.4426950408889634074;
 struct RowStats { float top, sum; int32_t arg, pad; };   // of a slice: largest logit, sum of exp((z - top) / temperature), where the largest is
 struct VerifyState {                                       // of a sequence
   double c;               // of a logit in front of exp2
+  double ratio;           // of the sums of the two rows' weights, in fp32's accuracy: what is left of p_i over q_i is something if its weight exceeds q_i's so many times
   float top_p, top_q;
   int32_t row_p, row_q;   // rows of the target and of the draft (-1: none) that the token is sampled from
   int32_t token;          // without draft logits: the token that is taken off, or -1
@@ -45,9 +48,7 @@ struct VerifyDev {
   int32_t* kept_len;
   RowStats* stats;     // [T + B rows of the target, T of the draft][slices]
   VerifyState* states; // [B]
-  double* sum_p;       // [B][4 parts], by strips
-  double* sum_q;
-  double* sum_w;
+  double* sums;        // [B][4 parts strips][4]: weights of p, of q, and both over the tokens of which something is left
 };
 
 template <bool F32> __device__ __forceinline__ const char* row_of(const void* base, int64_t stride, int64_t row) {
@@ -321,6 +322,7 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
         s.token = s.sample && a < n && !p.draft ? p.tokens[t0 + a] : -1;
         s.top_p = s.sample ? tops[a] : 0.f;
         s.top_q = s.row_q >= 0 ? tops[n + 1 + a] : 0.f;
+        s.ratio = s.row_q >= 0 ? sums[a] / sums[n + 1 + a] : 0.0;
         p.states[b] = s;
       }
     }
@@ -337,62 +339,49 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
   const int strip = part * 4 + (tid >> 6), first = strip * kStrip + (tid & 63) * E;
   load_logits<F32, kMine / E>(row_p, first, 64 * E, p.V, vp);
   if (with_q) load_logits<F32, kMine / E>(row_q, first, 64 * E, p.V, vq);
-  double z = 0.0, zd = 0.0;
-#pragma unroll
-  for (int k = 0; k < kMine / E; ++k)
-#pragma unroll
-    for (int e = 0; e < E; ++e) z += exp64(vp[k][e], top_p, c);
+  double z[4] = {0.0, 0.0, 0.0, 0.0};
   if (with_q) {
+    const double ratio = sums[a] / sums[n + 1 + a];
 #pragma unroll
     for (int k = 0; k < kMine / E; ++k)
 #pragma unroll
-      for (int e = 0; e < E; ++e) zd += exp64(vq[k][e], top_q, c);
+      for (int e = 0; e < E; ++e) {
+        const double wp = exp64(vp[k][e], top_p, c), wq = exp64(vq[k][e], top_q, c);
+        const bool left = wp > wq * ratio;
+        z[0] += wp;
+        z[1] += wq;
+        z[2] += left ? wp : 0.0;
+        z[3] += left ? wq : 0.0;
+      }
+  } else {
+    const int token = a < n ? p.tokens[t0 + a] : -1;
+#pragma unroll
+    for (int k = 0; k < kMine / E; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const double wp = exp64(vp[k][e], top_p, c);
+        z[0] += wp;
+        z[2] += first + k * 64 * E + e != token ? wp : 0.0;
+      }
   }
-  z = wave_prefix(z);
-  zd = wave_prefix(zd);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) z[i] = wave_prefix(z[i]);
   if ((tid & 63) == 63) {
-    p.sum_p[(int64_t)b * 4 * p.parts + strip] = z;
-    p.sum_q[(int64_t)b * 4 * p.parts + strip] = zd;
+    double* dst = p.sums + ((int64_t)b * 4 * p.parts + strip) * 4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = z[i];
   }
 }
 
-// what is left of p_i over the draft: max(p_i - q_i, 0), p and q normalised
-struct Residual { double c, top_p, top_q, inv_p, inv_q; int token; bool with_q; };
+// what is left of p_i over the draft, in units of p's weights
+struct Residual { double c, top_p, top_q, first_ratio, ratio; int token; bool with_q; };
 __device__ __forceinline__ double residual_weight(const Exp64& exp64, const Residual& s, float zp, float zq, int i) {
-  double w = zp == -INFINITY ? 0.0 : exp64(zp, s.top_p, s.c) * s.inv_p;
-  if (s.with_q) w = fmax(w - (zq == -INFINITY ? 0.0 : exp64(zq, s.top_q, s.c) * s.inv_q), 0.0);
-  return i == s.token ? 0.0 : w;
-}
-
-template <bool F32>
-__global__ __launch_bounds__(256) void verify_residual_kernel(const VerifyDev p) {
-  constexpr int E = kVec<F32>;
-  __shared__ double lds[4][2];
-  const int part = (int)(blockIdx.x % (uint32_t)p.parts), b = (int)(blockIdx.x / (uint32_t)p.parts), tid = threadIdx.x;
-  const VerifyState s = p.states[b];
-  if (!s.sample) return;
-  const bool with_q = s.row_q >= 0;
-  const char* row_p = row_of<F32>(p.target, p.target_stride, s.row_p);
-  const char* row_q = row_of<F32>(p.draft, p.draft_stride, s.row_q);
-  float vp[kMine / E][E], vq[kMine / E][E];
-  const Exp64 exp64;
-  const int strip = part * 4 + (tid >> 6), first = strip * kStrip + (tid & 63) * E;
-  load_logits<F32, kMine / E>(row_p, first, 64 * E, p.V, vp);
-  if (with_q) load_logits<F32, kMine / E>(row_q, first, 64 * E, p.V, vq);
-  double z[2] = {0.0, 0.0};
-  for (int i = tid; i < 4 * p.parts; i += 256) {
-    z[0] += p.sum_p[(int64_t)b * 4 * p.parts + i];
-    if (with_q) z[1] += p.sum_q[(int64_t)b * 4 * p.parts + i];
+  double w = zp == -INFINITY ? 0.0 : exp64(zp, s.top_p, s.c);
+  if (s.with_q) {
+    const double wq = zq == -INFINITY ? 0.0 : exp64(zq, s.top_q, s.c);
+    w = w > wq * s.first_ratio ? fmax(w - wq * s.ratio, 0.0) : 0.0;
   }
-  block_sums(z, lds);
-  const Residual w = {s.c, (double)s.top_p * s.c, (double)s.top_q * s.c, 1.0 / z[0], 1.0 / z[1], s.token, with_q};
-  double sum = 0.0;
-#pragma unroll
-  for (int k = 0; k < kMine / E; ++k)
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum += residual_weight(exp64, w, vp[k][e], with_q ? vq[k][e] : 0.f, first + k * 64 * E + e);
-  sum = wave_prefix(sum);
-  if ((tid & 63) == 63) p.sum_w[(int64_t)b * 4 * p.parts + strip] = sum;
+  return i == s.token ? 0.0 : w;
 }
 
 // exclusive sums over the workgroup's 256 threads
@@ -410,7 +399,7 @@ __device__ __forceinline__ double block_before(double v, double* lds) {
 template <bool F32>
 __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
   constexpr int M = kStrip / 256;
-  __shared__ double lds[4][3], run[4], start;
+  __shared__ double lds[4][4], run[4], start;
   __shared__ int found, last, hit_strip, last_strip;
   const int b = blockIdx.x, tid = threadIdx.x;
   const VerifyState s = p.states[b];
@@ -421,34 +410,30 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
   const char* row_q = row_of<F32>(p.draft, p.draft_stride, s.row_q);
   const int strips = 4 * p.parts;
   const Exp64 exp64;
-  const double* sum_p = p.sum_p + (int64_t)b * strips;
-  const double* sum_q = p.sum_q + (int64_t)b * strips;
-  const double* sums = p.sum_w + (int64_t)b * strips;
-  double z[3] = {0.0, 0.0, 0.0};
-  for (int i = tid; i < strips; i += 256) {
-    z[0] += sum_p[i];
-    if (with_q) z[1] += sum_q[i];
-    z[2] += sums[i];
-  }
+  const double* sums = p.sums + (int64_t)b * strips * 4;
+  double z[4] = {0.0, 0.0, 0.0, 0.0};
+  for (int i = tid; i < strips; i += 256)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) z[k] += sums[4 * i + k];
   block_sums(z, lds);
-  Residual res = {s.c, (double)s.top_p * s.c, (double)s.top_q * s.c, 1.0 / z[0], 1.0 / z[1], s.token, with_q};
-  double total = z[2], unit = 1.0;
-  if (!(total > 0.0)) {  // nothing is left: p itself
-    sums = sum_p;
-    unit = res.inv_p;
-    total = z[0] * unit;
+  Residual res = {s.c, (double)s.top_p * s.c, (double)s.top_q * s.c, s.ratio, with_q ? z[0] / z[1] : 0.0, s.token, with_q};
+  double total = z[2] - z[3] * res.ratio;
+  const bool nothing = !(total > 0.0);
+  if (nothing) {  // p itself
+    total = z[0];
     res.with_q = false;
     res.token = -1;
   }
+  const auto weight_of = [&](int i) { return nothing ? sums[4 * i] : fmax(sums[4 * i + 2] - sums[4 * i + 3] * res.ratio, 0.0); };
   const double bound = (double)p.r[b] * total;
   // the first strip whose end lies beyond the bound, else the last that has anything; every thread has neighbours of its own
   const int per = (strips + 255) / 256, i0 = min(strips, tid * per), i1 = min(strips, i0 + per);
   double sum = 0.0;
-  for (int i = i0; i < i1; ++i) sum += sums[i] * unit;
+  for (int i = i0; i < i1; ++i) sum += weight_of(i);
   const double before = block_before(sum, run);
   double at = before;
   for (int i = i0; i < i1; ++i) {
-    const double w = sums[i] * unit;
+    const double w = weight_of(i);
     if (w > 0.0) {
       atomicMax(&last_strip, i);
       if (at + w > bound) atomicMin(&hit_strip, i);
@@ -459,7 +444,7 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
   const int strip = hit_strip != 0x7fffffff ? hit_strip : max(last_strip, 0);
   if (strip >= i0 && strip < i1) {  // (the thread that has it says what lies before it)
     at = before;
-    for (int i = i0; i < strip; ++i) at += sums[i] * unit;
+    for (int i = i0; i < strip; ++i) at += weight_of(i);
     start = at;
   }
   const int first = strip * kStrip + tid * M;
@@ -493,7 +478,7 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
 
 namespace {
 
-struct VerifyLayout { size_t states, sum_p, sum_q, sum_w, bytes; };
+struct VerifyLayout { size_t states, sums, bytes; };
 
 int verify_slices(const sp_verify_args* a) { return (a->V + kSlice - 1) / kSlice; }
 int verify_parts(const sp_verify_args* a) { return (a->V + kPart - 1) / kPart; }
@@ -501,11 +486,8 @@ int verify_parts(const sp_verify_args* a) { return (a->V + kPart - 1) / kPart; }
 VerifyLayout verify_layout(const sp_verify_args* a) {
   VerifyLayout l;
   size_t at = align_up(sizeof(RowStats) * (size_t)(2 * a->T + a->B) * (size_t)verify_slices(a), 256);
-  const size_t sums = align_up(32 * (size_t)a->B * (size_t)verify_parts(a), 256);
   l.states = at; at += align_up(sizeof(VerifyState) * (size_t)a->B, 256);
-  l.sum_p = at; at += sums;
-  l.sum_q = at; at += sums;
-  l.sum_w = at; at += sums;
+  l.sums = at; at += align_up(4 * 32 * (size_t)a->B * (size_t)verify_parts(a), 256);
   l.bytes = at;
   return l;
 }
@@ -539,7 +521,6 @@ void launch_verify(const VerifyDev& p, hipStream_t stream) {
   const uint32_t rows = (uint32_t)(p.T + p.B + (p.draft ? p.T : 0));
   hipLaunchKernelGGL(verify_stats_kernel<F32>, dim3(rows * (uint32_t)p.slices), dim3(256), 0, stream, p);
   hipLaunchKernelGGL(verify_choose_kernel<F32>, dim3((uint32_t)(p.B * p.parts)), dim3(256), 0, stream, p);
-  hipLaunchKernelGGL(verify_residual_kernel<F32>, dim3((uint32_t)(p.B * p.parts)), dim3(256), 0, stream, p);
   hipLaunchKernelGGL(verify_pick_kernel<F32>, dim3((uint32_t)p.B), dim3(256), 0, stream, p);
 }
 
@@ -566,9 +547,7 @@ extern "C" sp_status sp_verify(const sp_verify_args* a, void* hip_stream) {
   p.n_accepted = a->d_n_accepted; p.out_tokens = a->d_out_tokens; p.logprob = a->d_logprob; p.kept_len = a->d_kept_len;
   p.stats = reinterpret_cast<RowStats*>(base);
   p.states = reinterpret_cast<VerifyState*>(base + l.states);
-  p.sum_p = reinterpret_cast<double*>(base + l.sum_p);
-  p.sum_q = reinterpret_cast<double*>(base + l.sum_q);
-  p.sum_w = reinterpret_cast<double*>(base + l.sum_w);
+  p.sums = reinterpret_cast<double*>(base + l.sums);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (a->logits_dtype == SP_LOGITS_F32) launch_verify<true>(p, stream);
   else launch_verify<false>(p, stream);

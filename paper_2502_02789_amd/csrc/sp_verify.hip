@@ -396,25 +396,49 @@ __device__ __forceinline__ double block_before(double v, double* lds) {
   return before + (x - v);
 }
 
+// The first of the workgroup's threads' hits (ascending with the threads; kNone: none), or, where no thread has one, the last of their ends (-1: none).  (LDS
+// atomics by all lanes on one word are done lane after lane: 4 us each here.)
+constexpr int kNone = 0x7fffffff;
+__device__ __forceinline__ int first_hit(int hit, int end, int (*lds)[2]) {
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const uint64_t hits = __builtin_amdgcn_ballot_w64(hit != kNone), ends = __builtin_amdgcn_ballot_w64(end >= 0);
+  if (hits ? l == __builtin_ctzll(hits) : l == 0) lds[w][0] = hit;
+  if (ends ? l == 63 - __builtin_clzll(ends) : l == 0) lds[w][1] = end;
+  __syncthreads();
+  int found = kNone, last = -1;
+#pragma unroll
+  for (int i = 3; i >= 0; --i)
+    if (lds[i][0] != kNone) found = lds[i][0];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) last = max(last, lds[i][1]);
+  return found != kNone ? found : last;
+}
+
 template <bool F32>
 __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
   constexpr int M = kStrip / 256;
-  __shared__ double lds[4][4], run[4], start;
-  __shared__ int found, last, hit_strip, last_strip;
+  __shared__ double lds[4][4], run[4], start, log_sum;
+  __shared__ int strip_hits[4][2], hits[4][2];
   const int b = blockIdx.x, tid = threadIdx.x;
+  // every thread has neighbours of its own among the strips, one in a vocabulary of up to 2^18: their sums stay in registers
+  const int strips = 4 * p.parts, per = (strips + 255) / 256, i0 = min(strips, tid * per), i1 = min(strips, i0 + per);
+  const double* sums = p.sums + (int64_t)b * strips * 4;
+  double own[4] = {0.0, 0.0, 0.0, 0.0}, z[4];
+  if (i0 < i1)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) own[k] = sums[4 * i0 + k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) z[k] = own[k];
+  const float r = p.r[b];
   const VerifyState s = p.states[b];
   if (!s.sample) return;
-  if (tid == 0) { found = hit_strip = 0x7fffffff; last = last_strip = -1; }
+  for (int i = i0 + 1; i < i1; ++i)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) z[k] += sums[4 * i + k];
+  const Exp64 exp64;
   const bool with_q = s.row_q >= 0;
   const char* row_p = row_of<F32>(p.target, p.target_stride, s.row_p);
   const char* row_q = row_of<F32>(p.draft, p.draft_stride, s.row_q);
-  const int strips = 4 * p.parts;
-  const Exp64 exp64;
-  const double* sums = p.sums + (int64_t)b * strips * 4;
-  double z[4] = {0.0, 0.0, 0.0, 0.0};
-  for (int i = tid; i < strips; i += 256)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) z[k] += sums[4 * i + k];
   block_sums(z, lds);
   Residual res = {s.c, (double)s.top_p * s.c, (double)s.top_q * s.c, s.ratio, with_q ? z[0] / z[1] : 0.0, s.token, with_q};
   double total = z[2] - z[3] * res.ratio;
@@ -424,56 +448,74 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
     res.with_q = false;
     res.token = -1;
   }
-  const auto weight_of = [&](int i) { return nothing ? sums[4 * i] : fmax(sums[4 * i + 2] - sums[4 * i + 3] * res.ratio, 0.0); };
-  const double bound = (double)p.r[b] * total;
-  // the first strip whose end lies beyond the bound, else the last that has anything; every thread has neighbours of its own
-  const int per = (strips + 255) / 256, i0 = min(strips, tid * per), i1 = min(strips, i0 + per);
+  const double bound = (double)r * total;
+  // the first strip whose end lies beyond the bound, else the last that has anything
+  const auto weight_of = [&](int i) {
+    double x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = i == i0 ? own[k] : sums[4 * i + k];
+    return nothing ? x[0] : fmax(x[2] - x[3] * res.ratio, 0.0);
+  };
   double sum = 0.0;
   for (int i = i0; i < i1; ++i) sum += weight_of(i);
   const double before = block_before(sum, run);
   double at = before;
+  int hit = kNone, end = -1;
   for (int i = i0; i < i1; ++i) {
     const double w = weight_of(i);
     if (w > 0.0) {
-      atomicMax(&last_strip, i);
-      if (at + w > bound) atomicMin(&hit_strip, i);
+      end = i;
+      if (at + w > bound && hit == kNone) hit = i;
     }
     at += w;
   }
-  __syncthreads();
-  const int strip = hit_strip != 0x7fffffff ? hit_strip : max(last_strip, 0);
+  const int strip = max(first_hit(hit, end, strip_hits), 0);
   if (strip >= i0 && strip < i1) {  // (the thread that has it says what lies before it)
     at = before;
     for (int i = i0; i < strip; ++i) at += weight_of(i);
     start = at;
   }
   const int first = strip * kStrip + tid * M;
+  float zp[M], zq[M];
+#pragma unroll
+  for (int k = 0; k < M; ++k) {
+    const int i = first + k < p.V ? first + k : 0;
+    zp[k] = logit<F32>(row_p, i);
+    zq[k] = res.with_q ? logit<F32>(row_q, i) : 0.f;
+  }
+  if (tid == 255 && p.logprob) log_sum = log(z[0]);
   double w[M], mine = 0.0;
 #pragma unroll
   for (int k = 0; k < M; ++k) {
-    const bool there = first + k < p.V;
-    w[k] = there ? residual_weight(exp64, res, logit<F32>(row_p, there ? first + k : 0), res.with_q ? logit<F32>(row_q, there ? first + k : 0) : 0.f, first + k) : 0.0;
+    w[k] = first + k < p.V ? residual_weight(exp64, res, zp[k], zq[k], first + k) : 0.0;
     mine += w[k];
   }
   at = block_before(mine, run);
   at += start;
-  int hit = 0x7fffffff, end = -1;
+  hit = kNone;
+  end = -1;
 #pragma unroll
   for (int k = 0; k < M; ++k) {
     at += w[k];
     if (w[k] > 0.0) {
       end = first + k;
-      if (at > bound && hit == 0x7fffffff) hit = first + k;
+      if (at > bound && hit == kNone) hit = first + k;
     }
   }
-  if (hit != 0x7fffffff) atomicMin(&found, hit);
-  if (end >= 0) atomicMax(&last, end);
-  __syncthreads();
-  if (tid == 0) {
-    const int y = found != 0x7fffffff ? found : max(last, 0);
-    p.out_tokens[s.row_p] = y;
-    if (p.logprob) p.logprob[s.row_p] = (float)(((double)logit<F32>(row_p, y) - (double)s.top_p) * s.c * 0.69314718055994530942 - log(z[0]));
+  int y = first_hit(hit, end, hits);
+  if (y < 0) {  // (what was left in the strip is no more than a rounding: its first token with a probability)
+    hit = kNone;
+#pragma unroll
+    for (int k = M - 1; k >= 0; --k)
+      if (first + k < p.V && first + k != res.token && zp[k] != -INFINITY) hit = first + k;
+    y = first_hit(hit, -1, strip_hits);
   }
+#pragma unroll
+  for (int k = 0; k < M; ++k)
+    if (first + k == y) {  // (one thread's)
+      p.out_tokens[s.row_p] = y;
+      if (p.logprob) p.logprob[s.row_p] = (float)(((double)zp[k] - (double)s.top_p) * s.c * 0.69314718055994530942 - log_sum);
+    }
 }
 
 namespace {

@@ -345,7 +345,7 @@ SP_API sp_status sp_gather(const sp_gather_args* args, void* hip_stream);
  * 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two to a byte, the even element in the low half, and one E8M0 scale, the
  * byte s for 2^(s - 127), 255 for NaN, to 32 elements that follow one another in a head.  Codes and scales are separate arrays of the
  * same layout: the codes of the elements from offset e on begin at byte e / 2, and the scale of the block that begins at offset e
- * is byte e / 32 of the scales.  The strides still count elements, and are multiples of 32 (16 bytes of codes).  Heads outermost in a page (token
+ * is byte e / 32 of the scales.  The strides still count elements, and are multiples of d.  Heads outermost in a page (token
  * stride d) keep a head's codes and scales of neighbouring tokens side by side, which sp_attend reads fastest.
  * n_rows is the number of token rows of the pool (pages * page_size) or of the contiguous cache.  Nothing outside it
  * is read or written, whatever the tables hold: a page number outside the pool or a row outside the cache is answered as
@@ -353,8 +353,8 @@ SP_API sp_status sp_gather(const sp_gather_args* args, void* hip_stream);
  * room for T_new tokens (d_cu_new[0] = 0, non-decreasing, d_cu_new[B] <= T_new; rows at and beyond d_cu_new[B] are
  * neither read nor written).  Limits: d 64 or 128, H <= 1024, H % H_kv == 0,
  * H / H_kv <= 16, T_new * H < 2^31, T_new of an append <= 2^25.  With T_new = 0 the pointers to new tokens may be NULL.
- * Pointers to bf16, 8-bit or 4-bit data are 16-byte aligned, those to block scales need not be; strides count elements and are multiples
- * of 8 (of an 8-bit cache: 16, of a 4-bit one: 32).
+ * Pointers to bf16, 8-bit or 4-bit data are 16-byte aligned, those to block scales d/32; strides count elements and are multiples
+ * of 8 (of an 8-bit cache: 16, of a 4-bit one: d).
  * --------------------------------------------------------------------------- */
 
 /* sp_cache_append: for new token j of sequence b (flat row t = cu_new[b] + j), at cache index i = cache_len[b] + j and

@@ -211,7 +211,8 @@ sp_status check_append(const sp_cache_append_args* a) {
   if (a->d_block_table && a->n_rows > a->page_size && a->cache_page_stride < a->d) return SP_EINVAL;
   if (a->d_k_cache == a->d_v_cache || (a->d_k_block_scale && a->d_k_block_scale == a->d_v_block_scale)) return SP_EINVAL;
   for (int64_t s : in) if (s & 7) return SP_EALIGN;
-  for (int64_t s : out) if (s & (cache_stride_unit(a->cache_dtype) - 1)) return SP_EALIGN;
+  for (int64_t s : out) if (s & (cache_stride_unit(a->cache_dtype, a->d) - 1)) return SP_EALIGN;
+  if (!aligned_scales(a->d_k_block_scale, a->d) || !aligned_scales(a->d_v_block_scale, a->d)) return SP_EALIGN;
   if (!aligned16(a->d_q) || !aligned16(a->d_k) || !aligned16(a->d_v) || !aligned16(a->d_q_out) || !aligned16(a->d_k_cache) ||
       !aligned16(a->d_v_cache))
     return SP_EALIGN;

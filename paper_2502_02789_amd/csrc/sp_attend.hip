@@ -436,33 +436,69 @@ __device__ __forceinline__ void attend_few(const AttendDev& p, const AttendUnit&
 }
 
 // ---------------------------------------------------------------- few rows, 4-bit keys and values
-// 64-key tiles.  Keys need no LDS: lane (key l & 15, quad) holds D/4 consecutive elements of a key, and as the order of
-// elements inside a product's sum is free, it hands them to the matrix cores as they are, turned into bf16, eight to a step;
-// the queries are laid out alike.  Values become bf16 on their way into LDS, where they are transposed.
-template <int D, bool PAGED>
+// Where the keys of a 64-key tile lie, a key to a lane: byte offsets of their codes (a sixteenth of that: of their scales).  Loads whose lanes take
+// other keys get theirs by lane permutes.  Pages as in KeyRows: requested a tile ahead of their use and before other loads.
+template <bool PAGED>
+struct KeyOffsets {
+  const int32_t* table;
+  int lg_page, first, last_key, lane;
+  uint32_t last, pages, ts;
+  int64_t ps, head;
+  __device__ __forceinline__ KeyOffsets(const AttendDev& p, const AttendUnit& u, int l, int g, int tile) {
+    ts = (uint32_t)p.c_ts; ps = p.c_ps; lg_page = p.lg_page; last_key = u.k1 - 1; lane = l;
+    head = (int64_t)g * p.c_hs;
+    first = PAGED ? 0 : u.seq;
+    last = PAGED ? p.last_page : p.last_row;
+    table = PAGED ? p.table + (int64_t)u.seq * p.blocks_per_seq : nullptr;
+    if (u.k0 < u.k1) ahead(tile);
+  }
+  __device__ __forceinline__ void ahead(int tile) {
+    if constexpr (PAGED) pages = (uint32_t)table[min(tile + lane, last_key) >> lg_page];
+  }
+  // (behind the last key: the last key's, whose weight is zero there.  Nothing outside the pool is addressed, a bad page is noted.)
+  __device__ __forceinline__ uint64_t at(int tile, bool& bad) const {
+    const int key = min(tile + lane, last_key);
+    if constexpr (PAGED) {
+      bad |= pages > last;
+      return (uint64_t)min(pages, last) * (uint64_t)ps + (uint64_t)((uint32_t)(key & ((1 << lg_page) - 1))) * ts + (uint64_t)head;
+    } else {
+      return (uint64_t)min((uint32_t)(first + key), last) * ts + (uint64_t)head;
+    }
+  }
+};
+
+__device__ __forceinline__ uint64_t of_lane(uint64_t v, int lane4) {  // lane4: four times the lane
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_ds_bpermute(lane4, (int)(uint32_t)v), hi = (uint32_t)__builtin_amdgcn_ds_bpermute(lane4, (int)(uint32_t)(v >> 32));
+  return (uint64_t)hi << 32 | lo;
+}
+
+// As swizzled(), for rows whose chunks are written four at a time by lanes of their own: of 16 lanes, four (d = 64: eight) rows times every fourth chunk.
+template <int C>
+__device__ __forceinline__ int swizzled_blocks(int r, int c) {
+  if constexpr (C == 16) return c ^ ((r & 3) | (r & 1) << 2 | (r >> 2 & 1) << 3);
+  else return c ^ ((r >> 1 & 3) | (r >> 1 & 1) << 2);
+}
+
+// A wave's 64-key tile on its way.  Keys need no LDS: lane (key l & 15, quad l >> 4) holds D/4 consecutive elements of a key, and as the order of
+// elements inside a product's sum is free, it hands them to the matrix cores as they are, turned into bf16, eight to a step; the
+// queries are laid out alike.  Values come by whole rows, become bf16 on their way into LDS, and are transposed there.
+template <int D>
 struct FourBitTile {
   static constexpr int KW = D / 32;    // 32-bit words of a lane's part of a key
-  static constexpr int C = D / 32;     // 16-byte chunks of a stored row, one block each
+  static constexpr int C = D / 32;     // 16-byte chunks of a stored row, a block each
   static constexpr int R = 64 / C;     // rows of a load of values
   static constexpr int N = 64 / R;     // loads of a tile of values
-  uint32_t k[4][KW], ks[4];
-  uint32_t v[N][4], vs[N];
-  int64_t base[8];                     // where the tile's octets lie
-  int octet[8];
-  __device__ __forceinline__ void place(KeyRows<PAGED>& rows, int tile, int next, uint32_t& bad) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      octet[j] = rows.octet(tile, 8 * j);
-      base[j] = rows.base(octet[j], 8 * j, bad);
-    }
-    rows.ahead(next);
+  uint32_t k[4][KW], v[N][4];
+  uint32_t ks, vs;                     // the scales of key number `lane` of the tile, a byte to a block
+  __device__ __forceinline__ static uint32_t load_scales(const uint8_t* scales, uint64_t at) {
+    if constexpr (D == 128) return *reinterpret_cast<const uint32_t*>(scales + (at >> 4));
+    else return *reinterpret_cast<const uint16_t*>(scales + (at >> 4));
   }
-  __device__ __forceinline__ void load_keys(const AttendDev& p, const KeyRows<PAGED>& rows, int tile, int64_t head, int l) {
+  __device__ __forceinline__ void load_keys(const AttendDev& p, uint64_t at, int l) {
+    ks = load_scales(p.k_block_scale, at);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
-      const bool second = (l & 8) != 0;
-      const int64_t at = head + (second ? base[2 * x + 1] : base[2 * x]) + rows.within(second ? octet[2 * x + 1] : octet[2 * x], tile + 16 * x + (l & 15));
-      const char* codes = p.k + at + (l >> 4) * (4 * KW);
+      const char* codes = p.k + of_lane(at, 4 * (16 * x + (l & 15))) + (l >> 4) * (4 * KW);
       if constexpr (KW == 4) {
         const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes));
 #pragma unroll
@@ -473,34 +509,39 @@ struct FourBitTile {
         k[x][0] = w[0];
         k[x][1] = w[1];
       }
-      ks[x] = p.k_block_scale[(at >> 4) + (l >> 4) * KW / 4];
     }
   }
-  __device__ __forceinline__ void load_values(const AttendDev& p, const KeyRows<PAGED>& rows, int tile, int64_t head, int l) {
+  __device__ __forceinline__ void place_values(uint64_t at, int l, uint64_t (&v_at)[N]) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v_at[i] = of_lane(at, 4 * (R * i + l / C));
+  }
+  __device__ __forceinline__ void load_values(const AttendDev& p, uint64_t at, const uint64_t (&v_at)[N], int l) {
+    vs = load_scales(p.v_block_scale, at);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int r = l / C;  // (and R i)
-      int64_t b = base[R * i / 8];
-      int oct = octet[R * i / 8];
-#pragma unroll
-      for (int j = 1; j < R / 8; ++j)
-        if (r >= 8 * j) { b = base[R * i / 8 + j]; oct = octet[R * i / 8 + j]; }
-      const int64_t at = head + b + rows.within(oct, tile + R * i + r);
-      const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p.v + at + l % C * 16));
+      const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p.v + v_at[i] + l % C * 16));
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[i][j] = w[j];
-      vs[i] = p.v_block_scale[(at >> 4) + l % C];
     }
+  }
+  // 16 keys as operands, eight elements to each
+  __device__ __forceinline__ void keys(int x, int l, bf16x8 (&out)[KW]) const {
+    const uint32_t scales = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * x + (l & 15)), (int)ks);
+    uint32_t w[4 * KW];
+    widen_e2m1<4 * KW>(k[x], scales >> ((l >> 4) * KW / 4 * 8) & 0xff, w);
+#pragma unroll
+    for (int i = 0; i < KW; ++i) out[i] = __builtin_bit_cast(bf16x8, u32x4{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]});
   }
   __device__ __forceinline__ void store_values(char* tile, int l) const {  // as bf16
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = l / C + R * i, ch = 4 * (l % C);
+      const uint32_t scales = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * r, (int)vs);
       uint32_t w[16];
-      widen_e2m1<16>(v[i], vs[i], w);
+      widen_e2m1<16>(v[i], scales >> (l % C * 8) & 0xff, w);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *reinterpret_cast<u32x4*>(tile + r * (D * 2) + swizzled<D / 8>(r, ch + j) * 16) = u32x4{w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]};
+        *reinterpret_cast<u32x4*>(tile + r * (D * 2) + swizzled_blocks<D / 8>(r, ch + j) * 16) = u32x4{w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]};
     }
   }
 };
@@ -510,7 +551,6 @@ __device__ __forceinline__ void attend_few_4bit(const AttendDev& p, const Attend
   constexpr int KS = D / 32;          // steps of the product with the queries
   constexpr int DB = D / 16;          // blocks of values
   constexpr int C = D / 8;            // 16-byte chunks of a bf16 row
-  using Tile = FourBitTile<D, PAGED>;
   const int tid = thread_of_piece(), w = __builtin_amdgcn_readfirstlane(tid >> 6), turn = w & (W - 1), l = tid & 63, row = l & 15, quad = l >> 4;
   bool mine[NR];
   RowPlace at[NR];
@@ -520,15 +560,20 @@ __device__ __forceinline__ void attend_few_4bit(const AttendDev& p, const Attend
     at[n] = row_place(p, u.r0 + (mine[n] ? row + 16 * n : 0), g);
   }
   int tile = u.k0 < u.k1 ? (u.k0 & ~63) + 64 * turn : u.k1;
-  KeyRows<PAGED> rows(p, u, l, tile);
-  const int64_t head = (int64_t)g * p.c_hs;
+  KeyOffsets<PAGED> offsets(p, u, l, g, tile);
   char* const vd = lds + w * (64 * D * 2);
-  uint32_t bad = 0;
-  Tile t;
+  bool bad = false;
+  FourBitTile<D> x;
+  uint64_t at_keys, v_at[FourBitTile<D>::N];
+  const auto load_keys = [&](int tile) {
+    at_keys = offsets.at(tile, bad);
+    offsets.ahead(tile + 64 * W);
+    x.load_keys(p, at_keys, l);
+    x.place_values(at_keys, l, v_at);
+  };
   if (tile < u.k1) {
-    t.place(rows, tile, tile + 64 * W, bad);
-    t.load_keys(p, rows, tile, head, l);
-    t.load_values(p, rows, tile, head, l);
+    load_keys(tile);
+    x.load_values(p, at_keys, v_at, l);
   }
 
   // the queries, in the order of the keys' elements
@@ -541,7 +586,7 @@ __device__ __forceinline__ void attend_few_4bit(const AttendDev& p, const Attend
       if (mine[n]) x = *reinterpret_cast<const u32x4*>(p.q + at[n].token * p.q_ts + at[n].h * p.q_hs + quad * (D / 4) + s * 8);
       qf[n][s] = __builtin_bit_cast(bf16x8, x);
     }
-  const float c = p.scale_log2;
+  const float c = p.scale_log2;  // (positive)
   int limit[NR], least = u.k1;
 #pragma unroll
   for (int n = 0; n < NR; ++n) limit[n] = u.k1;
@@ -569,40 +614,35 @@ __device__ __forceinline__ void attend_few_4bit(const AttendDev& p, const Attend
     const bool more = tile + 64 * W < u.k1;
     f32x4 s[NR][4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      uint32_t kw[4 * Tile::KW];
-      widen_e2m1<4 * Tile::KW>(t.k[x], t.ks[x], kw);
+    for (int y = 0; y < 4; ++y) {
+      bf16x8 kf[KS];
+      x.keys(y, l, kf);
 #pragma unroll
-      for (int n = 0; n < NR; ++n) s[n][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < NR; ++n) {
+        s[n][y] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        const bf16x8 kf = __builtin_bit_cast(bf16x8, u32x4{kw[4 * i], kw[4 * i + 1], kw[4 * i + 2], kw[4 * i + 3]});
-#pragma unroll
-        for (int n = 0; n < NR; ++n) s[n][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[n][i], s[n][x], 0, 0, 0);
+        for (int i = 0; i < KS; ++i) s[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i], qf[n][i], s[n][y], 0, 0, 0);
       }
     }
-    t.store_values(vd, l);
-    if (more) {
-      t.place(rows, tile + 64 * W, tile + 128 * W, bad);
-      t.load_keys(p, rows, tile + 64 * W, head, l);
-      t.load_values(p, rows, tile + 64 * W, head, l);
-    }
+    // (the lanes' exchange of offsets in front of the stores to LDS, behind which it would wait; with two tiles of rows registers do not do for that)
+    if (NR == 1 && more) load_keys(tile + 64 * W);
+    x.store_values(vd, l);
+    if (NR == 2 && more) load_keys(tile + 64 * W);
+    if (more) x.load_values(p, at_keys, v_at, l);
     bf16x8 pf[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      float x[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = s[n][i >> 2][i & 3] * c;
       if (tile + 64 > least || tile < u.k0) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = tile + 16 * (i >> 2) + 4 * quad + (i & 3);
-          if (key >= limit[n] || key < u.k0) x[i] = -INFINITY;
+          if (key >= limit[n] || key < u.k0) s[n][i >> 2][i & 3] = -INFINITY;
         }
       }
-      float top = x[0];
+      float top = s[n][0][0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[n][i >> 2][i & 3]);
+      top *= c;
       if (__builtin_amdgcn_ballot_w64(top > m[n] + kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16, kWave));
         top = fmaxf(top, __shfl_xor(top, 32, kWave));
@@ -615,29 +655,34 @@ __device__ __forceinline__ void attend_few_4bit(const AttendDev& p, const Attend
       }
       const float base_m = m[n] == -INFINITY ? 0.f : m[n];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) { x[i] = fast_exp2(x[i] - base_m); sum[n] += x[i]; }
-#pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const u32x4 pw = {pack_bf16_pair(x[8 * y], x[8 * y + 1]), pack_bf16_pair(x[8 * y + 2], x[8 * y + 3]),
-                          pack_bf16_pair(x[8 * y + 4], x[8 * y + 5]), pack_bf16_pair(x[8 * y + 6], x[8 * y + 7])};
+        float e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          e[i] = fast_exp2(__builtin_fmaf(s[n][2 * y + (i >> 2)][i & 3], c, -base_m));
+          sum[n] += e[i];
+        }
+        const u32x4 pw = {pack_bf16_pair(e[0], e[1]), pack_bf16_pair(e[2], e[3]), pack_bf16_pair(e[4], e[5]), pack_bf16_pair(e[6], e[7])};
         pf[n][y] = __builtin_bit_cast(bf16x8, pw);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int vr = 4 * quad + ((l & 15) >> 2);  // row of the tile that this lane reads from (and 16, 32, 48 + that)
+    int l2 = l;
+    if (NR == 2) asm volatile("" : "+v"(l2));
+    const int vr = (l2 >> 4) * 4 + ((l2 & 15) >> 2);  // row of the tile that this lane reads from (and 16, 32, 48 + that)
 #pragma unroll
     for (int y = 0; y < 2; ++y)
 #pragma unroll
       for (int i = 0; i < DB; ++i) {
-        const int ch = 2 * i + ((l & 3) >> 1);
-        const char* at0 = vd + (vr + 32 * y) * (D * 2) + swizzled<C>(vr, ch) * 16 + (l & 1) * 8;
+        const int ch = 2 * i + ((l2 & 3) >> 1);
+        const char* at0 = vd + (vr + 32 * y) * (D * 2) + swizzled_blocks<C>(vr, ch) * 16 + (l2 & 1) * 8;
         const bf16x8 vf = join8(lds_read_tr(at0), lds_read_tr(at0 + 16 * D * 2));
 #pragma unroll
         for (int n = 0; n < NR; ++n) o[n][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[n][y], o[n][i], 0, 0, 0);
       }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
-  finish_few<D, NR>(p, u, g, W, lds, w, turn, l, tid, bad, o, m, sum);
+  finish_few<D, NR>(p, u, g, W, lds, w, turn, l, tid, __builtin_amdgcn_ballot_w64(bad) != 0, o, m, sum);
 }
 
 // ---------------------------------------------------------------- many rows
@@ -1001,7 +1046,8 @@ sp_status check_attend(const sp_attend_args* a) {
   for (int64_t s : cache) if (s < 0) return SP_EINVAL;
   if ((a->H > 1 && a->out_head_stride < a->d) || (a->T_new > 1 && a->out_token_stride < a->d)) return SP_EINVAL;  // rows of out that lie in one another
   for (int64_t s : row) if (s & 7) return SP_EALIGN;
-  for (int64_t s : cache) if (s & (cache_stride_unit(a->cache_dtype) - 1)) return SP_EALIGN;
+  for (int64_t s : cache) if (s & (cache_stride_unit(a->cache_dtype, a->d) - 1)) return SP_EALIGN;
+  if (!aligned_scales(a->d_k_block_scale, a->d) || !aligned_scales(a->d_v_block_scale, a->d)) return SP_EALIGN;
   if (!aligned16(a->d_q) || !aligned16(a->d_k_cache) || !aligned16(a->d_v_cache) || !aligned16(a->d_out)) return SP_EALIGN;
   if (!a->d_workspace || a->workspace_bytes < sp_attend_workspace_bytes(a)) return SP_EWORKSPACE;
   if (reinterpret_cast<uintptr_t>(a->d_workspace) & 255u) return SP_EALIGN;

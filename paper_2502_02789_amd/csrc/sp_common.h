@@ -14,8 +14,9 @@ constexpr int kWave = 64;
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-// strides of a cache of this type (sp_k_dtype) are multiples of so many elements: 16 bytes
-inline int64_t cache_stride_unit(int dtype) { return dtype == SP_K_MXFP4 ? 32 : dtype == SP_K_FP8_E4M3 ? 16 : 8; }
+// strides of a cache of this type (sp_k_dtype) are multiples of so many elements: 16 bytes, or, so that a row's block scales can be read as one number, a row
+inline int64_t cache_stride_unit(int dtype, int d) { return dtype == SP_K_MXFP4 ? d : dtype == SP_K_FP8_E4M3 ? 16 : 8; }
+inline bool aligned_scales(const uint8_t* scales, int d) { return (reinterpret_cast<uintptr_t>(scales) & (uintptr_t)(d / 32 - 1)) == 0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // finite (neither NaN nor infinite), decided on the bit pattern so that no floating-point

@@ -147,7 +147,8 @@ sp_status check_read(const sp_cache_read_args* a) {
   if (a->H_kv > 1 && (out[1] < a->d || (values && out[3] < a->d))) return SP_EINVAL;
   if (a->T_rows > 1 && (out[0] < a->d || (values && out[2] < a->d))) return SP_EINVAL;
   if (values && a->d_k_out && a->d_k_out == a->d_v_out) return SP_EINVAL;
-  for (int64_t s : cache) if (s & (cache_stride_unit(a->cache_dtype) - 1)) return SP_EALIGN;
+  for (int64_t s : cache) if (s & (cache_stride_unit(a->cache_dtype, a->d) - 1)) return SP_EALIGN;
+  if (!aligned_scales(a->d_k_block_scale, a->d) || !aligned_scales(a->d_v_block_scale, a->d)) return SP_EALIGN;
   for (int64_t s : out) if (s & 7) return SP_EALIGN;
   if (!aligned16(a->d_k_cache) || !aligned16(a->d_v_cache) || !aligned16(a->d_k_out) || !aligned16(a->d_v_out)) return SP_EALIGN;
   return SP_OK;

@@ -31,6 +31,7 @@ BOTH_BAD = [
     (sp.SP_EINVAL, dict(FOUR, d_v_scale=P)), (sp.SP_EINVAL, dict(d_k_block_scale=P)), (sp.SP_EINVAL, dict(d_v_block_scale=P)),
     (sp.SP_EINVAL, dict(d_k_block_scale=P, cache_dtype=sp.SP_K_FP8_E4M3)), (sp.SP_EALIGN, dict(FOUR, cache_token_stride=144)),
     (sp.SP_EALIGN, dict(FOUR, cache_head_stride=80)), (sp.SP_EALIGN, dict(FOUR, cache_page_stride=2064)), (sp.SP_EALIGN, dict(FOUR, d_k_cache=P + 65544)),
+    (sp.SP_EALIGN, dict(FOUR, cache_token_stride=160)), (sp.SP_EALIGN, dict(FOUR, d_k_block_scale=P + 0x300001)), (sp.SP_EALIGN, dict(FOUR, d_v_block_scale=P + 0x310001)),
     (sp.SP_EINVAL, dict(FOUR, cache_dtype=3)), (sp.SP_EINVAL, dict(FOUR, cache_dtype=5)),
 ]
 

@@ -1,7 +1,7 @@
 // sp_cache_read: tokens of a (paged) cache as bf16 keys and values.
 //
 // One pass: bound by HBM (reads d/2 + d/32, d or 2 d bytes of a token's key or value of a head, writes 2 d).  A workgroup takes a few rows:
-// their places in the cache are looked up once, then every lane turns 8 elements into 16 bytes of the output, four of them on their way at a time.
+// their places in the cache are looked up once, then every lane turns 8 elements into 16 bytes of the output, of four rows at a time.
 #include "sp_score_internal.h"
 
 namespace sp {
@@ -9,7 +9,7 @@ namespace sp {
 namespace {
 
 constexpr int kRows = 8;    // most rows of a workgroup
-constexpr int kAhead = 4;   // loads of a lane that are on their way together
+constexpr int kAhead = 4;   // rows of a lane that are on their way together
 constexpr int64_t kMostRows = INT64_C(1) << 25;  // of a call: a launch has fewer than 2^32 threads
 
 struct ReadDev {
@@ -55,6 +55,20 @@ __device__ __forceinline__ u32x4 as_bf16(const Stored<SP_K_MXFP4>& s) {
                __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(s.x, scale, 3))};
 }
 
+// eight elements from element `at` of a cache on
+template <int KIND>
+__device__ __forceinline__ void load(Stored<KIND>& x, const char* cache, const uint8_t* block_scale, float scale, int64_t at) {
+  if constexpr (KIND == SP_K_MXFP4) {
+    x.x = *reinterpret_cast<const uint32_t*>(cache + at / 2);
+    x.scale = block_scale[at / 32];
+  } else if constexpr (KIND == SP_K_FP8_E4M3) {
+    x.x = *reinterpret_cast<const uint2*>(cache + at);
+    x.scale = scale;
+  } else {
+    x.x = *reinterpret_cast<const u32x4*>(cache + at * 2);
+  }
+}
+
 }  // namespace
 
 template <int D, int KIND>
@@ -84,37 +98,34 @@ __global__ __launch_bounds__(256) void read_kernel(const ReadDev p) {
     place[threadIdx.x] = at;
   }
   __syncthreads();
-  const int items = n * p.arrays * p.H_kv * C;
-  for (int it0 = blockIdx.y * (256 * kAhead) + threadIdx.x; it0 < items; it0 += 256 * kAhead * gridDim.y) {
-    Stored<KIND> x[kAhead];
-    bool there[kAhead];
-    uint16_t* dst[kAhead];
+  // 256 threads take as many rows' chunks as they are enough for, or one row's in turn
+  const int chunks = p.H_kv * C, together = max(256 / chunks, 1), step = chunks > 256 ? 256 : chunks;
+  const int sub = chunks > 256 ? 0 : (int)threadIdx.x / chunks;
+  if (sub >= together) return;
+  for (int ch = (int)threadIdx.x - sub * chunks; ch < chunks; ch += step) {
+    const int c = ch % C, g = ch / C;
+    const int64_t in = g * p.c_hs + 8 * c;
+    uint16_t* const k_out = p.out[0] + g * p.out_hs[0] + 8 * c;
+    uint16_t* const v_out = p.out[1] + g * p.out_hs[1] + 8 * c;
+    const float k_scale = KIND == SP_K_FP8_E4M3 && p.scale[0] ? p.scale[0][g] : 1.f, v_scale = KIND == SP_K_FP8_E4M3 && p.scale[1] ? p.scale[1][g] : 1.f;
+    for (int t0 = sub; t0 < n; t0 += together * kAhead) {
+      Stored<KIND> k[kAhead], v[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int it = it0 + 256 * k;
-      there[k] = false;
-      dst[k] = nullptr;
-      if (it >= items) continue;
-      const int c = it % C, row = it / C, g = row % p.H_kv, tl = row / p.H_kv % n, kv = row / p.H_kv / n;
-      dst[k] = p.out[kv] + (int64_t)(first + tl) * p.out_ts[kv] + g * p.out_hs[kv] + 8 * c;
-      there[k] = place[tl] >= 0;
-      if (!there[k]) continue;
-      const int64_t at = place[tl] + g * p.c_hs + 8 * c;
-      if constexpr (KIND == SP_K_MXFP4) {
-        x[k].x = *reinterpret_cast<const uint32_t*>(p.cache[kv] + at / 2);
-        x[k].scale = p.block_scale[kv][at / 32];
-      } else if constexpr (KIND == SP_K_FP8_E4M3) {
-        x[k].x = *reinterpret_cast<const uint2*>(p.cache[kv] + at);
-        x[k].scale = p.scale[kv] ? p.scale[kv][g] : 1.f;
-      } else {
-        x[k].x = *reinterpret_cast<const u32x4*>(p.cache[kv] + at * 2);
+      for (int i = 0; i < kAhead; ++i) {
+        const int64_t at = max(place[min(t0 + i * together, n - 1)], (int64_t)0) + in;  // (a row without a place: the pool's first, and not used)
+        load<KIND>(k[i], p.cache[0], p.block_scale[0], k_scale, at);
+        if (p.arrays == 2) load<KIND>(v[i], p.cache[1], p.block_scale[1], v_scale, at);
       }
-    }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (!dst[k]) continue;
-      constexpr uint32_t nan2 = 0x7fc07fc0u;
-      *reinterpret_cast<u32x4*>(dst[k]) = there[k] ? as_bf16(x[k]) : u32x4{nan2, nan2, nan2, nan2};
+      for (int i = 0; i < kAhead; ++i) {
+        const int tl = t0 + i * together;
+        if (tl >= n) break;
+        constexpr uint32_t nan2 = 0x7fc07fc0u;
+        const u32x4 none = {nan2, nan2, nan2, nan2};
+        const bool there = place[tl] >= 0;
+        *reinterpret_cast<u32x4*>(k_out + (int64_t)(first + tl) * p.out_ts[0]) = there ? as_bf16(k[i]) : none;
+        if (p.arrays == 2) *reinterpret_cast<u32x4*>(v_out + (int64_t)(first + tl) * p.out_ts[1]) = there ? as_bf16(v[i]) : none;
+      }
     }
   }
 }
@@ -187,12 +198,9 @@ extern "C" sp_status sp_cache_read(const sp_cache_read_args* a, void* hip_stream
   p.scale[0] = a->d_k_scale; p.scale[1] = a->d_v_scale;
   p.block_scale[0] = a->d_k_block_scale; p.block_scale[1] = a->d_v_block_scale;
   p.out[0] = static_cast<uint16_t*>(a->d_k_out); p.out[1] = static_cast<uint16_t*>(a->d_v_out);
-  // few rows: one to a workgroup, and several workgroups to a row where it has many heads
-  p.rows = (int)std::min<int64_t>(kRows, std::max<int64_t>(1, a->T_rows / 512));
-  const int64_t blocks = (a->T_rows + p.rows - 1) / p.rows;
-  const int passes = (p.rows * p.arrays * p.H_kv * (a->d / 8) + 256 * kAhead - 1) / (256 * kAhead);
-  const int parts = blocks >= 512 ? 1 : (int)std::min<int64_t>(passes, 512 / blocks);
-  const dim3 grid((unsigned)blocks, (unsigned)std::max(parts, 1));
+  // few rows: one to a workgroup
+  p.rows = (int)std::min<int64_t>(kRows, std::max<int64_t>(1, a->T_rows / 2048));
+  const dim3 grid((unsigned)((a->T_rows + p.rows - 1) / p.rows));
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (a->d == 128) launch_read<128>(p, a->cache_dtype, grid, stream);
   else launch_read<64>(p, a->cache_dtype, grid, stream);

@@ -612,6 +612,7 @@ __device__ __forceinline__ void attend_few_4bit(const AttendDev& p, const Attend
 
   for (; tile < u.k1; tile += 64 * W) {
     const bool more = tile + 64 * W < u.k1;
+    __builtin_amdgcn_s_setprio(1);
     f32x4 s[NR][4];
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
@@ -629,6 +630,7 @@ __device__ __forceinline__ void attend_few_4bit(const AttendDev& p, const Attend
     x.store_values(vd, l);
     if (NR == 2 && more) load_keys(tile + 64 * W);
     if (more) x.load_values(p, at_keys, v_at, l);
+    __builtin_amdgcn_s_setprio(0);
     bf16x8 pf[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
@@ -975,7 +977,14 @@ __global__ __launch_bounds__(64 * attend_waves(D), D == 64 ? 3 : 2) void attend_
   __shared__ __align__(16) char lds[attend_waves(D) * (64 * D * 2 + 2 * kFewRows * 4 + 4)];  // tiles: 16 KB a wave (8, d = 64), and few rows' statistics
   // The KV heads of a piece are neighbours: with eight of them, each has the L2 of one XCD, which the rows of a
   // block share, as workgroups go to the XCDs in turn.
-  const int n = (int)(blockIdx.x / (uint32_t)p.H_kv), g = (int)(blockIdx.x % (uint32_t)p.H_kv);
+  // Where rows of several heads share a cache line, the heads of a piece go to one XCD instead, eight pieces side by side: no line is read by two.
+  int n = (int)(blockIdx.x / (uint32_t)p.H_kv), g = (int)(blockIdx.x % (uint32_t)p.H_kv);
+  if (KIND == SP_K_MXFP4 && p.heads_together) {
+    const uint32_t group = blockIdx.x / (8u * (uint32_t)p.H_kv), in = blockIdx.x - group * (8u * (uint32_t)p.H_kv);
+    const uint32_t side = min(8u, gridDim.x / (uint32_t)p.H_kv - 8u * group);
+    n = (int)(8u * group + in % side);
+    g = (int)(in / side);
+  }
   // the plan through the scalar cache; header, stretch and its first piece together (the list has room for every workgroup's index)
   const auto header = reinterpret_cast<const __attribute__((address_space(4))) AttendHeader*>(reinterpret_cast<uintptr_t>(p.header));
   typedef const __attribute__((address_space(4))) AttendStretch* StretchPtr;
@@ -1106,6 +1115,7 @@ extern "C" sp_status sp_attend(const sp_attend_args* a, void* hip_stream) {
   p.k = static_cast<const char*>(a->d_k_cache); p.v = static_cast<const char*>(a->d_v_cache);
   p.k_scale = a->d_k_scale; p.v_scale = a->d_v_scale;
   p.k_block_scale = a->d_k_block_scale; p.v_block_scale = a->d_v_block_scale;
+  p.heads_together = a->H_kv > 1 && p.c_hs < 128;
   p.out = static_cast<uint16_t*>(a->d_out); p.lse = a->d_lse;
   p.sums = static_cast<float*>(a->d_workspace);
   p.stats = reinterpret_cast<float2*>(static_cast<char*>(a->d_workspace) + attend_sums_bytes(a));

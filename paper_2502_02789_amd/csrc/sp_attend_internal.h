@@ -34,6 +34,7 @@ struct AttendDev {
   float2* stats;                 // [slot][KV head][16]: row maximum (of logits in log2 units), sum of weights
   const uint8_t* k_block_scale;  // of a 4-bit cache: the scale of the codes from byte x on is byte x / 16
   const uint8_t* v_block_scale;
+  int heads_together;            // ... its rows are shorter than a cache line of 128 bytes, and those of a token's heads follow one another
 };
 
 sp_status check_attend_shape(const sp_attend_args* a);

@@ -542,7 +542,7 @@ SP_API sp_status sp_attend(const sp_attend_args* args, void* hip_stream);
  * (at temperature 0 everything at the largest logit, the lowest index of equal ones; without d_draft q_j is 1 at x_j: tokens that were looked up, not sampled)
  *     x_j stands  if all before it do and u_j * q_j(x_j) < p_j(x_j)
  *     a           = the number of tokens that stand
- *     w           = max(p_a - q_a, 0), or p_a where a = n_b, or where that leaves nothing
+ *     w           = max(p_a - q_a, 0), or p_a where a = n_b, or where that leaves nothing (less than 1e-12)
  *     y           = the lowest index k with  w(0) + .. + w(k) > r_b * (w(0) + .. + w(V-1))      (the last k with w(k) > 0, if rounding leaves none)
  * so that x_0 .. x_(a-1), y are distributed as the target's own tokens if u and r are independent and uniform in [0, 1) and x_j was drawn from q_j.  Outputs:
  *     n_accepted[b] = a;   out_tokens of rows cu_draft[b] + b + j: x_j for j < a, y for j = a, -1 behind;
@@ -554,7 +554,8 @@ SP_API sp_status sp_attend(const sp_attend_args* args, void* hip_stream);
  * In band: a sequence that meets a row with a NaN, a +infinity or nothing but -infinity, before or at its row a, or a drafted token outside [0, V), or a
  * negative or NaN temperature, gets n_accepted = -1, out_tokens -1 and logprob NaN in all of its rows, and kept_len = past_len.  What lies in rows behind row
  * a does not matter.
- * Limits: V < 2^24, T + B < 2^24, at most SP_VERIFY_MAX_DRAFTED drafted tokens for a sequence (one with more: as above).  Rows are contiguous, their strides in
+ * Limits: V < 2^24, (2 T + B) * ceil(V / 8192) < 2^24, at most SP_VERIFY_MAX_DRAFTED drafted tokens for a sequence (one with more: as above).  The outputs overlap
+ * no input, but for d_kept_len, which may be d_past_len.  Rows are contiguous, their strides in
  * elements >= V where there are several; the pointers are aligned to their type.  Rows of out_tokens and logprob at and beyond cu_draft[B] + B are left as they are.
  * --------------------------------------------------------------------------- */
 typedef enum { SP_LOGITS_BF16 = 0, SP_LOGITS_F32 = 1 } sp_logits_dtype;

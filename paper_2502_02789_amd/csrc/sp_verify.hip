@@ -103,10 +103,10 @@ __device__ __forceinline__ void load_logits(const char* row, int first, int step
   }
 }
 
-// of a logit in front of exp2
-__device__ __forceinline__ double exp2_factor(float t) { return t > 0.f ? kLog2e64 / (double)t : kLog2e64; }
+// of a logit in front of exp2 (finite in fp32 too)
+__device__ __forceinline__ double exp2_factor(float t) { return t > 0.f ? fmin(kLog2e64 / (double)t, 3e38) : kLog2e64; }
 
-// exp((z - top) / temperature) in fp64, c = log2(e) / temperature and top_c = top * c: 2^n times the Taylor series of exp(f ln 2), |f| <= 1/2, whose first
+// exp((z - top) / temperature) in fp64, c = log2(e) / temperature: 2^n times the Taylor series of exp(f ln 2), |f| <= 1/2, whose first
 // term left out is 7e-15.  (n comes out of the low bits of the sum with 1.5 2^52.)  -infinity becomes 2^-1000, which is nothing in a sum.
 struct Exp64 {
   double k[11] = {4.4455382718708114e-10, 7.0549116208011234e-9, 1.0178086009239699e-7, 1.3215486790144309e-6, 1.5252733804059841e-5, 1.5403530393381609e-4,
@@ -115,8 +115,8 @@ struct Exp64 {
 #pragma unroll
     for (int i = 0; i < 11; ++i) asm volatile("" : "+s"(k[i]));
   }
-  __device__ __forceinline__ double operator()(float z, double top_c, double c) const {
-    const double t = fmax(fma((double)z, c, -top_c), -1000.0), shifted = t + 6755399441055744.0, f = t - (shifted - 6755399441055744.0);
+  __device__ __forceinline__ double operator()(float z, double top, double c) const {
+    const double t = fmax(((double)z - top) * c, -1000.0), shifted = t + 6755399441055744.0, f = t - (shifted - 6755399441055744.0);
     double s = k[0];
 #pragma unroll
     for (int i = 1; i < 11; ++i) s = fma(s, f, k[i]);
@@ -282,8 +282,8 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
       bad = !there || !sound(tid) || (p.draft && !sound(n + 1 + tid));
       double px, qx = 1.0;
       if (t > 0.f) {
-        px = zp == -INFINITY ? 0.0 : exp64(zp, (double)tops[tid] * c, c) / sums[tid];
-        if (p.draft) qx = zq == -INFINITY ? 0.0 : exp64(zq, (double)tops[n + 1 + tid] * c, c) / sums[n + 1 + tid];
+        px = zp == -INFINITY ? 0.0 : exp64(zp, tops[tid], c) / sums[tid];
+        if (p.draft) qx = zq == -INFINITY ? 0.0 : exp64(zq, tops[n + 1 + tid], c) / sums[n + 1 + tid];
         if (p.logprob && part == 0) lp = ((double)zp - (double)tops[tid]) / (double)t - log(sums[tid]);
       } else {
         px = args[tid] == x ? 1.0 : 0.0;
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
   const bool with_q = a < n && p.draft;
   const char* row_p = row_of<F32>(p.target, p.target_stride, (int64_t)t0 + b + a);
   const char* row_q = with_q ? row_of<F32>(p.draft, p.draft_stride, (int64_t)t0 + a) : row_p;
-  const double top_p = (double)tops[a] * c, top_q = with_q ? (double)tops[n + 1 + a] * c : 0.0;
+  const double top_p = tops[a], top_q = with_q ? tops[n + 1 + a] : 0.0;
   float vp[kMine / E][E], vq[kMine / E][E];
   const int strip = part * 4 + (tid >> 6), first = strip * kStrip + (tid & 63) * E;
   load_logits<F32, kMine / E>(row_p, first, 64 * E, p.V, vp);
@@ -442,9 +442,9 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
   const char* row_p = row_of<F32>(p.target, p.target_stride, s.row_p);
   const char* row_q = row_of<F32>(p.draft, p.draft_stride, s.row_q);
   block_sums(z, lds);
-  Residual res = {s.c, (double)s.top_p * s.c, (double)s.top_q * s.c, s.ratio, with_q ? z[0] / z[1] : 0.0, s.token, with_q};
+  Residual res = {s.c, s.top_p, s.top_q, s.ratio, with_q ? z[0] / z[1] : 0.0, s.token, with_q};
   double total = z[2] - z[3] * res.ratio;
-  const bool nothing = !(total > 0.0);
+  const bool nothing = !(total > 1e-12 * z[0]);
   if (nothing) {  // p itself
     total = z[0];
     res.with_q = false;

@@ -235,6 +235,30 @@ def test_the_same_on_every_run_in_a_graph_and_on_another_stream():
             assert torch.equal(got, expect)
 
 
+def test_two_calls_at_once_on_streams_of_their_own():
+    import torch
+    rng = np.random.default_rng(11)
+    cs = [_case(rng, [4, 2, 8], 128256, temperature=[1.0, 0.0, 0.7]), _case(rng, [1, 7], 50257, bits=32, draft=False)]
+    wants, vs, streams = [_want(c) for c in cs], [_verifier(c) for c in cs], [torch.cuda.Stream() for _ in cs]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(20):
+        for v, s in zip(vs, streams):
+            v.run(s)
+    torch.cuda.synchronize()
+    for c, v, want in zip(cs, vs, wants):
+        _check(c, v, want)
+
+
+def test_the_smallest_temperatures():
+    """What is left of other tokens' probabilities underflows; the weights stay numbers."""
+    rng = np.random.default_rng(12)
+    for bits in (16, 32):
+        c = _case(rng, [2, 1, 0, 3], 700, bits=bits, temperature=[1e-6, 1e-30, 1e-38, 1e-42])
+        c["tokens"][:] = c["target"].float().argmax(dim=1)[[0, 1, 3, 6, 7, 8]].int().cpu().numpy()
+        _run(c)
+
+
 def test_kept_len_may_be_past_len_itself():
     import torch
     from paper_2502_02789_amd import binding as sp

@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 
 from oracle import cache_oracle as co
+from oracle import mxfp4_oracle as mx
 from tests import cache_cases as cc
 from tests import mxfp4_cases as mc
 from tests import test_gpu_attend as checks
@@ -210,3 +211,41 @@ def test_agrees_with_the_bf16_cache_of_the_same_values():
         assert (np.abs(a.out.double().cpu().numpy() - b.out.double().cpu().numpy()) <= 2 * tol).all()
         assert (np.abs(a.lse.double().cpu().numpy() - b.lse.double().cpu().numpy()) <= 2 * tol_l).all()
         assert math.isfinite(float(b.lse.sum()))
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_beyond_offsets_of_2_to_the_32(paged):
+    """More than 2^32 bytes of codes, token strides of 2^16 bytes: one key of all is aligned with the query, and its value comes out."""
+    import torch
+    from paper_2502_02789_amd import device as dev
+    rows, H_kv, d, page = 70016, 2, 128, 16
+
+    def wide(n):
+        pool = torch.zeros((rows, n), dtype=torch.uint8, device="cuda")
+        return pool, pool[:, :H_kv * d // (2 if n == 65536 else 32)].unflatten(1, (H_kv, d // (2 if n == 65536 else 32)))
+    (kp, k), (_, v), (_, ks), (_, vs) = wide(65536), wide(65536), wide(4096), wide(4096)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(14)
+    v.copy_(torch.randint(0, 256, v.shape, generator=g, device="cuda").to(torch.uint8))
+    ks.fill_(127)
+    vs.copy_(torch.randint(125, 130, vs.shape, generator=g, device="cuda").to(torch.uint8))
+    q = torch.full((1, 4, d), 4.0, dtype=torch.bfloat16, device="cuda")
+    parts = [k, v, ks, vs]
+    if paged:
+        parts = [x.unflatten(0, (rows // page, page)) for x in parts]
+        where = dict(block_table=torch.arange(rows // page, dtype=torch.int32, device="cuda").flip(0).view(1, -1).contiguous())
+    else:
+        where = dict(cu_cache=cc.cuda_ints([0, rows]))
+    kc, vc = (x.view(torch.float4_e2m1fn_x2) for x in parts[:2])
+    plan = dev.AttendPlan(cc.cuda_ints([0, 1]), cc.cuda_ints([rows - 5]), kc, H=4, total_new=1, **where)
+    plan.run()
+    a = dev.Attender(plan, q, kc, vc, scale=1.0, k_block_scale=parts[2], v_block_scale=parts[3])
+    for i in (0, 17, 40000, 65535, 65536, 69999, rows - 6):
+        row = (rows // page - 1 - i // page) * page + i % page if paged else i
+        k[row] = 0x77
+        got = a.run()
+        torch.cuda.synchronize()
+        kp[row] = 0
+        codes = torch.stack([v[row] & 15, v[row] >> 4], dim=-1).flatten(-2).cpu().numpy()
+        want = mx.values(codes, vs[row].cpu().numpy())
+        assert (got[0].view(H_kv, 2, d).double().cpu().numpy() == want[:, None]).all(), i

@@ -60,15 +60,31 @@ template <bool F32> __device__ __forceinline__ float logit(const char* row, int 
   else return bf16_lo(reinterpret_cast<const uint16_t*>(row)[i]);
 }
 
-// N times 16 bytes of logits, those of k from element first + k step on, wherever the row begins; those from V on are -infinity.  (All loads are on their way
+// N times 16 bytes of logits, those of k from element first + k step on, wherever the row begins; those from V on are -infinity.  inside: none of the workgroup's are.  (All loads are on their way
 // together: what would lie outside the row is read at its beginning instead, and the one vector that a row ends in comes element by element.)
 template <bool F32> constexpr int kVec = F32 ? 4 : 8;
 template <bool F32, int N>
-__device__ __forceinline__ void load_logits(const char* row, int first, int step, int V, float (&x)[N][kVec<F32>]) {
+__device__ __forceinline__ void load_logits(const char* row, int first, int step, int V, bool inside, float (&x)[N][kVec<F32>]) {
   constexpr int E = kVec<F32>;
   typedef u32x4 words_t __attribute__((aligned(2)));
 
   u32x4 w[N];
+  if (inside) {  // (the same for all lanes)
+#pragma unroll
+    for (int k = 0; k < N; ++k) w[k] = __builtin_nontemporal_load(reinterpret_cast<const words_t*>(row + (uint32_t)(first + k * step) * (F32 ? 4 : 2)));
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (F32) {
+          x[k][e] = __uint_as_float(w[k][e]);
+        } else {
+          x[k][2 * e] = bf16_lo(w[k][e]);
+          x[k][2 * e + 1] = bf16_hi(w[k][e]);
+        }
+      }
+    return;
+  }
   if (V >= E) {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
@@ -106,21 +122,22 @@ __device__ __forceinline__ void load_logits(const char* row, int first, int step
 // of a logit in front of exp2 (finite in fp32 too)
 __device__ __forceinline__ double exp2_factor(float t) { return t > 0.f ? fmin(kLog2e64 / (double)t, 3e38) : kLog2e64; }
 
-// exp((z - top) / temperature) in fp64, c = log2(e) / temperature: 2^n times the Taylor series of exp(f ln 2), |f| <= 1/2, whose first
-// term left out is 7e-15.  (n comes out of the low bits of the sum with 1.5 2^52.)  -infinity becomes 2^-1000, which is nothing in a sum.
+// exp((z - top) / temperature) in fp64, c = log2(e) / temperature: 2^n times a polynomial for 2^f, |f| <= 1/2, the one that equals it at the ten Chebyshev nodes of
+// that interval (2e-14 off at most; of the same degree, Taylor's would be 7e-12).  (n comes out of the low bits of the sum with 1.5 2^52.)  -infinity becomes 2^-1000,
+// which is nothing in a sum.
 struct Exp64 {
-  double k[11] = {4.4455382718708114e-10, 7.0549116208011234e-9, 1.0178086009239699e-7, 1.3215486790144309e-6, 1.5252733804059841e-5, 1.5403530393381609e-4,
-                  1.3333558146428443e-3, 9.6181291076284772e-3, 5.5504108664821580e-2, 0.24022650695910071, 0.69314718055994531};  // ln(2)^k / k!, k = 11 .. 1
+  static constexpr int N = 10;
+  double k[N] = {1.0205905413765595e-07, 1.325964524488711e-06, 1.5252672924850737e-05, 0.0001540343375125101, 0.0013333558200794592, 0.009618129193934313,
+                 0.05550410866465167, 0.2402265069564034, 0.6931471805599462, 1.0000000000000135};
   __device__ __forceinline__ Exp64() {  // (kept in scalar registers: as literals, each would be moved into a vector register in front of its use)
 #pragma unroll
-    for (int i = 0; i < 11; ++i) asm volatile("" : "+s"(k[i]));
+    for (int i = 0; i < N; ++i) asm volatile("" : "+s"(k[i]));
   }
   __device__ __forceinline__ double operator()(float z, double top, double c) const {
     const double t = fmax(((double)z - top) * c, -1000.0), shifted = t + 6755399441055744.0, f = t - (shifted - 6755399441055744.0);
     double s = k[0];
 #pragma unroll
-    for (int i = 1; i < 11; ++i) s = fma(s, f, k[i]);
-    s = fma(s, f, 1.0);
+    for (int i = 1; i < N; ++i) s = fma(s, f, k[i]);
     const uint64_t bits = (uint64_t)__double_as_longlong(s);
     return __longlong_as_double((long long)((bits & 0xffffffffull) | (uint64_t)((uint32_t)(bits >> 32) + ((uint32_t)__double_as_longlong(shifted) << 20)) << 32));
   }
@@ -170,7 +187,7 @@ __global__ __launch_bounds__(256) void verify_stats_kernel(const VerifyDev p) {
   if (r >= p.cu[p.B] + (target ? p.B : 0)) return;  // (a row of nobody)
   const char* at = target ? row_of<F32>(p.target, p.target_stride, r) : row_of<F32>(p.draft, p.draft_stride, r);
   float x[N][E];
-  load_logits<F32, N>(at, slice * kSlice + (int)threadIdx.x * E, 256 * E, p.V, x);
+  load_logits<F32, N>(at, slice * kSlice + (int)threadIdx.x * E, 256 * E, p.V, (slice + 1) * kSlice <= p.V, x);
   float c = (float)kLog2e64;
   bool greedy = false;
   if (p.temperature) {
@@ -339,8 +356,8 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
   const double top_p = tops[a], top_q = with_q ? tops[n + 1 + a] : 0.0;
   float vp[kMine / E][E], vq[kMine / E][E];
   const int strip = part * 4 + (tid >> 6), first = strip * kStrip + (tid & 63) * E;
-  load_logits<F32, kMine / E>(row_p, first, 64 * E, p.V, vp);
-  if (with_q) load_logits<F32, kMine / E>(row_q, first, 64 * E, p.V, vq);
+  load_logits<F32, kMine / E>(row_p, first, 64 * E, p.V, (part + 1) * PART <= p.V, vp);
+  if (with_q) load_logits<F32, kMine / E>(row_q, first, 64 * E, p.V, (part + 1) * PART <= p.V, vq);
   double z[4] = {0.0, 0.0, 0.0, 0.0};
   if (with_q) {
     const double ratio = sums[a] / sums[n + 1 + a];

@@ -552,7 +552,7 @@ SP_API sp_status sp_attend(const sp_attend_args* args, void* hip_stream);
  * fp64 (off by 1e-13 of the whole), in an order that does not change; u_j q_j < p_j is decided with sums in fp32 (1e-6 of p_j), and
  * tokens with |p_a - q_a| below 1e-6 p_a may count as w = 0.
  * In band: a sequence that meets a row with a NaN, a +infinity or nothing but -infinity, before or at its row a, or a drafted token outside [0, V), or a
- * negative or NaN temperature, gets n_accepted = -1, out_tokens -1 and logprob NaN in all of its rows, and kept_len = past_len.  What lies in rows behind row
+ * negative, infinite or NaN temperature, gets n_accepted = -1, out_tokens -1 and logprob NaN in all of its rows, and kept_len = past_len.  What lies in rows behind row
  * a does not matter.
  * Limits: V < 2^24, (2 T + B) * ceil(V / 8192) < 2^24, at most SP_VERIFY_MAX_DRAFTED drafted tokens for a sequence (one with more: as above).  The outputs overlap
  * no input, but for d_kept_len, which may be d_past_len.  Rows are contiguous, their strides in

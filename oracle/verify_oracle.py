@@ -26,7 +26,7 @@ def verify(target, tokens, cu, u, r, draft=None, temperature=None, past_len=None
     for b in range(B):
         t0, n = int(cu[b]), int(cu[b + 1] - cu[b])
         t = 1.0 if temperature is None else float(temperature[b])
-        first, a, y, wrong = t0 + b, 0, -1, not t >= 0
+        first, a, y, wrong = t0 + b, 0, -1, not 0 <= t < np.inf
         logs = []
         while not wrong:
             lp = log_probabilities(target[first + a], t)

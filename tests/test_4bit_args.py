@@ -142,3 +142,11 @@ def test_oracle_values_and_rounding():
         x[0, 5] = -top
         assert mx.quantise(x)[1][0, 0] == want, top
     assert (mx.unpack(mx.pack(codes)) == codes).all()
+
+
+def test_scoring_takes_no_4_bit_tensor():
+    """A tensor of 4-bit codes has elements of one byte, as an 8-bit cache has, but half as many."""
+    q, cu = torch.zeros(1, 1, 1, 8, 128, dtype=torch.bfloat16), torch.tensor([0, 16], dtype=torch.int32)
+    codes = torch.zeros(16, 2, 64, dtype=torch.uint8).view(torch.float4_e2m1fn_x2)
+    with pytest.raises(ValueError, match="4-bit"):
+        sp.make_score_args(q, [codes], cu, torch.zeros(16), H_kv=2, scale=1.0)

@@ -271,3 +271,13 @@ def test_kept_len_may_be_past_len_itself():
     sp.sp_verify(v.args)
     torch.cuda.synchronize()
     assert torch.equal(past, want)
+
+
+def test_a_temperature_that_is_none_is_answered_in_band():
+    import torch
+    c = _case(np.random.default_rng(21), [2, 2, 1], 700, temperature=[math.inf, 1.0, -0.5])
+    want = _want(c)
+    v = _run(c)
+    torch.cuda.synchronize()
+    _check(c, v, want)
+    assert v.n_accepted.tolist()[::2] == [-1, -1] and v.n_accepted.tolist()[1] >= 0

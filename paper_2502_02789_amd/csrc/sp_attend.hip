@@ -1,4 +1,4 @@
-// sp_attend: attention of new tokens over a (paged, bf16 or E4M3) cache, the keys of a shared prefix read once for a group.
+// sp_attend: attention of new tokens over a (paged, bf16, E4M3 or MXFP4) cache, the keys of a shared prefix read once for a group.
 //
 // One launch takes every piece of the plan (sp_attend_plan.h), a workgroup of eight waves (d = 128: one on a compute unit; four
 // and three of them, d = 64) a stretch of pieces for one KV head.  Two forms:
@@ -8,6 +8,9 @@
 //     there the waves wait for more than half of their time, the LDS is busy for 41 % (half of it the banks that the widened chunks meet in), the
 //     vector ALUs for 20 %.  Two tiles of rows instead of a large block, whose matrix tiles they would fill to a tenth: 14 to 27 % less
 //     time; 32 sequences of 1K-3K keys and 2 to 8 tokens of 4 heads: 62 us, 4.5 TB/s.
+//     4-bit caches have a form of their own (below, few rows, 4-bit keys and values): 64-key tiles, keys from registers to the matrix cores without LDS.
+//     64 sequences of 1K-4K keys 44 us, 128K keys 31 us (H 64), join and launches, 6 to 7 us, among them; the kernel alone reads 3.8 and 5.3 TB/s.  Loads alone,
+//     with the same start and join, take 36 and 29 us, 3.6 of the 36 for the scales.
 //   many rows (<= 256, d = 64 128: prompts, prefixes of groups)  bound by the matrix cores and the vector work between their products.
 //     The waves share 64-key tiles in LDS (two buffers, one barrier a tile; a second tile on its way in registers), each has 32 rows.
 //     6592 tokens, H 64, d 128, causal: 690-720 us, 1.0 PFLOP/s (matrix cores busy for 48 % of the clocks, vector ALUs for 43 %, at 1.93 GHz); eight
@@ -479,7 +482,7 @@ __device__ __forceinline__ int swizzled_blocks(int r, int c) {
   else return c ^ ((r >> 1 & 3) | (r >> 1 & 1) << 2);
 }
 
-// A wave's 64-key tile on its way.  Keys need no LDS: lane (key l & 15, quad l >> 4) holds D/4 consecutive elements of a key, and as the order of
+// A wave's 64-key tile on its way, one to a wave (two, in registers: 64 single tokens 50.5 us instead of 44.8).  Keys need no LDS: lane (key l & 15, quad l >> 4) holds D/4 consecutive elements of a key, and as the order of
 // elements inside a product's sum is free, it hands them to the matrix cores as they are, turned into bf16, eight to a step; the
 // queries are laid out alike.  Values come by whole rows, become bf16 on their way into LDS, and are transposed there.
 template <int D>

@@ -548,7 +548,8 @@ SP_API sp_status sp_attend(const sp_attend_args* args, void* hip_stream);
  *     n_accepted[b] = a;   out_tokens of rows cu_draft[b] + b + j: x_j for j < a, y for j = a, -1 behind;
  *     logprob: log p_j of these tokens, -infinity behind;   kept_len[b] = past_len[b] + 1 + a
  * (kept_len: of a step that appended the last token and the drafted ones behind past_len[b] tokens, what of the cache stands).
- * Logits may be off by a constant in each row (log-probabilities will do) and -infinity (probability 0).  The weights of y's row are formed and added in
+ * Logits may be off by a constant in each row (log-probabilities will do) and -infinity (probability 0); what is below 2^-1021 of a row's largest
+ * probability counts as 0.  The weights of y's row are formed and added in
  * fp64 (off by 1e-13 of the whole), in an order that does not change; u_j q_j < p_j is decided with sums in fp32 (1e-6 of p_j), and
  * tokens with |p_a - q_a| below 1e-6 p_a may count as w = 0.
  * In band: a sequence that meets a row with a NaN, a +infinity or nothing but -infinity, before or at its row a, or a drafted token outside [0, V), or a

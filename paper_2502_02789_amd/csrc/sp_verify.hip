@@ -126,8 +126,8 @@ __device__ __forceinline__ void load_logits(const char* row, int first, int step
 __device__ __forceinline__ double exp2_factor(float t) { return t > 0.f ? fmin(kLog2e64 / (double)t, 3e38) : kLog2e64; }
 
 // exp((z - top) / temperature) in fp64, c = log2(e) / temperature: 2^n times a polynomial for 2^f, |f| <= 1/2, the one that equals it at the ten Chebyshev nodes of
-// that interval (2e-14 off at most; of the same degree, Taylor's would be 7e-12).  (n comes out of the low bits of the sum with 1.5 2^52.)  -infinity becomes 2^-1000,
-// which is nothing in a sum.
+// that interval (2e-14 off at most; of the same degree, Taylor's would be 7e-12).  (n comes out of the low bits of the sum with 1.5 2^52.)  Below 2^-1021, where the exponent's
+// field ends, it is 0: a strip in which all is masked must weigh exactly nothing, or r = 0 would pick it.
 struct Exp64 {
   static constexpr int N = 10;
   double k[N] = {1.0205905413765595e-07, 1.325964524488711e-06, 1.5252672924850737e-05, 0.0001540343375125101, 0.0013333558200794592, 0.009618129193934313,
@@ -137,12 +137,13 @@ struct Exp64 {
     for (int i = 0; i < N; ++i) asm volatile("" : "+s"(k[i]));
   }
   __device__ __forceinline__ double operator()(float z, double top, double c) const {
-    const double t = fmax(((double)z - top) * c, -1000.0), shifted = t + 6755399441055744.0, f = t - (shifted - 6755399441055744.0);
+    const double t = ((double)z - top) * c, shifted = t + 6755399441055744.0, f = t - (shifted - 6755399441055744.0);
     double s = k[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) s = fma(s, f, k[i]);
     const uint64_t bits = (uint64_t)__double_as_longlong(s);
-    return __longlong_as_double((long long)((bits & 0xffffffffull) | (uint64_t)((uint32_t)(bits >> 32) + ((uint32_t)__double_as_longlong(shifted) << 20)) << 32));
+    const double y = __longlong_as_double((long long)((bits & 0xffffffffull) | (uint64_t)((uint32_t)(bits >> 32) + ((uint32_t)__double_as_longlong(shifted) << 20)) << 32));
+    return t >= -1021.0 ? y : 0.0;
   }
 };
 
@@ -302,8 +303,8 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
       bad = !there || !sound(tid) || (p.draft && !sound(n + 1 + tid));
       double px, qx = 1.0;
       if (t > 0.f) {
-        px = zp == -INFINITY ? 0.0 : exp64(zp, tops[tid], c) / sums[tid];
-        if (p.draft) qx = zq == -INFINITY ? 0.0 : exp64(zq, tops[n + 1 + tid], c) / sums[n + 1 + tid];
+        px = exp64(zp, tops[tid], c) / sums[tid];
+        if (p.draft) qx = exp64(zq, tops[n + 1 + tid], c) / sums[n + 1 + tid];
         if (p.logprob && part == 0) lp = ((double)zp - (double)tops[tid]) / (double)t - log(sums[tid]);
       } else {
         px = args[tid] == x ? 1.0 : 0.0;
@@ -331,6 +332,9 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
         } else if (t == 0.f) {
           p.out_tokens[first + j] = args[a];  // (where x_a does not stand, all of p is at another token, and q cannot have more there)
           if (p.logprob) p.logprob[first + j] = 0.f;
+        } else {  // (until one is picked)
+          p.out_tokens[first + j] = -1;
+          if (p.logprob) p.logprob[first + j] = __uint_as_float(0x7fc00000u);
         }
       }
       if (tid == 0) {
@@ -398,9 +402,9 @@ __global__ __launch_bounds__(256) void verify_choose_kernel(const VerifyDev p) {
 // what is left of p_i over the draft, in units of p's weights
 struct Residual { double c, top_p, top_q, first_ratio, ratio; int token; bool with_q; };
 __device__ __forceinline__ double residual_weight(const Exp64& exp64, const Residual& s, float zp, float zq, int i) {
-  double w = zp == -INFINITY ? 0.0 : exp64(zp, s.top_p, s.c);
+  double w = exp64(zp, s.top_p, s.c);
   if (s.with_q) {
-    const double wq = zq == -INFINITY ? 0.0 : exp64(zq, s.top_q, s.c);
+    const double wq = exp64(zq, s.top_q, s.c);
     w = w > wq * s.first_ratio ? fmax(w - wq * s.ratio, 0.0) : 0.0;
   }
   return i == s.token ? 0.0 : w;
@@ -525,11 +529,11 @@ __global__ __launch_bounds__(256) void verify_pick_kernel(const VerifyDev p) {
     }
   }
   int y = first_hit(hit, end, hits);
-  if (y < 0) {  // (what was left in the strip is no more than a rounding: its first token with a probability)
+  if (y < 0) {  // (what was left in the strip is no more than a rounding: its first token with a probability, and there is one, as the strip has a weight)
     hit = kNone;
 #pragma unroll
     for (int k = M - 1; k >= 0; --k)
-      if (first + k < p.V && first + k != res.token && zp[k] != -INFINITY) hit = first + k;
+      if (first + k < p.V && first + k != res.token && exp64(zp[k], s.top_p, s.c) > 0.0) hit = first + k;
     y = first_hit(hit, -1, strip_hits);
   }
 #pragma unroll

@@ -9,15 +9,12 @@
 // 52 us, 4.8 TB/s.
 #include <cmath>
 
+#include "sp_append_grid.h"
 #include "sp_score_internal.h"
 
 namespace sp {
 
 namespace {
-
-constexpr int kTokens = 4;  // most tokens of a workgroup (8192 tokens into 8 bits: 8 takes 2 % longer, 16 18 %; 100K of d = 64: 3 and 8 %)
-
-constexpr int64_t kMostTokens = INT64_C(1) << 25;  // of a call: a launch has fewer than 2^32 threads
 
 struct AppendDev {
   int B, H, H_kv, T_new, tokens, lg_page, blocks_per_seq;
@@ -264,15 +261,9 @@ extern "C" sp_status sp_cache_append(const sp_cache_append_args* a, void* hip_st
   p.q_out = static_cast<uint16_t*>(a->d_q_out);
   p.k_cache = static_cast<char*>(a->d_k_cache); p.v_cache = static_cast<char*>(a->d_v_cache);
   p.k_block_scale = a->d_k_block_scale; p.v_block_scale = a->d_v_block_scale;
-  // few tokens: one to a workgroup, and several workgroups to a token, until the device has some hundred
-  // (into 4 bits fewer, three chunks to a lane: with their reading back, 6592 tokens of 64 heads, one to a workgroup instead of four, 62.6 us instead of 69.0;
-  // 8192 of 8 heads, four instead of one, 16.2 instead of 20.9; 8192 of 32 heads and 100K of d = 64, two and four, the same within 2 %)
-  const int per_token = (p.H + 2 * p.H_kv) * (a->d / 16), most = a->cache_dtype == SP_K_MXFP4 ? std::max(1, std::min(kTokens, 768 / per_token)) : kTokens;
-  p.tokens = (int)std::min<int64_t>(most, std::max<int64_t>(1, a->T_new / 512));
-  const int64_t blocks = (a->T_new + p.tokens - 1) / p.tokens;
-  const int chunks = (p.tokens * (p.H + 2 * p.H_kv) * (a->d / 16) + 255) / 256;
-  const int parts = blocks >= 512 ? 1 : (int)std::min<int64_t>(chunks, 512 / blocks);
-  const dim3 grid((unsigned)blocks, (unsigned)std::max(parts, 1));
+  const AppendGrid cut = append_grid(a->T_new, p.H + 2 * p.H_kv, a->d, a->cache_dtype);
+  p.tokens = cut.tokens;
+  const dim3 grid(cut.blocks, cut.parts);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (a->d == 128) launch_append<128>(p, a->cache_dtype, rope, grid, stream);
   else launch_append<64>(p, a->cache_dtype, rope, grid, stream);

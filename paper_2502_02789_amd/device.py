@@ -182,7 +182,7 @@ def _check_block_scales(cache, scales, name: str):
 def _check_cache(k_cache, v_cache, block_table, cu_cache, B: int, scales=()):
     _need((block_table is None) != (cu_cache is None), "a cache is paged (block_table) or contiguous (cu_cache)")
     for c in (k_cache, v_cache):
-        _need(c is None or c.dtype in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn, torch.float4_e2m1fn_x2),
+        _need(c is None or sp.is_4bit(c) or c.dtype in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn),
               "the cache holds bf16, E4M3 (uint8, float8_e4m3fn) or E2M1 codes (float4_e2m1fn_x2)")
     if block_table is not None:
         _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous() and block_table.shape[0] == B,

@@ -227,7 +227,7 @@ def make_score_args(q, k_layers: Sequence, cu_seqlens, scores, *, H_kv: int, sca
     """q: bf16 [L,B,N,H,d]; k_layers: L bf16 tensors [T,H_kv,d] (any token/head strides), or, with
     block_table (int32 [B, blocks_per_seq]), L page pools [pages, page_size, H_kv, d] (then T must be given).
     uint8 layers are taken as an 8-bit float cache (SP_K_FP8_E4M3) with k_scale fp32 [L, H_kv] (None: all 1)."""
-    if is_4bit(k_layers[0]):
+    if any(is_4bit(k) for k in k_layers):
         raise ValueError("sp_score takes no 4-bit cache: sp_cache_read gives its keys in bf16")
     L, B, N, H, d = q.shape
     a = ScoreArgs()

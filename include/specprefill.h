@@ -592,7 +592,10 @@ SP_API sp_status sp_verify(const sp_verify_args* args, void* hip_stream);
 /* Static, never-NULL description of a status code. */
 SP_API const char* sp_strerror(sp_status status);
 
-/* Library version as major*10000 + minor*100 + patch. */
+/* Library version as major*10000 + minor*100 + patch, SP_VERSION that of this header.  The argument structs have no size field: a program passes
+ * those of its header, so it needs a library of the same major number, which goes up whenever one of them changes.  (Versions below 10000 counted otherwise: 300
+ * has today's structs, 200 shorter ones of sp_cache_append and sp_attend.) */
+#define SP_VERSION 30000
 SP_API int32_t sp_version(void);
 
 #ifdef __cplusplus

@@ -549,9 +549,11 @@ SP_API sp_status sp_attend(const sp_attend_args* args, void* hip_stream);
  *     logprob: log p_j of these tokens, -infinity behind;   kept_len[b] = past_len[b] + 1 + a
  * (kept_len: of a step that appended the last token and the drafted ones behind past_len[b] tokens, what of the cache stands).
  * Logits may be off by a constant in each row (log-probabilities will do) and -infinity (probability 0); what is below 2^-1021 of a row's largest
- * probability counts as 0.  The weights of y's row are formed and added in
- * fp64 (off by 1e-13 of the whole), in an order that does not change; u_j q_j < p_j is decided with sums in fp32 (1e-6 of p_j), and
- * tokens with |p_a - q_a| below 1e-6 p_a may count as w = 0.
+ * probability counts as 0.  The weights of y's row are formed and added in fp64, in an order that does not change: the sums of w = p_a are off by 1e-13 of the
+ * whole.  A row's own sum, with which tokens are decided on, is fp32's and off by at most E = 2^-22 (1 + log2 V) + 48 2^-24 of itself (7e-6 at V = 128256):
+ * u_j q_j < p_j is decided within 2 E of p_j, and so, of every token, is p_a > q_a.  With d_draft the sums of w = max(p_a - q_a, 0) may
+ * therefore be off by what tokens with |p_a - q_a| < 2 E p_a come to, less than 2 E of the whole of p_a; where p_a and q_a are so much alike that no more
+ * than that is left, y may be another token that p_a gives a probability.
  * In band: a sequence that meets a row with a NaN, a +infinity or nothing but -infinity, before or at its row a, or a drafted token outside [0, V), or a
  * negative, infinite or NaN temperature, gets n_accepted = -1, out_tokens -1 and logprob NaN in all of its rows, and kept_len = past_len.  What lies in rows behind row
  * a does not matter.

@@ -10,8 +10,9 @@
 // One sequence of four tokens: 13.5 us, three launches, each a chain of dependent reads.
 // Which token is picked depends on sums over the whole vocabulary: a vocabulary of 128K has so many borders between tokens that sums in fp32, off by 1e-7, would pick
 // another token once in some hundred calls.  The sampled row's weights are therefore formed and added in fp64; the order of all sums is fixed.  Only which
-// tokens have something left is decided with the ratio Zp/Zq of the first kernel's sums in fp32, so that one pass does: a token whose p and q are within 1e-6 of one another may
-// count as one of which nothing is left.
+// tokens have something left is decided with the ratio Zp/Zq of the first kernel's sums in fp32, so that one pass does: a token whose p and q are within the two sums' errors
+// of one another (1.4e-5 at most, V = 128256) may count as one of which nothing is left, or, with less than nothing, as one of which something is.  What such tokens come to
+// is that share of the whole at most: of 0.3 left and differences of the draft's logits of 0.7, as in the cases measured, some 1e-10.
 #include "sp_score_internal.h"
 
 namespace sp {

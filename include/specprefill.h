@@ -557,7 +557,7 @@ SP_API sp_status sp_attend(const sp_attend_args* args, void* hip_stream);
  * In band: a sequence that meets a row with a NaN, a +infinity or nothing but -infinity, before or at its row a, or a drafted token outside [0, V), or a
  * negative, infinite or NaN temperature, gets n_accepted = -1, out_tokens -1 and logprob NaN in all of its rows, and kept_len = past_len.  What lies in rows behind row
  * a does not matter.
- * Limits: V < 2^24, (2 T + B) * ceil(V / 8192) < 2^24, at most SP_VERIFY_MAX_DRAFTED drafted tokens for a sequence (one with more: as above).  The outputs overlap
+ * Limits: V < 2^24, (2 T + B) * ceil(V / 8192) < 2^24, B * ceil(V / 4096) < 2^24, at most SP_VERIFY_MAX_DRAFTED drafted tokens for a sequence (one with more: as above).  The outputs overlap
  * no input, but for d_kept_len, which may be d_past_len.  Rows are contiguous, their strides in
  * elements >= V where there are several; the pointers are aligned to their type.  Rows of out_tokens and logprob at and beyond cu_draft[B] + B are left as they are.
  * --------------------------------------------------------------------------- */

@@ -569,7 +569,7 @@ sp_status check_verify_shape(const sp_verify_args* a) {
   if (!a) return SP_ENULL;
   if (a->B < 1 || a->V < 1 || a->V >= 1 << 24 || a->T < 0 || a->T + a->B >= 1 << 24) return SP_EINVAL;
   if (a->logits_dtype != SP_LOGITS_BF16 && a->logits_dtype != SP_LOGITS_F32) return SP_EINVAL;
-  // threads of a launch
+  // workgroups of a launch (as many parts of the smaller size are far below)
   if ((2 * a->T + a->B) * verify_slices(a) >= 1 << 24 || (int64_t)a->B * verify_parts(a) >= 1 << 24) return SP_EINVAL;
   return SP_OK;
 }

@@ -2,7 +2,7 @@
 //
 // One pass: bound by HBM (reads d/2 + d/32, d or 2 d bytes of a token's key or value of a head, writes 2 d).  A workgroup takes a few rows:
 // their places in the cache are looked up once, then every lane turns 8 elements into 16 bytes of the output, of four rows at a time.
-// 100K tokens of d = 64 out of 4 bits: 60 us, 4.8 TB/s (a large copy: 5.2); 3200 chosen tokens, d 128, 7.8 us: a launch and four dependent reads.  (A division by the
+// 111K tokens of d = 64 out of 4 bits: 61 us, 4.8 TB/s (a large copy: 5.2); 3200 chosen tokens, d 128, 7.8 us: a launch and four dependent reads.  (A division by the
 // number of heads for every 16 bytes: 104 us.)
 #include "sp_score_internal.h"
 

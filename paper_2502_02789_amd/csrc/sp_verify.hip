@@ -5,7 +5,7 @@
 //   choose    per sequence: the rows' sums, how many tokens stand, hence the row that a token is sampled from; in strips of it, the sums of the weights of p and
 //             q, and of both over the tokens with something left: with Zp, Zq the sums over all, what is left in a strip is (sum of wp - Zp/Zq sum of wq) / Zp
 //   pick      the strip in which the sum passes r times the whole, and the token in it
-// 64 sequences of 1 to 8 tokens, V = 128256, bf16, with the draft's logits (149 MB): 49.5 to 50.6 us a pass; traced one by one, which counts each one's start and end, the
+// 64 sequences of 1 to 8 tokens, V = 128256, bf16, with the draft's logits (149 MB): 49.5 to 50.9 us a pass; traced one by one, which counts each one's start and end, the
 // kernels take 27 + 21 + 5.5.  The first kernel reads 5.5 TB/s, its vector ALUs busy for about
 // 60 % of the time; the second forms 16 M weights in fp64, ALUs busy for 40 %, its workgroups all at once first waiting (row sums, logits), then computing.
 // One sequence of four tokens: 13.3 us, three launches, each a chain of dependent reads.
